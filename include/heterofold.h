@@ -383,6 +383,157 @@ int32_t hf_transfer_kv_taps(int32_t B, const int32_t* s_len, const int32_t* r_le
                             size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* Using the caches: attention over them, and a paged cache held in 4 bits.  */
+/* ------------------------------------------------------------------------ */
+/*
+ * What the two models do around a hand-off: the sender's prefill that makes the
+ * cache, the receiver's pass over the suffix with the transferred cache before
+ * it, and the receiver's decoding.  The paged cache keeps a receiver's caches at
+ * 4 bits a value between these; hf_paged_read gives back the dense rows that the
+ * next hand-off takes as its sender cache.
+ */
+
+/*
+ * Rows of heads in device memory: element (l, row t of sequence b, head h,
+ * channel e) lives at ptr + seq_off[b] + l*stride_l + t*stride_t + h*stride_h + e
+ * (in elements; channels contiguous).  seq_off: host int64 [B], read during the
+ * call, or NULL: the sequences lie back to back (packed), sequence b's first row
+ * after those of the sequences before it.  So it describes packed projections
+ * ([N][H][d_h], also as a part of a fused one) and, with seq_off[b] =
+ * b*stride_b and ptr at a role, a cache that an hf_kv_desc describes.  stride_l
+ * is read by the paged calls only.  ptr, strides and offsets must be >= 0 and
+ * keep rows 16-byte aligned, and stride_t and stride_h of rows that a call
+ * writes must be >= d_h.  Rows of one call that overlap where it writes race.
+ */
+typedef struct hf_rows {
+  void* ptr;
+  int32_t dtype; /* hf_dtype */
+  int32_t H, d_h;
+  int64_t stride_t, stride_h, stride_l;
+  const int64_t* seq_off;
+} hf_rows;
+
+/*
+ * Workspace bytes hf_prompt_attention (paged = 0) or hf_paged_attention
+ * (paged = 1) needs for these lengths, heads, d_h and dtype: the unnormalized
+ * sums, maxima and weights of the parts that a long key range is split into when
+ * there are few query rows (each 4 (d_h + 2) bytes a query row, head and part),
+ * 0 when nothing is split.  Calls that share a workspace must not overlap.
+ */
+size_t hf_attention_workspace_bytes(int32_t B, const int32_t* q_len, const int32_t* kv_len,
+                                    int32_t H_q, int32_t H, int32_t d_h, int32_t dtype,
+                                    int32_t paged);
+
+/*
+ * Attention of a batch of query runs over dense keys and values, heads grouped:
+ * query head h reads key/value head h / (H_q / H).  Query row i of sequence b
+ * sees the keys j < kv_len[b], with `causal` those with
+ * j <= i + kv_len[b] - q_len[b] (the queries are the last q_len[b] of the
+ * kv_len[b] positions):
+ *   s_ij = scale * <q_i, k_j>;   w_ij = exp(s_ij - max_j s_ij);
+ *   out_i = sum_j w_ij v_j / sum_j w_ij;   lse_i = log sum_j exp(s_ij).
+ * A whole prompt has kv_len == q_len; a suffix over a transferred cache, or one
+ * decoded token, has q_len < kv_len.  A row that sees no key (kv_len == 0, or
+ * causal with q_len > kv_len) gets out = 0 and lse = -infinity.  What a row does
+ * not see has no influence on it, whatever its bits are.
+ *   q_len, kv_len  host int32 [B], >= 0.
+ *   q, out    hf_rows of H_q heads; out may be q itself, element for element.
+ *   k, v      hf_rows of H heads, H_q % H == 0; same dtype and d_h throughout.
+ *   scale     finite and > 0 (1/sqrt(d_h) as a rule).
+ *   lse       device fp32 [sum q_len][H_q] (rows packed), or NULL.
+ *   workspace device, >= hf_attention_workspace_bytes(..., paged = 0), 256-B
+ *             aligned; may be NULL where that is 0.
+ * Numerics: HF_BF16 multiplies on the bf16 matrix cores with fp32 accumulation;
+ * the softmax runs in fp32, its weights are rounded once to bf16 for the second
+ * product (their sum is taken before that), and the result is rounded once.
+ * HF_F32 computes in fp32 throughout.  Supported: d_h 64 and 128.
+ */
+int32_t hf_prompt_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len,
+                            const hf_rows* q, const hf_rows* k, const hf_rows* v,
+                            const hf_rows* out, float scale, int32_t causal, float* lse,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A paged cache held in 4 bits: n_pages pages of page_tokens tokens for each of L
+ * layers, page p of layer l at pages + (l*n_pages + p) * hf_paged_page_bytes(),
+ * and a page table: token t of sequence b is row t % page_tokens of page
+ * table[b*table_stride + t / page_tokens] (device int32; the same for all
+ * layers).  A table entry outside [0, n_pages) is a hole: appending drops its
+ * tokens, reading gives 0 and attention does not see them.  Pages may be shared
+ * by tables that only read them; the pages that one call appends to must be
+ * named once.
+ *
+ * Format.  A row (one token, head and role) is held in groups of 32 channels.
+ * With lo and hi a group's least and largest value, o = bf16(lo) and
+ * s = bf16((hi - lo) / 15) are kept in one 32-bit word (s in the upper half), and
+ * channel x as the code clamp(rint((x - o) / s), 0, 15), which stands for
+ * s * code + o.  s < 2^-100 counts as 0 (codes 0).  A group whose s or o is not
+ * finite (a value that is not, or a spread past the range) stands for NaN.  A
+ * page holds, for each head in turn, the codes of its keys, the codes of its
+ * values, the words of its keys [page_tokens][d_h/32], and those of its values.
+ * Key codes: token by token, channel 32 g + 8 m + j at nibble
+ * (m * d_h/32 + g) * 8 + j of the token's d_h/2 bytes.  Value codes: in blocks of
+ * 32 tokens, token 16 u + 4 m + j of the block and channel 16 n + c at nibble
+ * ((m * 16 + c) * d_h/16 + n) * 8 + 4 u + j.  The lower nibble of a byte first.
+ * Both orders are those in which the attention's matrix instructions take their
+ * operands, so that a lane loads 16 bytes of codes at a time and shuffles none.
+ */
+typedef struct hf_paged_kv {
+  void* pages;          /* device, 16-byte aligned */
+  const int32_t* table; /* device [B][table_stride] */
+  int64_t table_stride; /* entries a sequence, >= those that its tokens need */
+  int32_t n_pages;
+  int32_t L, H, d_h;
+  int32_t page_tokens;  /* 32, 64, 128 or 256 */
+} hf_paged_kv;
+
+/* Bytes of one page: H * page_tokens * (d_h + d_h/4).  0 on bad arguments. */
+size_t hf_paged_page_bytes(int32_t H, int32_t d_h, int32_t page_tokens);
+
+/*
+ * Append rows to a paged cache: token i < n[b] of sequence b becomes its token
+ * start[b] + i, in layers layer .. layer + n_layers - 1.  With theta > 0 the keys
+ * are rotated first (rotate-half, as hf_rope) at position
+ * pos0[b] + start[b] + i; theta == 0 stores them as given (rows of a transferred
+ * cache are rotated already).  Angles are formed in fp64, the rotation and the
+ * codes in fp32 from the rows' own values; a rotated key is not rounded before
+ * it is coded.
+ *   start, n  host int32 [B], >= 0; start[b] + n[b] <= table_stride * page_tokens.
+ *   pos0      host int32 [B] or NULL (0), >= 0.
+ *   k, v      hf_rows of the cache's H and d_h (HF_F32 or HF_BF16, the same).
+ * Rows outside [start, start + n) keep their bits.
+ */
+int32_t hf_paged_append(int32_t B, const int32_t* start, const int32_t* n,
+                        const hf_paged_kv* cache, int32_t layer, int32_t n_layers,
+                        const hf_rows* k, const hf_rows* v, double theta, const int32_t* pos0,
+                        void* stream);
+
+/*
+ * The values that tokens [start[b], start[b] + n[b]) of layers
+ * layer .. layer + n_layers - 1 stand for, as dense rows (row i is token
+ * start[b] + i): s * code + o in fp32, rounded once for HF_BF16.  Arguments as
+ * hf_paged_append; k and v are written.
+ */
+int32_t hf_paged_read(int32_t B, const int32_t* start, const int32_t* n, const hf_paged_kv* cache,
+                      int32_t layer, int32_t n_layers, const hf_rows* k, const hf_rows* v,
+                      void* stream);
+
+/*
+ * hf_prompt_attention over the first kv_len[b] tokens of one layer of a paged
+ * cache, for decoded tokens and short runs (any q_len is served; each 64 query
+ * rows of a group read the cache once more).  Arguments, masks, results and
+ * errors as there; workspace >= hf_attention_workspace_bytes(..., paged = 1).
+ * Numerics: the codes enter the matrix products as whole numbers, exactly, and
+ * scales and offsets are applied in fp32; for HF_BF16 the softmax weights times
+ * a value group's scale are rounded once to bf16, for HF_F32 q and these are
+ * split into three bf16 terms, which hold 24 bits.
+ */
+int32_t hf_paged_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len,
+                           const hf_rows* q, const hf_paged_kv* cache, int32_t layer,
+                           const hf_rows* out, float scale, int32_t causal, float* lse,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Offline construction of the maps (fp64, off the transfer path).           */
 /* ------------------------------------------------------------------------ */
 /*
@@ -518,7 +669,12 @@ typedef enum {
   HF_KERNEL_TRANSFER_STAGE = 8,/* per-tile alignment staging of hf_transfer_kv (bf16, tiled) */
   HF_KERNEL_STAGED_BUILD = 9,  /* staged path: aligned features of every slab to the workspace */
   HF_KERNEL_STAGED_GEMM = 10,  /* staged path: the map products with bias and RoPE */
-  HF_KERNEL_COUNT = 11
+  HF_KERNEL_PROMPT_ATTENTION = 11, /* hf_prompt_attention: the attention kernel */
+  HF_KERNEL_PAGED_ATTENTION = 12,  /* hf_paged_attention: the attention kernel */
+  HF_KERNEL_ATTENTION_JOIN = 13,   /* both: joining the parts of split key ranges */
+  HF_KERNEL_PAGED_APPEND = 14,     /* hf_paged_append */
+  HF_KERNEL_PAGED_READ = 15,       /* hf_paged_read */
+  HF_KERNEL_COUNT = 16
 } hf_kernel_id;
 
 /*

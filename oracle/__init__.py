@@ -19,9 +19,11 @@ Everything here is written to be checked against the paper by eye:
 * ``recolor``    -- the offline construction of those maps: sender RMS (Eq. 3),
   weighted moments, whitening + Procrustes (Eq. 4), Recolor (Eq. 5), and the
   low-rank correction folded into the map (Eq. 9).
+* ``attention``  -- attention with a causal mask and grouped heads, and the 4-bit
+  rows of the paged cache.
 
 Integer results are exact.  Floating-point results are fp64 computed from the
 exact stored input values (bf16 or fp32 widened to fp64).
 """
 
-from . import alignment, layer_map, recolor, rope, transfer  # noqa: F401
+from . import alignment, attention, layer_map, recolor, rope, transfer  # noqa: F401

@@ -763,6 +763,370 @@ int32_t hf_transfer_kv_taps(int32_t B, const int32_t* s_len, const int32_t* r_le
 }
 
 // ---------------------------------------------------------------------------
+// Attention and the paged cache.
+// ---------------------------------------------------------------------------
+
+namespace {
+
+int32_t check_lens(int32_t B, const char* na, const int32_t* a, const char* nb, const int32_t* b) {
+  if (B < 1 || B > HF_MAX_BATCH) return fail(HF_ERR_SHAPE, "B=%d outside [1, %d]", B, HF_MAX_BATCH);
+  if (!a || !b) return fail(HF_ERR_NULL, "%s / %s is NULL", na, nb);
+  for (int i = 0; i < B; ++i)
+    if (a[i] < 0 || b[i] < 0) return fail(HF_ERR_SHAPE, "negative %s or %s of sequence %d", na, nb, i);
+  return HF_OK;
+}
+
+// used: some row of it is read or written.  layers: stride_l is used.
+int32_t check_rows(const char* name, const hf_rows* r, int32_t B, bool used, bool written,
+                   bool layers) {
+  if (!r) return fail(HF_ERR_NULL, "%s is NULL", name);
+  if (r->dtype != HF_F32 && r->dtype != HF_BF16) return fail(HF_ERR_DTYPE, "%s->dtype %d unknown", name, r->dtype);
+  if (r->H < 1 || r->d_h < 1) return fail(HF_ERR_SHAPE, "%s: need H >= 1 and d_h >= 1", name);
+  const int64_t vec = r->dtype == HF_BF16 ? 8 : 4;  // elements per 16 bytes
+  if (used && !r->ptr) return fail(HF_ERR_NULL, "%s->ptr is NULL", name);
+  if (!aligned16(r->ptr)) return fail(HF_ERR_SHAPE, "%s->ptr is not 16-byte aligned", name);
+  const int64_t st[3] = {r->stride_t, r->stride_h, layers ? r->stride_l : 0};
+  for (int64_t x : st)
+    if (x < 0 || x % vec)
+      return fail(HF_ERR_SHAPE, "%s: strides must be >= 0 and keep rows 16-byte aligned", name);
+  if (written && (r->stride_t < r->d_h || (r->H > 1 && r->stride_h < r->d_h)))
+    return fail(HF_ERR_SHAPE, "%s: rows that are written need stride_t and stride_h >= d_h", name);
+  if (r->seq_off)
+    for (int b = 0; b < B; ++b)
+      if (r->seq_off[b] < 0 || r->seq_off[b] % vec)
+        return fail(HF_ERR_SHAPE, "%s: seq_off[%d] must be >= 0 and keep rows 16-byte aligned", name, b);
+  return HF_OK;
+}
+
+// Element offsets of the sequences' first rows.
+void offsets(const hf_rows* r, int32_t B, const int32_t* len, int64_t* off) {
+  int64_t at = 0;
+  for (int b = 0; b < B; ++b) {
+    off[b] = r->seq_off ? r->seq_off[b] : at * r->stride_t;
+    at += len[b];
+  }
+}
+
+// Cuts the batch into work items and long key ranges into parts.  A part is as long
+// as the whole work over the workgroups that fill the chip, so that the parts of one
+// launch take about equally long; a range that needs no cutting has one part.
+int32_t plan_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len, int32_t H_q,
+                       int32_t H, int32_t dtype, int32_t d_h, bool paged, int32_t causal,
+                       hf::AttnShape& sh, hf::AttnSeqs& s, int64_t& slots) {
+  std::memset(&s, 0, sizeof s);
+  const int32_t G = H_q / H;
+  int64_t max_rows = 0, total = 0;
+  for (int b = 0; b < B; ++b) {
+    max_rows = std::max(max_rows, (int64_t)q_len[b] * G);
+    total += q_len[b];
+  }
+  if (total > INT32_MAX || max_rows > INT32_MAX - 1024 || total * H_q > ((int64_t)1 << 40))
+    return fail(HF_ERR_SHAPE, "too many query rows");
+  sh = paged ? hf::paged_shape(dtype, d_h, max_rows) : hf::prompt_shape(dtype, d_h, max_rows);
+  int64_t work = 0;  // keys, summed over the row tiles
+  for (int b = 0; b < B; ++b) {
+    const int64_t tiles = ((int64_t)q_len[b] * G + sh.rows - 1) / sh.rows;
+    // (a causal prompt's tiles see half of its keys on average)
+    const int64_t seen = causal && q_len[b] > 0 ? std::max<int64_t>(kv_len[b] - q_len[b] / 2, (kv_len[b] + 1) / 2) : kv_len[b];
+    work += tiles * seen * H;
+  }
+  int64_t chunk = (work + sh.wg_target - 1) / sh.wg_target;
+  chunk = std::max<int64_t>((chunk + sh.step - 1) / sh.step * sh.step, 2 * sh.step);
+  s.chunk = (int32_t)std::min<int64_t>(chunk, INT32_MAX / 2 / sh.step * sh.step);
+  s.B = B;
+  s.H = H;
+  s.G = G;
+  s.causal = causal ? 1 : 0;
+  int64_t items = 0, row = 0, split = 0;
+  slots = 0;
+  for (int b = 0; b < B; ++b) {
+    const int64_t rows = (int64_t)q_len[b] * G;
+    const int64_t tiles = (rows + sh.rows - 1) / sh.rows;
+    int64_t parts = std::max<int64_t>((kv_len[b] + (int64_t)s.chunk - 1) / s.chunk, 1);
+    s.n[b] = q_len[b];
+    s.t[b] = kv_len[b];
+    s.row0[b] = (int32_t)row;
+    s.parts[b] = (int32_t)parts;
+    s.item0[b] = (int32_t)items;
+    s.split0[b] = (int32_t)split;
+    s.part0[b] = (int32_t)slots;
+    items += tiles * parts;
+    row += q_len[b];
+    if (parts > 1) {
+      split += rows * H;
+      slots += rows * H * parts;
+    }
+    if (items * H > INT32_MAX || split > INT32_MAX || slots > INT32_MAX)
+      return fail(HF_ERR_SHAPE, "too many work items");
+  }
+  s.item0[B] = (int32_t)items;
+  s.split0[B] = (int32_t)split;
+  return HF_OK;
+}
+
+size_t part_bytes(int64_t slots, int32_t d_h) {
+  return slots ? align_up((size_t)slots * d_h * 4, 256) + align_up((size_t)slots * 8, 256) : 0;
+}
+
+int32_t check_heads(int32_t H_q, int32_t H, int32_t d_h) {
+  if (H < 1 || H_q < 1 || H_q % H) return fail(HF_ERR_SHAPE, "need H >= 1 and H_q a multiple of H (got %d, %d)", H, H_q);
+  if (d_h != 64 && d_h != 128) return fail(HF_ERR_UNSUPPORTED, "attention needs d_h 64 or 128 (got %d)", d_h);
+  return HF_OK;
+}
+
+// What both attention calls check of their queries and results, and the plan.
+int32_t attention_common(int32_t B, const int32_t* q_len, const int32_t* kv_len, const hf_rows* q,
+                         const hf_rows* out, int32_t H, int32_t d_h, float scale, int32_t causal,
+                         float* lse, bool paged, void* workspace, size_t workspace_bytes,
+                         hf::AttnShape& sh, hf::AttnSeqs& s, hf::AttnIO& io) {
+  int64_t rows = 0;
+  for (int b = 0; b < B; ++b) rows += q_len[b];
+  int32_t st;
+  if ((st = check_rows("q", q, B, rows > 0, false, false)) ||
+      (st = check_rows("out", out, B, rows > 0, true, false)))
+    return st;
+  if (q->dtype != out->dtype) return fail(HF_ERR_DTYPE, "q and out dtypes differ");
+  if (q->H != out->H || q->d_h != out->d_h || q->d_h != d_h)
+    return fail(HF_ERR_SHAPE, "q, out and the cache differ in heads or d_h");
+  if ((st = check_heads(q->H, H, d_h))) return st;
+  if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(HF_ERR_SHAPE, "scale must be finite and > 0");
+  if (reinterpret_cast<uintptr_t>(lse) & 3u) return fail(HF_ERR_SHAPE, "lse not 4-byte aligned");
+  int64_t slots = 0;
+  if ((st = plan_attention(B, q_len, kv_len, q->H, H, q->dtype, d_h, paged, causal, sh, s, slots)))
+    return st;
+  offsets(q, B, q_len, s.q_off);
+  offsets(out, B, q_len, s.o_off);
+  std::memset(&io, 0, sizeof io);
+  if (slots) {
+    const size_t need = part_bytes(slots, d_h);
+    if (!workspace) return fail(HF_ERR_NULL, "workspace is NULL");
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u)
+      return fail(HF_ERR_SHAPE, "workspace is not 256-byte aligned");
+    if (workspace_bytes < need)
+      return fail(HF_ERR_CAPACITY, "workspace %zu bytes < required %zu", workspace_bytes, need);
+    io.part = static_cast<float*>(workspace);
+    io.ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + align_up((size_t)slots * d_h * 4, 256));
+  }
+  io.q = q->ptr;
+  io.out = out->ptr;
+  io.lse = lse;
+  io.q_st = q->stride_t;
+  io.q_sh = q->stride_h;
+  io.o_st = out->stride_t;
+  io.o_sh = out->stride_h;
+  io.c = scale * 1.44269504088896340736f;
+  return HF_OK;
+}
+
+int32_t join_parts(int32_t dtype, int32_t d_h, const hf::AttnIO& io, const hf::AttnSeqs& s,
+                   hipStream_t st) {
+  if (s.split0[s.B] == 0) return ok();
+  hipError_t e;
+  {
+    TimedLaunch t(HF_KERNEL_ATTENTION_JOIN, st);
+    e = hf::launch_attention_join(dtype, d_h, io, s, st);
+  }
+  if (e != hipSuccess) return hip_fail(e, "attention join launch");
+  return ok();
+}
+
+// page_bytes, 0 on bad arguments.
+size_t page_bytes(int32_t H, int32_t d_h, int32_t P) {
+  if (H < 1 || H > 65536 || (d_h != 64 && d_h != 128) || (P != 32 && P != 64 && P != 128 && P != 256)) return 0;
+  return (size_t)H * P * (d_h + d_h / 4);
+}
+
+int32_t check_paged(const hf_paged_kv* c, int32_t layer, int32_t n_layers) {
+  if (!c) return fail(HF_ERR_NULL, "cache is NULL");
+  if (c->L < 1 || c->H < 1 || c->H > 65536 || c->n_pages < 1)
+    return fail(HF_ERR_SHAPE, "cache: need L >= 1, 1 <= H <= 65536, n_pages >= 1");
+  if (c->d_h != 64 && c->d_h != 128) return fail(HF_ERR_UNSUPPORTED, "cache: d_h must be 64 or 128 (got %d)", c->d_h);
+  if (page_bytes(c->H, c->d_h, c->page_tokens) == 0)
+    return fail(HF_ERR_SHAPE, "cache: page_tokens must be 32, 64, 128 or 256 (got %d)", c->page_tokens);
+  if (!c->pages || !c->table) return fail(HF_ERR_NULL, "cache: pages or table is NULL");
+  if (!aligned16(c->pages)) return fail(HF_ERR_SHAPE, "cache: pages not 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(c->table) & 3u) return fail(HF_ERR_SHAPE, "cache: table not 4-byte aligned");
+  if (c->table_stride < 0) return fail(HF_ERR_SHAPE, "cache: table_stride must be >= 0");
+  if (layer < 0 || n_layers < 1 || layer > c->L - n_layers)
+    return fail(HF_ERR_SHAPE, "layers [%d, %d + %d) outside the cache's %d", layer, layer, n_layers, c->L);
+  return HF_OK;
+}
+
+int log2_of(int32_t p) {
+  int k = 0;
+  while ((1 << k) < p) ++k;
+  return k;
+}
+
+int32_t paged_rows(bool append, int32_t B, const int32_t* start, const int32_t* n,
+                   const hf_paged_kv* cache, int32_t layer, int32_t n_layers, const hf_rows* k,
+                   const hf_rows* v, double theta, const int32_t* pos0, void* stream) {
+  int32_t st;
+  if ((st = check_lens(B, "start", start, "n", n)) || (st = check_paged(cache, layer, n_layers))) return st;
+  int64_t total = 0;
+  for (int b = 0; b < B; ++b) total += n[b];
+  if ((st = check_rows("k", k, B, total > 0, !append, true)) ||
+      (st = check_rows("v", v, B, total > 0, !append, true)))
+    return st;
+  if (k->dtype != v->dtype) return fail(HF_ERR_DTYPE, "k and v dtypes differ");
+  if (k->H != cache->H || v->H != cache->H || k->d_h != cache->d_h || v->d_h != cache->d_h)
+    return fail(HF_ERR_SHAPE, "k, v and the cache differ in heads or d_h");
+  if (!(theta >= 0.0) || !std::isfinite(theta)) return fail(HF_ERR_SHAPE, "theta must be finite and >= 0");
+  if (n_layers > 65535) return fail(HF_ERR_SHAPE, "too many layers");
+  hf::PagedRowsArgs a;
+  std::memset(&a, 0, sizeof a);
+  int64_t blocks = 0;
+  for (int b = 0; b < B; ++b) {
+    const int64_t end = (int64_t)start[b] + n[b];
+    const int64_t p0 = pos0 ? pos0[b] : 0;
+    if (p0 < 0) return fail(HF_ERR_SHAPE, "start positions must be >= 0");
+    if (p0 + end > INT32_MAX - 64) return fail(HF_ERR_SHAPE, "positions overflow int32");
+    // (compared in pages: the table's tokens may pass 64 bits)
+    if (n[b] > 0 && (end + cache->page_tokens - 1) / cache->page_tokens > cache->table_stride)
+      return fail(HF_ERR_CAPACITY, "sequence %d: %lld tokens, the table has %lld pages of %d", b,
+                  (long long)end, (long long)cache->table_stride, cache->page_tokens);
+    a.start[b] = start[b];
+    a.n[b] = n[b];
+    a.pos0[b] = (int32_t)p0;
+    a.blk0[b] = (int32_t)blocks;
+    if (n[b] > 0) blocks += (end - 1) / 32 - start[b] / 32 + 1;
+    if (blocks * cache->H > INT32_MAX) return fail(HF_ERR_SHAPE, "too many rows");
+  }
+  a.blk0[B] = (int32_t)blocks;
+  if (blocks == 0) return ok();
+  offsets(k, B, n, a.k_off);
+  offsets(v, B, n, a.v_off);
+  a.k = k->ptr;
+  a.v = v->ptr;
+  a.k_st = k->stride_t; a.k_sh = k->stride_h; a.k_sl = k->stride_l;
+  a.v_st = v->stride_t; a.v_sh = v->stride_h; a.v_sl = v->stride_l;
+  a.page_bytes = (long long)page_bytes(cache->H, cache->d_h, cache->page_tokens);
+  a.pages = static_cast<uint8_t*>(cache->pages) + (int64_t)layer * cache->n_pages * a.page_bytes;
+  a.table = cache->table;
+  a.table_stride = cache->table_stride;
+  a.n_pages = cache->n_pages;
+  a.log2_page = log2_of(cache->page_tokens);
+  a.B = B;
+  a.H = cache->H;
+  a.n_layers = n_layers;
+  a.rotate = append && theta > 0.0;
+  if (a.rotate)
+    for (int i = 0; i < cache->d_h / 2; ++i) a.w[i] = std::pow(theta, -2.0 * i / cache->d_h);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  {
+    TimedLaunch t(append ? HF_KERNEL_PAGED_APPEND : HF_KERNEL_PAGED_READ, s);
+    e = append ? hf::launch_paged_append(k->dtype, cache->d_h, a, s)
+               : hf::launch_paged_read(k->dtype, cache->d_h, a, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, append ? "paged append launch" : "paged read launch");
+  return ok();
+}
+
+}  // namespace
+
+size_t hf_attention_workspace_bytes(int32_t B, const int32_t* q_len, const int32_t* kv_len,
+                                    int32_t H_q, int32_t H, int32_t d_h, int32_t dtype,
+                                    int32_t paged) {
+  if (check_lens(B, "q_len", q_len, "kv_len", kv_len) || check_heads(H_q, H, d_h)) return 0;
+  if (dtype != HF_F32 && dtype != HF_BF16) return 0;
+  hf::AttnShape sh;
+  hf::AttnSeqs s;
+  size_t most = 0;
+  for (int causal = 0; causal < 2; ++causal) {  // (the cutting depends on it)
+    int64_t slots = 0;
+    if (plan_attention(B, q_len, kv_len, H_q, H, dtype, d_h, paged != 0, causal, sh, s, slots)) return 0;
+    most = std::max(most, part_bytes(slots, d_h));
+  }
+  ok();
+  return most;
+}
+
+int32_t hf_prompt_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len,
+                            const hf_rows* q, const hf_rows* k, const hf_rows* v,
+                            const hf_rows* out, float scale, int32_t causal, float* lse,
+                            void* workspace, size_t workspace_bytes, void* stream) {
+  int32_t st;
+  if ((st = check_lens(B, "q_len", q_len, "kv_len", kv_len))) return st;
+  int64_t keys = 0;
+  for (int b = 0; b < B; ++b) keys += q_len[b] > 0 ? kv_len[b] : 0;
+  if ((st = check_rows("k", k, B, keys > 0, false, false)) ||
+      (st = check_rows("v", v, B, keys > 0, false, false)))
+    return st;
+  if (k->H != v->H || k->d_h != v->d_h) return fail(HF_ERR_SHAPE, "k and v differ in heads or d_h");
+  hf::AttnShape sh;
+  hf::AttnArgs a;
+  if ((st = attention_common(B, q_len, kv_len, q, out, k->H, k->d_h, scale, causal, lse, false,
+                             workspace, workspace_bytes, sh, a.s, a.io)))
+    return st;
+  if (k->dtype != v->dtype || k->dtype != q->dtype) return fail(HF_ERR_DTYPE, "q, k and v dtypes differ");
+  a.k = k->ptr;
+  a.v = v->ptr;
+  a.k_st = k->stride_t; a.k_sh = k->stride_h;
+  a.v_st = v->stride_t; a.v_sh = v->stride_h;
+  offsets(k, B, kv_len, a.k_off);
+  offsets(v, B, kv_len, a.v_off);
+  if (a.s.item0[B] == 0) return ok();
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  {
+    TimedLaunch t(HF_KERNEL_PROMPT_ATTENTION, s);
+    e = hf::launch_prompt_attention(q->dtype, k->d_h, sh, a, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "attention launch");
+  return join_parts(q->dtype, k->d_h, a.io, a.s, s);
+}
+
+int32_t hf_paged_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len,
+                           const hf_rows* q, const hf_paged_kv* cache, int32_t layer,
+                           const hf_rows* out, float scale, int32_t causal, float* lse,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+  int32_t st;
+  if ((st = check_lens(B, "q_len", q_len, "kv_len", kv_len)) || (st = check_paged(cache, layer, 1))) return st;
+  for (int b = 0; b < B; ++b)
+    if (q_len[b] > 0 && ((int64_t)kv_len[b] + cache->page_tokens - 1) / cache->page_tokens > cache->table_stride)
+      return fail(HF_ERR_CAPACITY, "sequence %d: %d tokens, the table has %lld pages of %d", b,
+                  kv_len[b], (long long)cache->table_stride, cache->page_tokens);
+  hf::AttnShape sh;
+  hf::PagedAttnArgs a;
+  if ((st = attention_common(B, q_len, kv_len, q, out, cache->H, cache->d_h, scale, causal, lse, true,
+                             workspace, workspace_bytes, sh, a.s, a.io)))
+    return st;
+  a.page_bytes = (long long)page_bytes(cache->H, cache->d_h, cache->page_tokens);
+  a.pages = static_cast<const uint8_t*>(cache->pages) + (int64_t)layer * cache->n_pages * a.page_bytes;
+  a.table = cache->table;
+  a.table_stride = cache->table_stride;
+  a.n_pages = cache->n_pages;
+  a.log2_page = log2_of(cache->page_tokens);
+  if (a.s.item0[B] == 0) return ok();
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  {
+    TimedLaunch t(HF_KERNEL_PAGED_ATTENTION, s);
+    e = hf::launch_paged_attention(q->dtype, cache->d_h, sh, a, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "paged attention launch");
+  return join_parts(q->dtype, cache->d_h, a.io, a.s, s);
+}
+
+size_t hf_paged_page_bytes(int32_t H, int32_t d_h, int32_t page_tokens) {
+  return page_bytes(H, d_h, page_tokens);
+}
+
+int32_t hf_paged_append(int32_t B, const int32_t* start, const int32_t* n,
+                        const hf_paged_kv* cache, int32_t layer, int32_t n_layers,
+                        const hf_rows* k, const hf_rows* v, double theta, const int32_t* pos0,
+                        void* stream) {
+  return paged_rows(true, B, start, n, cache, layer, n_layers, k, v, theta, pos0, stream);
+}
+
+int32_t hf_paged_read(int32_t B, const int32_t* start, const int32_t* n, const hf_paged_kv* cache,
+                      int32_t layer, int32_t n_layers, const hf_rows* k, const hf_rows* v,
+                      void* stream) {
+  return paged_rows(false, B, start, n, cache, layer, n_layers, k, v, 0.0, nullptr, stream);
+}
+
+// ---------------------------------------------------------------------------
 // Offline map construction.
 // ---------------------------------------------------------------------------
 

@@ -1,0 +1,662 @@
+// Attention over dense keys and values: whole prompts, suffixes over a transferred
+// cache, single tokens.
+//
+//   out_i = sum_j exp(s_ij - m_i) v_j / sum_j exp(s_ij - m_i),  s_ij = scale <q_i, k_j>
+//
+// in one pass over the keys with a running maximum and sum (a row's sums are
+// rescaled when its maximum is raised).  A wave owns a block of query rows and
+// computes S^T = K Q^T, so that a lane holds scores of one row: the row's maximum
+// and sum are sums over the lane's registers and one or two exchanges between
+// lanes, and the weights, as they lie in the result registers, are the operand of
+// the second product O^T = V^T P^T when V^T is read with its keys in the same
+// order.  So weights never leave the registers.
+//
+// Keys and values stream through two LDS stages filled by global-to-LDS loads, the
+// next tile's in flight while the current one is multiplied.
+//
+// Two kernel shapes, chosen by the number of query rows (prompt_shape):
+//  - by rows: the waves of a workgroup share a tile of keys, each with query rows
+//    of its own;
+//  - by keys: the waves share the rows (one block) and deal the tiles of keys among
+//    them, each with LDS stages of its own and no barrier in the loop; their
+//    results are joined in LDS at the end.  For single tokens and short runs, which
+//    the reading of the keys bounds.
+// Where the workgroups are too few to fill the chip the key range is cut into parts
+// as well, joined by attention_join_kernel.
+#include <hip/hip_runtime.h>
+
+#include "hf_attn.h"
+
+namespace hf {
+namespace {
+
+// ---------------------------------------------------------------------------
+// Operand layouts of one wave's tile: RW query rows against KT keys.
+// ---------------------------------------------------------------------------
+
+// bf16 on v_mfma_f32_32x32x16_bf16: lane l is row l % 32; with h = l / 32, result
+// register i of a 32-key block is key 8 (i / 4) + 4 h + i % 4, and of a 32-channel
+// block the channel of that number.
+template <int D_, int KT_>
+struct Bf16Tile {
+  static constexpr int D = D_, KT = KT_;
+  static constexpr int RW = 32;
+  static constexpr int NS = KT / 2, NO = D / 2;  // score and output registers
+  static constexpr int ROWB = D * 2;             // bytes of a row
+  typedef uint16_t T;
+  struct Q {
+    bf16x8 f[D / 16];
+  };
+
+  FI static int row(int lane) { return lane & 31; }
+  FI static int key(int lane, int i) { return 32 * (i / 16) + 8 * ((i & 15) >> 2) + 4 * (lane >> 5) + (i & 3); }
+  FI static int channel(int lane, int i) { return key(lane, i); }
+  FI static float across(float x, float (*op)(float, float)) { return op(x, __shfl_xor(x, 32)); }
+
+  // Where 16-byte chunk c of row r lies in a stage.  Keys are read 16 bytes a lane
+  // by 32 rows at once, values 32 bytes of 8 rows at once (transposing reads); the
+  // two exclusive-or orders put either on distinct banks.
+  FI static int slot_k(int r, int c) { return c ^ (D == 128 ? r & 15 : (r >> 1) & 7); }
+  FI static int slot_v(int r, int c) { return c ^ (2 * (D == 128 ? r & 7 : (r >> 1) & 3)); }
+
+  FI static void load_q(Q& q, const T* row, int lane) {
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c)
+      q.f[c] = *reinterpret_cast<const bf16x8*>(row + 16 * c + 8 * (lane >> 5));
+  }
+
+  FI static void scores(const Q& q, const unsigned char* sk, int lane, float (&s)[NS]) {
+    const int r = lane & 31;
+#pragma unroll
+    for (int kb = 0; kb < KT / 32; ++kb) {
+      f32x16 acc = {};
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) {
+        const bf16x8 a = *reinterpret_cast<const bf16x8*>(
+            sk + kb * 32 * ROWB + r * ROWB + slot_k(r, 2 * c + (lane >> 5)) * 16);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q.f[c], acc, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[16 * kb + i] = acc[i];
+    }
+  }
+
+  // O += V^T P^T.  CLEAN: values that are not finite enter as 0 (the masked tiles'
+  // slow path).
+  template <bool CLEAN>
+  FI static void values(f32x16 (&o)[D / 32], const unsigned char* sv, int lane,
+                        const float (&p)[NS]) {
+    // the transposing read gives lane i of 16 the values of 4 rows at channel i; its
+    // lane i names row i / 4 of them and 8 bytes there
+    const int h = lane >> 5, gb = (lane >> 4) & 1, i = lane & 15;
+    const int r = 4 * h + (i >> 2);
+#pragma unroll
+    for (int c = 0; c < KT / 16; ++c) {
+      union {
+        bf16x8 v;
+        uint32_t u[4];
+      } b;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) b.u[x] = pack_bf16(p[8 * c + 2 * x], p[8 * c + 2 * x + 1]);
+#pragma unroll
+      for (int n = 0; n < D / 32; ++n) {
+        const unsigned char* at = sv + (16 * c + r) * ROWB + slot_v(r, 4 * n + 2 * gb) * 16 + (i & 3) * 8;
+        union {
+          bf16x8 v;
+          s16x4 s[2];
+          uint32_t u[4];
+        } a;
+        a.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)at);
+        a.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(at + 8 * ROWB));
+        if (CLEAN) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            if ((a.u[x] & 0x7f80u) == 0x7f80u) a.u[x] &= 0xffff0000u;
+            if ((a.u[x] & 0x7f800000u) == 0x7f800000u) a.u[x] &= 0xffffu;
+          }
+        }
+        o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, o[n], 0, 0, 0);
+      }
+    }
+  }
+
+  FI static float value_at(const unsigned char* sv, int r, int ch) {
+    const uint16_t x = *reinterpret_cast<const uint16_t*>(sv + r * ROWB + slot_v(r, ch >> 3) * 16 + (ch & 7) * 2);
+    return __builtin_bit_cast(float, (uint32_t)x << 16);
+  }
+  FI static bool any_not_finite(u32x4 x) {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      bad = bad || (x[i] & 0x7f80u) == 0x7f80u || (x[i] & 0x7f800000u) == 0x7f800000u;
+    return bad;
+  }
+  typedef f32x16 O[D / 32];
+  FI static float get(const O& o, int i) { return o[i / 16][i & 15]; }
+  FI static void set(O& o, int i, float x) { o[i / 16][i & 15] = x; }
+  FI static void store4(T* p, const float (&x)[4]) {
+    const u32x2 v = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+    *reinterpret_cast<u32x2*>(p) = v;
+  }
+};
+
+// fp32 on v_mfma_f32_16x16x4_f32: lane l is row l % 16; with m = l / 16, result
+// register i of a 16-key (16-channel) block is key (channel) 4 m + i.  Step (u, j)
+// of the first product takes channel 16 u + 4 m + j, so that a lane's operands are
+// 16-byte loads; step i of the second takes key 4 m + i, so that the scores'
+// registers are its operands as they are.
+template <int D_, int KT_>
+struct F32Tile {
+  static constexpr int D = D_, KT = KT_;
+  static constexpr int RW = 16;
+  static constexpr int NS = KT / 4, NO = D / 4;
+  static constexpr int ROWB = D * 4;
+  typedef float T;
+  struct Q {
+    f32x4 f[D / 16];
+  };
+
+  FI static int row(int lane) { return lane & 15; }
+  FI static int key(int lane, int i) { return 16 * (i / 4) + 4 * (lane >> 4) + (i & 3); }
+  FI static int channel(int lane, int i) { return key(lane, i); }
+  FI static float across(float x, float (*op)(float, float)) {
+    x = op(x, __shfl_xor(x, 16));
+    return op(x, __shfl_xor(x, 32));
+  }
+
+  FI static int slot_k(int r, int c) { return c ^ (r & 15); }
+  FI static int slot_v(int r, int c) { return c ^ (((r >> 2) & 3) << 2); }
+
+  FI static void load_q(Q& q, const T* row, int lane) {
+#pragma unroll
+    for (int u = 0; u < D / 16; ++u)
+      q.f[u] = *reinterpret_cast<const f32x4*>(row + 16 * u + 4 * (lane >> 4));
+  }
+
+  FI static void scores(const Q& q, const unsigned char* sk, int lane, float (&s)[NS]) {
+    const int r = lane & 15;
+#pragma unroll
+    for (int kb = 0; kb < KT / 16; ++kb) {
+      f32x4 acc = {};
+#pragma unroll
+      for (int u = 0; u < D / 16; ++u) {
+        const f32x4 a = *reinterpret_cast<const f32x4*>(
+            sk + (kb * 16 + r) * ROWB + slot_k(r, 4 * u + (lane >> 4)) * 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], q.f[u][j], acc, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[4 * kb + i] = acc[i];
+    }
+  }
+
+  template <bool CLEAN>
+  FI static void values(f32x4 (&o)[D / 16], const unsigned char* sv, int lane,
+                        const float (&p)[NS]) {
+    const int m = lane >> 4, c = lane & 15;
+#pragma unroll
+    for (int x = 0; x < NS; ++x) {
+      const int r = 16 * (x / 4) + 4 * m + (x & 3);
+#pragma unroll
+      for (int n = 0; n < D / 16; ++n) {
+        float a = *reinterpret_cast<const float*>(sv + r * ROWB + slot_v(r, 4 * n + (c >> 2)) * 16 + (c & 3) * 4);
+        if (CLEAN) a = finite_bits(a) ? a : 0.0f;
+        o[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, p[x], o[n], 0, 0, 0);
+      }
+    }
+  }
+
+  FI static float value_at(const unsigned char* sv, int r, int ch) {
+    return *reinterpret_cast<const float*>(sv + r * ROWB + slot_v(r, ch >> 2) * 16 + (ch & 3) * 4);
+  }
+  FI static bool any_not_finite(u32x4 x) {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bad = bad || (x[i] & 0x7f800000u) == 0x7f800000u;
+    return bad;
+  }
+  typedef f32x4 O[D / 16];
+  FI static float get(const O& o, int i) { return o[i / 4][i & 3]; }
+  FI static void set(O& o, int i, float x) { o[i / 4][i & 3] = x; }
+  FI static void store4(T* p, const float (&x)[4]) {
+    const f32x4 v = {x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<f32x4*>(p) = v;
+  }
+};
+
+FI float op_max(float a, float b) { return fmaxf(a, b); }
+FI float op_add(float a, float b) { return a + b; }
+
+// ---------------------------------------------------------------------------
+// One tile of keys against a wave's rows.
+// ---------------------------------------------------------------------------
+template <class P>
+struct Rows {
+  typename P::Q q;
+  typename P::O o;
+  float m, l;    // the row's maximum; this lane's share of its weight
+  int last;      // the last key the row sees
+};
+
+// MASK: some row of the wave does not see every key of the tile (t0 is its first).
+template <class P, bool MASK>
+FI void attend(Rows<P>& w, const unsigned char* sk, const unsigned char* sv, int lane, float c,
+               int t0) {
+  float s[P::NS];
+  P::scores(w.q, sk, lane, s);
+  if (MASK) {
+#pragma unroll
+    for (int i = 0; i < P::NS; ++i)
+      if (t0 + P::key(lane, i) > w.last) s[i] = -INFINITY;
+  }
+  float mx = s[0];
+#pragma unroll
+  for (int i = 1; i < P::NS; ++i) mx = fmaxf(mx, s[i]);
+  mx = P::across(mx, op_max) * c;
+  if (__any(mx > w.m + kRaise)) {
+    const float m = mx > w.m + kRaise ? mx : w.m;  // (each row by its own scores alone)
+    const float f = __builtin_amdgcn_exp2f(w.m - m);
+    w.m = m;
+    w.l *= f;
+#pragma unroll
+    for (int i = 0; i < P::NO; ++i) P::set(w.o, i, P::get(w.o, i) * f);
+  }
+#pragma unroll
+  for (int i = 0; i < P::NS; ++i) {
+    s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -w.m));
+    w.l += s[i];
+  }
+  if (!MASK) {
+    P::template values<false>(w.o, sv, lane, s);
+    return;
+  }
+  // In a tile that some rows see only in part a value that is not finite must reach
+  // the rows that see it and no other: 0 * NaN would.  It enters the product as 0
+  // and is added to the rows that see its key.  (Everywhere else all rows see all
+  // keys, and the product does what it should.)
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < P::KT * P::ROWB / 1024; ++i)
+    bad = bad || P::any_not_finite(*reinterpret_cast<const u32x4*>(sv + i * 1024 + lane * 16));
+  if (!__any(bad)) {
+    P::template values<false>(w.o, sv, lane, s);
+    return;
+  }
+  P::template values<true>(w.o, sv, lane, s);
+  for (int r = 0; r < P::KT && t0 + r <= w.last; ++r) {
+#pragma unroll
+    for (int i = 0; i < P::NO; ++i) {
+      const float x = P::value_at(sv, r, P::channel(lane, i));
+      if (!finite_bits(x)) P::set(w.o, i, P::get(w.o, i) + x);
+    }
+  }
+}
+
+// Loads of one tile (keys t0 .. t0 + KT) into a stage: NB of the tile's 1 KB blocks
+// from block b0 in steps of `bstep`.  Rows past the last key hold copies of it.
+template <class P, bool V, int NB>
+FI void fetch(const typename P::T* base, long long st, int t0, int t, unsigned char* stage, int b0,
+              int bstep, int lane) {
+  constexpr int CPR = P::ROWB / 16;  // chunks a row
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    const int blk = b0 + i * bstep;
+    const int r = blk * (64 / CPR) + lane / CPR, slot = lane % CPR;
+    const int c = V ? P::slot_v(r, slot) : P::slot_k(r, slot);  // (each its own inverse)
+    const int row = min(t0 + r, t - 1);
+    __builtin_amdgcn_global_load_lds(
+        (const void*)(base + (long long)row * st + c * (16 / (int)sizeof(typename P::T))),
+        (lds_void_t*)(stage + blk * 1024), 16, 0, 0);
+  }
+}
+
+// Row r of a sequence: its token and head within the group.
+FI void place(int r, int G, int& token, int& g) {
+  token = r / G;
+  g = r - token * G;
+}
+
+// The result of a finished row, or its part.
+template <class P>
+FI void write_row(const AttnIO& io, const AttnSeqs& s, int b, int h, int part, int r, float m,
+                  float l, const typename P::O& o, int lane) {
+  typedef typename P::T T;
+  int token, g;
+  place(r, s.G, token, g);
+  const bool lead = lane < P::RW;  // one lane of the row's
+  if (s.parts[b] == 1) {
+    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+    T* out = static_cast<T*>(io.out) + s.o_off[b] + (long long)token * io.o_st +
+             (long long)(h * s.G + g) * io.o_sh;
+#pragma unroll
+    for (int i = 0; i < P::NO; i += 4) {
+      float x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = P::get(o, i + j) * inv;
+      P::store4(out + P::channel(lane, i), x);
+    }
+    if (lead && io.lse)
+      io.lse[(long long)(s.row0[b] + token) * (s.H * s.G) + h * s.G + g] =
+          l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    return;
+  }
+  const long long slot =
+      s.part0[b] + ((long long)h * s.n[b] * s.G + r) * s.parts[b] + part;
+  float* po = io.part + slot * P::D;
+#pragma unroll
+  for (int i = 0; i < P::NO; i += 4) {
+    const f32x4 v = {P::get(o, i), P::get(o, i + 1), P::get(o, i + 2), P::get(o, i + 3)};
+    *reinterpret_cast<f32x4*>(po + P::channel(lane, i)) = v;
+  }
+  if (lead) {
+    io.ml[2 * slot] = m;
+    io.ml[2 * slot + 1] = l;
+  }
+}
+
+template <class P>
+FI void start_rows(Rows<P>& w, const AttnArgs& a, int b, int h, int r, int lane) {
+  typedef typename P::T T;
+  const AttnSeqs& s = a.s;
+  const int n_rows = s.n[b] * s.G;
+  int token, g;
+  place(min(r, n_rows - 1), s.G, token, g);
+  P::load_q(w.q, static_cast<const T*>(a.io.q) + s.q_off[b] + (long long)token * a.io.q_st +
+                     (long long)(h * s.G + g) * a.io.q_sh, lane);
+#pragma unroll
+  for (int i = 0; i < P::NO; ++i) P::set(w.o, i, 0.0f);
+  w.m = kNoMax;
+  w.l = 0.0f;
+  w.last = last_key(s, b, token);
+}
+
+// By rows: NW waves, each RW rows of the tile, all against the same keys.
+template <class P, int NW>
+__global__ __launch_bounds__(NW * 64) void attention_rows_kernel(const AttnArgs a) {
+  typedef typename P::T T;
+  __shared__ __attribute__((aligned(1024))) unsigned char k0[P::KT * P::ROWB];
+  __shared__ __attribute__((aligned(1024))) unsigned char v0[P::KT * P::ROWB];
+  __shared__ __attribute__((aligned(1024))) unsigned char k1[P::KT * P::ROWB];
+  __shared__ __attribute__((aligned(1024))) unsigned char v1[P::KT * P::ROWB];
+  constexpr int NB = P::KT * P::ROWB / 1024 / NW;
+  static_assert(NB * NW * 1024 == P::KT * P::ROWB, "whole blocks a wave");
+
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const AttnSeqs& s = a.s;
+  const AttnItem it = attn_item(s, NW * P::RW);
+  const int b = it.b, t = s.t[b];
+  const int n_rows = s.n[b] * s.G;
+  const int row0 = it.tile * NW * P::RW;
+  Rows<P> w;
+  start_rows<P>(w, a, b, it.h, row0 + wave * P::RW + P::row(lane), lane);
+
+  // keys of this part that some row of the workgroup (of the wave: see masks) sees
+  const int wg_last = last_key(s, b, min(row0 + NW * P::RW - 1, n_rows - 1) / s.G);
+  const int wave_first = last_key(s, b, min(row0 + wave * P::RW, n_rows - 1) / s.G);
+  const int wave_last = last_key(s, b, min(row0 + wave * P::RW + P::RW - 1, n_rows - 1) / s.G);
+  const int lo = it.part * s.chunk;
+  const int hi = min(wg_last + 1, s.parts[b] == 1 ? t : min(t, lo + s.chunk));
+  const T* kb = static_cast<const T*>(a.k) + a.k_off[b] + (long long)it.h * a.k_sh;
+  const T* vb = static_cast<const T*>(a.v) + a.v_off[b] + (long long)it.h * a.v_sh;
+  const float c = a.io.c;
+
+  auto get = [&](int t0, unsigned char* sk, unsigned char* sv) {
+    fetch<P, false, NB>(kb, a.k_st, t0, t, sk, wave, NW, lane);
+    fetch<P, true, NB>(vb, a.v_st, t0, t, sv, wave, NW, lane);
+  };
+  auto step = [&](int t0, unsigned char* sk, unsigned char* sv, unsigned char* nk,
+                  unsigned char* nv) {
+    __builtin_amdgcn_s_waitcnt(wait_vm_only(0));
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();  // the tile is there; the other stage is no longer read
+    asm volatile("" ::: "memory");
+    if (t0 + P::KT < hi) get(t0 + P::KT, nk, nv);
+    if (t0 > wave_last) return;
+    if (t0 + P::KT - 1 > wave_first)
+      attend<P, true>(w, sk, sv, lane, c, t0);
+    else
+      attend<P, false>(w, sk, sv, lane, c, t0);
+  };
+  if (lo < hi) {
+    get(lo, k0, v0);
+    for (int t0 = lo; t0 < hi; t0 += 2 * P::KT) {
+      step(t0, k0, v0, k1, v1);
+      if (t0 + P::KT < hi) step(t0 + P::KT, k1, v1, k0, v0);
+    }
+  }
+  const int r = row0 + wave * P::RW + P::row(lane);
+  const float l = P::across(w.l, op_add);
+  if (r < n_rows) write_row<P>(a.io, s, b, it.h, it.part, r, w.m, l, w.o, lane);
+}
+
+// By keys: one block of RW rows, the tiles of keys dealt to NW waves.
+template <class P, int NW>
+__global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs a) {
+  typedef typename P::T T;
+  constexpr int TB = P::KT * P::ROWB;  // bytes of a tile of keys, or of values
+  __shared__ __attribute__((aligned(1024))) unsigned char s0[NW * 2 * TB];
+  __shared__ __attribute__((aligned(1024))) unsigned char s1[NW * 2 * TB];
+  __shared__ float sm[NW][P::RW], sl[NW][P::RW];
+
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const AttnSeqs& s = a.s;
+  const AttnItem it = attn_item(s, P::RW);
+  const int b = it.b, t = s.t[b];
+  const int n_rows = s.n[b] * s.G;
+  const int row0 = it.tile * P::RW;
+  Rows<P> w;
+  start_rows<P>(w, a, b, it.h, row0 + P::row(lane), lane);
+  const int first = last_key(s, b, min(row0, n_rows - 1) / s.G);
+  const int last = last_key(s, b, min(row0 + P::RW - 1, n_rows - 1) / s.G);
+  const int lo = it.part * s.chunk + wave * P::KT;
+  const int hi = min(last + 1, s.parts[b] == 1 ? t : min(t, it.part * s.chunk + s.chunk));
+  const T* kb = static_cast<const T*>(a.k) + a.k_off[b] + (long long)it.h * a.k_sh;
+  const T* vb = static_cast<const T*>(a.v) + a.v_off[b] + (long long)it.h * a.v_sh;
+  const float c = a.io.c;
+  unsigned char* w0 = s0 + wave * 2 * TB;
+  unsigned char* w1 = s1 + wave * 2 * TB;
+
+  auto get = [&](int t0, unsigned char* st) {
+    fetch<P, false, TB / 1024>(kb, a.k_st, t0, t, st, 0, 1, lane);
+    fetch<P, true, TB / 1024>(vb, a.v_st, t0, t, st + TB, 0, 1, lane);
+  };
+  auto step = [&](int t0, unsigned char* st, unsigned char* nst) {
+    if (t0 + NW * P::KT < hi) {
+      get(t0 + NW * P::KT, nst);
+      __builtin_amdgcn_s_waitcnt(wait_vm_only(2 * (TB / 1024)));
+    } else {
+      __builtin_amdgcn_s_waitcnt(wait_vm_only(0));
+    }
+    if (t0 + P::KT - 1 > first)
+      attend<P, true>(w, st, st + TB, lane, c, t0);
+    else
+      attend<P, false>(w, st, st + TB, lane, c, t0);
+  };
+  if (lo < hi) {
+    get(lo, w0);
+    for (int t0 = lo; t0 < hi; t0 += 2 * NW * P::KT) {
+      step(t0, w0, w1);
+      if (t0 + NW * P::KT < hi) step(t0 + NW * P::KT, w1, w0);
+    }
+  }
+
+  // join the waves: the common maximum, then the sums, 64 channels at a time in s0
+  const int rl = P::row(lane);
+  const float l = P::across(w.l, op_add);
+  if (lane < P::RW) {
+    sm[wave][rl] = w.m;
+    sl[wave][rl] = l;
+  }
+  __syncthreads();
+  float m = sm[0][rl];
+#pragma unroll
+  for (int x = 1; x < NW; ++x) m = fmaxf(m, sm[x][rl]);
+  float lt = 0.0f;
+#pragma unroll
+  for (int x = 0; x < NW; ++x) lt += sl[x][rl] * __builtin_amdgcn_exp2f(sm[x][rl] - m);
+  const float f = __builtin_amdgcn_exp2f(w.m - m);
+  constexpr int LD = P::RW;
+  float* buf = reinterpret_cast<float*>(s0);  // [NW][64][LD]
+  static_assert(NW * 64 * LD * 4 <= NW * 2 * TB, "joining buffer");
+#pragma unroll
+  for (int half = 0; half < P::D / 64; ++half) {
+    if (half) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < P::NO; ++i) {
+      const int ch = P::channel(lane, i) - 64 * half;
+      if (i / (P::NO / (P::D / 64)) == half) buf[(wave * 64 + ch) * LD + rl] = P::get(w.o, i) * f;
+    }
+    __syncthreads();
+    // wave x sums the channel blocks that lie on the same registers of its lanes
+#pragma unroll
+    for (int i = 0; i < P::NO; ++i) {
+      if (i / (P::NO / (P::D / 64)) != half || (i / 4) % NW != wave) continue;
+      const int ch = P::channel(lane, i) - 64 * half;
+      float x = 0.0f;
+#pragma unroll
+      for (int y = 0; y < NW; ++y) x += buf[(y * 64 + ch) * LD + rl];
+      P::set(w.o, i, x);
+    }
+  }
+  // each wave holds every NW-th group of four registers: it writes those channels
+  const int r = row0 + rl;
+  if (r >= n_rows) return;
+  int token, g;
+  place(r, s.G, token, g);
+  if (s.parts[b] == 1) {
+    const float inv = lt > 0.0f || lt != lt ? 1.0f / lt : 0.0f;
+    T* out = static_cast<T*>(a.io.out) + s.o_off[b] + (long long)token * a.io.o_st +
+             (long long)(it.h * s.G + g) * a.io.o_sh;
+#pragma unroll
+    for (int i = 0; i < P::NO; i += 4) {
+      if ((i / 4) % NW != wave) continue;
+      float x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = P::get(w.o, i + j) * inv;
+      P::store4(out + P::channel(lane, i), x);
+    }
+    if (wave == 0 && lane < P::RW && a.io.lse)
+      a.io.lse[(long long)(s.row0[b] + token) * (s.H * s.G) + it.h * s.G + g] =
+          lt == 0.0f ? -INFINITY : (m + log2f(lt)) * 0.6931471805599453f;
+    return;
+  }
+  const long long slot =
+      s.part0[b] + ((long long)it.h * n_rows + r) * s.parts[b] + it.part;
+#pragma unroll
+  for (int i = 0; i < P::NO; i += 4) {
+    if ((i / 4) % NW != wave) continue;
+    const f32x4 v = {P::get(w.o, i), P::get(w.o, i + 1), P::get(w.o, i + 2), P::get(w.o, i + 3)};
+    *reinterpret_cast<f32x4*>(a.io.part + slot * P::D + P::channel(lane, i)) = v;
+  }
+  if (wave == 0 && lane < P::RW) {
+    a.io.ml[2 * slot] = m;
+    a.io.ml[2 * slot + 1] = lt;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The parts of split rows: out = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p.
+// One wave a row.
+// ---------------------------------------------------------------------------
+struct JoinArgs {
+  AttnIO io;
+  AttnSeqs s;
+};
+
+template <bool F32, int D>
+__global__ __launch_bounds__(256) void attention_join_kernel(const JoinArgs a) {
+  const AttnSeqs& s = a.s;
+  const int lane = threadIdx.x & 63;
+  int i = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (i >= s.split0[s.B]) return;
+  int b = 0;
+  while (b + 1 < s.B && s.split0[b + 1] <= i) ++b;
+  i -= s.split0[b];
+  const int n_rows = s.n[b] * s.G, parts = s.parts[b];
+  const int h = i / n_rows, r = i - h * n_rows;
+  const long long slot = s.part0[b] + (long long)i * parts;
+  const float* ml = a.io.ml + 2 * slot;
+  float m = kNoMax;
+  for (int p = lane; p < parts; p += 64) m = fmaxf(m, ml[2 * p]);
+#pragma unroll
+  for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+  constexpr int E = D / 64;
+  float l = 0.0f, o[E] = {};
+  const float* po = a.io.part + slot * D + lane * E;
+  for (int p = 0; p < parts; ++p) {
+    const float f = __builtin_amdgcn_exp2f(ml[2 * p] - m);
+    l = fmaf(ml[2 * p + 1], f, l);
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = fmaf(po[(long long)p * D + e], f, o[e]);
+  }
+  int token, g;
+  place(r, s.G, token, g);
+  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+  const long long at = s.o_off[b] + (long long)token * a.io.o_st + (long long)(h * s.G + g) * a.io.o_sh + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if (F32)
+      static_cast<float*>(a.io.out)[at + e] = o[e] * inv;
+    else
+      static_cast<__bf16*>(a.io.out)[at + e] = (__bf16)(o[e] * inv);
+  }
+  if (lane == 0 && a.io.lse)
+    a.io.lse[(long long)(s.row0[b] + token) * (s.H * s.G) + h * s.G + g] =
+        l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+}
+
+constexpr int kRowWaves = 8, kRowWavesF32 = 4, kKeyWaves = 4;
+
+template <int D>
+hipError_t launch(int dtype, const AttnShape& sh, const AttnArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)(a.s.item0[a.s.B] * a.s.H));
+  if (dtype == HF_BF16) {
+    if (sh.by_keys)
+      attention_keys_kernel<Bf16Tile<D, 32>, kKeyWaves><<<grid, kKeyWaves * 64, 0, st>>>(a);
+    else
+      attention_rows_kernel<Bf16Tile<D, 64>, kRowWaves><<<grid, kRowWaves * 64, 0, st>>>(a);
+  } else {
+    if (sh.by_keys)
+      attention_keys_kernel<F32Tile<D, D == 128 ? 16 : 32>, kKeyWaves>
+          <<<grid, kKeyWaves * 64, 0, st>>>(a);
+    else
+      attention_rows_kernel<F32Tile<D, 32>, kRowWavesF32><<<grid, kRowWavesF32 * 64, 0, st>>>(a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+AttnShape prompt_shape(int dtype, int d_h, int64_t max_rows) {
+  AttnShape sh;
+  const int rw = dtype == HF_BF16 ? 32 : 16;
+  sh.by_keys = max_rows <= rw;
+  sh.rows = sh.by_keys ? rw : rw * (dtype == HF_BF16 ? kRowWaves : kRowWavesF32);
+  sh.wg_target = 256;
+  sh.step = sh.by_keys ? 32 * kKeyWaves : 64;
+  return sh;
+}
+
+hipError_t launch_prompt_attention(int dtype, int d_h, const AttnShape& sh, const AttnArgs& a,
+                                   hipStream_t s) {
+  return d_h == 128 ? launch<128>(dtype, sh, a, s) : launch<64>(dtype, sh, a, s);
+}
+
+hipError_t launch_attention_join(int dtype, int d_h, const AttnIO& io, const AttnSeqs& s,
+                                 hipStream_t st) {
+  JoinArgs a{io, s};
+  const dim3 grid((unsigned)((s.split0[s.B] + 3) / 4));
+  if (dtype == HF_F32) {
+    if (d_h == 128) attention_join_kernel<true, 128><<<grid, 256, 0, st>>>(a);
+    else attention_join_kernel<true, 64><<<grid, 256, 0, st>>>(a);
+  } else {
+    if (d_h == 128) attention_join_kernel<false, 128><<<grid, 256, 0, st>>>(a);
+    else attention_join_kernel<false, 64><<<grid, 256, 0, st>>>(a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace hf

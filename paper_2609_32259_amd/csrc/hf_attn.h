@@ -1,0 +1,77 @@
+// Device helpers shared by the attention kernels.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cfloat>
+
+#include "hf_internal.h"
+
+namespace hf {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void lds_void_t;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4_t;
+
+#define FI __device__ __forceinline__
+
+// A row's running maximum starts at the least finite value rather than at
+// -infinity, so that exp2(s - m) of a row that has seen no key is exp2(-inf) = 0.
+constexpr float kNoMax = -FLT_MAX;
+
+// The maximum that a row's weights are formed against is raised only when a new
+// score passes it by more than this (in powers of two): until then weights of up
+// to 2^8 are as exact as those of at most 1, in fp32 sums and in bf16 operands
+// alike, and the sums need no rescaling.  Most steps skip it.
+constexpr float kRaise = 8.0f;
+
+// s_waitcnt immediate that waits until at most n vector-memory operations are
+// outstanding and leaves the other counters alone (gfx9 encoding).
+constexpr int wait_vm_only(int n) { return (n & 0xF) | ((n >> 4) << 14) | (7 << 4) | (0xF << 8); }
+
+FI uint32_t pack_bf16(float a, float b) {
+  bf16x2 v = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+FI bool finite_bits(float x) {
+  return (__builtin_bit_cast(uint32_t, x) & 0x7f800000u) != 0x7f800000u;
+}
+
+// The work item of this workgroup: its head, sequence, row tile and part.  Heads
+// vary fastest, so that with 8 heads the workgroups of one head, which read the
+// same keys, run on one XCD (workgroup i runs on XCD i % 8) and share them in its
+// L2.  Row tiles run from the last to the first: a causal tile's work grows with
+// its rows, and the long ones go first.
+struct AttnItem {
+  int b, h, tile, part;
+};
+FI AttnItem attn_item(const AttnSeqs& s, int rows) {
+  AttnItem it;
+  const int wg = blockIdx.x;
+  int i = wg / s.H;
+  it.h = wg - i * s.H;
+  int b = 0;
+  while (b + 1 < s.B && s.item0[b + 1] <= i) ++b;
+  it.b = b;
+  i -= s.item0[b];
+  const int tiles = (s.n[b] * s.G + rows - 1) / rows;  // n * G < 2^31 (host check)
+  const int t = i / s.parts[b];
+  it.part = i - t * s.parts[b];
+  it.tile = tiles - 1 - t;
+  return it;
+}
+
+// The last key a row sees (-1: none), from its token.
+FI int last_key(const AttnSeqs& s, int b, int token) {
+  return s.causal ? min(s.t[b] - 1, token + s.t[b] - s.n[b]) : s.t[b] - 1;
+}
+
+}  // namespace hf

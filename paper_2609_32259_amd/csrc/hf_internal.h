@@ -166,4 +166,91 @@ hipError_t launch_gemm_f64(int m, int n, long long k, const double* A, long long
                            double alpha, double beta, const double* C, long long ldc,
                            double gamma, hipStream_t s);
 
+// Attention (attention.hip, paged.hip).  Query rows of one sequence and key/value
+// head are numbered r = token * G + (head in group), G = H_q / H, so that a tile of
+// rows shares its keys between the heads of a group as well as between tokens.
+// A split sequence writes, for each row and part, the unnormalized sum, the running
+// maximum and the weight into the workspace, and the join makes the result of them.
+struct AttnSeqs {
+  int32_t B, H, G;
+  int32_t chunk;                       // keys of one part (a multiple of every kernel's step)
+  int32_t causal;
+  int32_t n[HF_MAX_BATCH];             // query tokens
+  int32_t t[HF_MAX_BATCH];             // keys
+  int32_t row0[HF_MAX_BATCH];          // first query row of the sequence among the packed ones (lse)
+  int32_t parts[HF_MAX_BATCH];
+  int32_t item0[HF_MAX_BATCH + 1];     // first work item: (row tile, part) pairs of a head
+  int32_t split0[HF_MAX_BATCH + 1];    // first row of the sequence among those of split ones
+  int32_t part0[HF_MAX_BATCH];         // first slot of the sequence in the partial buffers
+  int64_t q_off[HF_MAX_BATCH];
+  int64_t o_off[HF_MAX_BATCH];
+};
+struct AttnIO {
+  const void* q;
+  void* out;
+  float* lse;       // or nullptr
+  float* part;      // [slots][d_h] unnormalized sums
+  float* ml;        // [slots][2] maximum (in units of log 2) and weight
+  long long q_st, q_sh, o_st, o_sh;
+  float c;          // scale * log2(e)
+};
+struct AttnArgs {
+  AttnIO io;
+  const void* k;
+  const void* v;
+  long long k_st, k_sh, v_st, v_sh;
+  AttnSeqs s;
+  int64_t k_off[HF_MAX_BATCH];
+  int64_t v_off[HF_MAX_BATCH];
+};
+struct PagedAttnArgs {
+  AttnIO io;
+  const uint8_t* pages;      // the layer's first page
+  const int32_t* table;
+  long long table_stride;
+  long long page_bytes;
+  int32_t n_pages;
+  int32_t log2_page;
+  AttnSeqs s;
+};
+static_assert(sizeof(AttnArgs) <= 4096 && sizeof(PagedAttnArgs) <= 4096, "kernel argument size");
+// How a call is cut: rows of a tile, whether the waves of a workgroup share the
+// keys (each with its own rows) or the rows (each with its own keys).
+struct AttnShape {
+  int32_t rows;       // of a workgroup's tile
+  int32_t by_keys;
+  int32_t wg_target;  // workgroups that fill the chip
+  int32_t step;       // keys that parts are cut in multiples of
+};
+AttnShape prompt_shape(int dtype, int d_h, int64_t max_rows);
+AttnShape paged_shape(int dtype, int d_h, int64_t max_rows);
+hipError_t launch_prompt_attention(int dtype, int d_h, const AttnShape& sh, const AttnArgs& a,
+                                   hipStream_t s);
+hipError_t launch_paged_attention(int dtype, int d_h, const AttnShape& sh, const PagedAttnArgs& a,
+                                  hipStream_t s);
+hipError_t launch_attention_join(int dtype, int d_h, const AttnIO& io, const AttnSeqs& s,
+                                 hipStream_t st);
+
+struct PagedRowsArgs {
+  const void* k;             // append: rows read; read: rows written
+  const void* v;
+  long long k_st, k_sh, k_sl, v_st, v_sh, v_sl;
+  uint8_t* pages;            // of the first layer of the call
+  const int32_t* table;
+  long long table_stride, page_bytes;
+  int32_t n_pages, log2_page;
+  int32_t B, H, n_layers;
+  int32_t rotate;
+  double w[64];              // angle of a position step of each channel pair
+  int32_t start[HF_MAX_BATCH];
+  int32_t n[HF_MAX_BATCH];
+  int32_t pos0[HF_MAX_BATCH];
+  int32_t blk0[HF_MAX_BATCH + 1];  // first 32-token block of the sequence
+  int64_t k_off[HF_MAX_BATCH];
+  int64_t v_off[HF_MAX_BATCH];
+};
+static_assert(sizeof(PagedRowsArgs) <= 4096, "kernel argument size");
+hipError_t launch_paged_append(int dtype, int d_h, const PagedRowsArgs& a, hipStream_t s);
+hipError_t launch_paged_read(int dtype, int d_h, const PagedRowsArgs& a, hipStream_t s);
+
 }  // namespace hf

@@ -1,0 +1,750 @@
+// A paged cache held in 4 bits: appending rows, reading them back, and attention
+// over it (the format stands in heterofold.h).
+//
+// Attention.  With the codes c and a group's scale s and offset o,
+//
+//   <q, k_t> = sum_g [ s_tg <q_g, c_tg> + o_tg sum(q_g) ]
+//   out_g    = sum_t (p_t s_tg) c_tg + sum_t p_t o_tg
+//
+// where g runs over the groups of 32 channels.  A group is the reduction length of
+// v_mfma_f32_16x16x32_bf16, so one instruction gives <q_g, c_tg> of 16 tokens and 16
+// rows, and the codes are exact in bf16: a code moved into the mantissa under the
+// exponent of 16 is 16 + code.  That costs a shift and an and-or for two codes, and
+// the 16s are taken out again with numbers that are needed anyway (o - 16 s, and a
+// product of the weights with 1).  Scales and offsets are applied in fp32.
+#include <hip/hip_runtime.h>
+
+#include "hf_attn.h"
+
+namespace hf {
+namespace {
+
+// ---------------------------------------------------------------------------
+// Rows in and out.  A workgroup takes a block of 32 tokens (the unit of the value
+// codes' order) of one sequence, layer, role and head; 16 channels a thread.
+// ---------------------------------------------------------------------------
+
+struct RowItem {
+  int b, l, h, role;
+  int tok0;          // first token of the block
+  int lo, hi;        // tokens of the call in it, relative to tok0
+  uint8_t* head;     // the head's part of the page, or nullptr (a hole)
+  int row0;          // the block's first row in the page
+};
+
+template <int D>
+FI RowItem row_item(const PagedRowsArgs& a, int hpw) {
+  RowItem it;
+  int i = blockIdx.x;
+  const int groups = (a.H + hpw - 1) / hpw;
+  it.h = (i % groups) * hpw;
+  i /= groups;
+  it.role = blockIdx.y;
+  it.l = blockIdx.z;
+  int b = 0;
+  while (b + 1 < a.B && a.blk0[b + 1] <= i) ++b;
+  it.b = b;
+  const int blk = a.start[b] / 32 + (i - a.blk0[b]);
+  it.tok0 = blk * 32;
+  it.lo = max(a.start[b] - it.tok0, 0);
+  it.hi = min(a.start[b] + a.n[b] - it.tok0, 32);
+  const int page = a.table[b * a.table_stride + (it.tok0 >> a.log2_page)];
+  it.row0 = it.tok0 & ((1 << a.log2_page) - 1);
+  it.head = nullptr;
+  if ((unsigned)page < (unsigned)a.n_pages)
+    it.head = a.pages + ((long long)it.l * a.n_pages + page) * a.page_bytes;
+  return it;
+}
+
+// Offsets in a head's part of a page.
+template <int D>
+struct PageHead {
+  static constexpr int G = D / 32;
+  int P;
+  FI PageHead(int log2_page) : P(1 << log2_page) {}
+  FI int bytes() const { return P * (D + 8 * G); }
+  FI int kcode(int row) const { return row * (D / 2); }
+  FI int vcode(int row) const { return P * (D / 2) + row * (D / 2); }  // row: of a block's first token
+  FI int word(int role, int row) const { return P * D + (role * P + row) * (4 * G); }
+};
+
+template <class T>
+FI void load8(const T* p, float (&x)[8]);
+template <>
+FI void load8<uint16_t>(const uint16_t* p, float (&x)[8]) {
+  const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __builtin_bit_cast(float, v[i] << 16);
+    x[2 * i + 1] = __builtin_bit_cast(float, v[i] & 0xffff0000u);
+  }
+}
+template <>
+FI void load8<float>(const float* p, float (&x)[8]) {
+  const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[i] = a[i];
+    x[4 + i] = b[i];
+  }
+}
+
+template <class T>
+FI void store8(T* p, const float (&x)[8]);
+template <>
+FI void store8<uint16_t>(uint16_t* p, const float (&x)[8]) {
+  u32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+  *reinterpret_cast<u32x4*>(p) = v;
+}
+template <>
+FI void store8<float>(float* p, const float (&x)[8]) {
+  const f32x4 a = {x[0], x[1], x[2], x[3]}, b = {x[4], x[5], x[6], x[7]};
+  reinterpret_cast<f32x4*>(p)[0] = a;
+  reinterpret_cast<f32x4*>(p)[1] = b;
+}
+
+FI float bf16_round(float x) { return (float)(__bf16)x; }
+
+// Codes and word of a group spread over four lanes (l, l ^ 1, l ^ 2, l ^ 3), eight
+// channels a lane.  Codes as a dword, channel j at nibble j.
+FI uint32_t code_group(const float (&x)[8], uint32_t& word) {
+#pragma clang fp contract(off)
+  float lo = x[0], hi = x[0];
+  bool nan = x[0] != x[0];
+#pragma unroll
+  for (int j = 1; j < 8; ++j) {
+    lo = fminf(lo, x[j]);
+    hi = fmaxf(hi, x[j]);
+    nan = nan || x[j] != x[j];
+  }
+  // (fminf and fmaxf pass NaN by)
+  lo = nan ? NAN : lo;
+#pragma unroll
+  for (int m = 1; m <= 2; m <<= 1) {
+    const float ol = __shfl_xor(lo, m), oh = __shfl_xor(hi, m);
+    lo = lo != lo || ol != ol ? NAN : fminf(lo, ol);
+    hi = fmaxf(hi, oh);
+  }
+  const float o = bf16_round(lo);
+  float s = bf16_round((hi - lo) / 15.0f);
+  if (!finite_bits(o) || !finite_bits(s)) {
+    word = 0x7fc07fc0u;  // NaN, NaN
+    return 0;
+  }
+  if (s < 0x1p-100f) s = 0.0f;
+  word = __builtin_bit_cast(uint32_t, s) | (__builtin_bit_cast(uint32_t, o) >> 16);
+  uint32_t c = 0;
+  const float d = s > 0.0f ? s : INFINITY;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    // a true quotient: what lies halfway between two codes goes to the even one
+    const float q = fminf(fmaxf(rintf((x[j] - o) / d), 0.0f), 15.0f);
+    c |= (uint32_t)(int)q << (4 * j);
+  }
+  return c;
+}
+
+// cos and sin of pos * w_k for the block's 32 positions, to LDS [32][D/2], fp64
+// angles rounded once.  Four chains a channel pair, eight positions each: one sine
+// and cosine at the chain's first position, then a complex product with the step's
+// (error 8 * 2^-53).  A block with up to four tokens computes just theirs.
+template <int D>
+FI void fill_angles(const PagedRowsArgs& a, const RowItem& it, float2* cs) {
+  constexpr int HD = D / 2;
+  const int k = threadIdx.x % HD, m = threadIdx.x / HD;  // m < 4
+  const double w = a.w[k];
+  const double base = (double)a.pos0[it.b] + it.tok0;
+  double c, s;
+  if (it.hi - it.lo <= 4) {
+    const int j = it.lo + m;
+    if (j < it.hi) {
+      sincos((base + j) * w, &s, &c);
+      cs[j * HD + k] = make_float2((float)c, (float)s);
+    }
+    return;
+  }
+  double dc, ds;
+  sincos(w, &ds, &dc);
+  sincos((base + 8 * m) * w, &s, &c);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    cs[(8 * m + j) * HD + k] = make_float2((float)c, (float)s);
+    const double t = c * dc - s * ds;
+    s = s * dc + c * ds;
+    c = t;
+  }
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(2 * D) void paged_append_kernel(const PagedRowsArgs a, const int hpw) {
+  constexpr int TPT = D / 16;  // threads a token
+  constexpr int G = D / 32;
+  __shared__ float2 cs[32 * D / 2];
+  __shared__ uint32_t codes[32 * D / 8];  // [token][channel] nibbles
+  const RowItem it = row_item<D>(a, hpw);
+  if (!it.head) return;
+  const int tok = threadIdx.x / TPT, j = threadIdx.x % TPT;
+  const bool on = tok >= it.lo && tok < it.hi;
+  const bool rot = a.rotate && it.role == 0;
+  if (rot) {
+    fill_angles<D>(a, it, cs);
+    __syncthreads();
+  }
+  const PageHead<D> ph(a.log2_page);
+  const int row = it.row0 + tok;
+  const T* src = it.role == 0
+                     ? static_cast<const T*>(a.k) + a.k_off[it.b] + it.l * a.k_sl +
+                           (long long)(it.tok0 + tok - a.start[it.b]) * a.k_st
+                     : static_cast<const T*>(a.v) + a.v_off[it.b] + it.l * a.v_sl +
+                           (long long)(it.tok0 + tok - a.start[it.b]) * a.v_st;
+  const long long sh = it.role == 0 ? a.k_sh : a.v_sh;
+  const int h_end = min(it.h + hpw, a.H);
+  for (int h = it.h; h < h_end; ++h) {
+    uint8_t* head = it.head + (long long)h * ph.bytes();
+    uint32_t c0 = 0, c1 = 0, w0 = 0, w1 = 0;
+    if (on) {  // (a group's four lanes hold the same token)
+      float x0[8], x1[8];  // channels 8 j .. and D/2 + 8 j ..: rotation pairs
+      load8<T>(src + h * sh + 8 * j, x0);
+      load8<T>(src + h * sh + D / 2 + 8 * j, x1);
+      if (rot) {
+#pragma clang fp contract(off)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float2 r = cs[tok * (D / 2) + 8 * j + e];
+          const float u = x0[e], v = x1[e];
+          x0[e] = u * r.x - v * r.y;
+          x1[e] = v * r.x + u * r.y;
+        }
+      }
+      c0 = code_group(x0, w0);
+      c1 = code_group(x1, w1);
+      uint32_t* words = reinterpret_cast<uint32_t*>(head + ph.word(it.role, row));
+      if ((j & 3) == 0) {
+        words[j >> 2] = w0;
+        words[G / 2 + (j >> 2)] = w1;
+      }
+      if (it.role == 0) {
+        uint32_t* kc = reinterpret_cast<uint32_t*>(head + ph.kcode(row));
+        kc[(j & 3) * G + (j >> 2)] = c0;
+        kc[(j & 3) * G + G / 2 + (j >> 2)] = c1;
+      }
+    }
+    if (it.role == 0) continue;
+    // Value codes: to the order of the block, through LDS.
+    codes[tok * (D / 8) + j] = c0;
+    codes[tok * (D / 8) + D / 16 + j] = c1;
+    __syncthreads();
+    const uint8_t* cb = reinterpret_cast<const uint8_t*>(codes);
+    uint32_t* vc = reinterpret_cast<uint32_t*>(head + ph.vcode(it.row0));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int at = threadIdx.x + i * 2 * D;  // dword of the block
+      const int n = at % (D / 16), c = at / (D / 16) % 16, m = at / D;
+      const int ch = 16 * n + c;
+      uint32_t x = 0, mask = 0;
+#pragma unroll
+      for (int y = 0; y < 8; ++y) {
+        const int t = 16 * (y >> 2) + 4 * m + (y & 3);
+        const uint32_t nib = (cb[t * (D / 2) + ch / 2] >> (4 * (ch & 1))) & 15;
+        if (t >= it.lo && t < it.hi) {
+          x |= nib << (4 * y);
+          mask |= 15u << (4 * y);
+        }
+      }
+      if (mask == 0xffffffffu)
+        vc[at] = x;
+      else if (mask)
+        vc[at] = (vc[at] & ~mask) | x;
+    }
+    if (h + 1 < h_end) __syncthreads();
+  }
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(2 * D) void paged_read_kernel(const PagedRowsArgs a, const int hpw) {
+  constexpr int TPT = D / 16;
+  constexpr int G = D / 32;
+  __shared__ uint32_t codes[16 * D / 8 * 2];
+  const RowItem it = row_item<D>(a, hpw);
+  const int tok = threadIdx.x / TPT, j = threadIdx.x % TPT;
+  const bool on = tok >= it.lo && tok < it.hi;
+  const PageHead<D> ph(a.log2_page);
+  const int row = it.row0 + tok;
+  T* dst = it.role == 0 ? static_cast<T*>(const_cast<void*>(a.k)) + a.k_off[it.b] + it.l * a.k_sl +
+                              (long long)(it.tok0 + tok - a.start[it.b]) * a.k_st
+                        : static_cast<T*>(const_cast<void*>(a.v)) + a.v_off[it.b] + it.l * a.v_sl +
+                              (long long)(it.tok0 + tok - a.start[it.b]) * a.v_st;
+  const long long sh = it.role == 0 ? a.k_sh : a.v_sh;
+  const int h_end = min(it.h + hpw, a.H);
+  for (int h = it.h; h < h_end; ++h) {
+    const uint8_t* head = it.head + (long long)h * ph.bytes();
+    uint32_t c0 = 0, c1 = 0, w0 = 0, w1 = 0;
+    if (it.head) {
+      if (it.role == 1) {
+        if (h > it.h) __syncthreads();
+        const uint32_t* vc = reinterpret_cast<const uint32_t*>(head + ph.vcode(it.row0));
+        codes[threadIdx.x] = vc[threadIdx.x];
+        codes[threadIdx.x + 2 * D] = vc[threadIdx.x + 2 * D];
+        __syncthreads();
+      }
+      if (on) {
+        const uint32_t* words = reinterpret_cast<const uint32_t*>(head + ph.word(it.role, row));
+        w0 = words[j >> 2];
+        w1 = words[G / 2 + (j >> 2)];
+        if (it.role == 0) {
+          const uint32_t* kc = reinterpret_cast<const uint32_t*>(head + ph.kcode(row));
+          c0 = kc[(j & 3) * G + (j >> 2)];
+          c1 = kc[(j & 3) * G + G / 2 + (j >> 2)];
+        } else {
+          const int m = (tok >> 2) & 3, y = 4 * (tok >> 4) + (tok & 3);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int a0 = 8 * j + e, a1 = D / 2 + 8 * j + e;
+            c0 |= ((codes[(m * 16 + a0 % 16) * (D / 16) + a0 / 16] >> (4 * y)) & 15) << (4 * e);
+            c1 |= ((codes[(m * 16 + a1 % 16) * (D / 16) + a1 / 16] >> (4 * y)) & 15) << (4 * e);
+          }
+        }
+      }
+    }
+    if (!on) continue;
+    float x0[8], x1[8];
+    const float s0 = __builtin_bit_cast(float, w0 & 0xffff0000u), o0 = __builtin_bit_cast(float, w0 << 16);
+    const float s1 = __builtin_bit_cast(float, w1 & 0xffff0000u), o1 = __builtin_bit_cast(float, w1 << 16);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {  // (s * code is exact in fp32)
+      x0[e] = fmaf(s0, (float)((c0 >> (4 * e)) & 15), o0);
+      x1[e] = fmaf(s1, (float)((c1 >> (4 * e)) & 15), o1);
+    }
+    store8<T>(dst + h * sh + 8 * j, x0);
+    store8<T>(dst + h * sh + D / 2 + 8 * j, x1);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Attention.  A workgroup takes 16 NT query rows of a group and a part of the
+// tokens; its four waves deal the blocks of 32 tokens among them.  On
+// v_mfma_f32_16x16x32_bf16, with m = lane / 16, S^T = K Q^T gives the lane its row
+// lane % 16 and tokens 4 m + i of each half of the block (i: the result register),
+// which is how the value codes lie: the lane's dword for channel block n holds
+// channel 16 n + lane % 16 of those eight tokens.
+// ---------------------------------------------------------------------------
+constexpr int kPagedWaves = 4;
+
+// Two codes of a dword, nibbles n and n + 4, as bf16 16 + code.
+FI uint32_t two_codes(uint32_t w, int n) {
+  // the code to bits 3..6 of each half, under the exponent of 16
+  const uint32_t x = n == 0 ? w << 3 : w >> (4 * n - 3);
+  return (x & 0x00780078u) | 0x41804180u;
+}
+FI bf16x8 eight_codes(uint32_t w) {
+  union {
+    uint32_t u[4];
+    bf16x8 v;
+  } x;
+#pragma unroll
+  for (int n = 0; n < 4; ++n) x.u[n] = two_codes(w, n);
+  return x.v;
+}
+
+// x as S bf16 terms whose sum holds 8 S bits of it.
+template <int S>
+FI void split(float x, float (&t)[S]) {
+#pragma unroll
+  for (int i = 0; i < S; ++i) {
+    t[i] = bf16_round(x);
+    x -= t[i];
+  }
+}
+
+template <int D, bool F32>
+struct Block {  // what a lane holds of a block of 32 tokens
+  static constexpr int G = D / 32;
+  uint32_t k[2][G];    // key codes of token 16 u + lane % 16, octet lane / 16 of each group
+  uint32_t v[D / 16];  // value codes
+  uint32_t w[G];       // words of token lane % 32: keys' in lanes below 32, values' above
+};
+
+template <int N>
+FI void load_dwords(const uint8_t* p, uint32_t (&x)[N]) {
+  if (N == 2) {
+    const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+    x[0] = v[0];
+    x[1] = v[1];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(p + 4 * i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[i + e] = v[e];
+    }
+  }
+}
+
+template <int D, int NT, bool F32>
+__global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const PagedAttnArgs a) {
+  constexpr int G = D / 32, NC = D / 16, S = F32 ? 3 : 1, R = 16 * NT;
+  constexpr int NW = kPagedWaves;
+  // scales, and offsets freed of the codes' 16 (keys) or moved to code 8 (values)
+  __shared__ __attribute__((aligned(16))) float lds[NW * 64 * G * 2 > NW * 64 * R ? NW * 64 * G * 2 : NW * 64 * R];
+  __shared__ float sm[NW][R], sl[NW][R];
+  typedef float fG __attribute__((ext_vector_type(G)));
+
+  const int lane = threadIdx.x & 63, col = lane & 15, m4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const AttnSeqs& s = a.s;
+  const AttnItem it = attn_item(s, R);
+  const int b = it.b, t = s.t[b];
+  const int n_rows = s.n[b] * s.G;
+  const int row0 = it.tile * R;
+  const float c = a.io.c;
+  fG* sc = reinterpret_cast<fG*>(lds) + wave * 128;  // [64] scales: key tokens, value tokens
+  fG* of = sc + 64;                                  // [64] offsets
+
+  bf16x8 q[NT][S][G];
+  float qs[NT][G];  // sum of the row's channels of a group
+  int last[NT];
+#pragma unroll
+  for (int x = 0; x < NT; ++x) {
+    const int r = min(row0 + 16 * x + col, n_rows - 1);
+    const int token = r / s.G, g = r - token * s.G;
+    last[x] = last_key(s, b, token);
+    const long long at = s.q_off[b] + (long long)token * a.io.q_st + (long long)(it.h * s.G + g) * a.io.q_sh;
+#pragma unroll
+    for (int y = 0; y < G; ++y) {
+      float f[8];
+      if (F32)
+        load8<float>(static_cast<const float*>(a.io.q) + at + 32 * y + 8 * m4, f);
+      else
+        load8<uint16_t>(static_cast<const uint16_t*>(a.io.q) + at + 32 * y + 8 * m4, f);
+      float sum = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        sum += f[e];
+        float p[S];
+        split<S>(f[e], p);
+#pragma unroll
+        for (int z = 0; z < S; ++z) q[x][z][y][e < 4 ? 2 * e : 2 * (e - 4) + 1] = (__bf16)p[z];
+      }
+      sum += __shfl_xor(sum, 16);
+      qs[x][y] = sum + __shfl_xor(sum, 32);
+    }
+  }
+
+  f32x4 o[NT][NC] = {};    // sum of (p s) (16 + code): row col, channels 16 n + 4 m4 + i
+  f32x4 ps[NT][G] = {};    // sum of the rounded p s
+  float po[NT][G] = {};    // sum of p times the offset, over the lane's tokens
+  float m[NT], l[NT];
+#pragma unroll
+  for (int x = 0; x < NT; ++x) {
+    m[x] = kNoMax;
+    l[x] = 0.0f;
+  }
+
+  const int first_last = last_key(s, b, min(row0, n_rows - 1) / s.G);
+  const int end_last = last_key(s, b, min(row0 + R - 1, n_rows - 1) / s.G);
+  const int lo = it.part * s.chunk;
+  const int hi = min(end_last + 1, s.parts[b] == 1 ? t : min(t, lo + s.chunk));
+  const int P = 1 << a.log2_page;
+  const PageHead<D> ph(a.log2_page);
+  const int32_t* table = a.table + b * a.table_stride;
+  const long long head_at = (long long)it.h * ph.bytes();
+
+  // The block at token t0 (a hole's, too: its loads go to page 0 and it is masked).
+  auto page_of = [&](int t0) { return table[t0 >> a.log2_page]; };
+  auto load = [&](Block<D, F32>& x, int t0, int page) {
+    const bool in = (unsigned)page < (unsigned)a.n_pages;
+    const uint8_t* head = a.pages + (long long)(in ? page : 0) * a.page_bytes + head_at;
+    const int row = t0 & (P - 1);
+    load_dwords<G>(head + ph.kcode(row + col) + m4 * 4 * G, x.k[0]);
+    load_dwords<G>(head + ph.kcode(row + 16 + col) + m4 * 4 * G, x.k[1]);
+    load_dwords<NC>(head + ph.vcode(row) + lane * 4 * NC, x.v);
+    load_dwords<G>(head + ph.word(lane >> 5, row + (lane & 31)), x.w);
+  };
+
+  auto block = [&](const Block<D, F32>& x, int t0, bool in) {
+    // words of tokens that no row sees count as 0, so that nothing below meets NaN of theirs
+    const bool live = in && t0 + (lane & 31) < hi;
+    fG vs, vo;
+#pragma unroll
+    for (int y = 0; y < G; ++y) {
+      const uint32_t w = live ? x.w[y] : 0u;
+      vs[y] = __builtin_bit_cast(float, w & 0xffff0000u);
+      vo[y] = fmaf(vs[y], lane < 32 ? -16.0f : 8.0f, __builtin_bit_cast(float, w << 16));
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    sc[lane] = vs;
+    of[lane] = vo;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+
+    float p[NT][8];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      bf16x8 kc[G];
+#pragma unroll
+      for (int y = 0; y < G; ++y) kc[y] = eight_codes(x.k[u][y]);
+      fG ks[4], ko[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        ks[i] = sc[16 * u + 4 * m4 + i];
+        ko[i] = of[16 * u + 4 * m4 + i];
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float v[4] = {};
+#pragma unroll
+        for (int y = 0; y < G; ++y) {
+          f32x4 d = {};
+#pragma unroll
+          for (int z = 0; z < S; ++z)
+            d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kc[y], q[n][z][y], d, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = fmaf(ks[i][y], d[i], fmaf(ko[i][y], qs[n][y], v[i]));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[n][4 * u + i] = v[i];
+      }
+    }
+    const bool masked = !in || t0 + 31 > first_last || t0 + 32 > hi;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int k = t0 + 16 * (i >> 2) + 4 * m4 + (i & 3);
+          if (!in || k > last[n] || k >= hi) p[n][i] = -INFINITY;
+        }
+      }
+      float mx = p[n][0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) mx = fmaxf(mx, p[n][i]);
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32)) * c;
+      if (__any(mx > m[n] + kRaise)) {
+        const float nm = mx > m[n] + kRaise ? mx : m[n];  // (each row by its own scores alone)
+        const float f = __builtin_amdgcn_exp2f(m[n] - nm);
+        m[n] = nm;
+        l[n] *= f;
+#pragma unroll
+        for (int y = 0; y < NC; ++y) o[n][y] *= f;
+#pragma unroll
+        for (int y = 0; y < G; ++y) {
+          ps[n][y] *= f;
+          po[n][y] *= f;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[n][i] = __builtin_amdgcn_exp2f(fmaf(p[n][i], c, -m[n]));
+        l[n] += p[n][i];
+      }
+    }
+
+    bf16x8 vc[NC];
+#pragma unroll
+    for (int y = 0; y < NC; ++y) vc[y] = eight_codes(x.v[y]);
+    fG zs[8], zo[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      zs[i] = sc[32 + 16 * (i >> 2) + 4 * m4 + (i & 3)];
+      zo[i] = of[32 + 16 * (i >> 2) + 4 * m4 + (i & 3)];
+    }
+    const bf16x8 one = {(__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f,
+                        (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int y = 0; y < G; ++y) {
+        float f[8], sum = po[n][y];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          f[i] = p[n][i] * zs[i][y];
+          float g = p[n][i] * zo[i][y];
+          // what a row does not see has weight 0, and may be NaN
+          if (masked && t0 + 16 * (i >> 2) + 4 * m4 + (i & 3) > last[n]) f[i] = g = 0.0f;
+          sum += g;
+        }
+        po[n][y] = sum;
+        float w[8][S];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) split<S>(f[i], w[i]);
+#pragma unroll
+        for (int z = 0; z < S; ++z) {
+          union {
+            uint32_t u[4];
+            bf16x8 v;
+          } pw;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) pw.u[i] = pack_bf16(w[i][z], w[4 + i][z]);
+          ps[n][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, pw.v, ps[n][y], 0, 0, 0);
+          o[n][2 * y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vc[2 * y], pw.v, o[n][2 * y], 0, 0, 0);
+          o[n][2 * y + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vc[2 * y + 1], pw.v, o[n][2 * y + 1], 0, 0, 0);
+        }
+      }
+    }
+  };
+
+  Block<D, F32> x0, x1;
+  int t0 = lo + 32 * wave;
+  int pg0 = 0, pg1 = 0;
+  if (t0 < hi) {
+    pg0 = page_of(t0);
+    load(x0, t0, pg0);
+  }
+  for (; t0 < hi; t0 += 64 * NW) {
+    const int t1 = t0 + 32 * NW, t2 = t1 + 32 * NW;
+    if (t1 < hi) {
+      pg1 = page_of(t1);
+      load(x1, t1, pg1);
+    }
+    block(x0, t0, (unsigned)pg0 < (unsigned)a.n_pages);
+    if (t2 < hi) {
+      pg0 = page_of(t2);
+      load(x0, t2, pg0);
+    }
+    if (t1 < hi) block(x1, t1, (unsigned)pg1 < (unsigned)a.n_pages);
+  }
+
+  // the lane's rows: out of the codes' 16 (with the 8 of the moved offsets), the
+  // offsets of all lanes' tokens
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    l[n] += __shfl_xor(l[n], 16);
+    l[n] += __shfl_xor(l[n], 32);
+#pragma unroll
+    for (int y = 0; y < G; ++y) {
+      float x = po[n][y];
+      x += __shfl_xor(x, 16);
+      x += __shfl_xor(x, 32);
+#pragma unroll
+      for (int z = 0; z < 2; ++z)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[n][2 * y + z][i] += fmaf(-24.0f, ps[n][y][i], x);
+    }
+    if (m4 == 0) {
+      sm[wave][16 * n + col] = m[n];
+      sl[wave][16 * n + col] = l[n];
+    }
+  }
+  __syncthreads();
+  // join the waves, 64 channels at a time: [wave][channel][row] in LDS
+  constexpr int QR = R / 4;  // rows a thread sums, of one channel: thread = (channel, quarter)
+#pragma unroll
+  for (int half = 0; half < D / 64; ++half) {
+    if (half) __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int r = 16 * n + col;
+      float mm = sm[0][r];
+#pragma unroll
+      for (int x = 1; x < NW; ++x) mm = fmaxf(mm, sm[x][r]);
+      const float f = __builtin_amdgcn_exp2f(m[n] - mm);
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          lds[(wave * R + r) * 64 + 16 * y + 4 * m4 + i] = o[n][4 * half + y][i] * f;
+    }
+    __syncthreads();
+    const int ch = threadIdx.x & 63, quarter = threadIdx.x >> 6;
+    for (int x = 0; x < QR; ++x) {
+      const int rl = quarter * QR + x, r = row0 + rl;
+      if (r >= n_rows) break;
+      float mm = sm[0][rl], v = 0.0f, lt = 0.0f;
+#pragma unroll
+      for (int y = 1; y < NW; ++y) mm = fmaxf(mm, sm[y][rl]);
+#pragma unroll
+      for (int y = 0; y < NW; ++y) {
+        v += lds[(y * R + rl) * 64 + ch];
+        lt = fmaf(sl[y][rl], __builtin_amdgcn_exp2f(sm[y][rl] - mm), lt);
+      }
+      const int token = r / s.G, g = r - token * s.G;
+      if (s.parts[b] == 1) {
+        const long long at = s.o_off[b] + (long long)token * a.io.o_st +
+                             (long long)(it.h * s.G + g) * a.io.o_sh + 64 * half + ch;
+        v *= lt > 0.0f || lt != lt ? 1.0f / lt : 0.0f;
+        if (F32)
+          static_cast<float*>(a.io.out)[at] = v;
+        else
+          static_cast<__bf16*>(a.io.out)[at] = (__bf16)v;
+        if (half == 0 && ch == 0 && a.io.lse)
+          a.io.lse[(long long)(s.row0[b] + token) * (s.H * s.G) + it.h * s.G + g] =
+              lt == 0.0f ? -INFINITY : (mm + log2f(lt)) * 0.6931471805599453f;
+      } else {
+        const long long slot = s.part0[b] + ((long long)it.h * n_rows + r) * s.parts[b] + it.part;
+        a.io.part[slot * D + 64 * half + ch] = v;
+        if (half == 0 && ch == 0) {
+          a.io.ml[2 * slot] = mm;
+          a.io.ml[2 * slot + 1] = lt;
+        }
+      }
+    }
+  }
+}
+
+template <int D>
+hipError_t launch(int dtype, const AttnShape& sh, const PagedAttnArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)(a.s.item0[a.s.B] * a.s.H));
+  const int threads = kPagedWaves * 64;
+  if (dtype == HF_F32) {
+    if (sh.rows == 16) paged_attention_kernel<D, 1, true><<<grid, threads, 0, st>>>(a);
+    else paged_attention_kernel<D, 2, true><<<grid, threads, 0, st>>>(a);
+  } else {
+    if (sh.rows == 16) paged_attention_kernel<D, 1, false><<<grid, threads, 0, st>>>(a);
+    else if (sh.rows == 32) paged_attention_kernel<D, 2, false><<<grid, threads, 0, st>>>(a);
+    else paged_attention_kernel<D, 4, false><<<grid, threads, 0, st>>>(a);
+  }
+  return hipGetLastError();
+}
+
+// Heads a workgroup: with many blocks to do all of them, so that the angles of a
+// block are formed once.
+int heads_per_workgroup(const PagedRowsArgs& a) {
+  return (int64_t)a.blk0[a.B] * a.n_layers * a.H >= 4096 ? a.H : 1;
+}
+
+}  // namespace
+
+AttnShape paged_shape(int dtype, int d_h, int64_t max_rows) {
+  AttnShape sh;
+  sh.rows = max_rows <= 16 ? 16 : max_rows <= 32 || dtype == HF_F32 ? 32 : 64;
+  sh.by_keys = 1;
+  sh.wg_target = 512;
+  sh.step = 32 * kPagedWaves;
+  return sh;
+}
+
+hipError_t launch_paged_attention(int dtype, int d_h, const AttnShape& sh, const PagedAttnArgs& a,
+                                  hipStream_t s) {
+  return d_h == 128 ? launch<128>(dtype, sh, a, s) : launch<64>(dtype, sh, a, s);
+}
+
+hipError_t launch_paged_append(int dtype, int d_h, const PagedRowsArgs& a, hipStream_t s) {
+  const int hpw = heads_per_workgroup(a);
+  const dim3 grid((unsigned)(a.blk0[a.B] * ((a.H + hpw - 1) / hpw)), 2, (unsigned)a.n_layers);
+  if (dtype == HF_BF16) {
+    if (d_h == 128) paged_append_kernel<uint16_t, 128><<<grid, 256, 0, s>>>(a, hpw);
+    else paged_append_kernel<uint16_t, 64><<<grid, 128, 0, s>>>(a, hpw);
+  } else {
+    if (d_h == 128) paged_append_kernel<float, 128><<<grid, 256, 0, s>>>(a, hpw);
+    else paged_append_kernel<float, 64><<<grid, 128, 0, s>>>(a, hpw);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_read(int dtype, int d_h, const PagedRowsArgs& a, hipStream_t s) {
+  const int hpw = heads_per_workgroup(a);
+  const dim3 grid((unsigned)(a.blk0[a.B] * ((a.H + hpw - 1) / hpw)), 2, (unsigned)a.n_layers);
+  if (dtype == HF_BF16) {
+    if (d_h == 128) paged_read_kernel<uint16_t, 128><<<grid, 256, 0, s>>>(a, hpw);
+    else paged_read_kernel<uint16_t, 64><<<grid, 128, 0, s>>>(a, hpw);
+  } else {
+    if (d_h == 128) paged_read_kernel<float, 128><<<grid, 256, 0, s>>>(a, hpw);
+    else paged_read_kernel<float, 64><<<grid, 128, 0, s>>>(a, hpw);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace hf

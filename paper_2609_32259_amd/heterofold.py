@@ -12,7 +12,9 @@ The library is loaded on first use; if it has not been built the call raises
 
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
+import math
 import os
 from dataclasses import dataclass
 from typing import Optional, Sequence
@@ -34,6 +36,8 @@ HF_KERNEL_TRANSFER, HF_KERNEL_ROPE_TABLES, HF_KERNEL_ALIGNMENT, HF_KERNEL_PACK =
 HF_KERNEL_MOMENTS_STATS, HF_KERNEL_MOMENTS_COV, HF_KERNEL_RECOLOR_SOLVE, HF_KERNEL_FOLD = 4, 5, 6, 7
 HF_KERNEL_TRANSFER_STAGE = 8
 HF_KERNEL_STAGED_BUILD, HF_KERNEL_STAGED_GEMM = 9, 10
+HF_KERNEL_PROMPT_ATTENTION, HF_KERNEL_PAGED_ATTENTION, HF_KERNEL_ATTENTION_JOIN = 11, 12, 13
+HF_KERNEL_PAGED_APPEND, HF_KERNEL_PAGED_READ = 14, 15
 HF_MAX_BATCH = 64
 ALIGN_MODES = {"overlap": HF_ALIGN_OVERLAP, "ta": HF_ALIGN_TA}
 
@@ -59,6 +63,18 @@ class hf_rope(C.Structure):
 
 class hf_transfer_opts(C.Structure):
     _fields_ = [("inv_r", C.c_void_p), ("k_norm", C.c_void_p), ("k_norm_eps", C.c_float)]
+
+
+class hf_rows(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("dtype", C.c_int32), ("H", C.c_int32), ("d_h", C.c_int32),
+                ("stride_t", C.c_int64), ("stride_h", C.c_int64), ("stride_l", C.c_int64),
+                ("seq_off", C.c_void_p)]
+
+
+class hf_paged_kv(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("table", C.c_void_p), ("table_stride", C.c_int64),
+                ("n_pages", C.c_int32), ("L", C.c_int32), ("H", C.c_int32), ("d_h", C.c_int32),
+                ("page_tokens", C.c_int32)]
 
 
 class hf_recolor_info(C.Structure):
@@ -106,6 +122,23 @@ _SIGNATURES = {
                                         C.c_size_t, C.c_void_p, C.POINTER(hf_rope),
                                         C.POINTER(hf_transfer_opts), C.c_void_p, C.c_size_t,
                                         C.c_void_p]),
+    "hf_attention_workspace_bytes": (C.c_size_t, [C.c_int32, _I32P, _I32P, C.c_int32, C.c_int32,
+                                                  C.c_int32, C.c_int32, C.c_int32]),
+    "hf_prompt_attention": (C.c_int32, [C.c_int32, _I32P, _I32P, C.POINTER(hf_rows),
+                                        C.POINTER(hf_rows), C.POINTER(hf_rows),
+                                        C.POINTER(hf_rows), C.c_float, C.c_int32, C.c_void_p,
+                                        C.c_void_p, C.c_size_t, C.c_void_p]),
+    "hf_paged_page_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
+    "hf_paged_append": (C.c_int32, [C.c_int32, _I32P, _I32P, C.POINTER(hf_paged_kv), C.c_int32,
+                                    C.c_int32, C.POINTER(hf_rows), C.POINTER(hf_rows), C.c_double,
+                                    _I32P, C.c_void_p]),
+    "hf_paged_read": (C.c_int32, [C.c_int32, _I32P, _I32P, C.POINTER(hf_paged_kv), C.c_int32,
+                                  C.c_int32, C.POINTER(hf_rows), C.POINTER(hf_rows),
+                                  C.c_void_p]),
+    "hf_paged_attention": (C.c_int32, [C.c_int32, _I32P, _I32P, C.POINTER(hf_rows),
+                                       C.POINTER(hf_paged_kv), C.c_int32, C.POINTER(hf_rows),
+                                       C.c_float, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t,
+                                       C.c_void_p]),
     "hf_recolor_moments_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int32, C.c_int32]),
     "hf_recolor_moments": (C.c_int32, [C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
                                        C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
@@ -494,6 +527,208 @@ def hf_transfer_kv_taps(s_len, r_len, alignment: Alignment, taps, S, R, A_packed
         _stream(stream))
     _check(st, "hf_transfer_kv_taps")
     return R
+
+
+# ---------------------------------------------------------------------------
+# Attention and the paged cache
+# ---------------------------------------------------------------------------
+
+def _call_on(dev, stream):
+    """Context in which a call's results and workspace are allocated and its kernels
+    launched: the tensors' device, and `stream` (None: that device's current one), so
+    that what is freed on it is not taken by another stream's work meanwhile."""
+    torch = _torch()
+    if stream is None:
+        if dev.index is None or dev.index == torch.cuda.current_device():
+            return contextlib.nullcontext()
+        return torch.cuda.device(dev)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=dev)
+    return torch.cuda.stream(stream)
+
+
+def _lens(a, name, B=None) -> np.ndarray:
+    a = _i32(a)
+    if a.ndim != 1 or (B is not None and a.size != B):
+        raise ValueError(f"{name} must be one length for each sequence")
+    return a
+
+
+def _head_rows(t, lens, name, dev, layers=None):
+    """(hf_rows of a CUDA tensor, what it points to): [N, H, d_h] (the sequences back to
+    back), [B, H, T, d_h] (a role and layer of a cache), or, where layers are asked for,
+    [B, layers, H, T, d_h]."""
+    torch = _torch()
+    nd = t.dim()
+    if not t.is_cuda or t.device != dev:
+        raise TypeError(f"{name} must be a CUDA tensor on {dev}")
+    if nd not in ((3, 4) if layers in (None, 1) else ()) and not (nd == 5 and layers is not None):
+        raise TypeError(f"{name}: shape {tuple(t.shape)} is not [N, H, d_h], [B, H, T, d_h]"
+                        + ("" if layers is None else f" or [B, {layers}, H, T, d_h]"))
+    shape, st = t.shape, t.stride()
+    if shape[-1] > 1 and st[-1] != 1:
+        raise TypeError(f"{name} must have contiguous channels")
+    code = HF_BF16 if t.dtype == torch.bfloat16 else _dtype_code(t)
+    if nd == 3:
+        if shape[0] < int(lens.sum()):
+            raise ValueError(f"{name} holds {shape[0]} rows, the lengths name {int(lens.sum())}")
+        return hf_rows(t.data_ptr(), code, shape[1], shape[2], st[0], st[1], 0, None), None
+    if shape[0] != lens.size or shape[-2] < int(lens.max(initial=0)):
+        raise ValueError(f"{name}: shape {tuple(shape)} does not hold {lens.size} sequences of up "
+                         f"to {int(lens.max(initial=0))} rows")
+    if nd == 5 and shape[1] != layers:
+        raise ValueError(f"{name} must hold {layers} layers")
+    off = np.arange(shape[0], dtype=np.int64) * st[0]
+    return hf_rows(t.data_ptr(), code, shape[-3], shape[-1], st[-2], st[-3],
+                   st[1] if nd == 5 else 0, _p32(off)), off
+
+
+class PagedKV:
+    """A paged cache held in 4 bits: ``pages``, a contiguous uint8 CUDA tensor
+    [L, n_pages, hf_paged_page_bytes(H, d_h, page_tokens)], and ``table``, a contiguous
+    int32 CUDA tensor [B, pages of a sequence] (entries outside [0, n_pages): holes).
+    Both stay the caller's; what they hold may change between calls."""
+
+    def __init__(self, pages, table, H: int, d_h: int, page_tokens: int = 64):
+        torch = _torch()
+        nbytes = hf_paged_page_bytes(H, d_h, page_tokens)
+        if nbytes == 0:
+            raise ValueError("need H >= 1, d_h 64 or 128 and page_tokens 32, 64, 128 or 256")
+        if pages.dtype != torch.uint8 or pages.dim() != 3 or pages.shape[2] != nbytes \
+                or not pages.is_contiguous() or not pages.is_cuda:
+            raise TypeError(f"pages must be a contiguous uint8 CUDA tensor [L, n_pages, {nbytes}]")
+        _dev_i32(table, "table")
+        if table.dim() != 2 or table.device != pages.device:
+            raise TypeError("table must be [B, pages of a sequence], on the pages' device")
+        self.pages, self.table = pages, table
+        self.L, self.H, self.d_h, self.page_tokens = int(pages.shape[0]), int(H), int(d_h), int(page_tokens)
+        self.desc = hf_paged_kv(pages.data_ptr(), table.data_ptr(), int(table.shape[1]),
+                                int(pages.shape[1]), self.L, self.H, self.d_h, self.page_tokens)
+
+    @property
+    def batch(self) -> int:
+        return int(self.table.shape[0])
+
+
+def hf_paged_page_bytes(H: int, d_h: int, page_tokens: int) -> int:
+    return int(lib().hf_paged_page_bytes(int(H), int(d_h), int(page_tokens)))
+
+
+def hf_attention_workspace_bytes(q_len, kv_len, H_q: int, H: int, d_h: int, dtype: int,
+                                 paged: bool = False) -> int:
+    """dtype: HF_BF16 or HF_F32."""
+    q_len = _lens(q_len, "q_len")
+    kv_len = _lens(kv_len, "kv_len", q_len.size)
+    return int(lib().hf_attention_workspace_bytes(q_len.size, _p32(q_len), _p32(kv_len), int(H_q),
+                                                  int(H), int(d_h), int(dtype), int(bool(paged))))
+
+
+def _attention_outputs(q, rq, q_len, kv_len, H, paged, scale, out, lse, return_lse, workspace):
+    """What both attention calls allocate where the caller passes nothing."""
+    torch = _torch()
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    if lse is None:
+        if return_lse:
+            lse = torch.empty((int(q_len.sum()), rq.H), dtype=torch.float32, device=q.device)
+    elif lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != q.device \
+            or lse.numel() < int(q_len.sum()) * rq.H:
+        raise TypeError("lse must be a contiguous fp32 CUDA tensor [rows, H_q]")
+    if workspace is None:
+        nbytes = lib().hf_attention_workspace_bytes(q_len.size, _p32(q_len), _p32(kv_len), rq.H, H,
+                                                    rq.d_h, rq.dtype, paged)
+        if nbytes:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+    return out, lse, workspace, 1.0 / math.sqrt(rq.d_h) if scale is None else float(scale)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def hf_prompt_attention(q, k, v, q_len, kv_len=None, causal=True, scale=None, out=None, lse=None,
+                        return_lse=False, workspace=None, stream=None):
+    """Attention of packed query runs q [N, H_q, d_h] over keys and values k, v: packed
+    [N_k, H, d_h], or views [B, H, T, d_h] of a cache (``R[:, l, 0]``, ``R[:, l, 1]``).
+    q_len, kv_len: lengths [B] (kv_len None: q_len, whole prompts); scale None: 1/sqrt(d_h).
+    Returns out [N, H_q, d_h], with ``return_lse`` (out, lse [N, H_q] fp32)."""
+    q_len = _lens(q_len, "q_len")
+    kv_len = q_len if kv_len is None else _lens(kv_len, "kv_len", q_len.size)
+    dev = q.device
+    with _call_on(dev, stream):
+        rq, kq = _head_rows(q, q_len, "q", dev)
+        rk, kk = _head_rows(k, kv_len, "k", dev)
+        rv, kv = _head_rows(v, kv_len, "v", dev)
+        out, lse, workspace, scale = _attention_outputs(q, rq, q_len, kv_len, rk.H, 0, scale, out,
+                                                        lse, return_lse, workspace)
+        ro, ko = _head_rows(out, q_len, "out", dev)
+        st = lib().hf_prompt_attention(
+            q_len.size, _p32(q_len), _p32(kv_len), C.byref(rq), C.byref(rk), C.byref(rv),
+            C.byref(ro), scale, int(bool(causal)), _ptr(lse), _ptr(workspace),
+            0 if workspace is None else _nbytes(workspace), _stream(stream))
+    _check(st, "hf_prompt_attention")
+    return (out, lse) if return_lse else out
+
+
+def hf_paged_attention(q, cache: PagedKV, q_len, kv_len, layer=0, causal=True, scale=None,
+                       out=None, lse=None, return_lse=False, workspace=None, stream=None):
+    """hf_prompt_attention over the first kv_len [B] tokens of one layer of a paged cache."""
+    q_len = _lens(q_len, "q_len")
+    kv_len = _lens(kv_len, "kv_len", q_len.size)
+    if q_len.size > cache.batch:
+        raise ValueError(f"{q_len.size} sequences, the table has {cache.batch}")
+    dev = cache.pages.device
+    with _call_on(dev, stream):
+        rq, kq = _head_rows(q, q_len, "q", dev)
+        out, lse, workspace, scale = _attention_outputs(q, rq, q_len, kv_len, cache.H, 1, scale,
+                                                        out, lse, return_lse, workspace)
+        ro, ko = _head_rows(out, q_len, "out", dev)
+        st = lib().hf_paged_attention(
+            q_len.size, _p32(q_len), _p32(kv_len), C.byref(rq), C.byref(cache.desc), int(layer),
+            C.byref(ro), scale, int(bool(causal)), _ptr(lse), _ptr(workspace),
+            0 if workspace is None else _nbytes(workspace), _stream(stream))
+    _check(st, "hf_paged_attention")
+    return (out, lse) if return_lse else out
+
+
+def _paged_rows(cache, start, n, k, v, what):
+    start = _lens(start, "start")
+    n = _lens(n, "n", start.size)
+    if n.size > cache.batch:
+        raise ValueError(f"{n.size} sequences, the table has {cache.batch}")
+    layers = int(k.shape[1]) if k.dim() == 5 else 1
+    dev = cache.pages.device
+    rk, kk = _head_rows(k, n, "k", dev, layers)
+    rv, kv = _head_rows(v, n, "v", dev, layers)
+    return start, n, rk, rv, layers, (kk, kv)
+
+
+def hf_paged_append(cache: PagedKV, start, n, k, v, theta=0.0, pos0=None, layer=0, stream=None):
+    """Append rows k, v to tokens start[b] .. start[b] + n[b] of a paged cache: packed
+    [sum n, H, d_h], [B, H, T, d_h], or several layers at once, [B, layers, H, T, d_h]
+    (``R[:, :, 0]``, ``R[:, :, 1]`` of a transferred cache).  theta > 0 rotates the keys at
+    positions pos0[b] + start[b] + i; 0 stores them as given."""
+    start, n, rk, rv, layers, keep = _paged_rows(cache, start, n, k, v, "hf_paged_append")
+    p0 = None if pos0 is None else _lens(pos0, "pos0", n.size)
+    with _call_on(cache.pages.device, stream):
+        st = lib().hf_paged_append(n.size, _p32(start), _p32(n), C.byref(cache.desc), int(layer),
+                                   layers, C.byref(rk), C.byref(rv), float(theta),
+                                   None if p0 is None else _p32(p0), _stream(stream))
+    _check(st, "hf_paged_append")
+    return cache
+
+
+def hf_paged_read(cache: PagedKV, start, n, k, v, layer=0, stream=None):
+    """Write the values of tokens start[b] .. start[b] + n[b] into the dense rows k, v
+    (shapes as hf_paged_append), and return (k, v)."""
+    start, n, rk, rv, layers, keep = _paged_rows(cache, start, n, k, v, "hf_paged_read")
+    with _call_on(cache.pages.device, stream):
+        st = lib().hf_paged_read(n.size, _p32(start), _p32(n), C.byref(cache.desc), int(layer),
+                                 layers, C.byref(rk), C.byref(rv), _stream(stream))
+    _check(st, "hf_paged_read")
+    return k, v
 
 
 # ---------------------------------------------------------------------------
