@@ -823,15 +823,35 @@ int32_t plan_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len, i
   if (total > INT32_MAX || max_rows > INT32_MAX - 1024 || total * H_q > ((int64_t)1 << 40))
     return fail(HF_ERR_SHAPE, "too many query rows");
   sh = paged ? hf::paged_shape(dtype, d_h, max_rows) : hf::prompt_shape(dtype, d_h, max_rows);
-  int64_t work = 0;  // keys, summed over the row tiles
+  // The cut with the least rounds of workgroups times the longest part, where the
+  // uncut items are not many rounds anyway (kStart keys: a part's fixed cost).
+  constexpr int64_t kStart = 192;
+  int64_t longest = 1, uncut = 0;
+  int64_t of_seq[HF_MAX_BATCH];
   for (int b = 0; b < B; ++b) {
-    const int64_t tiles = ((int64_t)q_len[b] * G + sh.rows - 1) / sh.rows;
-    // (a causal prompt's tiles see half of its keys on average)
-    const int64_t seen = causal && q_len[b] > 0 ? std::max<int64_t>(kv_len[b] - q_len[b] / 2, (kv_len[b] + 1) / 2) : kv_len[b];
-    work += tiles * seen * H;
+    of_seq[b] = ((int64_t)q_len[b] * G + sh.rows - 1) / sh.rows * H;
+    uncut += of_seq[b];
+    if (q_len[b] > 0) longest = std::max(longest, (int64_t)kv_len[b]);
   }
-  int64_t chunk = (work + sh.wg_target - 1) / sh.wg_target;
-  chunk = std::max<int64_t>((chunk + sh.step - 1) / sh.step * sh.step, 2 * sh.step);
+  int64_t chunk = longest;
+  if (uncut > 0 && uncut < 4 * (int64_t)sh.wg_target) {
+    int64_t best = INT64_MAX;
+    const int64_t most = std::min<int64_t>((longest + sh.step - 1) / sh.step, sh.wg_target);
+    for (int64_t k = 1; k <= most; ++k) {  // (k B H <= 4 wg_target: at most some thousand divisions)
+      const int64_t c = (longest + k * sh.step - 1) / (k * sh.step) * sh.step;
+      int64_t n = 0;
+      for (int b = 0; b < B; ++b)
+        n += of_seq[b] * std::max<uint32_t>(((uint32_t)kv_len[b] + (uint32_t)c - 1) / (uint32_t)c, 1);
+      const int64_t cost = (n + sh.wg_target - 1) / sh.wg_target * (std::min(c, longest) + kStart) +
+                           (k > 1 ? sh.join_keys : 0);
+      if (cost < best) {
+        best = cost;
+        chunk = c;
+      }
+      if (n > 4 * (int64_t)sh.wg_target) break;
+    }
+  }
+  chunk = (chunk + sh.step - 1) / sh.step * sh.step;
   s.chunk = (int32_t)std::min<int64_t>(chunk, INT32_MAX / 2 / sh.step * sh.step);
   s.B = B;
   s.H = H;
@@ -1032,14 +1052,10 @@ size_t hf_attention_workspace_bytes(int32_t B, const int32_t* q_len, const int32
   if (dtype != HF_F32 && dtype != HF_BF16) return 0;
   hf::AttnShape sh;
   hf::AttnSeqs s;
-  size_t most = 0;
-  for (int causal = 0; causal < 2; ++causal) {  // (the cutting depends on it)
-    int64_t slots = 0;
-    if (plan_attention(B, q_len, kv_len, H_q, H, dtype, d_h, paged != 0, causal, sh, s, slots)) return 0;
-    most = std::max(most, part_bytes(slots, d_h));
-  }
+  int64_t slots = 0;
+  if (plan_attention(B, q_len, kv_len, H_q, H, dtype, d_h, paged != 0, 0, sh, s, slots)) return 0;
   ok();
-  return most;
+  return part_bytes(slots, d_h);
 }
 
 int32_t hf_prompt_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len,

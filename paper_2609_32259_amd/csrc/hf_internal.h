@@ -221,6 +221,7 @@ struct AttnShape {
   int32_t by_keys;
   int32_t wg_target;  // workgroups that fill the chip
   int32_t step;       // keys that parts are cut in multiples of
+  int32_t join_keys;  // the joining launch's time, in keys of a part
 };
 AttnShape prompt_shape(int dtype, int d_h, int64_t max_rows);
 AttnShape paged_shape(int dtype, int d_h, int64_t max_rows);

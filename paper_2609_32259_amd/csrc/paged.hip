@@ -348,6 +348,28 @@ FI bf16x8 eight_codes(uint32_t w) {
   return x.v;
 }
 
+// The same as code - 8, for fp32: 16 + code beside sums of up to 16 would cost four
+// more bits of the fp32 accumulation than code - 8 does.
+FI bf16x8 eight_centred(uint32_t w) {
+  union {
+    uint32_t u[4];
+    bf16x8 v;
+  } x;
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    const uint32_t p = two_codes(w, n);
+    const float lo = __builtin_bit_cast(float, p << 16) - 24.0f;
+    const float hi = __builtin_bit_cast(float, p & 0xffff0000u) - 24.0f;
+    x.u[n] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo),
+                                   0x07060302u);  // (exact: the upper halves)
+  }
+  return x.v;
+}
+template <bool F32>
+FI bf16x8 code_operand(uint32_t w) {
+  return F32 ? eight_centred(w) : eight_codes(w);
+}
+
 // x as S bf16 terms whose sum holds 8 S bits of it.
 template <int S>
 FI void split(float x, float (&t)[S]) {
@@ -386,7 +408,7 @@ template <int D, int NT, bool F32>
 __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const PagedAttnArgs a) {
   constexpr int G = D / 32, NC = D / 16, S = F32 ? 3 : 1, R = 16 * NT;
   constexpr int NW = kPagedWaves;
-  // scales, and offsets freed of the codes' 16 (keys) or moved to code 8 (values)
+  // scales, and offsets freed of the operands' 16 (keys) or moved to code 8 (values; fp32: both)
   __shared__ __attribute__((aligned(16))) float lds[NW * 64 * G * 2 > NW * 64 * R ? NW * 64 * G * 2 : NW * 64 * R];
   __shared__ float sm[NW][R], sl[NW][R];
   typedef float fG __attribute__((ext_vector_type(G)));
@@ -427,12 +449,11 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
 #pragma unroll
         for (int z = 0; z < S; ++z) q[x][z][y][e < 4 ? 2 * e : 2 * (e - 4) + 1] = (__bf16)p[z];
       }
-      sum += __shfl_xor(sum, 16);
-      qs[x][y] = sum + __shfl_xor(sum, 32);
+      qs[x][y] = add_xor32(add_xor16(sum));
     }
   }
 
-  f32x4 o[NT][NC] = {};    // sum of (p s) (16 + code): row col, channels 16 n + 4 m4 + i
+  f32x4 o[NT][NC] = {};    // sum of (p s) times the operand: row col, channels 16 n + 4 m4 + i
   f32x4 ps[NT][G] = {};    // sum of the rounded p s
   float po[NT][G] = {};    // sum of p times the offset, over the lane's tokens
   float m[NT], l[NT];
@@ -471,7 +492,7 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
     for (int y = 0; y < G; ++y) {
       const uint32_t w = live ? x.w[y] : 0u;
       vs[y] = __builtin_bit_cast(float, w & 0xffff0000u);
-      vo[y] = fmaf(vs[y], lane < 32 ? -16.0f : 8.0f, __builtin_bit_cast(float, w << 16));
+      vo[y] = fmaf(vs[y], F32 || lane >= 32 ? 8.0f : -16.0f, __builtin_bit_cast(float, w << 16));
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     sc[lane] = vs;
@@ -484,7 +505,7 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
     for (int u = 0; u < 2; ++u) {
       bf16x8 kc[G];
 #pragma unroll
-      for (int y = 0; y < G; ++y) kc[y] = eight_codes(x.k[u][y]);
+      for (int y = 0; y < G; ++y) kc[y] = code_operand<F32>(x.k[u][y]);
       fG ks[4], ko[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -520,8 +541,7 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
       float mx = p[n][0];
 #pragma unroll
       for (int i = 1; i < 8; ++i) mx = fmaxf(mx, p[n][i]);
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32)) * c;
+      mx = max_xor32(max_xor16(mx)) * c;
       if (__any(mx > m[n] + kRaise)) {
         const float nm = mx > m[n] + kRaise ? mx : m[n];  // (each row by its own scores alone)
         const float f = __builtin_amdgcn_exp2f(m[n] - nm);
@@ -544,7 +564,7 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
 
     bf16x8 vc[NC];
 #pragma unroll
-    for (int y = 0; y < NC; ++y) vc[y] = eight_codes(x.v[y]);
+    for (int y = 0; y < NC; ++y) vc[y] = code_operand<F32>(x.v[y]);
     fG zs[8], zo[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -578,7 +598,7 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
           } pw;
 #pragma unroll
           for (int i = 0; i < 4; ++i) pw.u[i] = pack_bf16(w[i][z], w[4 + i][z]);
-          ps[n][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, pw.v, ps[n][y], 0, 0, 0);
+          if (!F32) ps[n][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, pw.v, ps[n][y], 0, 0, 0);
           o[n][2 * y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vc[2 * y], pw.v, o[n][2 * y], 0, 0, 0);
           o[n][2 * y + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vc[2 * y + 1], pw.v, o[n][2 * y + 1], 0, 0, 0);
         }
@@ -611,17 +631,14 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
   // offsets of all lanes' tokens
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    l[n] += __shfl_xor(l[n], 16);
-    l[n] += __shfl_xor(l[n], 32);
+    l[n] = add_xor32(add_xor16(l[n]));
 #pragma unroll
     for (int y = 0; y < G; ++y) {
-      float x = po[n][y];
-      x += __shfl_xor(x, 16);
-      x += __shfl_xor(x, 32);
+      const float x = add_xor32(add_xor16(po[n][y]));
 #pragma unroll
       for (int z = 0; z < 2; ++z)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[n][2 * y + z][i] += fmaf(-24.0f, ps[n][y][i], x);
+        for (int i = 0; i < 4; ++i) o[n][2 * y + z][i] += F32 ? x : fmaf(-24.0f, ps[n][y][i], x);
     }
     if (m4 == 0) {
       sm[wave][16 * n + col] = m[n];
@@ -713,6 +730,7 @@ AttnShape paged_shape(int dtype, int d_h, int64_t max_rows) {
   sh.by_keys = 1;
   sh.wg_target = 512;
   sh.step = 32 * kPagedWaves;
+  sh.join_keys = 512;
   return sh;
 }
 
