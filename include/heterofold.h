@@ -395,22 +395,20 @@ int32_t hf_transfer_kv_taps(int32_t B, const int32_t* s_len, const int32_t* r_le
 
 /*
  * Rows of heads in device memory: element (l, row t of sequence b, head h,
- * channel e) lives at ptr + seq_off[b] + l*stride_l + t*stride_t + h*stride_h + e
- * (in elements; channels contiguous).  seq_off: host int64 [B], read during the
- * call, or NULL: the sequences lie back to back (packed), sequence b's first row
- * after those of the sequences before it.  So it describes packed projections
- * ([N][H][d_h], also as a part of a fused one) and, with seq_off[b] =
- * b*stride_b and ptr at a role, a cache that an hf_kv_desc describes.  stride_l
- * is read by the paged calls only.  ptr, strides and offsets must be >= 0 and
- * keep rows 16-byte aligned, and stride_t and stride_h of rows that a call
+ * channel e) lives at ptr + b*stride_b + l*stride_l + t*stride_t + h*stride_h + e
+ * (in elements; channels contiguous).  stride_b == -1: the sequences lie back to
+ * back (packed), sequence b's first row after those of the sequences before it.
+ * So it describes packed projections ([N][H][d_h], also as a part of a fused one)
+ * and, with ptr at a role, a cache that an hf_kv_desc describes.  stride_l is
+ * read by the paged calls only.  ptr and strides must be >= 0 (but for that -1)
+ * and keep rows 16-byte aligned, and stride_t and stride_h of rows that a call
  * writes must be >= d_h.  Rows of one call that overlap where it writes race.
  */
 typedef struct hf_rows {
   void* ptr;
   int32_t dtype; /* hf_dtype */
   int32_t H, d_h;
-  int64_t stride_t, stride_h, stride_l;
-  const int64_t* seq_off;
+  int64_t stride_b, stride_l, stride_h, stride_t;
 } hf_rows;
 
 /*

@@ -777,24 +777,20 @@ int32_t check_lens(int32_t B, const char* na, const int32_t* a, const char* nb, 
 }
 
 // used: some row of it is read or written.  layers: stride_l is used.
-int32_t check_rows(const char* name, const hf_rows* r, int32_t B, bool used, bool written,
-                   bool layers) {
+int32_t check_rows(const char* name, const hf_rows* r, bool used, bool written, bool layers) {
   if (!r) return fail(HF_ERR_NULL, "%s is NULL", name);
   if (r->dtype != HF_F32 && r->dtype != HF_BF16) return fail(HF_ERR_DTYPE, "%s->dtype %d unknown", name, r->dtype);
   if (r->H < 1 || r->d_h < 1) return fail(HF_ERR_SHAPE, "%s: need H >= 1 and d_h >= 1", name);
   const int64_t vec = r->dtype == HF_BF16 ? 8 : 4;  // elements per 16 bytes
   if (used && !r->ptr) return fail(HF_ERR_NULL, "%s->ptr is NULL", name);
   if (!aligned16(r->ptr)) return fail(HF_ERR_SHAPE, "%s->ptr is not 16-byte aligned", name);
-  const int64_t st[3] = {r->stride_t, r->stride_h, layers ? r->stride_l : 0};
+  const int64_t st[4] = {r->stride_t, r->stride_h, layers ? r->stride_l : 0,
+                         r->stride_b == -1 ? 0 : r->stride_b};
   for (int64_t x : st)
     if (x < 0 || x % vec)
       return fail(HF_ERR_SHAPE, "%s: strides must be >= 0 and keep rows 16-byte aligned", name);
   if (written && (r->stride_t < r->d_h || (r->H > 1 && r->stride_h < r->d_h)))
     return fail(HF_ERR_SHAPE, "%s: rows that are written need stride_t and stride_h >= d_h", name);
-  if (r->seq_off)
-    for (int b = 0; b < B; ++b)
-      if (r->seq_off[b] < 0 || r->seq_off[b] % vec)
-        return fail(HF_ERR_SHAPE, "%s: seq_off[%d] must be >= 0 and keep rows 16-byte aligned", name, b);
   return HF_OK;
 }
 
@@ -802,7 +798,7 @@ int32_t check_rows(const char* name, const hf_rows* r, int32_t B, bool used, boo
 void offsets(const hf_rows* r, int32_t B, const int32_t* len, int64_t* off) {
   int64_t at = 0;
   for (int b = 0; b < B; ++b) {
-    off[b] = r->seq_off ? r->seq_off[b] : at * r->stride_t;
+    off[b] = r->stride_b == -1 ? at * r->stride_t : b * r->stride_b;
     at += len[b];
   }
 }
@@ -902,8 +898,8 @@ int32_t attention_common(int32_t B, const int32_t* q_len, const int32_t* kv_len,
   int64_t rows = 0;
   for (int b = 0; b < B; ++b) rows += q_len[b];
   int32_t st;
-  if ((st = check_rows("q", q, B, rows > 0, false, false)) ||
-      (st = check_rows("out", out, B, rows > 0, true, false)))
+  if ((st = check_rows("q", q, rows > 0, false, false)) ||
+      (st = check_rows("out", out, rows > 0, true, false)))
     return st;
   if (q->dtype != out->dtype) return fail(HF_ERR_DTYPE, "q and out dtypes differ");
   if (q->H != out->H || q->d_h != out->d_h || q->d_h != d_h)
@@ -985,8 +981,8 @@ int32_t paged_rows(bool append, int32_t B, const int32_t* start, const int32_t* 
   if ((st = check_lens(B, "start", start, "n", n)) || (st = check_paged(cache, layer, n_layers))) return st;
   int64_t total = 0;
   for (int b = 0; b < B; ++b) total += n[b];
-  if ((st = check_rows("k", k, B, total > 0, !append, true)) ||
-      (st = check_rows("v", v, B, total > 0, !append, true)))
+  if ((st = check_rows("k", k, total > 0, !append, true)) ||
+      (st = check_rows("v", v, total > 0, !append, true)))
     return st;
   if (k->dtype != v->dtype) return fail(HF_ERR_DTYPE, "k and v dtypes differ");
   if (k->H != cache->H || v->H != cache->H || k->d_h != cache->d_h || v->d_h != cache->d_h)
@@ -1066,8 +1062,8 @@ int32_t hf_prompt_attention(int32_t B, const int32_t* q_len, const int32_t* kv_l
   if ((st = check_lens(B, "q_len", q_len, "kv_len", kv_len))) return st;
   int64_t keys = 0;
   for (int b = 0; b < B; ++b) keys += q_len[b] > 0 ? kv_len[b] : 0;
-  if ((st = check_rows("k", k, B, keys > 0, false, false)) ||
-      (st = check_rows("v", v, B, keys > 0, false, false)))
+  if ((st = check_rows("k", k, keys > 0, false, false)) ||
+      (st = check_rows("v", v, keys > 0, false, false)))
     return st;
   if (k->H != v->H || k->d_h != v->d_h) return fail(HF_ERR_SHAPE, "k and v differ in heads or d_h");
   hf::AttnShape sh;

@@ -67,8 +67,8 @@ class hf_transfer_opts(C.Structure):
 
 class hf_rows(C.Structure):
     _fields_ = [("ptr", C.c_void_p), ("dtype", C.c_int32), ("H", C.c_int32), ("d_h", C.c_int32),
-                ("stride_t", C.c_int64), ("stride_h", C.c_int64), ("stride_l", C.c_int64),
-                ("seq_off", C.c_void_p)]
+                ("stride_b", C.c_int64), ("stride_l", C.c_int64), ("stride_h", C.c_int64),
+                ("stride_t", C.c_int64)]
 
 
 class hf_paged_kv(C.Structure):
@@ -533,54 +533,67 @@ def hf_transfer_kv_taps(s_len, r_len, alignment: Alignment, taps, S, R, A_packed
 # Attention and the paged cache
 # ---------------------------------------------------------------------------
 
+@contextlib.contextmanager
+def _other_stream(dev, stream):
+    torch = _torch()
+    if stream is None:
+        with torch.cuda.device(dev):
+            yield
+    else:
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=dev)
+        with torch.cuda.stream(stream):
+            yield
+
+
+_here = contextlib.nullcontext()
+
+
 def _call_on(dev, stream):
     """Context in which a call's results and workspace are allocated and its kernels
     launched: the tensors' device, and `stream` (None: that device's current one), so
     that what is freed on it is not taken by another stream's work meanwhile."""
-    torch = _torch()
-    if stream is None:
-        if dev.index is None or dev.index == torch.cuda.current_device():
-            return contextlib.nullcontext()
-        return torch.cuda.device(dev)
-    if isinstance(stream, int):
-        stream = torch.cuda.ExternalStream(stream, device=dev)
-    return torch.cuda.stream(stream)
+    if stream is None and dev.index == _torch()._C._cuda_getDevice():
+        return _here
+    return _other_stream(dev, stream)
 
 
-def _lens(a, name, B=None) -> np.ndarray:
-    a = _i32(a)
+def _raw_stream(dev) -> int:
+    """The current stream of a device (within _call_on: the call's)."""
+    return _torch()._C._cuda_getCurrentRawStream(dev.index)
+
+
+def _lens(a, name, B=None):
+    """Host int32 array and list of a batch's lengths."""
+    a = np.ascontiguousarray(a, dtype=np.int32)
     if a.ndim != 1 or (B is not None and a.size != B):
         raise ValueError(f"{name} must be one length for each sequence")
-    return a
+    return a, a.tolist()
 
 
-def _head_rows(t, lens, name, dev, layers=None):
-    """(hf_rows of a CUDA tensor, what it points to): [N, H, d_h] (the sequences back to
-    back), [B, H, T, d_h] (a role and layer of a cache), or, where layers are asked for,
-    [B, layers, H, T, d_h]."""
+def _head_rows(t, lens, name, dev, layers=None) -> hf_rows:
+    """Descriptor of a CUDA tensor [N, H, d_h] (the sequences back to back), [B, H, T, d_h]
+    (a role and layer of a cache), or, where layers are asked for, [B, layers, H, T, d_h]."""
     torch = _torch()
-    nd = t.dim()
-    if not t.is_cuda or t.device != dev:
+    if t.device != dev:
         raise TypeError(f"{name} must be a CUDA tensor on {dev}")
-    if nd not in ((3, 4) if layers in (None, 1) else ()) and not (nd == 5 and layers is not None):
-        raise TypeError(f"{name}: shape {tuple(t.shape)} is not [N, H, d_h], [B, H, T, d_h]"
-                        + ("" if layers is None else f" or [B, {layers}, H, T, d_h]"))
     shape, st = t.shape, t.stride()
-    if shape[-1] > 1 and st[-1] != 1:
+    nd = len(shape)
+    code = HF_BF16 if t.dtype is torch.bfloat16 else _dtype_code(t)
+    if st[-1] != 1 and shape[-1] > 1:
         raise TypeError(f"{name} must have contiguous channels")
-    code = HF_BF16 if t.dtype == torch.bfloat16 else _dtype_code(t)
-    if nd == 3:
-        if shape[0] < int(lens.sum()):
-            raise ValueError(f"{name} holds {shape[0]} rows, the lengths name {int(lens.sum())}")
-        return hf_rows(t.data_ptr(), code, shape[1], shape[2], st[0], st[1], 0, None), None
-    if shape[0] != lens.size or shape[-2] < int(lens.max(initial=0)):
-        raise ValueError(f"{name}: shape {tuple(shape)} does not hold {lens.size} sequences of up "
-                         f"to {int(lens.max(initial=0))} rows")
-    if nd == 5 and shape[1] != layers:
-        raise ValueError(f"{name} must hold {layers} layers")
-    off = np.arange(shape[0], dtype=np.int64) * st[0]
-    return hf_rows(t.data_ptr(), code, shape[-3], shape[-1], st[-2], st[-3],
-                   st[1] if nd == 5 else 0, _p32(off)), off
+    if nd == 3 and layers in (None, 1):
+        if shape[0] < sum(lens):
+            raise ValueError(f"{name} holds {shape[0]} rows, the lengths name {sum(lens)}")
+        return hf_rows(t.data_ptr(), code, shape[1], shape[2], -1, 0, st[1], st[0])
+    if not (nd == 4 and layers in (None, 1)) and not (nd == 5 and layers == shape[1]):
+        raise TypeError(f"{name}: shape {tuple(shape)} is not [N, H, d_h], [B, H, T, d_h]"
+                        + ("" if layers is None else f" or [B, {layers}, H, T, d_h]"))
+    if shape[0] != len(lens) or shape[-2] < max(lens, default=0):
+        raise ValueError(f"{name}: shape {tuple(shape)} does not hold {len(lens)} sequences of up "
+                         f"to {max(lens, default=0)} rows")
+    return hf_rows(t.data_ptr(), code, shape[-3], shape[-1], st[0], st[1] if nd == 5 else 0, st[-3],
+                   st[-2])
 
 
 class PagedKV:
@@ -600,14 +613,11 @@ class PagedKV:
         _dev_i32(table, "table")
         if table.dim() != 2 or table.device != pages.device:
             raise TypeError("table must be [B, pages of a sequence], on the pages' device")
-        self.pages, self.table = pages, table
+        self.pages, self.table, self.batch = pages, table, int(table.shape[0])
         self.L, self.H, self.d_h, self.page_tokens = int(pages.shape[0]), int(H), int(d_h), int(page_tokens)
         self.desc = hf_paged_kv(pages.data_ptr(), table.data_ptr(), int(table.shape[1]),
                                 int(pages.shape[1]), self.L, self.H, self.d_h, self.page_tokens)
 
-    @property
-    def batch(self) -> int:
-        return int(self.table.shape[0])
 
 
 def hf_paged_page_bytes(H: int, d_h: int, page_tokens: int) -> int:
@@ -617,13 +627,14 @@ def hf_paged_page_bytes(H: int, d_h: int, page_tokens: int) -> int:
 def hf_attention_workspace_bytes(q_len, kv_len, H_q: int, H: int, d_h: int, dtype: int,
                                  paged: bool = False) -> int:
     """dtype: HF_BF16 or HF_F32."""
-    q_len = _lens(q_len, "q_len")
-    kv_len = _lens(kv_len, "kv_len", q_len.size)
+    q_len, _ = _lens(q_len, "q_len")
+    kv_len, _ = _lens(kv_len, "kv_len", q_len.size)
     return int(lib().hf_attention_workspace_bytes(q_len.size, _p32(q_len), _p32(kv_len), int(H_q),
                                                   int(H), int(d_h), int(dtype), int(bool(paged))))
 
 
-def _attention_outputs(q, rq, q_len, kv_len, H, paged, scale, out, lse, return_lse, workspace):
+def _attention_outputs(q, rq, rows, q_len, kv_len, H, paged, scale, out, lse, return_lse,
+                       workspace):
     """What both attention calls allocate where the caller passes nothing."""
     torch = _torch()
     if out is None:
@@ -632,15 +643,17 @@ def _attention_outputs(q, rq, q_len, kv_len, H, paged, scale, out, lse, return_l
         raise ValueError("out must have q's shape")
     if lse is None:
         if return_lse:
-            lse = torch.empty((int(q_len.sum()), rq.H), dtype=torch.float32, device=q.device)
+            lse = torch.empty((rows, rq.H), dtype=torch.float32, device=q.device)
     elif lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != q.device \
-            or lse.numel() < int(q_len.sum()) * rq.H:
+            or lse.numel() < rows * rq.H:
         raise TypeError("lse must be a contiguous fp32 CUDA tensor [rows, H_q]")
     if workspace is None:
         nbytes = lib().hf_attention_workspace_bytes(q_len.size, _p32(q_len), _p32(kv_len), rq.H, H,
                                                     rq.d_h, rq.dtype, paged)
         if nbytes:
             workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+    elif workspace.device != q.device or not workspace.is_contiguous():
+        raise TypeError("workspace must be a contiguous CUDA tensor on q's device")
     return out, lse, workspace, 1.0 / math.sqrt(rq.d_h) if scale is None else float(scale)
 
 
@@ -654,20 +667,21 @@ def hf_prompt_attention(q, k, v, q_len, kv_len=None, causal=True, scale=None, ou
     [N_k, H, d_h], or views [B, H, T, d_h] of a cache (``R[:, l, 0]``, ``R[:, l, 1]``).
     q_len, kv_len: lengths [B] (kv_len None: q_len, whole prompts); scale None: 1/sqrt(d_h).
     Returns out [N, H_q, d_h], with ``return_lse`` (out, lse [N, H_q] fp32)."""
-    q_len = _lens(q_len, "q_len")
-    kv_len = q_len if kv_len is None else _lens(kv_len, "kv_len", q_len.size)
+    nq, lq = _lens(q_len, "q_len")
+    nk, lk = (nq, lq) if kv_len is None else _lens(kv_len, "kv_len", nq.size)
     dev = q.device
+    if not q.is_cuda:
+        raise TypeError("q must be a CUDA tensor")
     with _call_on(dev, stream):
-        rq, kq = _head_rows(q, q_len, "q", dev)
-        rk, kk = _head_rows(k, kv_len, "k", dev)
-        rv, kv = _head_rows(v, kv_len, "v", dev)
-        out, lse, workspace, scale = _attention_outputs(q, rq, q_len, kv_len, rk.H, 0, scale, out,
+        rq = _head_rows(q, lq, "q", dev)
+        rk = _head_rows(k, lk, "k", dev)
+        rv = _head_rows(v, lk, "v", dev)
+        out, lse, workspace, scale = _attention_outputs(q, rq, sum(lq), nq, nk, rk.H, 0, scale, out,
                                                         lse, return_lse, workspace)
-        ro, ko = _head_rows(out, q_len, "out", dev)
+        ro = _head_rows(out, lq, "out", dev)
         st = lib().hf_prompt_attention(
-            q_len.size, _p32(q_len), _p32(kv_len), C.byref(rq), C.byref(rk), C.byref(rv),
-            C.byref(ro), scale, int(bool(causal)), _ptr(lse), _ptr(workspace),
-            0 if workspace is None else _nbytes(workspace), _stream(stream))
+            nq.size, _p32(nq), _p32(nk), rq, rk, rv, ro, scale, 1 if causal else 0, _ptr(lse),
+            _ptr(workspace), 0 if workspace is None else _nbytes(workspace), _raw_stream(dev))
     _check(st, "hf_prompt_attention")
     return (out, lse) if return_lse else out
 
@@ -675,34 +689,32 @@ def hf_prompt_attention(q, k, v, q_len, kv_len=None, causal=True, scale=None, ou
 def hf_paged_attention(q, cache: PagedKV, q_len, kv_len, layer=0, causal=True, scale=None,
                        out=None, lse=None, return_lse=False, workspace=None, stream=None):
     """hf_prompt_attention over the first kv_len [B] tokens of one layer of a paged cache."""
-    q_len = _lens(q_len, "q_len")
-    kv_len = _lens(kv_len, "kv_len", q_len.size)
-    if q_len.size > cache.batch:
-        raise ValueError(f"{q_len.size} sequences, the table has {cache.batch}")
+    nq, lq = _lens(q_len, "q_len")
+    nk, lk = _lens(kv_len, "kv_len", nq.size)
+    if nq.size > cache.batch:
+        raise ValueError(f"{nq.size} sequences, the table has {cache.batch}")
     dev = cache.pages.device
     with _call_on(dev, stream):
-        rq, kq = _head_rows(q, q_len, "q", dev)
-        out, lse, workspace, scale = _attention_outputs(q, rq, q_len, kv_len, cache.H, 1, scale,
+        rq = _head_rows(q, lq, "q", dev)
+        out, lse, workspace, scale = _attention_outputs(q, rq, sum(lq), nq, nk, cache.H, 1, scale,
                                                         out, lse, return_lse, workspace)
-        ro, ko = _head_rows(out, q_len, "out", dev)
+        ro = _head_rows(out, lq, "out", dev)
         st = lib().hf_paged_attention(
-            q_len.size, _p32(q_len), _p32(kv_len), C.byref(rq), C.byref(cache.desc), int(layer),
-            C.byref(ro), scale, int(bool(causal)), _ptr(lse), _ptr(workspace),
-            0 if workspace is None else _nbytes(workspace), _stream(stream))
+            nq.size, _p32(nq), _p32(nk), rq, cache.desc, int(layer), ro, scale,
+            1 if causal else 0, _ptr(lse), _ptr(workspace),
+            0 if workspace is None else _nbytes(workspace), _raw_stream(dev))
     _check(st, "hf_paged_attention")
     return (out, lse) if return_lse else out
 
 
-def _paged_rows(cache, start, n, k, v, what):
-    start = _lens(start, "start")
-    n = _lens(n, "n", start.size)
+def _paged_rows(cache, start, n, k, v):
+    start, _ = _lens(start, "start")
+    n, ln = _lens(n, "n", start.size)
     if n.size > cache.batch:
         raise ValueError(f"{n.size} sequences, the table has {cache.batch}")
-    layers = int(k.shape[1]) if k.dim() == 5 else 1
+    layers = k.shape[1] if k.dim() == 5 else 1
     dev = cache.pages.device
-    rk, kk = _head_rows(k, n, "k", dev, layers)
-    rv, kv = _head_rows(v, n, "v", dev, layers)
-    return start, n, rk, rv, layers, (kk, kv)
+    return start, n, _head_rows(k, ln, "k", dev, layers), _head_rows(v, ln, "v", dev, layers), layers
 
 
 def hf_paged_append(cache: PagedKV, start, n, k, v, theta=0.0, pos0=None, layer=0, stream=None):
@@ -710,12 +722,13 @@ def hf_paged_append(cache: PagedKV, start, n, k, v, theta=0.0, pos0=None, layer=
     [sum n, H, d_h], [B, H, T, d_h], or several layers at once, [B, layers, H, T, d_h]
     (``R[:, :, 0]``, ``R[:, :, 1]`` of a transferred cache).  theta > 0 rotates the keys at
     positions pos0[b] + start[b] + i; 0 stores them as given."""
-    start, n, rk, rv, layers, keep = _paged_rows(cache, start, n, k, v, "hf_paged_append")
-    p0 = None if pos0 is None else _lens(pos0, "pos0", n.size)
-    with _call_on(cache.pages.device, stream):
-        st = lib().hf_paged_append(n.size, _p32(start), _p32(n), C.byref(cache.desc), int(layer),
-                                   layers, C.byref(rk), C.byref(rv), float(theta),
-                                   None if p0 is None else _p32(p0), _stream(stream))
+    start, n, rk, rv, layers = _paged_rows(cache, start, n, k, v)
+    p0 = None if pos0 is None else _lens(pos0, "pos0", n.size)[0]
+    dev = cache.pages.device
+    with _call_on(dev, stream):
+        st = lib().hf_paged_append(n.size, _p32(start), _p32(n), cache.desc, int(layer), layers, rk,
+                                   rv, float(theta), None if p0 is None else _p32(p0),
+                                   _raw_stream(dev))
     _check(st, "hf_paged_append")
     return cache
 
@@ -723,10 +736,11 @@ def hf_paged_append(cache: PagedKV, start, n, k, v, theta=0.0, pos0=None, layer=
 def hf_paged_read(cache: PagedKV, start, n, k, v, layer=0, stream=None):
     """Write the values of tokens start[b] .. start[b] + n[b] into the dense rows k, v
     (shapes as hf_paged_append), and return (k, v)."""
-    start, n, rk, rv, layers, keep = _paged_rows(cache, start, n, k, v, "hf_paged_read")
-    with _call_on(cache.pages.device, stream):
-        st = lib().hf_paged_read(n.size, _p32(start), _p32(n), C.byref(cache.desc), int(layer),
-                                 layers, C.byref(rk), C.byref(rv), _stream(stream))
+    start, n, rk, rv, layers = _paged_rows(cache, start, n, k, v)
+    dev = cache.pages.device
+    with _call_on(dev, stream):
+        st = lib().hf_paged_read(n.size, _p32(start), _p32(n), cache.desc, int(layer), layers, rk,
+                                 rv, _raw_stream(dev))
     _check(st, "hf_paged_read")
     return k, v
 
