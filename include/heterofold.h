@@ -518,7 +518,7 @@ int32_t hf_paged_read(int32_t B, const int32_t* start, const int32_t* n, const h
 
 /*
  * hf_prompt_attention over the first kv_len[b] tokens of one layer of a paged
- * cache, for decoded tokens and short runs (any q_len is served; each 64 query
+ * cache, for decoded tokens and short runs (any q_len is served; each 32 query
  * rows of a group read the cache once more).  Arguments, masks, results and
  * errors as there; workspace >= hf_attention_workspace_bytes(..., paged = 1).
  * Numerics: the codes enter the matrix products as whole numbers, exactly, and

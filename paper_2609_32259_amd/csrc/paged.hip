@@ -380,12 +380,14 @@ FI void split(float x, float (&t)[S]) {
   }
 }
 
-template <int D, bool F32>
-struct Block {  // what a lane holds of a block of 32 tokens
+// What a lane holds of a block of 32 tokens, as it is loaded.
+template <int D>
+struct Block {
   static constexpr int G = D / 32;
   uint32_t k[2][G];    // key codes of token 16 u + lane % 16, octet lane / 16 of each group
   uint32_t v[D / 16];  // value codes
   uint32_t w[G];       // words of token lane % 32: keys' in lanes below 32, values' above
+  int page;
 };
 
 template <int N>
@@ -404,14 +406,29 @@ FI void load_dwords(const uint8_t* p, uint32_t (&x)[N]) {
   }
 }
 
+template <bool M>
+struct Flag {
+  static constexpr bool value = M;
+};
+
+// Four waves a workgroup (two workgroups a CU with up to 16 rows), blocks of the part
+// dealt to them in turn, the next block's 5 KB in flight.  Per block a wave spends
+// about 130 instructions on taking codes out of dwords, 110 on scales and 60 on the
+// softmax, beside 22 matrix instructions.
+//
+// The keys' offsets cost a matrix instruction a tile: the words of a token, as they
+// are stored, are eight bf16 numbers (o_g, s_g), and the other operand holds
+// sum(q_g) and what takes the operands' 16 out again, -16 sum(q_g), each split into
+// three bf16 terms (24 bits) over three of its four octets.
 template <int D, int NT, bool F32>
-__global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const PagedAttnArgs a) {
+__global__ __launch_bounds__(kPagedWaves * 64, NT == 1 ? 2 : 1) void paged_attention_kernel(
+    const PagedAttnArgs a) {
   constexpr int G = D / 32, NC = D / 16, S = F32 ? 3 : 1, R = 16 * NT;
   constexpr int NW = kPagedWaves;
-  // scales, and offsets freed of the operands' 16 (keys) or moved to code 8 (values; fp32: both)
-  __shared__ __attribute__((aligned(16))) float lds[NW * 64 * G * 2 > NW * 64 * R ? NW * 64 * G * 2 : NW * 64 * R];
+  constexpr int WB = 64 * G * 3;  // floats a wave: scales and offsets [role][G][32], words [64][G]
+  __shared__ __attribute__((aligned(16))) float lds[NW * WB > NW * 64 * R ? NW * WB : NW * 64 * R];
   __shared__ float sm[NW][R], sl[NW][R];
-  typedef float fG __attribute__((ext_vector_type(G)));
+  typedef uint32_t uG __attribute__((ext_vector_type(G)));
 
   const int lane = threadIdx.x & 63, col = lane & 15, m4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -421,11 +438,40 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
   const int n_rows = s.n[b] * s.G;
   const int row0 = it.tile * R;
   const float c = a.io.c;
-  fG* sc = reinterpret_cast<fG*>(lds) + wave * 128;  // [64] scales: key tokens, value tokens
-  fG* of = sc + 64;                                  // [64] offsets
+  float* sc = lds + wave * WB;
+  float* of = sc + 64 * G;
+  uG* words = reinterpret_cast<uG*>(of + 64 * G);
+
+  const int first_last = last_key(s, b, min(row0, n_rows - 1) / s.G);
+  const int end_last = last_key(s, b, min(row0 + R - 1, n_rows - 1) / s.G);
+  const int lo = it.part * s.chunk;
+  const int hi = min(end_last + 1, s.parts[b] == 1 ? t : min(t, lo + s.chunk));
+  const int P = 1 << a.log2_page;
+  const PageHead<D> ph(a.log2_page);
+  const int32_t* table = a.table + b * a.table_stride;
+  const long long head_at = (long long)it.h * ph.bytes();
+
+  // Block at token t0 (a hole's, too: it loads from page 0 and is masked).
+  auto page_of = [&](int t0) { return t0 < hi ? table[t0 >> a.log2_page] : -1; };
+  auto load = [&](Block<D>& x, int t0, int page) {
+    x.page = page;
+    if (t0 >= hi) return;
+    const bool in = (unsigned)page < (unsigned)a.n_pages;
+    const uint8_t* head = a.pages + (long long)(in ? page : 0) * a.page_bytes + head_at;
+    const int row = t0 & (P - 1);
+    load_dwords<G>(head + ph.kcode(row) + (col * (D / 2) + m4 * 4 * G), x.k[0]);
+    load_dwords<G>(head + ph.kcode(row + 16) + (col * (D / 2) + m4 * 4 * G), x.k[1]);
+    load_dwords<G>(head + ph.word(lane >> 5, row + (lane & 31)), x.w);
+    load_dwords<NC>(head + ph.vcode(row) + lane * 4 * NC, x.v);
+  };
+  // the first blocks on their way before the queries
+  Block<D> x0, x1;
+  int t0 = lo + 32 * wave;
+  load(x0, t0, page_of(t0));
+  int next_page = page_of(t0 + 32 * NW);
 
   bf16x8 q[NT][S][G];
-  float qs[NT][G];  // sum of the row's channels of a group
+  bf16x8 qo[NT];   // against the words
   int last[NT];
 #pragma unroll
   for (int x = 0; x < NT; ++x) {
@@ -433,6 +479,7 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
     const int token = r / s.G, g = r - token * s.G;
     last[x] = last_key(s, b, token);
     const long long at = s.q_off[b] + (long long)token * a.io.q_st + (long long)(it.h * s.G + g) * a.io.q_sh;
+    qo[x] = bf16x8{};
 #pragma unroll
     for (int y = 0; y < G; ++y) {
       float f[8];
@@ -449,7 +496,12 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
 #pragma unroll
         for (int z = 0; z < S; ++z) q[x][z][y][e < 4 ? 2 * e : 2 * (e - 4) + 1] = (__bf16)p[z];
       }
-      qs[x][y] = add_xor32(add_xor16(sum));
+      sum = add_xor32(add_xor16(sum));
+      float p[3];
+      split<3>(sum, p);
+      const float mine = m4 == 0 ? p[0] : m4 == 1 ? p[1] : m4 == 2 ? p[2] : 0.0f;
+      qo[x][2 * y] = (__bf16)mine;
+      qo[x][2 * y + 1] = (__bf16)(mine * (F32 ? 8.0f : -16.0f));
     }
   }
 
@@ -463,75 +515,61 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
     l[x] = 0.0f;
   }
 
-  const int first_last = last_key(s, b, min(row0, n_rows - 1) / s.G);
-  const int end_last = last_key(s, b, min(row0 + R - 1, n_rows - 1) / s.G);
-  const int lo = it.part * s.chunk;
-  const int hi = min(end_last + 1, s.parts[b] == 1 ? t : min(t, lo + s.chunk));
-  const int P = 1 << a.log2_page;
-  const PageHead<D> ph(a.log2_page);
-  const int32_t* table = a.table + b * a.table_stride;
-  const long long head_at = (long long)it.h * ph.bytes();
-
-  // The block at token t0 (a hole's, too: its loads go to page 0 and it is masked).
-  auto page_of = [&](int t0) { return table[t0 >> a.log2_page]; };
-  auto load = [&](Block<D, F32>& x, int t0, int page) {
-    const bool in = (unsigned)page < (unsigned)a.n_pages;
-    const uint8_t* head = a.pages + (long long)(in ? page : 0) * a.page_bytes + head_at;
-    const int row = t0 & (P - 1);
-    load_dwords<G>(head + ph.kcode(row + col) + m4 * 4 * G, x.k[0]);
-    load_dwords<G>(head + ph.kcode(row + 16 + col) + m4 * 4 * G, x.k[1]);
-    load_dwords<NC>(head + ph.vcode(row) + lane * 4 * NC, x.v);
-    load_dwords<G>(head + ph.word(lane >> 5, row + (lane & 31)), x.w);
-  };
-
-  auto block = [&](const Block<D, F32>& x, int t0, bool in) {
-    // words of tokens that no row sees count as 0, so that nothing below meets NaN of theirs
-    const bool live = in && t0 + (lane & 31) < hi;
-    fG vs, vo;
+  // masked: some row of the tile does not see all of the block's tokens, or it is a hole
+  auto block = [&](auto masked, const Block<D>& x, int t0, bool in) {
+    constexpr bool M = decltype(masked)::value;
+    // scales, and the values' offsets moved to code 8, to the lanes that need them.  Words
+    // of tokens that no row sees count as 0, so that nothing below meets a NaN of theirs.
+    const bool live = !M || (in && t0 + (lane & 31) < hi);
+    uG raw;
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int y = 0; y < G; ++y) {
       const uint32_t w = live ? x.w[y] : 0u;
-      vs[y] = __builtin_bit_cast(float, w & 0xffff0000u);
-      vo[y] = fmaf(vs[y], F32 || lane >= 32 ? 8.0f : -16.0f, __builtin_bit_cast(float, w << 16));
+      raw[y] = w;
+      const float f = __builtin_bit_cast(float, w & 0xffff0000u);
+      sc[(lane >> 5) * 32 * G + 32 * y + (lane & 31)] = f;
+      of[(lane >> 5) * 32 * G + 32 * y + (lane & 31)] = fmaf(f, 8.0f, __builtin_bit_cast(float, w << 16));
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    sc[lane] = vs;
-    of[lane] = vo;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    words[lane] = raw;
     __builtin_amdgcn_wave_barrier();
 
     float p[NT][8];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      bf16x8 kc[G];
+      union {
+        uint32_t d[4];
+        bf16x8 v;
+      } wk = {{0, 0, 0, 0}};
+      const uG w = words[16 * u + col];
 #pragma unroll
-      for (int y = 0; y < G; ++y) kc[y] = code_operand<F32>(x.k[u][y]);
-      fG ks[4], ko[4];
+      for (int y = 0; y < G; ++y) wk.d[y] = w[y];
+      f32x4 v[NT];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        ks[i] = sc[16 * u + 4 * m4 + i];
-        ko[i] = of[16 * u + 4 * m4 + i];
-      }
+      for (int n = 0; n < NT; ++n)
+        v[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wk.v, qo[n], f32x4{}, 0, 0, 0);
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        float v[4] = {};
+      for (int y = 0; y < G; ++y) {
+        const bf16x8 kc = code_operand<F32>(x.k[u][y]);
+        const f32x4 ks = *reinterpret_cast<const f32x4*>(sc + 32 * y + 16 * u + 4 * m4);
 #pragma unroll
-        for (int y = 0; y < G; ++y) {
+        for (int n = 0; n < NT; ++n) {
           f32x4 d = {};
 #pragma unroll
           for (int z = 0; z < S; ++z)
-            d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kc[y], q[n][z][y], d, 0, 0, 0);
+            d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kc, q[n][z][y], d, 0, 0, 0);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = fmaf(ks[i][y], d[i], fmaf(ko[i][y], qs[n][y], v[i]));
+          for (int i = 0; i < 4; ++i) v[n][i] = fmaf(ks[i], d[i], v[n][i]);
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[n][4 * u + i] = v[i];
       }
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[n][4 * u + i] = v[n][i];
     }
-    const bool masked = !in || t0 + 31 > first_last || t0 + 32 > hi;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      if (masked) {
+      if (M) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int k = t0 + 16 * (i >> 2) + 4 * m4 + (i & 3);
@@ -551,7 +589,7 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
         for (int y = 0; y < NC; ++y) o[n][y] *= f;
 #pragma unroll
         for (int y = 0; y < G; ++y) {
-          ps[n][y] *= f;
+          if (!F32) ps[n][y] *= f;
           po[n][y] *= f;
         }
       }
@@ -562,29 +600,31 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
       }
     }
 
-    bf16x8 vc[NC];
-#pragma unroll
-    for (int y = 0; y < NC; ++y) vc[y] = code_operand<F32>(x.v[y]);
-    fG zs[8], zo[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      zs[i] = sc[32 + 16 * (i >> 2) + 4 * m4 + (i & 3)];
-      zo[i] = of[32 + 16 * (i >> 2) + 4 * m4 + (i & 3)];
-    }
     const bf16x8 one = {(__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f,
                         (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+    for (int y = 0; y < G; ++y) {
+      const bf16x8 v0 = code_operand<F32>(x.v[2 * y]), v1 = code_operand<F32>(x.v[2 * y + 1]);
+      f32x4 zs[2], zo[2];
 #pragma unroll
-      for (int y = 0; y < G; ++y) {
+      for (int u = 0; u < 2; ++u) {
+        zs[u] = *reinterpret_cast<const f32x4*>(sc + 32 * G + 32 * y + 16 * u + 4 * m4);
+        zo[u] = *reinterpret_cast<const f32x4*>(of + 32 * G + 32 * y + 16 * u + 4 * m4);
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
         float f[8], sum = po[n][y];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          f[i] = p[n][i] * zs[i][y];
-          float g = p[n][i] * zo[i][y];
-          // what a row does not see has weight 0, and may be NaN
-          if (masked && t0 + 16 * (i >> 2) + 4 * m4 + (i & 3) > last[n]) f[i] = g = 0.0f;
-          sum += g;
+          f[i] = p[n][i] * zs[i >> 2][i & 3];
+          if (M) {
+            // what a row does not see has weight 0, and may be NaN
+            const bool seen = t0 + 16 * (i >> 2) + 4 * m4 + (i & 3) <= last[n];
+            f[i] = seen ? f[i] : 0.0f;
+            sum = seen ? fmaf(p[n][i], zo[i >> 2][i & 3], sum) : sum;
+          } else {
+            sum = fmaf(p[n][i], zo[i >> 2][i & 3], sum);
+          }
         }
         po[n][y] = sum;
         float w[8][S];
@@ -599,32 +639,24 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
 #pragma unroll
           for (int i = 0; i < 4; ++i) pw.u[i] = pack_bf16(w[i][z], w[4 + i][z]);
           if (!F32) ps[n][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, pw.v, ps[n][y], 0, 0, 0);
-          o[n][2 * y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vc[2 * y], pw.v, o[n][2 * y], 0, 0, 0);
-          o[n][2 * y + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vc[2 * y + 1], pw.v, o[n][2 * y + 1], 0, 0, 0);
+          o[n][2 * y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pw.v, o[n][2 * y], 0, 0, 0);
+          o[n][2 * y + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pw.v, o[n][2 * y + 1], 0, 0, 0);
         }
       }
     }
   };
-
-  Block<D, F32> x0, x1;
-  int t0 = lo + 32 * wave;
-  int pg0 = 0, pg1 = 0;
-  if (t0 < hi) {
-    pg0 = page_of(t0);
-    load(x0, t0, pg0);
-  }
-  for (; t0 < hi; t0 += 64 * NW) {
-    const int t1 = t0 + 32 * NW, t2 = t1 + 32 * NW;
-    if (t1 < hi) {
-      pg1 = page_of(t1);
-      load(x1, t1, pg1);
-    }
-    block(x0, t0, (unsigned)pg0 < (unsigned)a.n_pages);
-    if (t2 < hi) {
-      pg0 = page_of(t2);
-      load(x0, t2, pg0);
-    }
-    if (t1 < hi) block(x1, t1, (unsigned)pg1 < (unsigned)a.n_pages);
+  auto any_block = [&](const Block<D>& x, int t0) {
+    const bool in = (unsigned)x.page < (unsigned)a.n_pages;
+    if (!in || t0 + 31 > first_last || t0 + 32 > hi)
+      block(Flag<true>(), x, t0, in);
+    else
+      block(Flag<false>(), x, t0, true);
+  };
+  for (; t0 < hi; t0 += 32 * NW) {
+    load(x1, t0 + 32 * NW, next_page);
+    next_page = page_of(t0 + 64 * NW);
+    any_block(x0, t0);
+    x0 = x1;
   }
 
   // the lane's rows: out of the codes' 16 (with the 8 of the moved offsets), the
@@ -710,8 +742,7 @@ hipError_t launch(int dtype, const AttnShape& sh, const PagedAttnArgs& a, hipStr
     else paged_attention_kernel<D, 2, true><<<grid, threads, 0, st>>>(a);
   } else {
     if (sh.rows == 16) paged_attention_kernel<D, 1, false><<<grid, threads, 0, st>>>(a);
-    else if (sh.rows == 32) paged_attention_kernel<D, 2, false><<<grid, threads, 0, st>>>(a);
-    else paged_attention_kernel<D, 4, false><<<grid, threads, 0, st>>>(a);
+    else paged_attention_kernel<D, 2, false><<<grid, threads, 0, st>>>(a);
   }
   return hipGetLastError();
 }
@@ -726,7 +757,7 @@ int heads_per_workgroup(const PagedRowsArgs& a) {
 
 AttnShape paged_shape(int dtype, int d_h, int64_t max_rows) {
   AttnShape sh;
-  sh.rows = max_rows <= 16 ? 16 : max_rows <= 32 || dtype == HF_F32 ? 32 : 64;
+  sh.rows = max_rows <= 16 ? 16 : 32;
   sh.by_keys = 1;
   sh.wg_target = 512;
   sh.step = 32 * kPagedWaves;
