@@ -635,8 +635,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const JoinArgs a) {
   __shared__ float sm[4], sl[SL];
   const AttnSeqs& s = a.s;
   int i = blockIdx.x;
-  int b = 0;
-  while (b + 1 < s.B && s.split0[b + 1] <= i) ++b;
+  const int b = find_seq(s.split0, s.B, i);
   i -= s.split0[b];
   const int n_rows = s.n[b] * s.G, parts = s.parts[b];
   const int h = i / n_rows, r = i - h * n_rows;

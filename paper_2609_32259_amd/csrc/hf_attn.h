@@ -74,6 +74,16 @@ FI float add_xor16(float x) {
   return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
 }
 
+// The sequence that item i of a prefix array belongs to: a lane looks at each (at most
+// HF_MAX_BATCH = 64), where a walk would wait for memory once a step.
+static_assert(HF_MAX_BATCH <= 64, "one lane a sequence");
+FI int find_seq(const int32_t* first, int B, int i) {
+  if (B == 1) return 0;
+  const int lane = threadIdx.x & 63;
+  const bool before = lane < B && first[lane] <= i;
+  return __builtin_amdgcn_readfirstlane(__popcll(__ballot(before)) - 1);
+}
+
 // The work item of this workgroup: its head, sequence, row tile and part.  Heads
 // vary fastest, so that with 8 heads the workgroups of one head, which read the
 // same keys, run on one XCD (workgroup i runs on XCD i % 8) and share them in its
@@ -87,8 +97,7 @@ FI AttnItem attn_item(const AttnSeqs& s, int rows) {
   const int wg = blockIdx.x;
   int i = wg / s.H;
   it.h = wg - i * s.H;
-  int b = 0;
-  while (b + 1 < s.B && s.item0[b + 1] <= i) ++b;
+  const int b = find_seq(s.item0, s.B, i);
   it.b = b;
   i -= s.item0[b];
   const int tiles = (s.n[b] * s.G + rows - 1) / rows;  // n * G < 2^31 (host check)

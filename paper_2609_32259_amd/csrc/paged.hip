@@ -41,8 +41,7 @@ FI RowItem row_item(const PagedRowsArgs& a, int hpw) {
   i /= groups;
   it.role = blockIdx.y;
   it.l = blockIdx.z;
-  int b = 0;
-  while (b + 1 < a.B && a.blk0[b + 1] <= i) ++b;
+  const int b = find_seq(a.blk0, a.B, i);
   it.b = b;
   const int blk = a.start[b] / 32 + (i - a.blk0[b]);
   it.tok0 = blk * 32;
@@ -426,7 +425,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 ? 2 : 1) void paged_atten
   constexpr int G = D / 32, NC = D / 16, S = F32 ? 3 : 1, R = 16 * NT;
   constexpr int NW = kPagedWaves;
   constexpr int WB = 64 * G * 3;  // floats a wave: scales and offsets [role][G][32], words [64][G]
-  __shared__ __attribute__((aligned(16))) float lds[NW * WB > NW * 64 * R ? NW * WB : NW * 64 * R];
+  __shared__ __attribute__((aligned(16))) float lds[WB > D * R ? NW * WB : NW * D * R];
   __shared__ float sm[NW][R], sl[NW][R];
   typedef uint32_t uG __attribute__((ext_vector_type(G)));
 
@@ -464,14 +463,9 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 ? 2 : 1) void paged_atten
     load_dwords<G>(head + ph.word(lane >> 5, row + (lane & 31)), x.w);
     load_dwords<NC>(head + ph.vcode(row) + lane * 4 * NC, x.v);
   };
-  // the first blocks on their way before the queries
-  Block<D> x0, x1;
-  int t0 = lo + 32 * wave;
-  load(x0, t0, page_of(t0));
-  int next_page = page_of(t0 + 32 * NW);
-
-  bf16x8 q[NT][S][G];
-  bf16x8 qo[NT];   // against the words
+  // the queries and the first block on their way before either is used
+  typedef uint32_t QRaw[F32 ? 8 : 4];
+  QRaw raw_q[NT][G];
   int last[NT];
 #pragma unroll
   for (int x = 0; x < NT; ++x) {
@@ -479,20 +473,31 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 ? 2 : 1) void paged_atten
     const int token = r / s.G, g = r - token * s.G;
     last[x] = last_key(s, b, token);
     const long long at = s.q_off[b] + (long long)token * a.io.q_st + (long long)(it.h * s.G + g) * a.io.q_sh;
+    const uint8_t* row = static_cast<const uint8_t*>(a.io.q) + at * (F32 ? 4 : 2);
+#pragma unroll
+    for (int y = 0; y < G; ++y) load_dwords<F32 ? 8 : 4>(row + (32 * y + 8 * m4) * (F32 ? 4 : 2), raw_q[x][y]);
+  }
+  Block<D> x0, x1;
+  int t0 = lo + 32 * wave;
+  const int page0 = page_of(t0);
+  int next_page = page_of(t0 + 32 * NW);
+  load(x0, t0, page0);
+
+  bf16x8 q[NT][S][G];
+  bf16x8 qo[NT];   // against the words
+#pragma unroll
+  for (int x = 0; x < NT; ++x) {
     qo[x] = bf16x8{};
 #pragma unroll
     for (int y = 0; y < G; ++y) {
-      float f[8];
-      if (F32)
-        load8<float>(static_cast<const float*>(a.io.q) + at + 32 * y + 8 * m4, f);
-      else
-        load8<uint16_t>(static_cast<const uint16_t*>(a.io.q) + at + 32 * y + 8 * m4, f);
       float sum = 0.0f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        sum += f[e];
+        const uint32_t w = raw_q[x][y][F32 ? e : e / 2];
+        const float f = __builtin_bit_cast(float, F32 ? w : e & 1 ? w & 0xffff0000u : w << 16);
+        sum += f;
         float p[S];
-        split<S>(f[e], p);
+        split<S>(f, p);
 #pragma unroll
         for (int z = 0; z < S; ++z) q[x][z][y][e < 4 ? 2 * e : 2 * (e - 4) + 1] = (__bf16)p[z];
       }
@@ -678,56 +683,55 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 ? 2 : 1) void paged_atten
     }
   }
   __syncthreads();
-  // join the waves, 64 channels at a time: [wave][channel][row] in LDS
-  constexpr int QR = R / 4;  // rows a thread sums, of one channel: thread = (channel, quarter)
+  // join the waves: their sums against the common maximum to LDS, [wave][row][channel]
+  // with 16-byte chunk x of row r at slot x ^ (r % 16), so that the 16 rows a write
+  // touches lie on distinct banks; then four channels of a row a thread
+  f32x4* sums = reinterpret_cast<f32x4*>(lds);
 #pragma unroll
-  for (int half = 0; half < D / 64; ++half) {
-    if (half) __syncthreads();
+  for (int n = 0; n < NT; ++n) {
+    const int r = 16 * n + col;
+    float mm = sm[0][r];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int r = 16 * n + col;
-      float mm = sm[0][r];
+    for (int x = 1; x < NW; ++x) mm = fmaxf(mm, sm[x][r]);
+    const float f = __builtin_amdgcn_exp2f(m[n] - mm);
 #pragma unroll
-      for (int x = 1; x < NW; ++x) mm = fmaxf(mm, sm[x][r]);
-      const float f = __builtin_amdgcn_exp2f(m[n] - mm);
+    for (int y = 0; y < NC; ++y) sums[(wave * R + r) * (D / 4) + ((4 * y + m4) ^ col)] = o[n][y] * f;
+  }
+  __syncthreads();
 #pragma unroll
-      for (int y = 0; y < 4; ++y)
+  for (int i = 0; i < R * D / 4 / (64 * NW); ++i) {
+    const int at = threadIdx.x + i * 64 * NW, rl = at / (D / 4), ch = at % (D / 4);
+    const int r = row0 + rl;
+    if (r >= n_rows) continue;
+    float mm = sm[0][rl], lt = 0.0f;
+    f32x4 v = {};
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          lds[(wave * R + r) * 64 + 16 * y + 4 * m4 + i] = o[n][4 * half + y][i] * f;
+    for (int y = 1; y < NW; ++y) mm = fmaxf(mm, sm[y][rl]);
+#pragma unroll
+    for (int y = 0; y < NW; ++y) {
+      v += sums[(y * R + rl) * (D / 4) + (ch ^ (rl & 15))];
+      lt = fmaf(sl[y][rl], __builtin_amdgcn_exp2f(sm[y][rl] - mm), lt);
     }
-    __syncthreads();
-    const int ch = threadIdx.x & 63, quarter = threadIdx.x >> 6;
-    for (int x = 0; x < QR; ++x) {
-      const int rl = quarter * QR + x, r = row0 + rl;
-      if (r >= n_rows) break;
-      float mm = sm[0][rl], v = 0.0f, lt = 0.0f;
-#pragma unroll
-      for (int y = 1; y < NW; ++y) mm = fmaxf(mm, sm[y][rl]);
-#pragma unroll
-      for (int y = 0; y < NW; ++y) {
-        v += lds[(y * R + rl) * 64 + ch];
-        lt = fmaf(sl[y][rl], __builtin_amdgcn_exp2f(sm[y][rl] - mm), lt);
-      }
+    if (s.parts[b] == 1) {
       const int token = r / s.G, g = r - token * s.G;
-      if (s.parts[b] == 1) {
-        const long long at = s.o_off[b] + (long long)token * a.io.o_st +
-                             (long long)(it.h * s.G + g) * a.io.o_sh + 64 * half + ch;
-        v *= lt > 0.0f || lt != lt ? 1.0f / lt : 0.0f;
-        if (F32)
-          static_cast<float*>(a.io.out)[at] = v;
-        else
-          static_cast<__bf16*>(a.io.out)[at] = (__bf16)v;
-        if (half == 0 && ch == 0 && a.io.lse)
-          a.io.lse[(long long)(s.row0[b] + token) * (s.H * s.G) + it.h * s.G + g] =
-              lt == 0.0f ? -INFINITY : (mm + log2f(lt)) * 0.6931471805599453f;
+      const long long to = s.o_off[b] + (long long)token * a.io.o_st +
+                           (long long)(it.h * s.G + g) * a.io.o_sh + 4 * ch;
+      v *= lt > 0.0f || lt != lt ? 1.0f / lt : 0.0f;
+      if (F32) {
+        *reinterpret_cast<f32x4*>(static_cast<float*>(a.io.out) + to) = v;
       } else {
-        const long long slot = s.part0[b] + ((long long)it.h * n_rows + r) * s.parts[b] + it.part;
-        a.io.part[slot * D + 64 * half + ch] = v;
-        if (half == 0 && ch == 0) {
-          a.io.ml[2 * slot] = mm;
-          a.io.ml[2 * slot + 1] = lt;
-        }
+        const u32x2 x = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.io.out) + to) = x;
+      }
+      if (ch == 0 && a.io.lse)
+        a.io.lse[(long long)(s.row0[b] + token) * (s.H * s.G) + it.h * s.G + g] =
+            lt == 0.0f ? -INFINITY : (mm + log2f(lt)) * 0.6931471805599453f;
+    } else {
+      const long long slot = s.part0[b] + ((long long)it.h * n_rows + r) * s.parts[b] + it.part;
+      *reinterpret_cast<f32x4*>(a.io.part + slot * D + 4 * ch) = v;
+      if (ch == 0) {
+        a.io.ml[2 * slot] = mm;
+        a.io.ml[2 * slot + 1] = lt;
       }
     }
   }
