@@ -794,15 +794,6 @@ int32_t check_rows(const char* name, const hf_rows* r, bool used, bool written, 
   return HF_OK;
 }
 
-// Element offsets of the sequences' first rows.
-void offsets(const hf_rows* r, int32_t B, const int32_t* len, int64_t* off) {
-  int64_t at = 0;
-  for (int b = 0; b < B; ++b) {
-    off[b] = r->stride_b == -1 ? at * r->stride_t : b * r->stride_b;
-    at += len[b];
-  }
-}
-
 // Cuts the batch into work items and long key ranges into parts.  A part is as long
 // as the whole work over the workgroups that fill the chip, so that the parts of one
 // launch take about equally long; a range that needs no cutting has one part.
@@ -853,30 +844,29 @@ int32_t plan_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len, i
   s.H = H;
   s.G = G;
   s.causal = causal ? 1 : 0;
-  int64_t items = 0, row = 0, split = 0;
+  s.by_g = hf::make_divide(G);
+  s.by_h = hf::make_divide(H);
+  int64_t items = 0, row = 0, key = 0, split = 0;
   slots = 0;
   for (int b = 0; b < B; ++b) {
     const int64_t rows = (int64_t)q_len[b] * G;
     const int64_t tiles = (rows + sh.rows - 1) / sh.rows;
     int64_t parts = std::max<int64_t>((kv_len[b] + (int64_t)s.chunk - 1) / s.chunk, 1);
-    s.n[b] = q_len[b];
-    s.t[b] = kv_len[b];
-    s.row0[b] = (int32_t)row;
-    s.parts[b] = (int32_t)parts;
-    s.item0[b] = (int32_t)items;
-    s.split0[b] = (int32_t)split;
-    s.part0[b] = (int32_t)slots;
+    s.q[b] = {(int32_t)items, (int32_t)split, q_len[b], kv_len[b], (int32_t)row, (int32_t)key,
+              (int32_t)parts, (int32_t)slots};
     items += tiles * parts;
     row += q_len[b];
+    key += kv_len[b];
     if (parts > 1) {
       split += rows * H;
       slots += rows * H * parts;
     }
     if (items * H > INT32_MAX || split > INT32_MAX || slots > INT32_MAX)
       return fail(HF_ERR_SHAPE, "too many work items");
+    if (key > INT32_MAX) return fail(HF_ERR_SHAPE, "too many keys");
   }
-  s.item0[B] = (int32_t)items;
-  s.split0[B] = (int32_t)split;
+  s.n_items = (int32_t)items;
+  s.n_split = (int32_t)split;
   return HF_OK;
 }
 
@@ -910,8 +900,6 @@ int32_t attention_common(int32_t B, const int32_t* q_len, const int32_t* kv_len,
   int64_t slots = 0;
   if ((st = plan_attention(B, q_len, kv_len, q->H, H, q->dtype, d_h, paged, causal, sh, s, slots)))
     return st;
-  offsets(q, B, q_len, s.q_off);
-  offsets(out, B, q_len, s.o_off);
   std::memset(&io, 0, sizeof io);
   if (slots) {
     const size_t need = part_bytes(slots, d_h);
@@ -926,6 +914,8 @@ int32_t attention_common(int32_t B, const int32_t* q_len, const int32_t* kv_len,
   io.q = q->ptr;
   io.out = out->ptr;
   io.lse = lse;
+  io.q_sb = q->stride_b;
+  io.o_sb = out->stride_b;
   io.q_st = q->stride_t;
   io.q_sh = q->stride_h;
   io.o_st = out->stride_t;
@@ -936,7 +926,7 @@ int32_t attention_common(int32_t B, const int32_t* q_len, const int32_t* kv_len,
 
 int32_t join_parts(int32_t dtype, int32_t d_h, const hf::AttnIO& io, const hf::AttnSeqs& s,
                    hipStream_t st) {
-  if (s.split0[s.B] == 0) return ok();
+  if (s.n_split == 0) return ok();
   hipError_t e;
   {
     TimedLaunch t(HF_KERNEL_ATTENTION_JOIN, st);
@@ -991,7 +981,7 @@ int32_t paged_rows(bool append, int32_t B, const int32_t* start, const int32_t* 
   if (n_layers > 65535) return fail(HF_ERR_SHAPE, "too many layers");
   hf::PagedRowsArgs a;
   std::memset(&a, 0, sizeof a);
-  int64_t blocks = 0;
+  int64_t blocks = 0, row = 0;
   for (int b = 0; b < B; ++b) {
     const int64_t end = (int64_t)start[b] + n[b];
     const int64_t p0 = pos0 ? pos0[b] : 0;
@@ -1001,21 +991,17 @@ int32_t paged_rows(bool append, int32_t B, const int32_t* start, const int32_t* 
     if (n[b] > 0 && (end + cache->page_tokens - 1) / cache->page_tokens > cache->table_stride)
       return fail(HF_ERR_CAPACITY, "sequence %d: %lld tokens, the table has %lld pages of %d", b,
                   (long long)end, (long long)cache->table_stride, cache->page_tokens);
-    a.start[b] = start[b];
-    a.n[b] = n[b];
-    a.pos0[b] = (int32_t)p0;
-    a.blk0[b] = (int32_t)blocks;
+    a.q[b] = {(int32_t)blocks, start[b], n[b], (int32_t)p0, (int32_t)row, {}};
+    row += n[b];
     if (n[b] > 0) blocks += (end - 1) / 32 - start[b] / 32 + 1;
-    if (blocks * cache->H > INT32_MAX) return fail(HF_ERR_SHAPE, "too many rows");
+    if (blocks * cache->H > INT32_MAX || row > INT32_MAX) return fail(HF_ERR_SHAPE, "too many rows");
   }
-  a.blk0[B] = (int32_t)blocks;
+  a.n_blocks = (int32_t)blocks;
   if (blocks == 0) return ok();
-  offsets(k, B, n, a.k_off);
-  offsets(v, B, n, a.v_off);
   a.k = k->ptr;
   a.v = v->ptr;
-  a.k_st = k->stride_t; a.k_sh = k->stride_h; a.k_sl = k->stride_l;
-  a.v_st = v->stride_t; a.v_sh = v->stride_h; a.v_sl = v->stride_l;
+  a.k_sb = k->stride_b; a.k_st = k->stride_t; a.k_sh = k->stride_h; a.k_sl = k->stride_l;
+  a.v_sb = v->stride_b; a.v_st = v->stride_t; a.v_sh = v->stride_h; a.v_sl = v->stride_l;
   a.page_bytes = (long long)page_bytes(cache->H, cache->d_h, cache->page_tokens);
   a.pages = static_cast<uint8_t*>(cache->pages) + (int64_t)layer * cache->n_pages * a.page_bytes;
   a.table = cache->table;
@@ -1074,11 +1060,9 @@ int32_t hf_prompt_attention(int32_t B, const int32_t* q_len, const int32_t* kv_l
   if (k->dtype != v->dtype || k->dtype != q->dtype) return fail(HF_ERR_DTYPE, "q, k and v dtypes differ");
   a.k = k->ptr;
   a.v = v->ptr;
-  a.k_st = k->stride_t; a.k_sh = k->stride_h;
-  a.v_st = v->stride_t; a.v_sh = v->stride_h;
-  offsets(k, B, kv_len, a.k_off);
-  offsets(v, B, kv_len, a.v_off);
-  if (a.s.item0[B] == 0) return ok();
+  a.k_sb = k->stride_b; a.k_st = k->stride_t; a.k_sh = k->stride_h;
+  a.v_sb = v->stride_b; a.v_st = v->stride_t; a.v_sh = v->stride_h;
+  if (a.s.n_items == 0) return ok();
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e;
   {
@@ -1110,7 +1094,7 @@ int32_t hf_paged_attention(int32_t B, const int32_t* q_len, const int32_t* kv_le
   a.table_stride = cache->table_stride;
   a.n_pages = cache->n_pages;
   a.log2_page = log2_of(cache->page_tokens);
-  if (a.s.item0[B] == 0) return ok();
+  if (a.s.n_items == 0) return ok();
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e;
   {

@@ -335,24 +335,15 @@ struct Fetch {
   }
 };
 
-// Row r of a sequence: its token and head within the group.
-FI void place(int r, int G, int& token, int& g) {
-  token = r / G;
-  g = r - token * G;
-}
-
-// The result of a finished row, or its part.
+// The result of a finished row r, or its part.
 template <class P>
-FI void write_row(const AttnIO& io, const AttnSeqs& s, int b, int h, int part, int r, float m,
-                  float l, const typename P::O& o, int lane) {
+FI void write_row(const AttnIO& io, const AttnSeqs& s, const AttnItem& it, int r, float m, float l,
+                  const typename P::O& o, int lane) {
   typedef typename P::T T;
-  int token, g;
-  place(r, s.G, token, g);
-  const bool lead = lane < P::RW;  // one lane of the row's
-  if (s.parts[b] == 1) {
-    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-    T* out = static_cast<T*>(io.out) + s.o_off[b] + (long long)token * io.o_st +
-             (long long)(h * s.G + g) * io.o_sh;
+  if (it.parts == 1) {
+    const int token = divide(r, s.by_g), head = it.h * s.G + r - token * s.G;
+    const float inv = inverse_weight(l);
+    T* out = static_cast<T*>(io.out) + out_at(io, s, it, token, head);
 #pragma unroll
     for (int i = 0; i < P::NO; i += 4) {
       float x[4];
@@ -360,39 +351,36 @@ FI void write_row(const AttnIO& io, const AttnSeqs& s, int b, int h, int part, i
       for (int j = 0; j < 4; ++j) x[j] = P::get(o, i + j) * inv;
       P::store4(out + P::channel(lane, i), x);
     }
-    if (lead && io.lse)
-      io.lse[(long long)(s.row0[b] + token) * (s.H * s.G) + h * s.G + g] =
-          l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    if (lane < P::RW) write_lse(io, s, it, token, head, m, l);
     return;
   }
-  const long long slot =
-      s.part0[b] + ((long long)h * s.n[b] * s.G + r) * s.parts[b] + part;
+  const long long slot = part_slot(it, r);
   float* po = io.part + slot * P::D;
 #pragma unroll
   for (int i = 0; i < P::NO; i += 4) {
     const f32x4 v = {P::get(o, i), P::get(o, i + 1), P::get(o, i + 2), P::get(o, i + 3)};
     *reinterpret_cast<f32x4*>(po + P::channel(lane, i)) = v;
   }
-  if (lead) {
+  if (lane < P::RW) {
     io.ml[2 * slot] = m;
     io.ml[2 * slot + 1] = l;
   }
 }
 
+// Row r (the last one for rows past it, which are not written).
 template <class P>
-FI void start_rows(Rows<P>& w, const AttnArgs& a, int b, int h, int r, int lane) {
+FI void start_rows(Rows<P>& w, const AttnArgs& a, const AttnItem& it, int r, int lane) {
   typedef typename P::T T;
   const AttnSeqs& s = a.s;
-  const int n_rows = s.n[b] * s.G;
-  int token, g;
-  place(min(r, n_rows - 1), s.G, token, g);
-  P::load_q(w.q, static_cast<const T*>(a.io.q) + s.q_off[b] + (long long)token * a.io.q_st +
-                     (long long)(h * s.G + g) * a.io.q_sh, lane);
+  r = min(r, it.rows - 1);
+  const int token = divide(r, s.by_g), head = it.h * s.G + r - token * s.G;
+  P::load_q(w.q, static_cast<const T*>(a.io.q) + seq_at(it.b, it.row0, a.io.q_sb, a.io.q_st) +
+                     token * a.io.q_st + head * a.io.q_sh, lane);
 #pragma unroll
   for (int i = 0; i < P::NO; ++i) P::set(w.o, i, 0.0f);
   w.m = kNoMax;
   w.l = 0.0f;
-  w.last = last_key(s, b, token);
+  w.last = last_key(s, it, token);
 }
 
 // By rows: NW waves, each RW rows of the tile, all against the same keys.  A wave
@@ -413,20 +401,19 @@ __global__ __launch_bounds__(NW * 64) void attention_rows_kernel(const AttnArgs 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const AttnSeqs& s = a.s;
   const AttnItem it = attn_item(s, NW * P::RW);
-  const int b = it.b, t = s.t[b];
-  const int n_rows = s.n[b] * s.G;
+  const int t = it.t, n_rows = it.rows;
   const int row0 = it.tile * NW * P::RW;
   Rows<P> w;
-  start_rows<P>(w, a, b, it.h, row0 + wave * P::RW + P::row(lane), lane);
+  start_rows<P>(w, a, it, row0 + wave * P::RW + P::row(lane), lane);
 
   // keys of this part that some row of the workgroup sees, and that all of them see
-  const int wg_last = last_key(s, b, min(row0 + NW * P::RW - 1, n_rows - 1) / s.G);
-  const int wg_first = last_key(s, b, row0 / s.G);
-  const int wave_last = last_key(s, b, min(row0 + wave * P::RW + P::RW - 1, n_rows - 1) / s.G);
+  const int wg_last = last_key(s, it, divide(min(row0 + NW * P::RW - 1, n_rows - 1), s.by_g));
+  const int wg_first = last_key(s, it, divide(row0, s.by_g));
+  const int wave_last = last_key(s, it, divide(min(row0 + wave * P::RW + P::RW - 1, n_rows - 1), s.by_g));
   const int lo = it.part * s.chunk;
-  const int hi = min(wg_last + 1, s.parts[b] == 1 ? t : min(t, lo + s.chunk));
-  const T* kb = static_cast<const T*>(a.k) + a.k_off[b] + (long long)it.h * a.k_sh;
-  const T* vb = static_cast<const T*>(a.v) + a.v_off[b] + (long long)it.h * a.v_sh;
+  const int hi = min(wg_last + 1, it.parts == 1 ? t : min(t, lo + s.chunk));
+  const T* kb = static_cast<const T*>(a.k) + seq_at(it.b, it.key0, a.k_sb, a.k_st) + (long long)it.h * a.k_sh;
+  const T* vb = static_cast<const T*>(a.v) + seq_at(it.b, it.key0, a.v_sb, a.v_st) + (long long)it.h * a.v_sh;
   const float c = a.io.c;
 
   Fetch<P, false, NB> fk;
@@ -484,7 +471,7 @@ __global__ __launch_bounds__(NW * 64) void attention_rows_kernel(const AttnArgs 
   }
   const int r = row0 + wave * P::RW + P::row(lane);
   const float l = P::row_sum(w.l);
-  if (r < n_rows) write_row<P>(a.io, s, b, it.h, it.part, r, w.m, l, w.o, lane);
+  if (r < n_rows) write_row<P>(a.io, s, it, r, w.m, l, w.o, lane);
 }
 
 // By keys: one block of RW rows, the tiles of keys dealt to NW waves.
@@ -500,17 +487,16 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const AttnSeqs& s = a.s;
   const AttnItem it = attn_item(s, P::RW);
-  const int b = it.b, t = s.t[b];
-  const int n_rows = s.n[b] * s.G;
+  const int t = it.t, n_rows = it.rows;
   const int row0 = it.tile * P::RW;
   Rows<P> w;
-  start_rows<P>(w, a, b, it.h, row0 + P::row(lane), lane);
-  const int first = last_key(s, b, min(row0, n_rows - 1) / s.G);
-  const int last = last_key(s, b, min(row0 + P::RW - 1, n_rows - 1) / s.G);
+  start_rows<P>(w, a, it, row0 + P::row(lane), lane);
+  const int first = last_key(s, it, divide(min(row0, n_rows - 1), s.by_g));
+  const int last = last_key(s, it, divide(min(row0 + P::RW - 1, n_rows - 1), s.by_g));
   const int lo = it.part * s.chunk + wave * P::KT;
-  const int hi = min(last + 1, s.parts[b] == 1 ? t : min(t, it.part * s.chunk + s.chunk));
-  const T* kb = static_cast<const T*>(a.k) + a.k_off[b] + (long long)it.h * a.k_sh;
-  const T* vb = static_cast<const T*>(a.v) + a.v_off[b] + (long long)it.h * a.v_sh;
+  const int hi = min(last + 1, it.parts == 1 ? t : min(t, it.part * s.chunk + s.chunk));
+  const T* kb = static_cast<const T*>(a.k) + seq_at(it.b, it.key0, a.k_sb, a.k_st) + (long long)it.h * a.k_sh;
+  const T* vb = static_cast<const T*>(a.v) + seq_at(it.b, it.key0, a.v_sb, a.v_st) + (long long)it.h * a.v_sh;
   const float c = a.io.c;
   unsigned char* w0 = s0 + wave * 2 * TB;
   unsigned char* w1 = s1 + wave * 2 * TB;
@@ -584,12 +570,10 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
   // each wave holds every NW-th group of four registers: it writes those channels
   const int r = row0 + rl;
   if (r >= n_rows) return;
-  int token, g;
-  place(r, s.G, token, g);
-  if (s.parts[b] == 1) {
-    const float inv = lt > 0.0f || lt != lt ? 1.0f / lt : 0.0f;
-    T* out = static_cast<T*>(a.io.out) + s.o_off[b] + (long long)token * a.io.o_st +
-             (long long)(it.h * s.G + g) * a.io.o_sh;
+  if (it.parts == 1) {
+    const int token = divide(r, s.by_g), head = it.h * s.G + r - token * s.G;
+    const float inv = inverse_weight(lt);
+    T* out = static_cast<T*>(a.io.out) + out_at(a.io, s, it, token, head);
 #pragma unroll
     for (int i = 0; i < P::NO; i += 4) {
       if ((i / 4) % NW != wave) continue;
@@ -598,13 +582,10 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
       for (int j = 0; j < 4; ++j) x[j] = P::get(w.o, i + j) * inv;
       P::store4(out + P::channel(lane, i), x);
     }
-    if (wave == 0 && lane < P::RW && a.io.lse)
-      a.io.lse[(long long)(s.row0[b] + token) * (s.H * s.G) + it.h * s.G + g] =
-          lt == 0.0f ? -INFINITY : (m + log2f(lt)) * 0.6931471805599453f;
+    if (wave == 0 && lane < P::RW) write_lse(a.io, s, it, token, head, m, lt);
     return;
   }
-  const long long slot =
-      s.part0[b] + ((long long)it.h * n_rows + r) * s.parts[b] + it.part;
+  const long long slot = part_slot(it, r);
 #pragma unroll
   for (int i = 0; i < P::NO; i += 4) {
     if ((i / 4) % NW != wave) continue;
@@ -635,11 +616,14 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const JoinArgs a) {
   __shared__ float sm[4], sl[SL];
   const AttnSeqs& s = a.s;
   int i = blockIdx.x;
-  const int b = find_seq(s.split0, s.B, i);
-  i -= s.split0[b];
-  const int n_rows = s.n[b] * s.G, parts = s.parts[b];
+  AttnItem it;
+  it.b = find_seq(s.q, &AttnSeq::split0, s.B, i);
+  const AttnSeq sq = s.q[it.b];
+  it.row0 = sq.row0;
+  i -= sq.split0;
+  const int n_rows = sq.n * s.G, parts = sq.parts;
   const int h = i / n_rows, r = i - h * n_rows;
-  const long long slot = s.part0[b] + (long long)i * parts;
+  const long long slot = sq.part0 + (long long)i * parts;
   const float* ml = a.io.ml + 2 * slot;
   float m = kNoMax;
   for (int p = threadIdx.x; p < parts; p += 256) m = fmaxf(m, ml[2 * p]);
@@ -670,10 +654,9 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const JoinArgs a) {
     o += so[x][c];
     l += sl[x];
   }
-  int token, g;
-  place(r, s.G, token, g);
-  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-  const long long at = s.o_off[b] + (long long)token * a.io.o_st + (long long)(h * s.G + g) * a.io.o_sh + 4 * c;
+  const int token = divide(r, s.by_g), head = h * s.G + r - token * s.G;
+  const float inv = inverse_weight(l);
+  const long long at = out_at(a.io, s, it, token, head) + 4 * c;
   o *= inv;
   if (F32) {
     *reinterpret_cast<f32x4*>(static_cast<float*>(a.io.out) + at) = o;
@@ -681,16 +664,14 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const JoinArgs a) {
     const u32x2 v = {pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
     *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.io.out) + at) = v;
   }
-  if (c == 0 && a.io.lse)
-    a.io.lse[(long long)(s.row0[b] + token) * (s.H * s.G) + h * s.G + g] =
-        l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+  if (c == 0) write_lse(a.io, s, it, token, head, m, l);
 }
 
 constexpr int kRowWaves = 8, kRowWavesF32 = 4, kKeyWaves = 4;
 
 template <int D>
 hipError_t launch(int dtype, const AttnShape& sh, const AttnArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)(a.s.item0[a.s.B] * a.s.H));
+  const dim3 grid((unsigned)(a.s.n_items * a.s.H));
   if (dtype == HF_BF16) {
     if (sh.by_keys)
       attention_keys_kernel<Bf16Tile<D, 32>, kKeyWaves><<<grid, kKeyWaves * 64, 0, st>>>(a);
@@ -727,7 +708,7 @@ hipError_t launch_prompt_attention(int dtype, int d_h, const AttnShape& sh, cons
 hipError_t launch_attention_join(int dtype, int d_h, const AttnIO& io, const AttnSeqs& s,
                                  hipStream_t st) {
   JoinArgs a{io, s};
-  const dim3 grid((unsigned)s.split0[s.B]);
+  const dim3 grid((unsigned)s.n_split);
   if (dtype == HF_F32) {
     if (d_h == 128) attention_join_kernel<true, 128><<<grid, 256, 0, st>>>(a);
     else attention_join_kernel<true, 64><<<grid, 256, 0, st>>>(a);

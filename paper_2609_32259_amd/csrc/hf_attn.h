@@ -38,6 +38,10 @@ constexpr int wait_vm_only(int n) { return (n & 0xF) | ((n >> 4) << 14) | (7 << 
 // All vector-memory and LDS operations.
 constexpr int kWaitMemory = 7 << 4;
 
+FI uint32_t lds_addr(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+
 FI uint32_t pack_bf16(float a, float b) {
   bf16x2 v = {(__bf16)a, (__bf16)b};
   return __builtin_bit_cast(uint32_t, v);
@@ -74,14 +78,25 @@ FI float add_xor16(float x) {
   return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
 }
 
-// The sequence that item i of a prefix array belongs to: a lane looks at each (at most
-// HF_MAX_BATCH = 64), where a walk would wait for memory once a step.
+FI int divide(int n, const Divide& d) {
+  return (int)(((uint64_t)(uint32_t)n * d.magic) >> d.shift);
+}
+
+// The sequence that item i of a prefix array (a member of the sequences' records)
+// belongs to: a lane looks at each (at most HF_MAX_BATCH = 64), where a walk would
+// wait for memory once a step.
 static_assert(HF_MAX_BATCH <= 64, "one lane a sequence");
-FI int find_seq(const int32_t* first, int B, int i) {
+template <class S>
+FI int find_seq(const S* q, int32_t S::*first, int B, int i) {
   if (B == 1) return 0;
   const int lane = threadIdx.x & 63;
-  const bool before = lane < B && first[lane] <= i;
+  const bool before = lane < B && q[lane].*first <= i;
   return __builtin_amdgcn_readfirstlane(__popcll(__ballot(before)) - 1);
+}
+
+// Elements to a sequence's first row.
+FI long long seq_at(int b, int rows_before, long long sb, long long st) {
+  return sb == -1 ? rows_before * st : b * sb;
 }
 
 // The work item of this workgroup: its head, sequence, row tile and part.  Heads
@@ -91,25 +106,52 @@ FI int find_seq(const int32_t* first, int B, int i) {
 // its rows, and the long ones go first.
 struct AttnItem {
   int b, h, tile, part;
+  int n, t, rows;           // query tokens, keys, query rows of a head (n G < 2^31: host check)
+  int row0, key0, parts, part0;
 };
-FI AttnItem attn_item(const AttnSeqs& s, int rows) {
+FI AttnItem attn_item(const AttnSeqs& s, int tile_rows) {
   AttnItem it;
   const int wg = blockIdx.x;
-  int i = wg / s.H;
+  int i = divide(wg, s.by_h);
   it.h = wg - i * s.H;
-  const int b = find_seq(s.item0, s.B, i);
-  it.b = b;
-  i -= s.item0[b];
-  const int tiles = (s.n[b] * s.G + rows - 1) / rows;  // n * G < 2^31 (host check)
-  const int t = i / s.parts[b];
-  it.part = i - t * s.parts[b];
-  it.tile = tiles - 1 - t;
+  it.b = find_seq(s.q, &AttnSeq::item0, s.B, i);
+  const AttnSeq q = s.q[it.b];
+  it.n = q.n;
+  it.t = q.t;
+  it.rows = q.n * s.G;
+  it.row0 = q.row0;
+  it.key0 = q.key0;
+  it.parts = q.parts;
+  it.part0 = q.part0;
+  i -= q.item0;
+  it.part = 0;
+  if (q.parts > 1) {
+    const int x = i / q.parts;
+    it.part = i - x * q.parts;
+    i = x;
+  }
+  it.tile = (it.rows + tile_rows - 1) / tile_rows - 1 - i;
   return it;
 }
 
 // The last key a row sees (-1: none), from its token.
-FI int last_key(const AttnSeqs& s, int b, int token) {
-  return s.causal ? min(s.t[b] - 1, token + s.t[b] - s.n[b]) : s.t[b] - 1;
+FI int last_key(const AttnSeqs& s, const AttnItem& it, int token) {
+  return s.causal ? min(it.t - 1, token + it.t - it.n) : it.t - 1;
+}
+
+// Where a row's result goes, and its log-sum-exp.
+FI long long out_at(const AttnIO& io, const AttnSeqs& s, const AttnItem& it, int token, int head) {
+  return seq_at(it.b, it.row0, io.o_sb, io.o_st) + token * io.o_st + head * io.o_sh;
+}
+FI void write_lse(const AttnIO& io, const AttnSeqs& s, const AttnItem& it, int token, int head,
+                  float m, float l) {
+  if (io.lse)
+    io.lse[(long long)(it.row0 + token) * (s.H * s.G) + head] =
+        l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+}
+FI float inverse_weight(float l) { return l > 0.0f || l != l ? 1.0f / l : 0.0f; }
+FI long long part_slot(const AttnItem& it, int r) {
+  return it.part0 + ((long long)it.h * it.rows + r) * it.parts + it.part;
 }
 
 }  // namespace hf

@@ -171,19 +171,34 @@ hipError_t launch_gemm_f64(int m, int n, long long k, const double* A, long long
 // rows shares its keys between the heads of a group as well as between tokens.
 // A split sequence writes, for each row and part, the unnormalized sum, the running
 // maximum and the weight into the workspace, and the join makes the result of them.
+// A sequence's numbers lie in one 32-byte record, which a wave loads at once: the
+// arguments of a launch come from memory that no cache holds yet.
+struct AttnSeq {
+  int32_t item0;   // first work item: (row tile, part) pairs of a head
+  int32_t split0;  // first row of the sequence among those of split ones (all heads)
+  int32_t n, t;    // query tokens, keys
+  int32_t row0, key0;  // rows and keys of the sequences before it
+  int32_t parts;
+  int32_t part0;   // first slot of the sequence in the partial buffers
+};
+struct Divide {  // n / d of n < 2^31 as (n * magic) >> shift
+  uint32_t magic, shift;
+};
+// d >= 1: with 2^s >= d and magic = ceil(2^(31+s) / d), magic d - 2^(31+s) < 2^s, which
+// leaves the quotient exact below 2^31.
+inline Divide make_divide(uint32_t d) {
+  uint32_t s = 0;
+  while (((uint64_t)1 << s) < d) ++s;
+  const uint64_t p = (uint64_t)1 << (31 + s);
+  return Divide{(uint32_t)((p + d - 1) / d), 31 + s};
+}
 struct AttnSeqs {
   int32_t B, H, G;
   int32_t chunk;                       // keys of one part (a multiple of every kernel's step)
   int32_t causal;
-  int32_t n[HF_MAX_BATCH];             // query tokens
-  int32_t t[HF_MAX_BATCH];             // keys
-  int32_t row0[HF_MAX_BATCH];          // first query row of the sequence among the packed ones (lse)
-  int32_t parts[HF_MAX_BATCH];
-  int32_t item0[HF_MAX_BATCH + 1];     // first work item: (row tile, part) pairs of a head
-  int32_t split0[HF_MAX_BATCH + 1];    // first row of the sequence among those of split ones
-  int32_t part0[HF_MAX_BATCH];         // first slot of the sequence in the partial buffers
-  int64_t q_off[HF_MAX_BATCH];
-  int64_t o_off[HF_MAX_BATCH];
+  int32_t n_items, n_split;
+  Divide by_g, by_h;
+  alignas(32) AttnSeq q[HF_MAX_BATCH];
 };
 struct AttnIO {
   const void* q;
@@ -191,17 +206,15 @@ struct AttnIO {
   float* lse;       // or nullptr
   float* part;      // [slots][d_h] unnormalized sums
   float* ml;        // [slots][2] maximum (in units of log 2) and weight
-  long long q_st, q_sh, o_st, o_sh;
+  long long q_sb, q_st, q_sh, o_sb, o_st, o_sh;  // (a stride of -1 between sequences: packed)
   float c;          // scale * log2(e)
 };
 struct AttnArgs {
   AttnIO io;
   const void* k;
   const void* v;
-  long long k_st, k_sh, v_st, v_sh;
+  long long k_sb, k_st, k_sh, v_sb, v_st, v_sh;
   AttnSeqs s;
-  int64_t k_off[HF_MAX_BATCH];
-  int64_t v_off[HF_MAX_BATCH];
 };
 struct PagedAttnArgs {
   AttnIO io;
@@ -232,23 +245,26 @@ hipError_t launch_paged_attention(int dtype, int d_h, const AttnShape& sh, const
 hipError_t launch_attention_join(int dtype, int d_h, const AttnIO& io, const AttnSeqs& s,
                                  hipStream_t st);
 
+struct RowsSeq {
+  int32_t blk0;        // first 32-token block of the sequence
+  int32_t start, n;
+  int32_t pos0;
+  int32_t row0;        // rows of the sequences before it
+  int32_t pad[3];
+};
 struct PagedRowsArgs {
   const void* k;             // append: rows read; read: rows written
   const void* v;
-  long long k_st, k_sh, k_sl, v_st, v_sh, v_sl;
+  long long k_sb, k_st, k_sh, k_sl, v_sb, v_st, v_sh, v_sl;
   uint8_t* pages;            // of the first layer of the call
   const int32_t* table;
   long long table_stride, page_bytes;
   int32_t n_pages, log2_page;
-  int32_t B, H, n_layers;
+  int32_t B, H, n_layers, n_blocks;
   int32_t rotate;
+  Divide by_groups;          // head groups of a block
   double w[64];              // angle of a position step of each channel pair
-  int32_t start[HF_MAX_BATCH];
-  int32_t n[HF_MAX_BATCH];
-  int32_t pos0[HF_MAX_BATCH];
-  int32_t blk0[HF_MAX_BATCH + 1];  // first 32-token block of the sequence
-  int64_t k_off[HF_MAX_BATCH];
-  int64_t v_off[HF_MAX_BATCH];
+  alignas(32) RowsSeq q[HF_MAX_BATCH];
 };
 static_assert(sizeof(PagedRowsArgs) <= 4096, "kernel argument size");
 hipError_t launch_paged_append(int dtype, int d_h, const PagedRowsArgs& a, hipStream_t s);

@@ -26,6 +26,7 @@ namespace {
 
 struct RowItem {
   int b, l, h, role;
+  int start, pos0, src0;  // the sequence's first token, position offset, rows before it
   int tok0;          // first token of the block
   int lo, hi;        // tokens of the call in it, relative to tok0
   uint8_t* head;     // the head's part of the page, or nullptr (a hole)
@@ -35,24 +36,32 @@ struct RowItem {
 template <int D>
 FI RowItem row_item(const PagedRowsArgs& a, int hpw) {
   RowItem it;
-  int i = blockIdx.x;
-  const int groups = (a.H + hpw - 1) / hpw;
-  it.h = (i % groups) * hpw;
-  i /= groups;
+  const int wg = blockIdx.x, groups = (a.H + hpw - 1) / hpw;
+  const int i = divide(wg, a.by_groups);
+  it.h = (wg - i * groups) * hpw;
   it.role = blockIdx.y;
   it.l = blockIdx.z;
-  const int b = find_seq(a.blk0, a.B, i);
-  it.b = b;
-  const int blk = a.start[b] / 32 + (i - a.blk0[b]);
-  it.tok0 = blk * 32;
-  it.lo = max(a.start[b] - it.tok0, 0);
-  it.hi = min(a.start[b] + a.n[b] - it.tok0, 32);
-  const int page = a.table[b * a.table_stride + (it.tok0 >> a.log2_page)];
+  it.b = find_seq(a.q, &RowsSeq::blk0, a.B, i);
+  const RowsSeq q = a.q[it.b];
+  it.start = q.start;
+  it.pos0 = q.pos0;
+  it.src0 = q.row0;
+  it.tok0 = (q.start / 32 + (i - q.blk0)) * 32;
+  it.lo = max(q.start - it.tok0, 0);
+  it.hi = min(q.start + q.n - it.tok0, 32);
+  const int page = a.table[it.b * a.table_stride + (it.tok0 >> a.log2_page)];
   it.row0 = it.tok0 & ((1 << a.log2_page) - 1);
   it.head = nullptr;
   if ((unsigned)page < (unsigned)a.n_pages)
     it.head = a.pages + ((long long)it.l * a.n_pages + page) * a.page_bytes;
   return it;
+}
+
+// Elements to the dense row of token tok of the block, head 0.
+FI long long rows_at(const PagedRowsArgs& a, const RowItem& it, int tok) {
+  const long long sb = it.role == 0 ? a.k_sb : a.v_sb, st = it.role == 0 ? a.k_st : a.v_st;
+  return seq_at(it.b, it.src0, sb, st) + it.l * (it.role == 0 ? a.k_sl : a.v_sl) +
+         (it.tok0 + tok - it.start) * st;
 }
 
 // Offsets in a head's part of a page.
@@ -154,7 +163,7 @@ FI void fill_angles(const PagedRowsArgs& a, const RowItem& it, float2* cs) {
   constexpr int HD = D / 2;
   const int k = threadIdx.x % HD, m = threadIdx.x / HD;  // m < 4
   const double w = a.w[k];
-  const double base = (double)a.pos0[it.b] + it.tok0;
+  const double base = (double)it.pos0 + it.tok0;
   double c, s;
   if (it.hi - it.lo <= 4) {
     const int j = it.lo + m;
@@ -193,11 +202,7 @@ __global__ __launch_bounds__(2 * D) void paged_append_kernel(const PagedRowsArgs
   }
   const PageHead<D> ph(a.log2_page);
   const int row = it.row0 + tok;
-  const T* src = it.role == 0
-                     ? static_cast<const T*>(a.k) + a.k_off[it.b] + it.l * a.k_sl +
-                           (long long)(it.tok0 + tok - a.start[it.b]) * a.k_st
-                     : static_cast<const T*>(a.v) + a.v_off[it.b] + it.l * a.v_sl +
-                           (long long)(it.tok0 + tok - a.start[it.b]) * a.v_st;
+  const T* src = static_cast<const T*>(it.role == 0 ? a.k : a.v) + rows_at(a, it, tok);
   const long long sh = it.role == 0 ? a.k_sh : a.v_sh;
   const int h_end = min(it.h + hpw, a.H);
   for (int h = it.h; h < h_end; ++h) {
@@ -271,10 +276,7 @@ __global__ __launch_bounds__(2 * D) void paged_read_kernel(const PagedRowsArgs a
   const bool on = tok >= it.lo && tok < it.hi;
   const PageHead<D> ph(a.log2_page);
   const int row = it.row0 + tok;
-  T* dst = it.role == 0 ? static_cast<T*>(const_cast<void*>(a.k)) + a.k_off[it.b] + it.l * a.k_sl +
-                              (long long)(it.tok0 + tok - a.start[it.b]) * a.k_st
-                        : static_cast<T*>(const_cast<void*>(a.v)) + a.v_off[it.b] + it.l * a.v_sl +
-                              (long long)(it.tok0 + tok - a.start[it.b]) * a.v_st;
+  T* dst = static_cast<T*>(const_cast<void*>(it.role == 0 ? a.k : a.v)) + rows_at(a, it, tok);
   const long long sh = it.role == 0 ? a.k_sh : a.v_sh;
   const int h_end = min(it.h + hpw, a.H);
   for (int h = it.h; h < h_end; ++h) {
@@ -331,77 +333,137 @@ __global__ __launch_bounds__(2 * D) void paged_read_kernel(const PagedRowsArgs a
 // ---------------------------------------------------------------------------
 constexpr int kPagedWaves = 4;
 
-// Two codes of a dword, nibbles n and n + 4, as bf16 16 + code.
-FI uint32_t two_codes(uint32_t w, int n) {
-  // the code to bits 3..6 of each half, under the exponent of 16
-  const uint32_t x = n == 0 ? w << 3 : w >> (4 * n - 3);
-  return (x & 0x00780078u) | 0x41804180u;
-}
-FI bf16x8 eight_codes(uint32_t w) {
-  union {
-    uint32_t u[4];
-    bf16x8 v;
-  } x;
-#pragma unroll
-  for (int n = 0; n < 4; ++n) x.u[n] = two_codes(w, n);
-  return x.v;
-}
-
-// The same as code - 8, for fp32: 16 + code beside sums of up to 16 would cost four
-// more bits of the fp32 accumulation than code - 8 does.
-FI bf16x8 eight_centred(uint32_t w) {
-  union {
-    uint32_t u[4];
-    bf16x8 v;
-  } x;
-#pragma unroll
-  for (int n = 0; n < 4; ++n) {
-    const uint32_t p = two_codes(w, n);
-    const float lo = __builtin_bit_cast(float, p << 16) - 24.0f;
-    const float hi = __builtin_bit_cast(float, p & 0xffff0000u) - 24.0f;
-    x.u[n] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo),
-                                   0x07060302u);  // (exact: the upper halves)
+// Two codes of a dword, nibbles n and n + 4, as bf16 16 + code: moved to bits 3..6 of
+// each half, under the exponent of 16.  The two constants are kept in registers
+// (an instruction takes one literal at most), which makes a shift and one and-or of it.
+struct Codes {
+  uint32_t mask = 0x00780078u, sixteen = 0x41804180u;
+  FI Codes() { asm volatile("" : "+v"(mask), "+v"(sixteen)); }
+  FI uint32_t two(uint32_t w, int n) const {
+    return ((n == 0 ? w << 3 : w >> (4 * n - 3)) & mask) | sixteen;
   }
-  return x.v;
-}
-template <bool F32>
-FI bf16x8 code_operand(uint32_t w) {
-  return F32 ? eight_centred(w) : eight_codes(w);
-}
+  // CENTRED: as code - 8, exact, for fp32: 16 + code beside sums of up to 16 would cost
+  // four more bits of the fp32 accumulation than code - 8 does.
+  template <bool CENTRED>
+  FI bf16x8 operand(uint32_t w) const {
+    union {
+      uint32_t u[4];
+      bf16x8 v;
+    } x;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const uint32_t p = two(w, n);
+      if (CENTRED) {
+        const float lo = __builtin_bit_cast(float, p << 16) - 24.0f;
+        const float hi = __builtin_bit_cast(float, p & 0xffff0000u) - 24.0f;
+        x.u[n] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo),
+                                       0x07060302u);  // (exact: the upper halves)
+      } else {
+        x.u[n] = p;
+      }
+    }
+    return x.v;
+  }
+};
 
 // x as S bf16 terms whose sum holds 8 S bits of it.
+// (S = 1: x itself, which the conversion after it rounds)
 template <int S>
 FI void split(float x, float (&t)[S]) {
 #pragma unroll
   for (int i = 0; i < S; ++i) {
-    t[i] = bf16_round(x);
+    t[i] = S == 1 ? x : bf16_round(x);
     x -= t[i];
   }
 }
 
-// What a lane holds of a block of 32 tokens, as it is loaded.
+// Blocks of 32 tokens on their way through LDS: three stages a wave, filled by
+// global-to-LDS loads two blocks ahead.
 template <int D>
-struct Block {
+struct Stage {
   static constexpr int G = D / 32;
-  uint32_t k[2][G];    // key codes of token 16 u + lane % 16, octet lane / 16 of each group
-  uint32_t v[D / 16];  // value codes
-  uint32_t w[G];       // words of token lane % 32: keys' in lanes below 32, values' above
-  int page;
+  static constexpr int V = 16 * D, W = 32 * D, BYTES = 32 * D + 1024;  // key codes; value codes; words
+  static constexpr int LOADS = 2 * (D / 64) + 1;
+  static constexpr int COUNT = 3;
+
+  // The block of tokens row .. row + 32 of a page.
+  FI static void fill(const uint8_t* head, const PageHead<D>& ph, int row, unsigned char* st, int lane) {
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i)
+      __builtin_amdgcn_global_load_lds((const void*)(head + ph.kcode(row) + i * 1024 + lane * 16),
+                                       (lds_void_t*)(st + i * 1024), 16, 0, 0);
+    constexpr int CW = 2 * G;  // 16-byte pieces of 8 tokens' words
+    const int wl = lane % (8 * CW);
+    __builtin_amdgcn_global_load_lds(
+        (const void*)(head + ph.word(wl / (4 * CW), row) + wl % (4 * CW) * 16), (lds_void_t*)(st + W), 16, 0, 0);
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i)
+      __builtin_amdgcn_global_load_lds((const void*)(head + ph.vcode(row) + i * 1024 + lane * 16),
+                                       (lds_void_t*)(st + V + i * 1024), 16, 0, 0);
+  }
+};
+
+// What a lane reads of a stage.  The reads are written as instructions that the
+// compiler does not see as LDS accesses: it cannot tell which load in flight fills
+// which stage, and would wait for all of them.  They end with their own wait.
+template <int D>
+struct Block;
+template <>
+struct Block<128> {
+  u32x4 k[2];  // key codes of token 16 u + lane % 16, octet lane / 16 of each group
+  u32x4 v[2];  // value codes
+  u32x4 w;     // words of token lane % 32: keys' in lanes below 32, values' above
+  u32x4 wk[2]; // words of key token 16 u + lane % 16
+  FI void read(uint32_t st, int lane) {
+    const uint32_t ak = st + (lane & 15) * 64 + (lane >> 4) * 16, av = st + lane * 32;
+    const uint32_t aw = st + lane * 16, ax = st + (lane & 15) * 16;
+    asm volatile(
+        "ds_read_b128 %0, %7\n\t"
+        "ds_read_b128 %1, %7 offset:1024\n\t"
+        "ds_read_b128 %2, %8 offset:2048\n\t"
+        "ds_read_b128 %3, %8 offset:2064\n\t"
+        "ds_read_b128 %4, %9 offset:4096\n\t"
+        "ds_read_b128 %5, %10 offset:4096\n\t"
+        "ds_read_b128 %6, %10 offset:4352\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(k[0]), "=&v"(k[1]), "=&v"(v[0]), "=&v"(v[1]), "=&v"(w), "=&v"(wk[0]), "=&v"(wk[1])
+        : "v"(ak), "v"(av), "v"(aw), "v"(ax)
+        : "memory");
+  }
+  FI uint32_t key(int u, int g) const { return k[u][g]; }
+  FI uint32_t value(int n) const { return v[n / 4][n & 3]; }
+};
+template <>
+struct Block<64> {
+  u32x2 k[2];
+  u32x4 v;
+  u32x2 w, wk[2];
+  FI void read(uint32_t st, int lane) {
+    const uint32_t ak = st + (lane & 15) * 32 + (lane >> 4) * 8, av = st + lane * 16;
+    const uint32_t aw = st + lane * 8, ax = st + (lane & 15) * 8;
+    asm volatile(
+        "ds_read_b64 %0, %6\n\t"
+        "ds_read_b64 %1, %6 offset:512\n\t"
+        "ds_read_b128 %2, %7 offset:1024\n\t"
+        "ds_read_b64 %3, %8 offset:2048\n\t"
+        "ds_read_b64 %4, %9 offset:2048\n\t"
+        "ds_read_b64 %5, %9 offset:2176\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(k[0]), "=&v"(k[1]), "=&v"(v), "=&v"(w), "=&v"(wk[0]), "=&v"(wk[1])
+        : "v"(ak), "v"(av), "v"(aw), "v"(ax)
+        : "memory");
+  }
+  FI uint32_t key(int u, int g) const { return k[u][g]; }
+  FI uint32_t value(int n) const { return v[n]; }
 };
 
 template <int N>
 FI void load_dwords(const uint8_t* p, uint32_t (&x)[N]) {
-  if (N == 2) {
-    const u32x2 v = *reinterpret_cast<const u32x2*>(p);
-    x[0] = v[0];
-    x[1] = v[1];
-  } else {
 #pragma unroll
-    for (int i = 0; i < N; i += 4) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(p + 4 * i);
+  for (int i = 0; i < N; i += 4) {
+    const u32x4 v = *reinterpret_cast<const u32x4*>(p + 4 * i);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[i + e] = v[e];
-    }
+    for (int e = 0; e < 4; ++e) x[i + e] = v[e];
   }
 }
 
@@ -424,64 +486,74 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 ? 2 : 1) void paged_atten
     const PagedAttnArgs a) {
   constexpr int G = D / 32, NC = D / 16, S = F32 ? 3 : 1, R = 16 * NT;
   constexpr int NW = kPagedWaves;
-  constexpr int WB = 64 * G * 3;  // floats a wave: scales and offsets [role][G][32], words [64][G]
-  __shared__ __attribute__((aligned(16))) float lds[WB > D * R ? NW * WB : NW * D * R];
+  typedef Stage<D> St;
+  constexpr int WB = 64 * G * 2;  // floats a wave: scales and offsets [role][G][32]
+  constexpr int STAGED = NW * (St::COUNT * St::BYTES), JOINED = NW * D * R * 4;
+  __shared__ __attribute__((aligned(1024))) unsigned char stages[STAGED > JOINED ? STAGED : JOINED];
+  __shared__ __attribute__((aligned(16))) float lds[NW * WB];
   __shared__ float sm[NW][R], sl[NW][R];
-  typedef uint32_t uG __attribute__((ext_vector_type(G)));
 
   const int lane = threadIdx.x & 63, col = lane & 15, m4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const AttnSeqs& s = a.s;
   const AttnItem it = attn_item(s, R);
-  const int b = it.b, t = s.t[b];
-  const int n_rows = s.n[b] * s.G;
+  const int t = it.t, n_rows = it.rows;
   const int row0 = it.tile * R;
   const float c = a.io.c;
   float* sc = lds + wave * WB;
   float* of = sc + 64 * G;
-  uG* words = reinterpret_cast<uG*>(of + 64 * G);
+  unsigned char* my_stages = stages + wave * (St::COUNT * St::BYTES);
 
-  const int first_last = last_key(s, b, min(row0, n_rows - 1) / s.G);
-  const int end_last = last_key(s, b, min(row0 + R - 1, n_rows - 1) / s.G);
+  const int first_last = last_key(s, it, divide(min(row0, n_rows - 1), s.by_g));
+  const int end_last = last_key(s, it, divide(min(row0 + R - 1, n_rows - 1), s.by_g));
   const int lo = it.part * s.chunk;
-  const int hi = min(end_last + 1, s.parts[b] == 1 ? t : min(t, lo + s.chunk));
+  const int hi = min(end_last + 1, it.parts == 1 ? t : min(t, lo + s.chunk));
   const int P = 1 << a.log2_page;
   const PageHead<D> ph(a.log2_page);
-  const int32_t* table = a.table + b * a.table_stride;
+  const int32_t* table = a.table + it.b * a.table_stride;
   const long long head_at = (long long)it.h * ph.bytes();
 
-  // Block at token t0 (a hole's, too: it loads from page 0 and is masked).
-  auto page_of = [&](int t0) { return t0 < hi ? table[t0 >> a.log2_page] : -1; };
-  auto load = [&](Block<D>& x, int t0, int page) {
-    x.page = page;
-    if (t0 >= hi) return;
+  // The wave's blocks: i = 0, 1, .. at tokens first + i * 32 NW.  Lane i holds the page
+  // of block i of each 64.
+  const int first = lo + 32 * wave;
+  const int n_blocks = first < hi ? (hi - first + 32 * NW - 1) / (32 * NW) : 0;
+  auto pages_from = [&](int i) {
+    const int at = first + (i + lane) * 32 * NW;
+    return at < hi ? table[at >> a.log2_page] : -1;
+  };
+  int pages = -1;
+  auto page_of = [&](int i) { return __builtin_amdgcn_readlane(pages, i & 63); };
+  int held = 0;  // bit s: stage s holds a block of a page, not of a hole
+  // Block i to stage i % 3 (a hole's, too: it loads from page 0 and is masked).
+  auto fill = [&](int i, int st) {
+    if (i >= n_blocks) return;
+    if ((i & 63) == 0) {
+      pages = pages_from(i);
+      asm volatile("" : "+v"(pages));  // (waited for here, not at every block's fill)
+    }
+    const int page = page_of(i);
     const bool in = (unsigned)page < (unsigned)a.n_pages;
+    held = (held & ~(1 << st)) | ((int)in << st);
     const uint8_t* head = a.pages + (long long)(in ? page : 0) * a.page_bytes + head_at;
-    const int row = t0 & (P - 1);
-    load_dwords<G>(head + ph.kcode(row) + (col * (D / 2) + m4 * 4 * G), x.k[0]);
-    load_dwords<G>(head + ph.kcode(row + 16) + (col * (D / 2) + m4 * 4 * G), x.k[1]);
-    load_dwords<G>(head + ph.word(lane >> 5, row + (lane & 31)), x.w);
-    load_dwords<NC>(head + ph.vcode(row) + lane * 4 * NC, x.v);
+    St::fill(head, ph, (first + i * 32 * NW) & (P - 1), my_stages + st * St::BYTES, lane);
   };
   // the queries and the first block on their way before either is used
   typedef uint32_t QRaw[F32 ? 8 : 4];
   QRaw raw_q[NT][G];
   int last[NT];
+  const long long q0 = seq_at(it.b, it.row0, a.io.q_sb, a.io.q_st);
 #pragma unroll
   for (int x = 0; x < NT; ++x) {
     const int r = min(row0 + 16 * x + col, n_rows - 1);
-    const int token = r / s.G, g = r - token * s.G;
-    last[x] = last_key(s, b, token);
-    const long long at = s.q_off[b] + (long long)token * a.io.q_st + (long long)(it.h * s.G + g) * a.io.q_sh;
+    const int token = divide(r, s.by_g), head = it.h * s.G + r - token * s.G;
+    last[x] = last_key(s, it, token);
+    const long long at = q0 + token * a.io.q_st + head * a.io.q_sh;
     const uint8_t* row = static_cast<const uint8_t*>(a.io.q) + at * (F32 ? 4 : 2);
 #pragma unroll
     for (int y = 0; y < G; ++y) load_dwords<F32 ? 8 : 4>(row + (32 * y + 8 * m4) * (F32 ? 4 : 2), raw_q[x][y]);
   }
-  Block<D> x0, x1;
-  int t0 = lo + 32 * wave;
-  const int page0 = page_of(t0);
-  int next_page = page_of(t0 + 32 * NW);
-  load(x0, t0, page0);
+  fill(0, 0);
+  fill(1, 1);
 
   bf16x8 q[NT][S][G];
   bf16x8 qo[NT];   // against the words
@@ -510,6 +582,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 ? 2 : 1) void paged_atten
     }
   }
 
+  const Codes codes;
   f32x4 o[NT][NC] = {};    // sum of (p s) times the operand: row col, channels 16 n + 4 m4 + i
   f32x4 ps[NT][G] = {};    // sum of the rounded p s
   float po[NT][G] = {};    // sum of p times the offset, over the lane's tokens
@@ -526,17 +599,14 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 ? 2 : 1) void paged_atten
     // scales, and the values' offsets moved to code 8, to the lanes that need them.  Words
     // of tokens that no row sees count as 0, so that nothing below meets a NaN of theirs.
     const bool live = !M || (in && t0 + (lane & 31) < hi);
-    uG raw;
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int y = 0; y < G; ++y) {
       const uint32_t w = live ? x.w[y] : 0u;
-      raw[y] = w;
       const float f = __builtin_bit_cast(float, w & 0xffff0000u);
       sc[(lane >> 5) * 32 * G + 32 * y + (lane & 31)] = f;
       of[(lane >> 5) * 32 * G + 32 * y + (lane & 31)] = fmaf(f, 8.0f, __builtin_bit_cast(float, w << 16));
     }
-    words[lane] = raw;
     __builtin_amdgcn_wave_barrier();
 
     float p[NT][8];
@@ -546,16 +616,15 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 ? 2 : 1) void paged_atten
         uint32_t d[4];
         bf16x8 v;
       } wk = {{0, 0, 0, 0}};
-      const uG w = words[16 * u + col];
 #pragma unroll
-      for (int y = 0; y < G; ++y) wk.d[y] = w[y];
+      for (int y = 0; y < G; ++y) wk.d[y] = x.wk[u][y];
       f32x4 v[NT];
 #pragma unroll
       for (int n = 0; n < NT; ++n)
         v[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wk.v, qo[n], f32x4{}, 0, 0, 0);
 #pragma unroll
       for (int y = 0; y < G; ++y) {
-        const bf16x8 kc = code_operand<F32>(x.k[u][y]);
+        const bf16x8 kc = codes.operand<F32>(x.key(u, y));
         const f32x4 ks = *reinterpret_cast<const f32x4*>(sc + 32 * y + 16 * u + 4 * m4);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -609,7 +678,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 ? 2 : 1) void paged_atten
                         (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
     for (int y = 0; y < G; ++y) {
-      const bf16x8 v0 = code_operand<F32>(x.v[2 * y]), v1 = code_operand<F32>(x.v[2 * y + 1]);
+      const bf16x8 v0 = codes.operand<F32>(x.value(2 * y)), v1 = codes.operand<F32>(x.value(2 * y + 1));
       f32x4 zs[2], zo[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -650,18 +719,31 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 ? 2 : 1) void paged_atten
       }
     }
   };
-  auto any_block = [&](const Block<D>& x, int t0) {
-    const bool in = (unsigned)x.page < (unsigned)a.n_pages;
+  auto turn = [&](int i, int st, int later) {
+    if (i >= n_blocks) return;
+    fill(i + 2, later);
+    // at most the loads of the blocks after this one are outstanding
+    const int after = min(n_blocks - 1 - i, 2);
+    if (after == 2)
+      __builtin_amdgcn_s_waitcnt(wait_vm_only(2 * St::LOADS));
+    else if (after == 1)
+      __builtin_amdgcn_s_waitcnt(wait_vm_only(St::LOADS));
+    else
+      __builtin_amdgcn_s_waitcnt(wait_vm_only(0));
+    Block<D> x;
+    x.read(lds_addr(my_stages + st * St::BYTES), lane);
+    const int t0 = first + i * 32 * NW;
+    const bool in = (held >> st) & 1;
     if (!in || t0 + 31 > first_last || t0 + 32 > hi)
       block(Flag<true>(), x, t0, in);
     else
       block(Flag<false>(), x, t0, true);
   };
-  for (; t0 < hi; t0 += 32 * NW) {
-    load(x1, t0 + 32 * NW, next_page);
-    next_page = page_of(t0 + 64 * NW);
-    any_block(x0, t0);
-    x0 = x1;
+  int st = 0;
+  for (int i = 0; i < n_blocks; ++i) {
+    const int later = st == 0 ? 2 : st - 1;  // (i + 2) % 3
+    turn(i, st, later);
+    st = st == 2 ? 0 : st + 1;
   }
 
   // the lane's rows: out of the codes' 16 (with the 8 of the moved offsets), the
@@ -686,7 +768,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 ? 2 : 1) void paged_atten
   // join the waves: their sums against the common maximum to LDS, [wave][row][channel]
   // with 16-byte chunk x of row r at slot x ^ (r % 16), so that the 16 rows a write
   // touches lie on distinct banks; then four channels of a row a thread
-  f32x4* sums = reinterpret_cast<f32x4*>(lds);
+  f32x4* sums = reinterpret_cast<f32x4*>(stages);
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int r = 16 * n + col;
@@ -712,22 +794,19 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 ? 2 : 1) void paged_atten
       v += sums[(y * R + rl) * (D / 4) + (ch ^ (rl & 15))];
       lt = fmaf(sl[y][rl], __builtin_amdgcn_exp2f(sm[y][rl] - mm), lt);
     }
-    if (s.parts[b] == 1) {
-      const int token = r / s.G, g = r - token * s.G;
-      const long long to = s.o_off[b] + (long long)token * a.io.o_st +
-                           (long long)(it.h * s.G + g) * a.io.o_sh + 4 * ch;
-      v *= lt > 0.0f || lt != lt ? 1.0f / lt : 0.0f;
+    if (it.parts == 1) {
+      const int token = divide(r, s.by_g), head = it.h * s.G + r - token * s.G;
+      const long long to = out_at(a.io, s, it, token, head) + 4 * ch;
+      v *= inverse_weight(lt);
       if (F32) {
         *reinterpret_cast<f32x4*>(static_cast<float*>(a.io.out) + to) = v;
       } else {
         const u32x2 x = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
         *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.io.out) + to) = x;
       }
-      if (ch == 0 && a.io.lse)
-        a.io.lse[(long long)(s.row0[b] + token) * (s.H * s.G) + it.h * s.G + g] =
-            lt == 0.0f ? -INFINITY : (mm + log2f(lt)) * 0.6931471805599453f;
+      if (ch == 0) write_lse(a.io, s, it, token, head, mm, lt);
     } else {
-      const long long slot = s.part0[b] + ((long long)it.h * n_rows + r) * s.parts[b] + it.part;
+      const long long slot = part_slot(it, r);
       *reinterpret_cast<f32x4*>(a.io.part + slot * D + 4 * ch) = v;
       if (ch == 0) {
         a.io.ml[2 * slot] = mm;
@@ -739,7 +818,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 ? 2 : 1) void paged_atten
 
 template <int D>
 hipError_t launch(int dtype, const AttnShape& sh, const PagedAttnArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)(a.s.item0[a.s.B] * a.s.H));
+  const dim3 grid((unsigned)(a.s.n_items * a.s.H));
   const int threads = kPagedWaves * 64;
   if (dtype == HF_F32) {
     if (sh.rows == 16) paged_attention_kernel<D, 1, true><<<grid, threads, 0, st>>>(a);
@@ -754,7 +833,7 @@ hipError_t launch(int dtype, const AttnShape& sh, const PagedAttnArgs& a, hipStr
 // Heads a workgroup: with many blocks to do all of them, so that the angles of a
 // block are formed once.
 int heads_per_workgroup(const PagedRowsArgs& a) {
-  return (int64_t)a.blk0[a.B] * a.n_layers * a.H >= 4096 ? a.H : 1;
+  return (int64_t)a.n_blocks * a.n_layers * a.H >= 4096 ? a.H : 1;
 }
 
 }  // namespace
@@ -774,9 +853,11 @@ hipError_t launch_paged_attention(int dtype, int d_h, const AttnShape& sh, const
   return d_h == 128 ? launch<128>(dtype, sh, a, s) : launch<64>(dtype, sh, a, s);
 }
 
-hipError_t launch_paged_append(int dtype, int d_h, const PagedRowsArgs& a, hipStream_t s) {
+hipError_t launch_paged_append(int dtype, int d_h, const PagedRowsArgs& a0, hipStream_t s) {
+  PagedRowsArgs a = a0;
   const int hpw = heads_per_workgroup(a);
-  const dim3 grid((unsigned)(a.blk0[a.B] * ((a.H + hpw - 1) / hpw)), 2, (unsigned)a.n_layers);
+  a.by_groups = make_divide((a.H + hpw - 1) / hpw);
+  const dim3 grid((unsigned)(a.n_blocks * ((a.H + hpw - 1) / hpw)), 2, (unsigned)a.n_layers);
   if (dtype == HF_BF16) {
     if (d_h == 128) paged_append_kernel<uint16_t, 128><<<grid, 256, 0, s>>>(a, hpw);
     else paged_append_kernel<uint16_t, 64><<<grid, 128, 0, s>>>(a, hpw);
@@ -787,9 +868,11 @@ hipError_t launch_paged_append(int dtype, int d_h, const PagedRowsArgs& a, hipSt
   return hipGetLastError();
 }
 
-hipError_t launch_paged_read(int dtype, int d_h, const PagedRowsArgs& a, hipStream_t s) {
+hipError_t launch_paged_read(int dtype, int d_h, const PagedRowsArgs& a0, hipStream_t s) {
+  PagedRowsArgs a = a0;
   const int hpw = heads_per_workgroup(a);
-  const dim3 grid((unsigned)(a.blk0[a.B] * ((a.H + hpw - 1) / hpw)), 2, (unsigned)a.n_layers);
+  a.by_groups = make_divide((a.H + hpw - 1) / hpw);
+  const dim3 grid((unsigned)(a.n_blocks * ((a.H + hpw - 1) / hpw)), 2, (unsigned)a.n_layers);
   if (dtype == HF_BF16) {
     if (d_h == 128) paged_read_kernel<uint16_t, 128><<<grid, 256, 0, s>>>(a, hpw);
     else paged_read_kernel<uint16_t, 64><<<grid, 128, 0, s>>>(a, hpw);
