@@ -436,7 +436,8 @@ size_t hf_attention_workspace_bytes(int32_t B, const int32_t* q_len, const int32
  * not see has no influence on it, whatever its bits are.
  *   q_len, kv_len  host int32 [B], >= 0.
  *   q, out    hf_rows of H_q heads; out may be q itself, element for element.
- *   k, v      hf_rows of H heads, H_q % H == 0; same dtype and d_h throughout.
+ *   k, v      hf_rows of H heads, H_q % H == 0, stride_t <= 2^23; same dtype and
+ *             d_h throughout.
  *   scale     finite and > 0 (1/sqrt(d_h) as a rule).
  *   lse       device fp32 [sum q_len][H_q] (rows packed), or NULL.
  *   workspace device, >= hf_attention_workspace_bytes(..., paged = 0), 256-B

@@ -874,6 +874,8 @@ size_t part_bytes(int64_t slots, int32_t d_h) {
   return slots ? align_up((size_t)slots * d_h * 4, 256) + align_up((size_t)slots * 8, 256) : 0;
 }
 
+constexpr int64_t kMaxRowStride = 1 << 23;  // of keys and values: 32-bit offsets within a tile
+
 int32_t check_heads(int32_t H_q, int32_t H, int32_t d_h) {
   if (H < 1 || H_q < 1 || H_q % H) return fail(HF_ERR_SHAPE, "need H >= 1 and H_q a multiple of H (got %d, %d)", H, H_q);
   if (d_h != 64 && d_h != 128) return fail(HF_ERR_UNSUPPORTED, "attention needs d_h 64 or 128 (got %d)", d_h);
@@ -1058,6 +1060,8 @@ int32_t hf_prompt_attention(int32_t B, const int32_t* q_len, const int32_t* kv_l
                              workspace, workspace_bytes, sh, a.s, a.io)))
     return st;
   if (k->dtype != v->dtype || k->dtype != q->dtype) return fail(HF_ERR_DTYPE, "q, k and v dtypes differ");
+  if (k->stride_t > kMaxRowStride || v->stride_t > kMaxRowStride)
+    return fail(HF_ERR_UNSUPPORTED, "k, v: stride_t must be at most %lld", (long long)kMaxRowStride);
   a.k = k->ptr;
   a.v = v->ptr;
   a.k_sb = k->stride_b; a.k_st = k->stride_t; a.k_sh = k->stride_h;

@@ -37,10 +37,10 @@ namespace {
 // bf16 on v_mfma_f32_32x32x16_bf16: lane l is row l % 32; with h = l / 32, result
 // register i of a 32-key block is key 8 (i / 4) + 4 h + i % 4, and of a 32-channel
 // block the channel of that number.
-template <int D_, int KT_>
+template <int D_, int KT_, int RB_>
 struct Bf16Tile {
   static constexpr int D = D_, KT = KT_;
-  static constexpr int RW = 32;
+  static constexpr int RB = RB_, RW = 32;        // blocks of query rows a wave, rows a block
   static constexpr int NS = KT / 2, NO = D / 2;  // score and output registers
   static constexpr int ROWB = D * 2;             // bytes of a row
   typedef uint16_t T;
@@ -66,27 +66,30 @@ struct Bf16Tile {
       q.f[c] = *reinterpret_cast<const bf16x8*>(row + 16 * c + 8 * (lane >> 5));
   }
 
-  FI static void scores(const Q& q, const unsigned char* sk, int lane, float (&s)[NS]) {
+  FI static void scores(const Q (&q)[RB], const unsigned char* sk, int lane, float (&s)[RB][NS]) {
     const int r = lane & 31;
 #pragma unroll
     for (int kb = 0; kb < KT / 32; ++kb) {
-      f32x16 acc = {};
+      f32x16 acc[RB] = {};
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) {
         const bf16x8 a = *reinterpret_cast<const bf16x8*>(
             sk + kb * 32 * ROWB + r * ROWB + slot_k(r, 2 * c + (lane >> 5)) * 16);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q.f[c], acc, 0, 0, 0);
+#pragma unroll
+        for (int x = 0; x < RB; ++x)
+          acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[x].f[c], acc[x], 0, 0, 0);
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[16 * kb + i] = acc[i];
+      for (int x = 0; x < RB; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[x][16 * kb + i] = acc[x][i];
     }
   }
 
-  // O += V^T P^T.  CLEAN: values that are not finite enter as 0 (the masked tiles'
-  // slow path).
+  typedef f32x16 O[D / 32];
+  // O += V^T P^T.  CLEAN: values that are not finite enter as 0.
   template <bool CLEAN>
-  FI static void values(f32x16 (&o)[D / 32], const unsigned char* sv, int lane,
-                        const float (&p)[NS]) {
+  FI static void values(O (&o)[RB], const unsigned char* sv, int lane, const float (&p)[RB][NS]) {
     // the transposing read gives lane i of 16 the values of 4 rows at channel i; its
     // lane i names row i / 4 of them and 8 bytes there
     const int h = lane >> 5, gb = (lane >> 4) & 1, i = lane & 15;
@@ -96,9 +99,11 @@ struct Bf16Tile {
       union {
         bf16x8 v;
         uint32_t u[4];
-      } b;
+      } b[RB];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) b.u[x] = pack_bf16(p[8 * c + 2 * x], p[8 * c + 2 * x + 1]);
+      for (int x = 0; x < RB; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) b[x].u[y] = pack_bf16(p[x][8 * c + 2 * y], p[x][8 * c + 2 * y + 1]);
 #pragma unroll
       for (int n = 0; n < D / 32; ++n) {
         const unsigned char* at = sv + (16 * c + r) * ROWB + slot_v(r, 4 * n + 2 * gb) * 16 + (i & 3) * 8;
@@ -111,12 +116,14 @@ struct Bf16Tile {
         a.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(at + 8 * ROWB));
         if (CLEAN) {
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            if ((a.u[x] & 0x7f80u) == 0x7f80u) a.u[x] &= 0xffff0000u;
-            if ((a.u[x] & 0x7f800000u) == 0x7f800000u) a.u[x] &= 0xffffu;
+          for (int y = 0; y < 4; ++y) {
+            if ((a.u[y] & 0x7f80u) == 0x7f80u) a.u[y] &= 0xffff0000u;
+            if ((a.u[y] & 0x7f800000u) == 0x7f800000u) a.u[y] &= 0xffffu;
           }
         }
-        o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, o[n], 0, 0, 0);
+#pragma unroll
+        for (int x = 0; x < RB; ++x)
+          o[x][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b[x].v, o[x][n], 0, 0, 0);
       }
     }
   }
@@ -125,10 +132,6 @@ struct Bf16Tile {
     const uint16_t x = *reinterpret_cast<const uint16_t*>(sv + r * ROWB + slot_v(r, ch >> 3) * 16 + (ch & 7) * 2);
     return __builtin_bit_cast(float, (uint32_t)x << 16);
   }
-  // An exponent of all ones carries into bit 15 or 31.
-  static constexpr uint32_t kOver = 0x80008000u;
-  FI static uint32_t over(uint32_t x) { return (x & 0x7f807f80u) + 0x00800080u; }
-  typedef f32x16 O[D / 32];
   FI static float get(const O& o, int i) { return o[i / 16][i & 15]; }
   FI static void set(O& o, int i, float x) { o[i / 16][i & 15] = x; }
   FI static void store4(T* p, const float (&x)[4]) {
@@ -142,10 +145,10 @@ struct Bf16Tile {
 // of the first product takes channel 16 u + 4 m + j, so that a lane's operands are
 // 16-byte loads; step i of the second takes key 4 m + i, so that the scores'
 // registers are its operands as they are.
-template <int D_, int KT_>
+template <int D_, int KT_, int RB_>
 struct F32Tile {
   static constexpr int D = D_, KT = KT_;
-  static constexpr int RW = 16;
+  static constexpr int RB = RB_, RW = 16;
   static constexpr int NS = KT / 4, NO = D / 4;
   static constexpr int ROWB = D * 4;
   typedef float T;
@@ -168,36 +171,42 @@ struct F32Tile {
       q.f[u] = *reinterpret_cast<const f32x4*>(row + 16 * u + 4 * (lane >> 4));
   }
 
-  FI static void scores(const Q& q, const unsigned char* sk, int lane, float (&s)[NS]) {
+  FI static void scores(const Q (&q)[RB], const unsigned char* sk, int lane, float (&s)[RB][NS]) {
     const int r = lane & 15;
 #pragma unroll
     for (int kb = 0; kb < KT / 16; ++kb) {
-      f32x4 acc = {};
+      f32x4 acc[RB] = {};
 #pragma unroll
       for (int u = 0; u < D / 16; ++u) {
         const f32x4 a = *reinterpret_cast<const f32x4*>(
             sk + (kb * 16 + r) * ROWB + slot_k(r, 4 * u + (lane >> 4)) * 16);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], q.f[u][j], acc, 0, 0, 0);
+#pragma unroll
+          for (int x = 0; x < RB; ++x)
+            acc[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], q[x].f[u][j], acc[x], 0, 0, 0);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[4 * kb + i] = acc[i];
+      for (int x = 0; x < RB; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[x][4 * kb + i] = acc[x][i];
     }
   }
 
+  typedef f32x4 O[D / 16];
   template <bool CLEAN>
-  FI static void values(f32x4 (&o)[D / 16], const unsigned char* sv, int lane,
-                        const float (&p)[NS]) {
+  FI static void values(O (&o)[RB], const unsigned char* sv, int lane, const float (&p)[RB][NS]) {
     const int m = lane >> 4, c = lane & 15;
 #pragma unroll
-    for (int x = 0; x < NS; ++x) {
-      const int r = 16 * (x / 4) + 4 * m + (x & 3);
+    for (int k = 0; k < NS; ++k) {
+      const int r = 16 * (k / 4) + 4 * m + (k & 3);
 #pragma unroll
       for (int n = 0; n < D / 16; ++n) {
         float a = *reinterpret_cast<const float*>(sv + r * ROWB + slot_v(r, 4 * n + (c >> 2)) * 16 + (c & 3) * 4);
         if (CLEAN) a = finite_bits(a) ? a : 0.0f;
-        o[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, p[x], o[n], 0, 0, 0);
+#pragma unroll
+        for (int x = 0; x < RB; ++x)
+          o[x][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, p[x][k], o[x][n], 0, 0, 0);
       }
     }
   }
@@ -205,9 +214,6 @@ struct F32Tile {
   FI static float value_at(const unsigned char* sv, int r, int ch) {
     return *reinterpret_cast<const float*>(sv + r * ROWB + slot_v(r, ch >> 2) * 16 + (ch & 3) * 4);
   }
-  static constexpr uint32_t kOver = 0x80000000u;
-  FI static uint32_t over(uint32_t x) { return (x & 0x7f800000u) + 0x00800000u; }
-  typedef f32x4 O[D / 16];
   FI static float get(const O& o, int i) { return o[i / 4][i & 3]; }
   FI static void set(O& o, int i, float x) { o[i / 4][i & 3] = x; }
   FI static void store4(T* p, const float (&x)[4]) {
@@ -221,116 +227,119 @@ struct F32Tile {
 // ---------------------------------------------------------------------------
 template <class P>
 struct Rows {
-  typename P::Q q;
-  typename P::O o;
-  float m, l;    // the row's maximum; this lane's share of its weight
-  int last;      // the last key the row sees
+  typename P::Q q[P::RB];
+  typename P::O o[P::RB];
+  float m[P::RB], l[P::RB];  // each row's maximum; this lane's share of its weight
+  int last[P::RB];           // the last key it sees
 };
 
 // The weights of a tile's scores and their product with its values.  MASK: some row
 // of the wave does not see every key of the tile (t0 is its first).
+// In such a tile a value that is not finite would reach rows that do not see it, as
+// 0 * NaN.  That shows in their results: the kernels look at them at the end and in
+// that case compute once more with `careful`, where such a value enters the product
+// as 0 and is added to the rows that see its key.  (In other tiles all rows see all
+// keys, and the product does what it should.)
 template <class P, bool MASK>
-FI void finish(Rows<P>& w, float (&s)[P::NS], const unsigned char* sv, int lane, float c, int t0) {
-  if (MASK) {
+FI void finish(Rows<P>& w, float (&s)[P::RB][P::NS], const unsigned char* sv, int lane, float c,
+               int t0, bool careful) {
 #pragma unroll
-    for (int i = 0; i < P::NS; ++i)
-      if (t0 + P::key(lane, i) > w.last) s[i] = -INFINITY;
-  }
-  float mx = s[0];
+  for (int x = 0; x < P::RB; ++x) {
+    if (MASK) {
 #pragma unroll
-  for (int i = 1; i < P::NS; ++i) mx = fmaxf(mx, s[i]);
-  mx = P::row_max(mx) * c;
-  if (__any(mx > w.m + kRaise)) {
-    const float m = mx > w.m + kRaise ? mx : w.m;  // (each row by its own scores alone)
-    const float f = __builtin_amdgcn_exp2f(w.m - m);
-    w.m = m;
-    w.l *= f;
+      for (int i = 0; i < P::NS; ++i)
+        if (t0 + P::key(lane, i) > w.last[x]) s[x][i] = -INFINITY;
+    }
+    float mx = s[x][0];
 #pragma unroll
-    for (int i = 0; i < P::NO; ++i) P::set(w.o, i, P::get(w.o, i) * f);
+    for (int i = 1; i < P::NS; ++i) mx = fmaxf(mx, s[x][i]);
+    mx = P::row_max(mx) * c;
+    if (__any(mx > w.m[x] + kRaise)) {
+      const float m = mx > w.m[x] + kRaise ? mx : w.m[x];  // (each row by its own scores alone)
+      const float f = __builtin_amdgcn_exp2f(w.m[x] - m);
+      w.m[x] = m;
+      w.l[x] *= f;
+#pragma unroll
+      for (int i = 0; i < P::NO; ++i) P::set(w.o[x], i, P::get(w.o[x], i) * f);
+    }
   }
 #pragma unroll
-  for (int i = 0; i < P::NS; ++i) {
-    s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -w.m));
-    w.l += s[i];
-  }
-  if (!MASK) {
-    P::template values<false>(w.o, sv, lane, s);
-    return;
-  }
-  // In a tile that some rows see only in part a value that is not finite must reach
-  // the rows that see it and no other: 0 * NaN would.  It enters the product as 0
-  // and is added to the rows that see its key.  (Everywhere else all rows see all
-  // keys, and the product does what it should.)
-  uint32_t over = 0;
-#pragma unroll 4
-  for (int i = 0; i < P::KT * P::ROWB / 1024; ++i) {
-    const u32x4 x = *reinterpret_cast<const u32x4*>(sv + i * 1024 + lane * 16);
+  for (int x = 0; x < P::RB; ++x) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) over |= P::over(x[j]);
+    for (int i = 0; i < P::NS; ++i) {
+      s[x][i] = __builtin_amdgcn_exp2f(fmaf(s[x][i], c, -w.m[x]));
+      w.l[x] += s[x][i];
+    }
   }
-  if (!__any((over & P::kOver) != 0)) {
+  if (!MASK || !careful) {
     P::template values<false>(w.o, sv, lane, s);
     return;
   }
   P::template values<true>(w.o, sv, lane, s);
-  for (int r = 0; r < P::KT && t0 + r <= w.last; ++r) {
-    int at = lane;  // (opaque: the addresses below are formed here, not kept across the kernel)
-    asm volatile("" : "+v"(at));
 #pragma unroll
-    for (int i = 0; i < P::NO; ++i) {
-      const float x = P::value_at(sv, r, P::channel(at, i));
-      if (!finite_bits(x)) P::set(w.o, i, P::get(w.o, i) + x);
+  for (int x = 0; x < P::RB; ++x) {
+    for (int r = 0; r < P::KT && t0 + r <= w.last[x]; ++r) {
+      int at = lane;  // (opaque: the addresses below are formed here, not kept across the kernel)
+      asm volatile("" : "+v"(at));
+#pragma unroll
+      for (int i = 0; i < P::NO; ++i) {
+        const float v = P::value_at(sv, r, P::channel(at, i));
+        if (!finite_bits(v)) P::set(w.o[x], i, P::get(w.o[x], i) + v);
+      }
     }
   }
 }
 
-template <class P, bool MASK>
-FI void attend(Rows<P>& w, const unsigned char* sk, const unsigned char* sv, int lane, float c,
-               int t0) {
-  float s[P::NS];
-  P::scores(w.q, sk, lane, s);
-  finish<P, MASK>(w, s, sv, lane, c, t0);
+template <class P>
+FI bool not_finite(const Rows<P>& w) {
+  bool bad = false;
+#pragma unroll
+  for (int x = 0; x < P::RB; ++x)
+#pragma unroll
+    for (int i = 0; i < P::NO; ++i) bad |= !finite_bits(P::get(w.o[x], i));
+  return bad;
 }
 
 // Loads of one tile (keys t0 .. t0 + KT) into a stage: NB of the tile's 1 KB blocks
-// from block b0 in steps of `bstep`.  Rows past the last key hold copies of it.
+// from block b0 in steps of `bstep`.  Rows past the last key hold copies of it.  The
+// tile's address is in scalar registers, a lane's place in the tile a 32-bit offset
+// (rows lie at most 2^23 elements apart: host check).
 template <class P, bool V, int NB>
 struct Fetch {
   typedef typename P::T T;
   static constexpr int CPR = P::ROWB / 16;  // chunks a row
-  const T* base;
-  long long st;
-  int t, whole;      // keys; those before which a tile is loaded without a look at its rows
-  uint32_t off[NB];  // this lane's bytes from the tile's first row
+  static_assert(P::KT * (1ll << 23) * sizeof(T) <= 1ll << 31, "32-bit offsets");
+  const char* base;
+  long long st;  // bytes
+  int t;
+  int off[NB];
 
+  FI static int row(int i, int b0, int bstep, int lane) { return (b0 + i * bstep) * (64 / CPR) + lane / CPR; }
+  FI static int chunk(int r, int lane) {  // (its own inverse)
+    return (V ? P::slot_v(r, lane % CPR) : P::slot_k(r, lane % CPR)) * 16;
+  }
   FI void init(const T* base_, long long st_, int t_, int b0, int bstep, int lane) {
-    base = base_;
-    st = st_;
+    base = reinterpret_cast<const char*>(base_);
+    st = st_ * (int)sizeof(T);
     t = t_;
-    whole = st * (long long)sizeof(T) * P::KT < (1ll << 31) ? t : 0;
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-      const int r = (b0 + i * bstep) * (64 / CPR) + lane / CPR, slot = lane % CPR;
-      const int ch = (V ? P::slot_v(r, slot) : P::slot_k(r, slot)) * 16;  // (its own inverse)
-      off[i] = (uint32_t)(r * st * (long long)sizeof(T)) + ch;
+      const int r = row(i, b0, bstep, lane);
+      off[i] = r * (int)st + chunk(r, lane);
     }
   }
   FI void get(int t0, unsigned char* stage, int b0, int bstep, int lane) const {
-    const char* tile = reinterpret_cast<const char*>(base) + t0 * st * (long long)sizeof(T);
-    if (t0 + P::KT <= whole) {
-#pragma unroll
-      for (int i = 0; i < NB; ++i)
-        __builtin_amdgcn_global_load_lds((const void*)(tile + off[i]),
-                                         (lds_void_t*)(stage + (b0 + i * bstep) * 1024), 16, 0, 0);
-      return;
-    }
+    const __amdgpu_buffer_rsrc_t rsrc = buffer_at(base + t0 * st);
+    const bool whole = t0 + P::KT <= t;
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-      const int row = (b0 + i * bstep) * (64 / CPR) + lane / CPR, slot = lane % CPR;
-      const int ch = (V ? P::slot_v(row, slot) : P::slot_k(row, slot)) * 16;
-      const long long at = (long long)min(row, t - 1 - t0) * st * (long long)sizeof(T);
-      __builtin_amdgcn_global_load_lds((const void*)(tile + at + ch),
-                                       (lds_void_t*)(stage + (b0 + i * bstep) * 1024), 16, 0, 0);
+      int at = off[i];
+      if (!whole) {
+        const int r = row(i, b0, bstep, lane);
+        at = min(r, t - 1 - t0) * (int)st + chunk(r, lane);
+      }
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_t*)(stage + (b0 + i * bstep) * 1024), 16, at,
+                                               0, 0, 0);
     }
   }
 };
@@ -367,29 +376,38 @@ FI void write_row(const AttnIO& io, const AttnSeqs& s, const AttnItem& it, int r
   }
 }
 
-// Row r (the last one for rows past it, which are not written).
+// Rows r, r + RW, .. (the last one for rows past it, which are not written).
 template <class P>
-FI void start_rows(Rows<P>& w, const AttnArgs& a, const AttnItem& it, int r, int lane) {
+FI void load_rows(Rows<P>& w, const AttnArgs& a, const AttnItem& it, int r0, int lane) {
   typedef typename P::T T;
   const AttnSeqs& s = a.s;
-  r = min(r, it.rows - 1);
-  const int token = divide(r, s.by_g), head = it.h * s.G + r - token * s.G;
-  P::load_q(w.q, static_cast<const T*>(a.io.q) + seq_at(it.b, it.row0, a.io.q_sb, a.io.q_st) +
-                     token * a.io.q_st + head * a.io.q_sh, lane);
+  const T* q = static_cast<const T*>(a.io.q) + seq_at(it.b, it.row0, a.io.q_sb, a.io.q_st);
 #pragma unroll
-  for (int i = 0; i < P::NO; ++i) P::set(w.o, i, 0.0f);
-  w.m = kNoMax;
-  w.l = 0.0f;
-  w.last = last_key(s, it, token);
+  for (int x = 0; x < P::RB; ++x) {
+    const int r = min(r0 + x * P::RW, it.rows - 1);
+    const int token = divide(r, s.by_g), head = it.h * s.G + r - token * s.G;
+    P::load_q(w.q[x], q + token * a.io.q_st + head * a.io.q_sh, lane);
+    w.last[x] = last_key(s, it, token);
+  }
+}
+template <class P>
+FI void clear_rows(Rows<P>& w) {
+#pragma unroll
+  for (int x = 0; x < P::RB; ++x) {
+#pragma unroll
+    for (int i = 0; i < P::NO; ++i) P::set(w.o[x], i, 0.0f);
+    w.m[x] = kNoMax;
+    w.l[x] = 0.0f;
+  }
 }
 
-// By rows: NW waves, each RW rows of the tile, all against the same keys.  A wave
-// computes the scores of the next tile before it finishes this one's, so that matrix
-// instructions and the softmax's are there to be issued side by side.
+// By rows: NW waves, each with RB blocks of RW rows of the tile, all against the same
+// keys.  A wave computes the scores of the next tile before it finishes this one's, so
+// that matrix instructions and the softmax's are there to be issued side by side.
 template <class P, int NW>
 __global__ __launch_bounds__(NW * 64) void attention_rows_kernel(const AttnArgs a) {
   typedef typename P::T T;
-  constexpr int KT = P::KT;
+  constexpr int KT = P::KT, WR = P::RB * P::RW;  // keys a tile, rows a wave
   __shared__ __attribute__((aligned(1024))) unsigned char k0[KT * P::ROWB];
   __shared__ __attribute__((aligned(1024))) unsigned char v0[KT * P::ROWB];
   __shared__ __attribute__((aligned(1024))) unsigned char k1[KT * P::ROWB];
@@ -400,16 +418,16 @@ __global__ __launch_bounds__(NW * 64) void attention_rows_kernel(const AttnArgs 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const AttnSeqs& s = a.s;
-  const AttnItem it = attn_item(s, NW * P::RW);
+  const AttnItem it = attn_item(s, NW * WR);
   const int t = it.t, n_rows = it.rows;
-  const int row0 = it.tile * NW * P::RW;
+  const int row0 = it.tile * NW * WR, my0 = row0 + wave * WR;
   Rows<P> w;
-  start_rows<P>(w, a, it, row0 + wave * P::RW + P::row(lane), lane);
+  load_rows<P>(w, a, it, my0 + P::row(lane), lane);
 
   // keys of this part that some row of the workgroup sees, and that all of them see
-  const int wg_last = last_key(s, it, divide(min(row0 + NW * P::RW - 1, n_rows - 1), s.by_g));
+  const int wg_last = last_key(s, it, divide(min(row0 + NW * WR - 1, n_rows - 1), s.by_g));
   const int wg_first = last_key(s, it, divide(row0, s.by_g));
-  const int wave_last = last_key(s, it, divide(min(row0 + wave * P::RW + P::RW - 1, n_rows - 1), s.by_g));
+  const int wave_last = last_key(s, it, divide(min(my0 + WR - 1, n_rows - 1), s.by_g));
   const int lo = it.part * s.chunk;
   const int hi = min(wg_last + 1, it.parts == 1 ? t : min(t, lo + s.chunk));
   const T* kb = static_cast<const T*>(a.k) + seq_at(it.b, it.key0, a.k_sb, a.k_st) + (long long)it.h * a.k_sh;
@@ -433,51 +451,62 @@ __global__ __launch_bounds__(NW * 64) void attention_rows_kernel(const AttnArgs 
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
+  typedef float Scores[P::RB][P::NS];
   // Tile t0, whose scores are in s, with its values in sv; the next tile's keys in nk.
-  auto step = [&](int t0, float (&s0)[P::NS], float (&s1)[P::NS], unsigned char* sk,
-                  unsigned char* sv, unsigned char* nk, unsigned char* nv) {
+  auto step = [&](int t0, Scores& s0, Scores& s1, unsigned char* sk, unsigned char* sv,
+                  unsigned char* nk, unsigned char* nv) {
     ready();
     get_k(t0 + 2 * KT, sk);
     get_v(t0 + KT, nv);
     P::scores(w.q, nk, lane, s1);
-    finish<P, false>(w, s0, sv, lane, c, t0);
+    finish<P, false>(w, s0, sv, lane, c, t0, false);
   };
+  bool careful = false;
   // Near a causal edge or the last key, one tile's scores at a time.
-  auto masked_step = [&](int t0, float (&s)[P::NS], unsigned char* sk, unsigned char* sv,
+  auto masked_step = [&](int t0, Scores& s, unsigned char* sk, unsigned char* sv,
                          unsigned char* nk, unsigned char* nv) {
     ready();
     get_k(t0 + 2 * KT, sk);
     get_v(t0 + KT, nv);
-    if (t0 <= wave_last) finish<P, true>(w, s, sv, lane, c, t0);
+    if (t0 <= wave_last) finish<P, true>(w, s, sv, lane, c, t0, careful);
     if (t0 + KT <= wave_last && t0 + KT < hi) P::scores(w.q, nk, lane, s);
   };
-  if (lo < hi) {
-    float s0[P::NS], s1[P::NS];
-    get_k(lo, k0);
-    ready();
-    get_k(lo + KT, k1);
-    get_v(lo, v0);
-    P::scores(w.q, k0, lane, s0);
-    // pairs of tiles that every row sees whole, with a tile after them
-    int t0 = lo;
-    for (; t0 + 2 * KT - 1 <= wg_first && t0 + 2 * KT < hi; t0 += 2 * KT) {
-      step(t0, s0, s1, k0, v0, k1, v1);
-      step(t0 + KT, s1, s0, k1, v1, k0, v0);
+  for (;;) {
+    clear_rows<P>(w);
+    if (lo < hi) {
+      Scores s0, s1;
+      get_k(lo, k0);
+      ready();
+      get_k(lo + KT, k1);
+      get_v(lo, v0);
+      P::scores(w.q, k0, lane, s0);
+      // pairs of tiles that every row sees whole, with a tile after them
+      int t0 = lo;
+      for (; t0 + 2 * KT - 1 <= wg_first && t0 + 2 * KT < hi; t0 += 2 * KT) {
+        step(t0, s0, s1, k0, v0, k1, v1);
+        step(t0 + KT, s1, s0, k1, v1, k0, v0);
+      }
+      for (; t0 < hi; t0 += 2 * KT) {
+        masked_step(t0, s0, k0, v0, k1, v1);
+        if (t0 + KT < hi) masked_step(t0 + KT, s0, k1, v1, k0, v0);
+      }
     }
-    for (; t0 < hi; t0 += 2 * KT) {
-      masked_step(t0, s0, k0, v0, k1, v1);
-      if (t0 + KT < hi) masked_step(t0 + KT, s0, k1, v1, k0, v0);
-    }
+    if (careful || !__syncthreads_or(not_finite(w))) break;
+    careful = true;
   }
-  const int r = row0 + wave * P::RW + P::row(lane);
-  const float l = P::row_sum(w.l);
-  if (r < n_rows) write_row<P>(a.io, s, it, r, w.m, l, w.o, lane);
+#pragma unroll
+  for (int x = 0; x < P::RB; ++x) {
+    const int r = my0 + x * P::RW + P::row(lane);
+    const float l = P::row_sum(w.l[x]);
+    if (r < n_rows) write_row<P>(a.io, s, it, r, w.m[x], l, w.o[x], lane);
+  }
 }
 
 // By keys: one block of RW rows, the tiles of keys dealt to NW waves.
 template <class P, int NW>
 __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs a) {
   typedef typename P::T T;
+  static_assert(P::RB == 1, "one block of rows");
   constexpr int TB = P::KT * P::ROWB;  // bytes of a tile of keys, or of values
   __shared__ __attribute__((aligned(1024))) unsigned char s0[NW * 2 * TB];
   __shared__ __attribute__((aligned(1024))) unsigned char s1[NW * 2 * TB];
@@ -490,7 +519,7 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
   const int t = it.t, n_rows = it.rows;
   const int row0 = it.tile * P::RW;
   Rows<P> w;
-  start_rows<P>(w, a, it, row0 + P::row(lane), lane);
+  load_rows<P>(w, a, it, row0 + P::row(lane), lane);
   const int first = last_key(s, it, divide(min(row0, n_rows - 1), s.by_g));
   const int last = last_key(s, it, divide(min(row0 + P::RW - 1, n_rows - 1), s.by_g));
   const int lo = it.part * s.chunk + wave * P::KT;
@@ -509,6 +538,7 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
     fk.get(t0, st, 0, 1, lane);
     fv.get(t0, st + TB, 0, 1, lane);
   };
+  bool careful = false;
   auto step = [&](int t0, unsigned char* st, unsigned char* nst) {
     if (t0 + NW * P::KT < hi) {
       get(t0 + NW * P::KT, nst);
@@ -516,24 +546,31 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
     } else {
       __builtin_amdgcn_s_waitcnt(wait_vm_only(0));
     }
+    float s[1][P::NS];
+    P::scores(w.q, st, lane, s);
     if (t0 + P::KT - 1 > first)
-      attend<P, true>(w, st, st + TB, lane, c, t0);
+      finish<P, true>(w, s, st + TB, lane, c, t0, careful);
     else
-      attend<P, false>(w, st, st + TB, lane, c, t0);
+      finish<P, false>(w, s, st + TB, lane, c, t0, false);
   };
-  if (lo < hi) {
-    get(lo, w0);
-    for (int t0 = lo; t0 < hi; t0 += 2 * NW * P::KT) {
-      step(t0, w0, w1);
-      if (t0 + NW * P::KT < hi) step(t0 + NW * P::KT, w1, w0);
+  for (;;) {
+    clear_rows<P>(w);
+    if (lo < hi) {
+      get(lo, w0);
+      for (int t0 = lo; t0 < hi; t0 += 2 * NW * P::KT) {
+        step(t0, w0, w1);
+        if (t0 + NW * P::KT < hi) step(t0 + NW * P::KT, w1, w0);
+      }
     }
+    if (careful || !__any(not_finite(w))) break;
+    careful = true;
   }
 
   // join the waves: the common maximum, then the sums, 64 channels at a time in s0
   const int rl = P::row(lane);
-  const float l = P::row_sum(w.l);
+  const float l = P::row_sum(w.l[0]);
   if (lane < P::RW) {
-    sm[wave][rl] = w.m;
+    sm[wave][rl] = w.m[0];
     sl[wave][rl] = l;
   }
   __syncthreads();
@@ -543,7 +580,7 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
   float lt = 0.0f;
 #pragma unroll
   for (int x = 0; x < NW; ++x) lt += sl[x][rl] * __builtin_amdgcn_exp2f(sm[x][rl] - m);
-  const float f = __builtin_amdgcn_exp2f(w.m - m);
+  const float f = __builtin_amdgcn_exp2f(w.m[0] - m);
   constexpr int LD = P::RW;
   float* buf = reinterpret_cast<float*>(s0);  // [NW][64][LD]
   static_assert(NW * 64 * LD * 4 <= NW * 2 * TB, "joining buffer");
@@ -553,7 +590,7 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
 #pragma unroll
     for (int i = 0; i < P::NO; ++i) {
       const int ch = P::channel(lane, i) - 64 * half;
-      if (i / (P::NO / (P::D / 64)) == half) buf[(wave * 64 + ch) * LD + rl] = P::get(w.o, i) * f;
+      if (i / (P::NO / (P::D / 64)) == half) buf[(wave * 64 + ch) * LD + rl] = P::get(w.o[0], i) * f;
     }
     __syncthreads();
     // wave x sums the channel blocks that lie on the same registers of its lanes
@@ -564,7 +601,7 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
       float x = 0.0f;
 #pragma unroll
       for (int y = 0; y < NW; ++y) x += buf[(y * 64 + ch) * LD + rl];
-      P::set(w.o, i, x);
+      P::set(w.o[0], i, x);
     }
   }
   // each wave holds every NW-th group of four registers: it writes those channels
@@ -579,7 +616,7 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
       if ((i / 4) % NW != wave) continue;
       float x[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = P::get(w.o, i + j) * inv;
+      for (int j = 0; j < 4; ++j) x[j] = P::get(w.o[0], i + j) * inv;
       P::store4(out + P::channel(lane, i), x);
     }
     if (wave == 0 && lane < P::RW) write_lse(a.io, s, it, token, head, m, lt);
@@ -589,7 +626,7 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
 #pragma unroll
   for (int i = 0; i < P::NO; i += 4) {
     if ((i / 4) % NW != wave) continue;
-    const f32x4 v = {P::get(w.o, i), P::get(w.o, i + 1), P::get(w.o, i + 2), P::get(w.o, i + 3)};
+    const f32x4 v = {P::get(w.o[0], i), P::get(w.o[0], i + 1), P::get(w.o[0], i + 2), P::get(w.o[0], i + 3)};
     *reinterpret_cast<f32x4*>(a.io.part + slot * P::D + P::channel(lane, i)) = v;
   }
   if (wave == 0 && lane < P::RW) {
@@ -667,22 +704,22 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const JoinArgs a) {
   if (c == 0) write_lse(a.io, s, it, token, head, m, l);
 }
 
-constexpr int kRowWaves = 8, kRowWavesF32 = 4, kKeyWaves = 4;
+constexpr int kRowWaves = 8, kRowBlocks = 1, kRowWavesF32 = 4, kKeyWaves = 4;
 
 template <int D>
 hipError_t launch(int dtype, const AttnShape& sh, const AttnArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)(a.s.n_items * a.s.H));
   if (dtype == HF_BF16) {
     if (sh.by_keys)
-      attention_keys_kernel<Bf16Tile<D, 32>, kKeyWaves><<<grid, kKeyWaves * 64, 0, st>>>(a);
+      attention_keys_kernel<Bf16Tile<D, 32, 1>, kKeyWaves><<<grid, kKeyWaves * 64, 0, st>>>(a);
     else
-      attention_rows_kernel<Bf16Tile<D, 64>, kRowWaves><<<grid, kRowWaves * 64, 0, st>>>(a);
+      attention_rows_kernel<Bf16Tile<D, 64, kRowBlocks>, kRowWaves><<<grid, kRowWaves * 64, 0, st>>>(a);
   } else {
     if (sh.by_keys)
-      attention_keys_kernel<F32Tile<D, D == 128 ? 16 : 32>, kKeyWaves>
+      attention_keys_kernel<F32Tile<D, D == 128 ? 16 : 32, 1>, kKeyWaves>
           <<<grid, kKeyWaves * 64, 0, st>>>(a);
     else
-      attention_rows_kernel<F32Tile<D, 32>, kRowWavesF32><<<grid, kRowWavesF32 * 64, 0, st>>>(a);
+      attention_rows_kernel<F32Tile<D, 32, 1>, kRowWavesF32><<<grid, kRowWavesF32 * 64, 0, st>>>(a);
   }
   return hipGetLastError();
 }
@@ -693,7 +730,7 @@ AttnShape prompt_shape(int dtype, int d_h, int64_t max_rows) {
   AttnShape sh;
   const int rw = dtype == HF_BF16 ? 32 : 16;
   sh.by_keys = max_rows <= rw;
-  sh.rows = sh.by_keys ? rw : rw * (dtype == HF_BF16 ? kRowWaves : kRowWavesF32);
+  sh.rows = sh.by_keys ? rw : rw * (dtype == HF_BF16 ? kRowWaves * kRowBlocks : kRowWavesF32);
   sh.wg_target = 256;
   sh.step = sh.by_keys ? 32 * kKeyWaves : 64;
   sh.join_keys = sh.by_keys ? 512 : 256;
