@@ -566,7 +566,6 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
     careful = true;
   }
 
-  // join the waves: the common maximum, then the sums, 64 channels at a time in s0
   const int rl = P::row(lane);
   const float l = P::row_sum(w.l[0]);
   if (lane < P::RW) {
@@ -577,62 +576,16 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
   float m = sm[0][rl];
 #pragma unroll
   for (int x = 1; x < NW; ++x) m = fmaxf(m, sm[x][rl]);
-  float lt = 0.0f;
-#pragma unroll
-  for (int x = 0; x < NW; ++x) lt += sl[x][rl] * __builtin_amdgcn_exp2f(sm[x][rl] - m);
   const float f = __builtin_amdgcn_exp2f(w.m[0] - m);
-  constexpr int LD = P::RW;
-  float* buf = reinterpret_cast<float*>(s0);  // [NW][64][LD]
-  static_assert(NW * 64 * LD * 4 <= NW * 2 * TB, "joining buffer");
-#pragma unroll
-  for (int half = 0; half < P::D / 64; ++half) {
-    if (half) __syncthreads();
-#pragma unroll
-    for (int i = 0; i < P::NO; ++i) {
-      const int ch = P::channel(lane, i) - 64 * half;
-      if (i / (P::NO / (P::D / 64)) == half) buf[(wave * 64 + ch) * LD + rl] = P::get(w.o[0], i) * f;
-    }
-    __syncthreads();
-    // wave x sums the channel blocks that lie on the same registers of its lanes
-#pragma unroll
-    for (int i = 0; i < P::NO; ++i) {
-      if (i / (P::NO / (P::D / 64)) != half || (i / 4) % NW != wave) continue;
-      const int ch = P::channel(lane, i) - 64 * half;
-      float x = 0.0f;
-#pragma unroll
-      for (int y = 0; y < NW; ++y) x += buf[(y * 64 + ch) * LD + rl];
-      P::set(w.o[0], i, x);
-    }
-  }
-  // each wave holds every NW-th group of four registers: it writes those channels
-  const int r = row0 + rl;
-  if (r >= n_rows) return;
-  if (it.parts == 1) {
-    const int token = divide(r, s.by_g), head = it.h * s.G + r - token * s.G;
-    const float inv = inverse_weight(lt);
-    T* out = static_cast<T*>(a.io.out) + out_at(a.io, s, it, token, head);
-#pragma unroll
-    for (int i = 0; i < P::NO; i += 4) {
-      if ((i / 4) % NW != wave) continue;
-      float x[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = P::get(w.o[0], i + j) * inv;
-      P::store4(out + P::channel(lane, i), x);
-    }
-    if (wave == 0 && lane < P::RW) write_lse(a.io, s, it, token, head, m, lt);
-    return;
-  }
-  const long long slot = part_slot(it, r);
+  f32x4* sums = reinterpret_cast<f32x4*>(s0);
+  static_assert(NW * P::RW * P::D * 4 <= NW * 2 * TB, "joining buffer");
 #pragma unroll
   for (int i = 0; i < P::NO; i += 4) {
-    if ((i / 4) % NW != wave) continue;
     const f32x4 v = {P::get(w.o[0], i), P::get(w.o[0], i + 1), P::get(w.o[0], i + 2), P::get(w.o[0], i + 3)};
-    *reinterpret_cast<f32x4*>(a.io.part + slot * P::D + P::channel(lane, i)) = v;
+    sums[sum_slot<P::RW, P::D>(wave, rl, P::channel(lane, i) / 4)] = v * f;
   }
-  if (wave == 0 && lane < P::RW) {
-    a.io.ml[2 * slot] = m;
-    a.io.ml[2 * slot + 1] = lt;
-  }
+  __syncthreads();
+  write_joined<P::RW, P::D, NW, sizeof(T) == 4>(a.io, s, it, row0, sums, sm, sl);
 }
 
 // ---------------------------------------------------------------------------

@@ -162,4 +162,50 @@ FI long long part_slot(const AttnItem& it, int r) {
   return it.part0 + ((long long)it.h * it.rows + r) * it.parts + it.part;
 }
 
+// Where four waves share R query rows and deal the keys among them: their sums, each
+// against the waves' common maximum, lie in LDS as [wave][row][channel] with 16-byte
+// chunk x of row r at slot x ^ (r % 16), so that the 16 rows that a write touches at
+// once lie on distinct banks.  Each thread adds four channels of a row and writes the
+// result, or the part.  sm, sl: the waves' maxima and weights.
+template <int R, int D>
+FI int sum_slot(int wave, int r, int chunk) {
+  return (wave * R + r) * (D / 4) + (chunk ^ (r & 15));
+}
+template <int R, int D, int NW, bool F32>
+FI void write_joined(const AttnIO& io, const AttnSeqs& s, const AttnItem& it, int row0,
+                     const f32x4* sums, const float (&sm)[NW][R], const float (&sl)[NW][R]) {
+  const int rows = min(R, it.rows - row0);
+  for (int at = threadIdx.x; at < rows * (D / 4); at += 64 * NW) {
+    const int rl = at / (D / 4), ch = at % (D / 4), r = row0 + rl;
+    float m = sm[0][rl], l = 0.0f;
+    f32x4 v = {};
+#pragma unroll
+    for (int y = 1; y < NW; ++y) m = fmaxf(m, sm[y][rl]);
+#pragma unroll
+    for (int y = 0; y < NW; ++y) {
+      v += sums[sum_slot<R, D>(y, rl, ch)];
+      l = fmaf(sl[y][rl], __builtin_amdgcn_exp2f(sm[y][rl] - m), l);
+    }
+    if (it.parts == 1) {
+      const int token = divide(r, s.by_g), head = it.h * s.G + r - token * s.G;
+      const long long to = out_at(io, s, it, token, head) + 4 * ch;
+      v *= inverse_weight(l);
+      if (F32) {
+        *reinterpret_cast<f32x4*>(static_cast<float*>(io.out) + to) = v;
+      } else {
+        const u32x2 x = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(io.out) + to) = x;
+      }
+      if (ch == 0) write_lse(io, s, it, token, head, m, l);
+    } else {
+      const long long slot = part_slot(it, r);
+      *reinterpret_cast<f32x4*>(io.part + slot * D + 4 * ch) = v;
+      if (ch == 0) {
+        io.ml[2 * slot] = m;
+        io.ml[2 * slot + 1] = l;
+      }
+    }
+  }
+}
+
 }  // namespace hf

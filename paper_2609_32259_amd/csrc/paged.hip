@@ -76,26 +76,22 @@ struct PageHead {
   FI int word(int role, int row) const { return P * D + (role * P + row) * (4 * G); }
 };
 
+// Eight channels as they are loaded, and their values.
 template <class T>
-FI void load8(const T* p, float (&x)[8]);
-template <>
-FI void load8<uint16_t>(const uint16_t* p, float (&x)[8]) {
-  const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+struct Raw8 {
+  u32x4 v[sizeof(T) / 2];
+  FI void load(const T* p) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __builtin_bit_cast(float, v[i] << 16);
-    x[2 * i + 1] = __builtin_bit_cast(float, v[i] & 0xffff0000u);
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = reinterpret_cast<const u32x4*>(p)[i];
   }
-}
-template <>
-FI void load8<float>(const float* p, float (&x)[8]) {
-  const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+  FI void values(float (&x)[8]) const {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[i] = a[i];
-    x[4 + i] = b[i];
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t w = sizeof(T) == 4 ? v[i / 4 % (sizeof(T) / 2)][i & 3] : v[0][i / 2];
+      x[i] = __builtin_bit_cast(float, sizeof(T) == 4 ? w : i & 1 ? w & 0xffff0000u : w << 16);
+    }
   }
-}
+};
 
 template <class T>
 FI void store8(T* p, const float (&x)[8]);
@@ -117,41 +113,77 @@ FI float bf16_round(float x) { return (float)(__bf16)x; }
 
 // Codes and word of a group spread over four lanes (l, l ^ 1, l ^ 2, l ^ 3), eight
 // channels a lane.  Codes as a dword, channel j at nibble j.
+FI float quad_xor1(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0xb1, 0xf, 0xf, true));
+}
+FI float quad_xor2(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x4e, 0xf, 0xf, true));
+}
 FI uint32_t code_group(const float (&x)[8], uint32_t& word) {
 #pragma clang fp contract(off)
+  // minimum and maximum pass a NaN on
   float lo = x[0], hi = x[0];
-  bool nan = x[0] != x[0];
 #pragma unroll
   for (int j = 1; j < 8; ++j) {
-    lo = fminf(lo, x[j]);
-    hi = fmaxf(hi, x[j]);
-    nan = nan || x[j] != x[j];
+    lo = __builtin_elementwise_minimum(lo, x[j]);
+    hi = __builtin_elementwise_maximum(hi, x[j]);
   }
-  // (fminf and fmaxf pass NaN by)
-  lo = nan ? NAN : lo;
-#pragma unroll
-  for (int m = 1; m <= 2; m <<= 1) {
-    const float ol = __shfl_xor(lo, m), oh = __shfl_xor(hi, m);
-    lo = lo != lo || ol != ol ? NAN : fminf(lo, ol);
-    hi = fmaxf(hi, oh);
-  }
+  lo = __builtin_elementwise_minimum(lo, quad_xor1(lo));
+  hi = __builtin_elementwise_maximum(hi, quad_xor1(hi));
+  lo = __builtin_elementwise_minimum(lo, quad_xor2(lo));
+  hi = __builtin_elementwise_maximum(hi, quad_xor2(hi));
   const float o = bf16_round(lo);
   float s = bf16_round((hi - lo) / 15.0f);
-  if (!finite_bits(o) || !finite_bits(s)) {
+  if (s < 0x1p-100f) s = 0.0f;
+  word = __builtin_bit_cast(uint32_t, s) | (__builtin_bit_cast(uint32_t, o) >> 16);
+  float q[8];
+  // True quotients: what lies halfway between two codes goes to the even one.  With the
+  // rounded reciprocal r of s, q = d r and its remainder d - q s (exact), q + rem r is
+  // the rounded quotient, wherever r and the remainder are normal numbers or the
+  // quotient rounds to 0; a third of a division's instructions.
+  if (s >= 0x1p-100f && s <= 0x1p100f) {
+    const float r = 1.0f / s;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float d = x[j] - o, e = d * r;
+      q[j] = __builtin_amdgcn_fmed3f(rintf(fmaf(fmaf(-e, s, d), r, e)), 0.0f, 15.0f);
+    }
+  } else if (finite_bits(o) && finite_bits(s)) {
+    const float div = s > 0.0f ? s : INFINITY;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[j] = __builtin_amdgcn_fmed3f(rintf((x[j] - o) / div), 0.0f, 15.0f);
+  } else {
     word = 0x7fc07fc0u;  // NaN, NaN
     return 0;
   }
-  if (s < 0x1p-100f) s = 0.0f;
-  word = __builtin_bit_cast(uint32_t, s) | (__builtin_bit_cast(uint32_t, o) >> 16);
-  uint32_t c = 0;
-  const float d = s > 0.0f ? s : INFINITY;
+  // four codes to a float: whole numbers below 2^16
+  const float c0 = fmaf(fmaf(fmaf(q[3], 16.0f, q[2]), 16.0f, q[1]), 16.0f, q[0]);
+  const float c1 = fmaf(fmaf(fmaf(q[7], 16.0f, q[6]), 16.0f, q[5]), 16.0f, q[4]);
+  return (uint32_t)c0 | ((uint32_t)c1 << 16);
+}
+
+// Nibble j of a[t] to nibble t of a[j].
+FI void transpose_nibbles(uint32_t (&a)[8]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    // a true quotient: what lies halfway between two codes goes to the even one
-    const float q = fminf(fmaxf(rintf((x[j] - o) / d), 0.0f), 15.0f);
-    c |= (uint32_t)(int)q << (4 * j);
+  for (int t = 0; t < 4; ++t) {  // halves of dwords t and t + 4
+    const uint32_t x = a[t], y = a[t + 4];
+    a[t] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+    a[t + 4] = __builtin_amdgcn_perm(y, x, 0x07060302u);
   }
-  return c;
+#pragma unroll
+  for (int t = 0; t < 8; t += 4)
+#pragma unroll
+    for (int u = t; u < t + 2; ++u) {  // bytes
+      const uint32_t x = a[u], y = a[u + 2];
+      a[u] = __builtin_amdgcn_perm(y, x, 0x06020400u);
+      a[u + 2] = __builtin_amdgcn_perm(y, x, 0x07030501u);
+    }
+#pragma unroll
+  for (int t = 0; t < 8; t += 2) {
+    const uint32_t x = a[t], y = a[t + 1];
+    a[t] = (x & 0x0f0f0f0fu) | ((y << 4) & 0xf0f0f0f0u);
+    a[t + 1] = ((x >> 4) & 0x0f0f0f0fu) | (y & 0xf0f0f0f0u);
+  }
 }
 
 // cos and sin of pos * w_k for the block's 32 positions, to LDS [32][D/2], fp64
@@ -185,84 +217,103 @@ FI void fill_angles(const PagedRowsArgs& a, const RowItem& it, float2* cs) {
   }
 }
 
-template <class T, int D>
+// A transfer's cache of 40 layers and 7.3K tokens (1.19 GB in, 0.37 GB out) takes
+// 365 us, 4.3 TB/s.  Four heads' rows are loaded at a time.
+// ROT: a call that rotates its keys.  (Their angles take registers that a call which
+// only moves rows would miss for loads in flight: 377 -> 365 us at that size.)
+template <class T, int D, bool ROT>
 __global__ __launch_bounds__(2 * D) void paged_append_kernel(const PagedRowsArgs a, const int hpw) {
   constexpr int TPT = D / 16;  // threads a token
-  constexpr int G = D / 32;
-  __shared__ float2 cs[32 * D / 2];
-  __shared__ uint32_t codes[32 * D / 8];  // [token][channel] nibbles
+  constexpr int G = D / 32, O = D / 8;
+  constexpr int LD = O + (D == 128 ? 4 : 2);  // dwords a token in LDS: tokens 4 apart on other banks
+  constexpr int NH = 4;
+  __shared__ float2 cs[ROT ? 32 * D / 2 : 1];
+  __shared__ uint32_t codes[NH][32 * LD];
   const RowItem it = row_item<D>(a, hpw);
   if (!it.head) return;
   const int tok = threadIdx.x / TPT, j = threadIdx.x % TPT;
   const bool on = tok >= it.lo && tok < it.hi;
-  const bool rot = a.rotate && it.role == 0;
-  if (rot) {
-    fill_angles<D>(a, it, cs);
-    __syncthreads();
-  }
+  const bool rot = ROT && it.role == 0;
   const PageHead<D> ph(a.log2_page);
   const int row = it.row0 + tok;
   const T* src = static_cast<const T*>(it.role == 0 ? a.k : a.v) + rows_at(a, it, tok);
   const long long sh = it.role == 0 ? a.k_sh : a.v_sh;
   const int h_end = min(it.h + hpw, a.H);
-  for (int h = it.h; h < h_end; ++h) {
-    uint8_t* head = it.head + (long long)h * ph.bytes();
-    uint32_t c0 = 0, c1 = 0, w0 = 0, w1 = 0;
+  for (int h0 = it.h; h0 < h_end; h0 += NH) {
+    Raw8<T> r0[NH], r1[NH];  // channels 8 j .. and D/2 + 8 j ..: rotation pairs
     if (on) {  // (a group's four lanes hold the same token)
-      float x0[8], x1[8];  // channels 8 j .. and D/2 + 8 j ..: rotation pairs
-      load8<T>(src + h * sh + 8 * j, x0);
-      load8<T>(src + h * sh + D / 2 + 8 * j, x1);
-      if (rot) {
+#pragma unroll
+      for (int i = 0; i < NH; ++i)
+        if (h0 + i < h_end) {
+          r0[i].load(src + (h0 + i) * sh + 8 * j);
+          r1[i].load(src + (h0 + i) * sh + D / 2 + 8 * j);
+        }
+    }
+    if (ROT && rot && h0 == it.h) {  // (while the rows are on their way)
+      fill_angles<D>(a, it, cs);
+      __syncthreads();
+    }
+    if (on) {
+#pragma unroll
+      for (int i = 0; i < NH; ++i) {
+        if (h0 + i >= h_end) break;
+        float x0[8], x1[8];
+        r0[i].values(x0);
+        r1[i].values(x1);
+        if (ROT && rot) {
 #pragma clang fp contract(off)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float2 r = cs[tok * (D / 2) + 8 * j + e];
-          const float u = x0[e], v = x1[e];
-          x0[e] = u * r.x - v * r.y;
-          x1[e] = v * r.x + u * r.y;
+          for (int e = 0; e < 8; ++e) {
+            const float2 r = cs[tok * (D / 2) + 8 * j + e];
+            const float u = x0[e], v = x1[e];
+            x0[e] = u * r.x - v * r.y;
+            x1[e] = v * r.x + u * r.y;
+          }
         }
-      }
-      c0 = code_group(x0, w0);
-      c1 = code_group(x1, w1);
-      uint32_t* words = reinterpret_cast<uint32_t*>(head + ph.word(it.role, row));
-      if ((j & 3) == 0) {
-        words[j >> 2] = w0;
-        words[G / 2 + (j >> 2)] = w1;
-      }
-      if (it.role == 0) {
-        uint32_t* kc = reinterpret_cast<uint32_t*>(head + ph.kcode(row));
-        kc[(j & 3) * G + (j >> 2)] = c0;
-        kc[(j & 3) * G + G / 2 + (j >> 2)] = c1;
+        uint32_t w0, w1;
+        const uint32_t c0 = code_group(x0, w0), c1 = code_group(x1, w1);
+        uint8_t* head = it.head + (long long)(h0 + i) * ph.bytes();
+        uint32_t* words = reinterpret_cast<uint32_t*>(head + ph.word(it.role, row));
+        if ((j & 3) == 0) {
+          words[j >> 2] = w0;
+          words[G / 2 + (j >> 2)] = w1;
+        }
+        if (it.role == 0) {
+          uint32_t* kc = reinterpret_cast<uint32_t*>(head + ph.kcode(row));
+          kc[(j & 3) * G + (j >> 2)] = c0;
+          kc[(j & 3) * G + G / 2 + (j >> 2)] = c1;
+        } else {
+          codes[i][tok * LD + j] = c0;
+          codes[i][tok * LD + O / 2 + j] = c1;
+        }
       }
     }
     if (it.role == 0) continue;
-    // Value codes: to the order of the block, through LDS.
-    codes[tok * (D / 8) + j] = c0;
-    codes[tok * (D / 8) + D / 16 + j] = c1;
+    // Value codes to the order of the block, eight tokens by eight channels a thread.
+    // Tokens that are not the call's keep what is there.
     __syncthreads();
-    const uint8_t* cb = reinterpret_cast<const uint8_t*>(codes);
-    uint32_t* vc = reinterpret_cast<uint32_t*>(head + ph.vcode(it.row0));
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int at = threadIdx.x + i * 2 * D;  // dword of the block
-      const int n = at % (D / 16), c = at / (D / 16) % 16, m = at / D;
-      const int ch = 16 * n + c;
-      uint32_t x = 0, mask = 0;
+    const int i = threadIdx.x / (D / 2), m = threadIdx.x / O % 4, oct = threadIdx.x % O;
+    if (h0 + i < h_end) {
+      uint32_t c[8], mask = 0;
 #pragma unroll
       for (int y = 0; y < 8; ++y) {
         const int t = 16 * (y >> 2) + 4 * m + (y & 3);
-        const uint32_t nib = (cb[t * (D / 2) + ch / 2] >> (4 * (ch & 1))) & 15;
-        if (t >= it.lo && t < it.hi) {
-          x |= nib << (4 * y);
-          mask |= 15u << (4 * y);
-        }
+        const bool in = t >= it.lo && t < it.hi;
+        c[y] = in ? codes[i][t * LD + oct] : 0u;
+        mask |= in ? 15u << (4 * y) : 0u;
       }
-      if (mask == 0xffffffffu)
-        vc[at] = x;
-      else if (mask)
-        vc[at] = (vc[at] & ~mask) | x;
+      transpose_nibbles(c);
+      uint32_t* vc = reinterpret_cast<uint32_t*>(it.head + (long long)(h0 + i) * ph.bytes() + ph.vcode(it.row0)) +
+                     (m * 16 + 8 * (oct & 1)) * (D / 16) + oct / 2;
+      if (mask == 0xffffffffu) {
+#pragma unroll
+        for (int y = 0; y < 8; ++y) vc[y * (D / 16)] = c[y];
+      } else if (mask) {
+#pragma unroll
+        for (int y = 0; y < 8; ++y) vc[y * (D / 16)] = (vc[y * (D / 16)] & ~mask) | c[y];
+      }
     }
-    if (h + 1 < h_end) __syncthreads();
+    if (h0 + NH < h_end) __syncthreads();
   }
 }
 
@@ -765,9 +816,6 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 ? 2 : 1) void paged_atten
     }
   }
   __syncthreads();
-  // join the waves: their sums against the common maximum to LDS, [wave][row][channel]
-  // with 16-byte chunk x of row r at slot x ^ (r % 16), so that the 16 rows a write
-  // touches lie on distinct banks; then four channels of a row a thread
   f32x4* sums = reinterpret_cast<f32x4*>(stages);
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
@@ -777,43 +825,10 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 ? 2 : 1) void paged_atten
     for (int x = 1; x < NW; ++x) mm = fmaxf(mm, sm[x][r]);
     const float f = __builtin_amdgcn_exp2f(m[n] - mm);
 #pragma unroll
-    for (int y = 0; y < NC; ++y) sums[(wave * R + r) * (D / 4) + ((4 * y + m4) ^ col)] = o[n][y] * f;
+    for (int y = 0; y < NC; ++y) sums[sum_slot<R, D>(wave, r, 4 * y + m4)] = o[n][y] * f;
   }
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < R * D / 4 / (64 * NW); ++i) {
-    const int at = threadIdx.x + i * 64 * NW, rl = at / (D / 4), ch = at % (D / 4);
-    const int r = row0 + rl;
-    if (r >= n_rows) continue;
-    float mm = sm[0][rl], lt = 0.0f;
-    f32x4 v = {};
-#pragma unroll
-    for (int y = 1; y < NW; ++y) mm = fmaxf(mm, sm[y][rl]);
-#pragma unroll
-    for (int y = 0; y < NW; ++y) {
-      v += sums[(y * R + rl) * (D / 4) + (ch ^ (rl & 15))];
-      lt = fmaf(sl[y][rl], __builtin_amdgcn_exp2f(sm[y][rl] - mm), lt);
-    }
-    if (it.parts == 1) {
-      const int token = divide(r, s.by_g), head = it.h * s.G + r - token * s.G;
-      const long long to = out_at(a.io, s, it, token, head) + 4 * ch;
-      v *= inverse_weight(lt);
-      if (F32) {
-        *reinterpret_cast<f32x4*>(static_cast<float*>(a.io.out) + to) = v;
-      } else {
-        const u32x2 x = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.io.out) + to) = x;
-      }
-      if (ch == 0) write_lse(a.io, s, it, token, head, mm, lt);
-    } else {
-      const long long slot = part_slot(it, r);
-      *reinterpret_cast<f32x4*>(a.io.part + slot * D + 4 * ch) = v;
-      if (ch == 0) {
-        a.io.ml[2 * slot] = mm;
-        a.io.ml[2 * slot + 1] = lt;
-      }
-    }
-  }
+  write_joined<R, D, NW, F32>(a.io, s, it, row0, sums, sm, sl);
 }
 
 template <int D>
@@ -834,6 +849,14 @@ hipError_t launch(int dtype, const AttnShape& sh, const PagedAttnArgs& a, hipStr
 // block are formed once.
 int heads_per_workgroup(const PagedRowsArgs& a) {
   return (int64_t)a.n_blocks * a.n_layers * a.H >= 4096 ? a.H : 1;
+}
+
+template <class T, int D>
+void append(dim3 grid, const PagedRowsArgs& a, int hpw, hipStream_t s) {
+  if (a.rotate)
+    paged_append_kernel<T, D, true><<<grid, 2 * D, 0, s>>>(a, hpw);
+  else
+    paged_append_kernel<T, D, false><<<grid, 2 * D, 0, s>>>(a, hpw);
 }
 
 }  // namespace
@@ -858,13 +881,10 @@ hipError_t launch_paged_append(int dtype, int d_h, const PagedRowsArgs& a0, hipS
   const int hpw = heads_per_workgroup(a);
   a.by_groups = make_divide((a.H + hpw - 1) / hpw);
   const dim3 grid((unsigned)(a.n_blocks * ((a.H + hpw - 1) / hpw)), 2, (unsigned)a.n_layers);
-  if (dtype == HF_BF16) {
-    if (d_h == 128) paged_append_kernel<uint16_t, 128><<<grid, 256, 0, s>>>(a, hpw);
-    else paged_append_kernel<uint16_t, 64><<<grid, 128, 0, s>>>(a, hpw);
-  } else {
-    if (d_h == 128) paged_append_kernel<float, 128><<<grid, 256, 0, s>>>(a, hpw);
-    else paged_append_kernel<float, 64><<<grid, 128, 0, s>>>(a, hpw);
-  }
+  if (dtype == HF_BF16)
+    d_h == 128 ? append<uint16_t, 128>(grid, a, hpw, s) : append<uint16_t, 64>(grid, a, hpw, s);
+  else
+    d_h == 128 ? append<float, 128>(grid, a, hpw, s) : append<float, 64>(grid, a, hpw, s);
   return hipGetLastError();
 }
 
