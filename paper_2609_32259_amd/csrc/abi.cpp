@@ -810,15 +810,23 @@ int32_t plan_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len, i
   if (total > INT32_MAX || max_rows > INT32_MAX - 1024 || total * H_q > ((int64_t)1 << 40))
     return fail(HF_ERR_SHAPE, "too many query rows");
   sh = paged ? hf::paged_shape(dtype, d_h, max_rows) : hf::prompt_shape(dtype, d_h, max_rows);
-  // The cut with the least rounds of workgroups times the longest part, where the
-  // uncut items are not many rounds anyway (kStart keys: a part's fixed cost).
-  constexpr int64_t kStart = 192;
-  int64_t longest = 1, uncut = 0;
+  // The cut with the least estimated time, where the uncut items are not many rounds of
+  // workgroups anyway: the rounds times a part's time, or, where the items differ in
+  // length as those of causal prompts do, the whole work over the workgroups; then the
+  // join, which writes and reads every part.
+  constexpr int64_t kStart = 192;   // a part's fixed cost, in keys
+  constexpr int64_t kJoin = 5000;   // ns of a second launch
+  constexpr int64_t kBytesNs = 3000;  // that the join moves in a ns
+  int64_t longest = 1, uncut = 0, rows = 0, seen = 0;
   int64_t of_seq[HF_MAX_BATCH];
+  bool triangular = causal != 0;
   for (int b = 0; b < B; ++b) {
     of_seq[b] = ((int64_t)q_len[b] * G + sh.rows - 1) / sh.rows * H;
     uncut += of_seq[b];
+    rows += (int64_t)q_len[b] * H_q;
     if (q_len[b] > 0) longest = std::max(longest, (int64_t)kv_len[b]);
+    if (2 * (int64_t)q_len[b] < kv_len[b]) triangular = false;
+    seen += of_seq[b] * (kv_len[b] / 2);
   }
   int64_t chunk = longest;
   if (uncut > 0 && uncut < 4 * (int64_t)sh.wg_target) {
@@ -829,8 +837,10 @@ int32_t plan_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len, i
       int64_t n = 0;
       for (int b = 0; b < B; ++b)
         n += of_seq[b] * std::max<uint32_t>(((uint32_t)kv_len[b] + (uint32_t)c - 1) / (uint32_t)c, 1);
-      const int64_t cost = (n + sh.wg_target - 1) / sh.wg_target * (std::min(c, longest) + kStart) +
-                           (k > 1 ? sh.join_keys : 0);
+      const int64_t part = std::min(c, longest) + kStart;
+      const int64_t keys = triangular ? std::max(part, (seen + n * kStart) / sh.wg_target)
+                                      : (n + sh.wg_target - 1) / sh.wg_target * part;
+      const int64_t cost = keys * sh.ns_key + (k > 1 ? kJoin + rows * k * d_h * 8 / kBytesNs : 0);
       if (cost < best) {
         best = cost;
         chunk = c;
@@ -849,8 +859,8 @@ int32_t plan_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len, i
   int64_t items = 0, row = 0, key = 0, split = 0;
   slots = 0;
   for (int b = 0; b < B; ++b) {
-    const int64_t rows = (int64_t)q_len[b] * G;
-    const int64_t tiles = (rows + sh.rows - 1) / sh.rows;
+    const int64_t mine = (int64_t)q_len[b] * G;
+    const int64_t tiles = (mine + sh.rows - 1) / sh.rows;
     int64_t parts = std::max<int64_t>((kv_len[b] + (int64_t)s.chunk - 1) / s.chunk, 1);
     s.q[b] = {(int32_t)items, (int32_t)split, q_len[b], kv_len[b], (int32_t)row, (int32_t)key,
               (int32_t)parts, (int32_t)slots};
@@ -858,13 +868,14 @@ int32_t plan_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len, i
     row += q_len[b];
     key += kv_len[b];
     if (parts > 1) {
-      split += rows * H;
-      slots += rows * H * parts;
+      split += mine * H;
+      slots += mine * H * parts;
     }
     if (items * H > INT32_MAX || split > INT32_MAX || slots > INT32_MAX)
       return fail(HF_ERR_SHAPE, "too many work items");
     if (key > INT32_MAX) return fail(HF_ERR_SHAPE, "too many keys");
   }
+  if (sh.resident > 1 && triangular && B == 1) s.snake = std::max(sh.wg_target / H, 1);
   s.n_items = (int32_t)items;
   s.n_split = (int32_t)split;
   return HF_OK;
@@ -1036,10 +1047,14 @@ size_t hf_attention_workspace_bytes(int32_t B, const int32_t* q_len, const int32
   if (dtype != HF_F32 && dtype != HF_BF16) return 0;
   hf::AttnShape sh;
   hf::AttnSeqs s;
-  int64_t slots = 0;
-  if (plan_attention(B, q_len, kv_len, H_q, H, dtype, d_h, paged != 0, 0, sh, s, slots)) return 0;
+  size_t most = 0;
+  for (int causal = 0; causal < 2; ++causal) {  // (the cut depends on it)
+    int64_t slots = 0;
+    if (plan_attention(B, q_len, kv_len, H_q, H, dtype, d_h, paged != 0, causal, sh, s, slots)) return 0;
+    most = std::max(most, part_bytes(slots, d_h));
+  }
   ok();
-  return part_bytes(slots, d_h);
+  return most;
 }
 
 int32_t hf_prompt_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len,

@@ -25,6 +25,8 @@
 // as well, joined by attention_join_kernel.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "hf_attn.h"
 
 namespace hf {
@@ -37,10 +39,10 @@ namespace {
 // bf16 on v_mfma_f32_32x32x16_bf16: lane l is row l % 32; with h = l / 32, result
 // register i of a 32-key block is key 8 (i / 4) + 4 h + i % 4, and of a 32-channel
 // block the channel of that number.
-template <int D_, int KT_, int RB_>
+template <int D_, int KT_>
 struct Bf16Tile {
   static constexpr int D = D_, KT = KT_;
-  static constexpr int RB = RB_, RW = 32;        // blocks of query rows a wave, rows a block
+  static constexpr int RW = 32;
   static constexpr int NS = KT / 2, NO = D / 2;  // score and output registers
   static constexpr int ROWB = D * 2;             // bytes of a row
   typedef uint16_t T;
@@ -66,30 +68,26 @@ struct Bf16Tile {
       q.f[c] = *reinterpret_cast<const bf16x8*>(row + 16 * c + 8 * (lane >> 5));
   }
 
-  FI static void scores(const Q (&q)[RB], const unsigned char* sk, int lane, float (&s)[RB][NS]) {
+  FI static void scores(const Q& q, const unsigned char* sk, int lane, float (&s)[NS]) {
     const int r = lane & 31;
 #pragma unroll
     for (int kb = 0; kb < KT / 32; ++kb) {
-      f32x16 acc[RB] = {};
+      f32x16 acc = {};
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) {
         const bf16x8 a = *reinterpret_cast<const bf16x8*>(
             sk + kb * 32 * ROWB + r * ROWB + slot_k(r, 2 * c + (lane >> 5)) * 16);
-#pragma unroll
-        for (int x = 0; x < RB; ++x)
-          acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[x].f[c], acc[x], 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q.f[c], acc, 0, 0, 0);
       }
 #pragma unroll
-      for (int x = 0; x < RB; ++x)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[x][16 * kb + i] = acc[x][i];
+      for (int i = 0; i < 16; ++i) s[16 * kb + i] = acc[i];
     }
   }
 
   typedef f32x16 O[D / 32];
   // O += V^T P^T.  CLEAN: values that are not finite enter as 0.
   template <bool CLEAN>
-  FI static void values(O (&o)[RB], const unsigned char* sv, int lane, const float (&p)[RB][NS]) {
+  FI static void values(O& o, const unsigned char* sv, int lane, const float (&p)[NS]) {
     // the transposing read gives lane i of 16 the values of 4 rows at channel i; its
     // lane i names row i / 4 of them and 8 bytes there
     const int h = lane >> 5, gb = (lane >> 4) & 1, i = lane & 15;
@@ -99,11 +97,9 @@ struct Bf16Tile {
       union {
         bf16x8 v;
         uint32_t u[4];
-      } b[RB];
+      } b;
 #pragma unroll
-      for (int x = 0; x < RB; ++x)
-#pragma unroll
-        for (int y = 0; y < 4; ++y) b[x].u[y] = pack_bf16(p[x][8 * c + 2 * y], p[x][8 * c + 2 * y + 1]);
+      for (int y = 0; y < 4; ++y) b.u[y] = pack_bf16(p[8 * c + 2 * y], p[8 * c + 2 * y + 1]);
 #pragma unroll
       for (int n = 0; n < D / 32; ++n) {
         const unsigned char* at = sv + (16 * c + r) * ROWB + slot_v(r, 4 * n + 2 * gb) * 16 + (i & 3) * 8;
@@ -121,9 +117,7 @@ struct Bf16Tile {
             if ((a.u[y] & 0x7f800000u) == 0x7f800000u) a.u[y] &= 0xffffu;
           }
         }
-#pragma unroll
-        for (int x = 0; x < RB; ++x)
-          o[x][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b[x].v, o[x][n], 0, 0, 0);
+        o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, o[n], 0, 0, 0);
       }
     }
   }
@@ -145,10 +139,10 @@ struct Bf16Tile {
 // of the first product takes channel 16 u + 4 m + j, so that a lane's operands are
 // 16-byte loads; step i of the second takes key 4 m + i, so that the scores'
 // registers are its operands as they are.
-template <int D_, int KT_, int RB_>
+template <int D_, int KT_>
 struct F32Tile {
   static constexpr int D = D_, KT = KT_;
-  static constexpr int RB = RB_, RW = 16;
+  static constexpr int RW = 16;
   static constexpr int NS = KT / 4, NO = D / 4;
   static constexpr int ROWB = D * 4;
   typedef float T;
@@ -171,31 +165,26 @@ struct F32Tile {
       q.f[u] = *reinterpret_cast<const f32x4*>(row + 16 * u + 4 * (lane >> 4));
   }
 
-  FI static void scores(const Q (&q)[RB], const unsigned char* sk, int lane, float (&s)[RB][NS]) {
+  FI static void scores(const Q& q, const unsigned char* sk, int lane, float (&s)[NS]) {
     const int r = lane & 15;
 #pragma unroll
     for (int kb = 0; kb < KT / 16; ++kb) {
-      f32x4 acc[RB] = {};
+      f32x4 acc = {};
 #pragma unroll
       for (int u = 0; u < D / 16; ++u) {
         const f32x4 a = *reinterpret_cast<const f32x4*>(
             sk + (kb * 16 + r) * ROWB + slot_k(r, 4 * u + (lane >> 4)) * 16);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int x = 0; x < RB; ++x)
-            acc[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], q[x].f[u][j], acc[x], 0, 0, 0);
+        for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], q.f[u][j], acc, 0, 0, 0);
       }
 #pragma unroll
-      for (int x = 0; x < RB; ++x)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[x][4 * kb + i] = acc[x][i];
+      for (int i = 0; i < 4; ++i) s[4 * kb + i] = acc[i];
     }
   }
 
   typedef f32x4 O[D / 16];
   template <bool CLEAN>
-  FI static void values(O (&o)[RB], const unsigned char* sv, int lane, const float (&p)[RB][NS]) {
+  FI static void values(O& o, const unsigned char* sv, int lane, const float (&p)[NS]) {
     const int m = lane >> 4, c = lane & 15;
 #pragma unroll
     for (int k = 0; k < NS; ++k) {
@@ -204,9 +193,7 @@ struct F32Tile {
       for (int n = 0; n < D / 16; ++n) {
         float a = *reinterpret_cast<const float*>(sv + r * ROWB + slot_v(r, 4 * n + (c >> 2)) * 16 + (c & 3) * 4);
         if (CLEAN) a = finite_bits(a) ? a : 0.0f;
-#pragma unroll
-        for (int x = 0; x < RB; ++x)
-          o[x][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, p[x][k], o[x][n], 0, 0, 0);
+        o[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, p[k], o[n], 0, 0, 0);
       }
     }
   }
@@ -227,10 +214,10 @@ struct F32Tile {
 // ---------------------------------------------------------------------------
 template <class P>
 struct Rows {
-  typename P::Q q[P::RB];
-  typename P::O o[P::RB];
-  float m[P::RB], l[P::RB];  // each row's maximum; this lane's share of its weight
-  int last[P::RB];           // the last key it sees
+  typename P::Q q;
+  typename P::O o;
+  float m, l;  // the row's maximum; this lane's share of its weight
+  int last;    // the last key it sees
 };
 
 // The weights of a tile's scores and their product with its values.  MASK: some row
@@ -241,51 +228,42 @@ struct Rows {
 // as 0 and is added to the rows that see its key.  (In other tiles all rows see all
 // keys, and the product does what it should.)
 template <class P, bool MASK>
-FI void finish(Rows<P>& w, float (&s)[P::RB][P::NS], const unsigned char* sv, int lane, float c,
-               int t0, bool careful) {
+FI void finish(Rows<P>& w, float (&s)[P::NS], const unsigned char* sv, int lane, float c, int t0,
+               bool careful) {
+  if (MASK) {
 #pragma unroll
-  for (int x = 0; x < P::RB; ++x) {
-    if (MASK) {
+    for (int i = 0; i < P::NS; ++i)
+      if (t0 + P::key(lane, i) > w.last) s[i] = -INFINITY;
+  }
+  float mx = s[0];
 #pragma unroll
-      for (int i = 0; i < P::NS; ++i)
-        if (t0 + P::key(lane, i) > w.last[x]) s[x][i] = -INFINITY;
-    }
-    float mx = s[x][0];
+  for (int i = 1; i < P::NS; ++i) mx = fmaxf(mx, s[i]);
+  mx = P::row_max(mx) * c;
+  if (__any(mx > w.m + kRaise)) {
+    const float m = mx > w.m + kRaise ? mx : w.m;  // (each row by its own scores alone)
+    const float f = __builtin_amdgcn_exp2f(w.m - m);
+    w.m = m;
+    w.l *= f;
 #pragma unroll
-    for (int i = 1; i < P::NS; ++i) mx = fmaxf(mx, s[x][i]);
-    mx = P::row_max(mx) * c;
-    if (__any(mx > w.m[x] + kRaise)) {
-      const float m = mx > w.m[x] + kRaise ? mx : w.m[x];  // (each row by its own scores alone)
-      const float f = __builtin_amdgcn_exp2f(w.m[x] - m);
-      w.m[x] = m;
-      w.l[x] *= f;
-#pragma unroll
-      for (int i = 0; i < P::NO; ++i) P::set(w.o[x], i, P::get(w.o[x], i) * f);
-    }
+    for (int i = 0; i < P::NO; ++i) P::set(w.o, i, P::get(w.o, i) * f);
   }
 #pragma unroll
-  for (int x = 0; x < P::RB; ++x) {
-#pragma unroll
-    for (int i = 0; i < P::NS; ++i) {
-      s[x][i] = __builtin_amdgcn_exp2f(fmaf(s[x][i], c, -w.m[x]));
-      w.l[x] += s[x][i];
-    }
+  for (int i = 0; i < P::NS; ++i) {
+    s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -w.m));
+    w.l += s[i];
   }
   if (!MASK || !careful) {
     P::template values<false>(w.o, sv, lane, s);
     return;
   }
   P::template values<true>(w.o, sv, lane, s);
+  for (int r = 0; r < P::KT && t0 + r <= w.last; ++r) {
+    int at = lane;  // (opaque: the addresses below are formed here, not kept across the kernel)
+    asm volatile("" : "+v"(at));
 #pragma unroll
-  for (int x = 0; x < P::RB; ++x) {
-    for (int r = 0; r < P::KT && t0 + r <= w.last[x]; ++r) {
-      int at = lane;  // (opaque: the addresses below are formed here, not kept across the kernel)
-      asm volatile("" : "+v"(at));
-#pragma unroll
-      for (int i = 0; i < P::NO; ++i) {
-        const float v = P::value_at(sv, r, P::channel(at, i));
-        if (!finite_bits(v)) P::set(w.o[x], i, P::get(w.o[x], i) + v);
-      }
+    for (int i = 0; i < P::NO; ++i) {
+      const float v = P::value_at(sv, r, P::channel(at, i));
+      if (!finite_bits(v)) P::set(w.o, i, P::get(w.o, i) + v);
     }
   }
 }
@@ -294,9 +272,7 @@ template <class P>
 FI bool not_finite(const Rows<P>& w) {
   bool bad = false;
 #pragma unroll
-  for (int x = 0; x < P::RB; ++x)
-#pragma unroll
-    for (int i = 0; i < P::NO; ++i) bad |= !finite_bits(P::get(w.o[x], i));
+  for (int i = 0; i < P::NO; ++i) bad |= !finite_bits(P::get(w.o, i));
   return bad;
 }
 
@@ -376,38 +352,32 @@ FI void write_row(const AttnIO& io, const AttnSeqs& s, const AttnItem& it, int r
   }
 }
 
-// Rows r, r + RW, .. (the last one for rows past it, which are not written).
+// Row r (the last one for rows past it, which are not written).
 template <class P>
-FI void load_rows(Rows<P>& w, const AttnArgs& a, const AttnItem& it, int r0, int lane) {
+FI void load_row(Rows<P>& w, const AttnArgs& a, const AttnItem& it, int r, int lane) {
   typedef typename P::T T;
   const AttnSeqs& s = a.s;
-  const T* q = static_cast<const T*>(a.io.q) + seq_at(it.b, it.row0, a.io.q_sb, a.io.q_st);
-#pragma unroll
-  for (int x = 0; x < P::RB; ++x) {
-    const int r = min(r0 + x * P::RW, it.rows - 1);
-    const int token = divide(r, s.by_g), head = it.h * s.G + r - token * s.G;
-    P::load_q(w.q[x], q + token * a.io.q_st + head * a.io.q_sh, lane);
-    w.last[x] = last_key(s, it, token);
-  }
+  r = min(r, it.rows - 1);
+  const int token = divide(r, s.by_g), head = it.h * s.G + r - token * s.G;
+  P::load_q(w.q, static_cast<const T*>(a.io.q) + seq_at(it.b, it.row0, a.io.q_sb, a.io.q_st) +
+                     token * a.io.q_st + head * a.io.q_sh, lane);
+  w.last = last_key(s, it, token);
 }
 template <class P>
-FI void clear_rows(Rows<P>& w) {
+FI void clear_row(Rows<P>& w) {
 #pragma unroll
-  for (int x = 0; x < P::RB; ++x) {
-#pragma unroll
-    for (int i = 0; i < P::NO; ++i) P::set(w.o[x], i, 0.0f);
-    w.m[x] = kNoMax;
-    w.l[x] = 0.0f;
-  }
+  for (int i = 0; i < P::NO; ++i) P::set(w.o, i, 0.0f);
+  w.m = kNoMax;
+  w.l = 0.0f;
 }
 
-// By rows: NW waves, each with RB blocks of RW rows of the tile, all against the same
-// keys.  A wave computes the scores of the next tile before it finishes this one's, so
+// By rows: NW waves, each with RW rows of the tile, all against the same keys.  A wave
+// computes the scores of the next tile before it finishes this one's, so
 // that matrix instructions and the softmax's are there to be issued side by side.
 template <class P, int NW>
 __global__ __launch_bounds__(NW * 64) void attention_rows_kernel(const AttnArgs a) {
   typedef typename P::T T;
-  constexpr int KT = P::KT, WR = P::RB * P::RW;  // keys a tile, rows a wave
+  constexpr int KT = P::KT, WR = P::RW;  // keys a tile, rows a wave
   __shared__ __attribute__((aligned(1024))) unsigned char k0[KT * P::ROWB];
   __shared__ __attribute__((aligned(1024))) unsigned char v0[KT * P::ROWB];
   __shared__ __attribute__((aligned(1024))) unsigned char k1[KT * P::ROWB];
@@ -422,7 +392,7 @@ __global__ __launch_bounds__(NW * 64) void attention_rows_kernel(const AttnArgs 
   const int t = it.t, n_rows = it.rows;
   const int row0 = it.tile * NW * WR, my0 = row0 + wave * WR;
   Rows<P> w;
-  load_rows<P>(w, a, it, my0 + P::row(lane), lane);
+  load_row<P>(w, a, it, my0 + P::row(lane), lane);
 
   // keys of this part that some row of the workgroup sees, and that all of them see
   const int wg_last = last_key(s, it, divide(min(row0 + NW * WR - 1, n_rows - 1), s.by_g));
@@ -451,7 +421,7 @@ __global__ __launch_bounds__(NW * 64) void attention_rows_kernel(const AttnArgs 
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  typedef float Scores[P::RB][P::NS];
+  typedef float Scores[P::NS];
   // Tile t0, whose scores are in s, with its values in sv; the next tile's keys in nk.
   auto step = [&](int t0, Scores& s0, Scores& s1, unsigned char* sk, unsigned char* sv,
                   unsigned char* nk, unsigned char* nv) {
@@ -472,7 +442,7 @@ __global__ __launch_bounds__(NW * 64) void attention_rows_kernel(const AttnArgs 
     if (t0 + KT <= wave_last && t0 + KT < hi) P::scores(w.q, nk, lane, s);
   };
   for (;;) {
-    clear_rows<P>(w);
+    clear_row<P>(w);
     if (lo < hi) {
       Scores s0, s1;
       get_k(lo, k0);
@@ -494,19 +464,15 @@ __global__ __launch_bounds__(NW * 64) void attention_rows_kernel(const AttnArgs 
     if (careful || !__syncthreads_or(not_finite(w))) break;
     careful = true;
   }
-#pragma unroll
-  for (int x = 0; x < P::RB; ++x) {
-    const int r = my0 + x * P::RW + P::row(lane);
-    const float l = P::row_sum(w.l[x]);
-    if (r < n_rows) write_row<P>(a.io, s, it, r, w.m[x], l, w.o[x], lane);
-  }
+  const int r = my0 + P::row(lane);
+  const float l = P::row_sum(w.l);
+  if (r < n_rows) write_row<P>(a.io, s, it, r, w.m, l, w.o, lane);
 }
 
 // By keys: one block of RW rows, the tiles of keys dealt to NW waves.
 template <class P, int NW>
 __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs a) {
   typedef typename P::T T;
-  static_assert(P::RB == 1, "one block of rows");
   constexpr int TB = P::KT * P::ROWB;  // bytes of a tile of keys, or of values
   __shared__ __attribute__((aligned(1024))) unsigned char s0[NW * 2 * TB];
   __shared__ __attribute__((aligned(1024))) unsigned char s1[NW * 2 * TB];
@@ -519,7 +485,7 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
   const int t = it.t, n_rows = it.rows;
   const int row0 = it.tile * P::RW;
   Rows<P> w;
-  load_rows<P>(w, a, it, row0 + P::row(lane), lane);
+  load_row<P>(w, a, it, row0 + P::row(lane), lane);
   const int first = last_key(s, it, divide(min(row0, n_rows - 1), s.by_g));
   const int last = last_key(s, it, divide(min(row0 + P::RW - 1, n_rows - 1), s.by_g));
   const int lo = it.part * s.chunk + wave * P::KT;
@@ -546,7 +512,7 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
     } else {
       __builtin_amdgcn_s_waitcnt(wait_vm_only(0));
     }
-    float s[1][P::NS];
+    float s[P::NS];
     P::scores(w.q, st, lane, s);
     if (t0 + P::KT - 1 > first)
       finish<P, true>(w, s, st + TB, lane, c, t0, careful);
@@ -554,7 +520,7 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
       finish<P, false>(w, s, st + TB, lane, c, t0, false);
   };
   for (;;) {
-    clear_rows<P>(w);
+    clear_row<P>(w);
     if (lo < hi) {
       get(lo, w0);
       for (int t0 = lo; t0 < hi; t0 += 2 * NW * P::KT) {
@@ -567,21 +533,21 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
   }
 
   const int rl = P::row(lane);
-  const float l = P::row_sum(w.l[0]);
+  const float l = P::row_sum(w.l);
   if (lane < P::RW) {
-    sm[wave][rl] = w.m[0];
+    sm[wave][rl] = w.m;
     sl[wave][rl] = l;
   }
   __syncthreads();
   float m = sm[0][rl];
 #pragma unroll
   for (int x = 1; x < NW; ++x) m = fmaxf(m, sm[x][rl]);
-  const float f = __builtin_amdgcn_exp2f(w.m[0] - m);
+  const float f = __builtin_amdgcn_exp2f(w.m - m);
   f32x4* sums = reinterpret_cast<f32x4*>(s0);
   static_assert(NW * P::RW * P::D * 4 <= NW * 2 * TB, "joining buffer");
 #pragma unroll
   for (int i = 0; i < P::NO; i += 4) {
-    const f32x4 v = {P::get(w.o[0], i), P::get(w.o[0], i + 1), P::get(w.o[0], i + 2), P::get(w.o[0], i + 3)};
+    const f32x4 v = {P::get(w.o, i), P::get(w.o, i + 1), P::get(w.o, i + 2), P::get(w.o, i + 3)};
     sums[sum_slot<P::RW, P::D>(wave, rl, P::channel(lane, i) / 4)] = v * f;
   }
   __syncthreads();
@@ -590,64 +556,64 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
 
 // ---------------------------------------------------------------------------
 // The parts of split rows: out = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p.
-// A workgroup a row: D / 4 threads of four channels each for every eighth
-// (sixteenth) part, so that a row's parts are loaded at the same time; one wave a
-// row, part after part, took 19 us for 57 parts, this takes 5.
+// A row has D / 4 threads of four channels for every SL-th part, so that its parts are
+// loaded at the same time: one wave a row, part after part, took 19 us for 57 parts of
+// 40 rows, this takes 4.5.  With few parts a workgroup takes several rows.
 // ---------------------------------------------------------------------------
 struct JoinArgs {
   AttnIO io;
   AttnSeqs s;
 };
 
-template <bool F32, int D>
+template <bool F32, int D, int SL>
 __global__ __launch_bounds__(256) void attention_join_kernel(const JoinArgs a) {
-  constexpr int TC = D / 4, SL = 256 / TC;
-  __shared__ f32x4 so[SL][TC];
-  __shared__ float sm[4], sl[SL];
+  constexpr int TC = D / 4, NR = 256 / (TC * SL);
+  __shared__ f32x4 so[NR][SL][TC];
+  __shared__ float sm[NR][SL], sl[NR][SL];
   const AttnSeqs& s = a.s;
-  int i = blockIdx.x;
+  const int c = threadIdx.x % TC, q = threadIdx.x / TC % SL, rr = threadIdx.x / (TC * SL);
+  int i = blockIdx.x * NR + rr;
+  const bool on = i < s.n_split;
+  static_assert(TC * SL >= 64, "a wave has one row");
   AttnItem it;
-  it.b = find_seq(s.q, &AttnSeq::split0, s.B, i);
+  it.b = find_seq(s.q, &AttnSeq::split0, s.B, __builtin_amdgcn_readfirstlane(i));
   const AttnSeq sq = s.q[it.b];
   it.row0 = sq.row0;
   i -= sq.split0;
-  const int n_rows = sq.n * s.G, parts = sq.parts;
-  const int h = i / n_rows, r = i - h * n_rows;
+  const int parts = on ? sq.parts : 0;
   const long long slot = sq.part0 + (long long)i * parts;
   const float* ml = a.io.ml + 2 * slot;
-  float m = kNoMax;
-  for (int p = threadIdx.x; p < parts; p += 256) m = fmaxf(m, ml[2 * p]);
-#pragma unroll
-  for (int x = 1; x < 16; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
-  m = max_xor32(max_xor16(m));
-  if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
-  const int c = threadIdx.x % TC, q = threadIdx.x / TC;
-  float l = 0.0f;
-  f32x4 o = {};
   const float* po = a.io.part + slot * D + 4 * c;
+  float m = kNoMax, l = 0.0f;
+  f32x4 o = {};
+#pragma unroll 4
+  for (int p = q; p < parts; p += SL) m = fmaxf(m, ml[2 * p]);
 #pragma unroll 4
   for (int p = q; p < parts; p += SL) {
     const float f = __builtin_amdgcn_exp2f(ml[2 * p] - m);
     const f32x4 v = *reinterpret_cast<const f32x4*>(po + (long long)p * D);
     l = fmaf(ml[2 * p + 1], f, l);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = fmaf(v[e], f, o[e]);
+    o += v * f;
   }
-  so[q][c] = o;
-  if (c == 0) sl[q] = l;
+  so[rr][q][c] = o;
+  if (c == 0) {
+    sm[rr][q] = m;
+    sl[rr][q] = l;
+  }
   __syncthreads();
-  if (q != 0) return;
-  const int used = min(parts, SL);
-  for (int x = 1; x < used; ++x) {
-    o += so[x][c];
-    l += sl[x];
+  if (q != 0 || !on) return;
+  for (int x = 1; x < SL; ++x) m = fmaxf(m, sm[rr][x]);
+  o = f32x4{};
+  l = 0.0f;
+  for (int x = 0; x < SL; ++x) {
+    const float f = __builtin_amdgcn_exp2f(sm[rr][x] - m);
+    o += so[rr][x][c] * f;
+    l = fmaf(sl[rr][x], f, l);
   }
+  const int n_rows = sq.n * s.G, h = i / n_rows, r = i - h * n_rows;
   const int token = divide(r, s.by_g), head = h * s.G + r - token * s.G;
-  const float inv = inverse_weight(l);
   const long long at = out_at(a.io, s, it, token, head) + 4 * c;
-  o *= inv;
+  o *= inverse_weight(l);
   if (F32) {
     *reinterpret_cast<f32x4*>(static_cast<float*>(a.io.out) + at) = o;
   } else {
@@ -657,24 +623,39 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const JoinArgs a) {
   if (c == 0) write_lse(a.io, s, it, token, head, m, l);
 }
 
-constexpr int kRowWaves = 8, kRowBlocks = 1, kRowWavesF32 = 4, kKeyWaves = 4;
+constexpr int kRowWaves = 8, kRowWavesF32 = 4, kKeyWaves = 4;
 
 template <int D>
 hipError_t launch(int dtype, const AttnShape& sh, const AttnArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)(a.s.n_items * a.s.H));
   if (dtype == HF_BF16) {
     if (sh.by_keys)
-      attention_keys_kernel<Bf16Tile<D, 32, 1>, kKeyWaves><<<grid, kKeyWaves * 64, 0, st>>>(a);
+      attention_keys_kernel<Bf16Tile<D, 32>, kKeyWaves><<<grid, kKeyWaves * 64, 0, st>>>(a);
     else
-      attention_rows_kernel<Bf16Tile<D, 64, kRowBlocks>, kRowWaves><<<grid, kRowWaves * 64, 0, st>>>(a);
+      attention_rows_kernel<Bf16Tile<D, 64>, kRowWaves><<<grid, kRowWaves * 64, 0, st>>>(a);
   } else {
     if (sh.by_keys)
-      attention_keys_kernel<F32Tile<D, D == 128 ? 16 : 32, 1>, kKeyWaves>
+      attention_keys_kernel<F32Tile<D, D == 128 ? 16 : 32>, kKeyWaves>
           <<<grid, kKeyWaves * 64, 0, st>>>(a);
     else
-      attention_rows_kernel<F32Tile<D, 32, 1>, kRowWavesF32><<<grid, kRowWavesF32 * 64, 0, st>>>(a);
+      attention_rows_kernel<F32Tile<D, 32>, kRowWavesF32><<<grid, kRowWavesF32 * 64, 0, st>>>(a);
   }
   return hipGetLastError();
+}
+
+template <bool F32, int D, int SL>
+void join_by(const JoinArgs& a, hipStream_t st) {
+  constexpr int NR = 256 / (D / 4 * SL);
+  attention_join_kernel<F32, D, SL><<<(unsigned)((a.s.n_split + NR - 1) / NR), 256, 0, st>>>(a);
+}
+template <bool F32, int D>
+void join(const JoinArgs& a, int most_parts, hipStream_t st) {
+  if (most_parts > 4)
+    join_by<F32, D, 8>(a, st);
+  else if (D == 128 && most_parts > 2)
+    join_by<F32, D, 4>(a, st);
+  else
+    join_by<F32, D, 256 / D>(a, st);
 }
 
 }  // namespace
@@ -683,10 +664,12 @@ AttnShape prompt_shape(int dtype, int d_h, int64_t max_rows) {
   AttnShape sh;
   const int rw = dtype == HF_BF16 ? 32 : 16;
   sh.by_keys = max_rows <= rw;
-  sh.rows = sh.by_keys ? rw : rw * (dtype == HF_BF16 ? kRowWaves * kRowBlocks : kRowWavesF32);
+  sh.rows = sh.by_keys ? rw : rw * (dtype == HF_BF16 ? kRowWaves : kRowWavesF32);
   sh.wg_target = 256;
   sh.step = sh.by_keys ? 32 * kKeyWaves : 64;
-  sh.join_keys = sh.by_keys ? 512 : 256;
+  sh.resident = sh.by_keys || dtype == HF_BF16 ? 1 : 3;
+  // (measured: 8192 keys of 8 -> 4 -> 1 heads, one workgroup a CU)
+  sh.ns_key = sh.by_keys ? (d_h == 128 ? 20 : 12) : dtype == HF_BF16 ? (d_h == 128 ? 33 : 24) : d_h == 128 ? 56 : 28;
   return sh;
 }
 
@@ -698,14 +681,12 @@ hipError_t launch_prompt_attention(int dtype, int d_h, const AttnShape& sh, cons
 hipError_t launch_attention_join(int dtype, int d_h, const AttnIO& io, const AttnSeqs& s,
                                  hipStream_t st) {
   JoinArgs a{io, s};
-  const dim3 grid((unsigned)s.n_split);
-  if (dtype == HF_F32) {
-    if (d_h == 128) attention_join_kernel<true, 128><<<grid, 256, 0, st>>>(a);
-    else attention_join_kernel<true, 64><<<grid, 256, 0, st>>>(a);
-  } else {
-    if (d_h == 128) attention_join_kernel<false, 128><<<grid, 256, 0, st>>>(a);
-    else attention_join_kernel<false, 64><<<grid, 256, 0, st>>>(a);
-  }
+  int most = 0;
+  for (int b = 0; b < s.B; ++b) most = std::max(most, s.q[b].parts);
+  if (dtype == HF_F32)
+    d_h == 128 ? join<true, 128>(a, most, st) : join<true, 64>(a, most, st);
+  else
+    d_h == 128 ? join<false, 128>(a, most, st) : join<false, 64>(a, most, st);
   return hipGetLastError();
 }
 

@@ -122,6 +122,12 @@ FI AttnItem attn_item(const AttnSeqs& s, int tile_rows) {
   const int wg = blockIdx.x;
   int i = divide(wg, s.by_h);
   it.h = wg - i * s.H;
+  // Where a CU runs several workgroups at once, which it gets in rounds of one a CU,
+  // every other round turns, so that long tiles are joined by short ones.
+  if (s.snake) {
+    const int r = i / s.snake;
+    if (r & 1) i = min(s.n_items, (r + 1) * s.snake) - 1 - (i - r * s.snake);
+  }
   it.b = find_seq(s.q, &AttnSeq::item0, s.B, i);
   const AttnSeq q = s.q[it.b];
   it.n = q.n;

@@ -197,6 +197,7 @@ struct AttnSeqs {
   int32_t chunk;                       // keys of one part (a multiple of every kernel's step)
   int32_t causal;
   int32_t n_items, n_split;
+  int32_t snake;                       // items a round whose order turns every other round, or 0
   Divide by_g, by_h;
   alignas(32) AttnSeq q[HF_MAX_BATCH];
 };
@@ -233,8 +234,9 @@ struct AttnShape {
   int32_t rows;       // of a workgroup's tile
   int32_t by_keys;
   int32_t wg_target;  // workgroups that fill the chip
+  int32_t resident;   // workgroups of several tiles' lengths that a CU runs at once
   int32_t step;       // keys that parts are cut in multiples of
-  int32_t join_keys;  // the joining launch's time, in keys of a part
+  int32_t ns_key;     // time of a workgroup for each key of its part, when the chip is full
 };
 AttnShape prompt_shape(int dtype, int d_h, int64_t max_rows);
 AttnShape paged_shape(int dtype, int d_h, int64_t max_rows);

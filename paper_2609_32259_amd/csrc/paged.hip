@@ -533,7 +533,7 @@ struct Flag {
 // sum(q_g) and what takes the operands' 16 out again, -16 sum(q_g), each split into
 // three bf16 terms (24 bits) over three of its four octets.
 template <int D, int NT, bool F32>
-__global__ __launch_bounds__(kPagedWaves * 64, NT == 1 ? 2 : 1) void paged_attention_kernel(
+__global__ __launch_bounds__(kPagedWaves * 64, NT == 1 || D == 64 ? 2 : 1) void paged_attention_kernel(
     const PagedAttnArgs a) {
   constexpr int G = D / 32, NC = D / 16, S = F32 ? 3 : 1, R = 16 * NT;
   constexpr int NW = kPagedWaves;
@@ -865,9 +865,10 @@ AttnShape paged_shape(int dtype, int d_h, int64_t max_rows) {
   AttnShape sh;
   sh.rows = max_rows <= 16 ? 16 : 32;
   sh.by_keys = 1;
+  sh.resident = 1;
   sh.wg_target = 512;
   sh.step = 32 * kPagedWaves;
-  sh.join_keys = 512;
+  sh.ns_key = d_h == 128 ? 16 : 10;
   return sh;
 }
 
