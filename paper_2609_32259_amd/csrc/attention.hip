@@ -68,6 +68,11 @@ struct Bf16Tile {
       q.f[c] = *reinterpret_cast<const bf16x8*>(row + 16 * c + 8 * (lane >> 5));
   }
 
+  FI static void keep(Q& q) {
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) asm volatile("" : "+v"(q.f[c]));
+  }
+
   FI static void scores(const Q& q, const unsigned char* sk, int lane, float (&s)[NS]) {
     const int r = lane & 31;
 #pragma unroll
@@ -163,6 +168,11 @@ struct F32Tile {
 #pragma unroll
     for (int u = 0; u < D / 16; ++u)
       q.f[u] = *reinterpret_cast<const f32x4*>(row + 16 * u + 4 * (lane >> 4));
+  }
+
+  FI static void keep(Q& q) {
+#pragma unroll
+    for (int u = 0; u < D / 16; ++u) asm volatile("" : "+v"(q.f[u]));
   }
 
   FI static void scores(const Q& q, const unsigned char* sk, int lane, float (&s)[NS]) {
@@ -280,7 +290,10 @@ FI bool not_finite(const Rows<P>& w) {
 // from block b0 in steps of `bstep`.  Rows past the last key hold copies of it.  The
 // tile's address is in scalar registers, a lane's place in the tile a 32-bit offset
 // (rows lie at most 2^23 elements apart: host check).
-template <class P, bool V, int NB>
+// UNSEEN: as instructions that the compiler does not see as LDS accesses.  By keys it
+// would wait for all loads before it reads a stage, the next tile's in flight among
+// them; the kernel's own waits are what there has to be.
+template <class P, bool V, int NB, bool UNSEEN>
 struct Fetch {
   typedef typename P::T T;
   static constexpr int CPR = P::ROWB / 16;  // chunks a row
@@ -305,7 +318,7 @@ struct Fetch {
     }
   }
   FI void get(int t0, unsigned char* stage, int b0, int bstep, int lane) const {
-    const __amdgpu_buffer_rsrc_t rsrc = buffer_at(base + t0 * st);
+    const char* tile = base + t0 * st;
     const bool whole = t0 + P::KT <= t;
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
@@ -314,8 +327,11 @@ struct Fetch {
         const int r = row(i, b0, bstep, lane);
         at = min(r, t - 1 - t0) * (int)st + chunk(r, lane);
       }
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_t*)(stage + (b0 + i * bstep) * 1024), 16, at,
-                                               0, 0, 0);
+      unsigned char* to = stage + (b0 + i * bstep) * 1024;
+      if (UNSEEN)
+        load_lds_unseen(tile, at, to);
+      else
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer_at(tile), (lds_void_t*)to, 16, at, 0, 0, 0);
     }
   }
 };
@@ -371,11 +387,16 @@ FI void clear_row(Rows<P>& w) {
   w.l = 0.0f;
 }
 
+template <bool M>
+struct Flag {
+  static constexpr bool value = M;
+};
+
 // By rows: NW waves, each with RW rows of the tile, all against the same keys.  A wave
 // computes the scores of the next tile before it finishes this one's, so
 // that matrix instructions and the softmax's are there to be issued side by side.
 template <class P, int NW>
-__global__ __launch_bounds__(NW * 64) void attention_rows_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(NW * 64, 2) void attention_rows_kernel(const AttnArgs a) {
   typedef typename P::T T;
   constexpr int KT = P::KT, WR = P::RW;  // keys a tile, rows a wave
   __shared__ __attribute__((aligned(1024))) unsigned char k0[KT * P::ROWB];
@@ -404,8 +425,8 @@ __global__ __launch_bounds__(NW * 64) void attention_rows_kernel(const AttnArgs 
   const T* vb = static_cast<const T*>(a.v) + seq_at(it.b, it.key0, a.v_sb, a.v_st) + (long long)it.h * a.v_sh;
   const float c = a.io.c;
 
-  Fetch<P, false, NB> fk;
-  Fetch<P, true, NB> fv;
+  Fetch<P, false, NB, false> fk;
+  Fetch<P, true, NB, false> fv;
   fk.init(kb, a.k_st, t, wave, NW, lane);
   fv.init(vb, a.v_st, t, wave, NW, lane);
   // nothing past the range's last tile is loaded, or used
@@ -484,8 +505,6 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
   const AttnItem it = attn_item(s, P::RW);
   const int t = it.t, n_rows = it.rows;
   const int row0 = it.tile * P::RW;
-  Rows<P> w;
-  load_row<P>(w, a, it, row0 + P::row(lane), lane);
   const int first = last_key(s, it, divide(min(row0, n_rows - 1), s.by_g));
   const int last = last_key(s, it, divide(min(row0 + P::RW - 1, n_rows - 1), s.by_g));
   const int lo = it.part * s.chunk + wave * P::KT;
@@ -496,33 +515,47 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
   unsigned char* w0 = s0 + wave * 2 * TB;
   unsigned char* w1 = s1 + wave * 2 * TB;
 
-  Fetch<P, false, TB / 1024> fk;
-  Fetch<P, true, TB / 1024> fv;
+  Fetch<P, false, TB / 1024, true> fk;
+  Fetch<P, true, TB / 1024, true> fv;
   fk.init(kb, a.k_st, t, 0, 1, lane);
   fv.init(vb, a.v_st, t, 0, 1, lane);
   auto get = [&](int t0, unsigned char* st) {
     fk.get(t0, st, 0, 1, lane);
     fv.get(t0, st + TB, 0, 1, lane);
   };
+  Rows<P> w;
   bool careful = false;
+  // Waits until at most n loads after those of the tile at hand are outstanding.
+  constexpr int NL = TB / 1024;  // loads of a tile's keys, or values
+  auto ready = [&](bool next, auto values) {
+    constexpr int n = decltype(values)::value ? 0 : NL;
+    if (next)
+      __builtin_amdgcn_s_waitcnt(wait_vm_only(n + 2 * NL));
+    else
+      __builtin_amdgcn_s_waitcnt(wait_vm_only(n));
+    asm volatile("" ::: "memory");
+  };
   auto step = [&](int t0, unsigned char* st, unsigned char* nst) {
-    if (t0 + NW * P::KT < hi) {
-      get(t0 + NW * P::KT, nst);
-      __builtin_amdgcn_s_waitcnt(wait_vm_only(2 * (TB / 1024)));
-    } else {
-      __builtin_amdgcn_s_waitcnt(wait_vm_only(0));
-    }
+    const bool next = t0 + NW * P::KT < hi;
+    if (next) get(t0 + NW * P::KT, nst);
+    ready(next, Flag<false>());
     float s[P::NS];
     P::scores(w.q, st, lane, s);
+    ready(next, Flag<true>());
     if (t0 + P::KT - 1 > first)
       finish<P, true>(w, s, st + TB, lane, c, t0, careful);
     else
       finish<P, false>(w, s, st + TB, lane, c, t0, false);
   };
+  // The first tile on its way, then the queries; both are waited for here, for a wait for
+  // the queries inside the loop would wait for the tiles in flight as well.
+  if (lo < hi) get(lo, w0);
+  load_row<P>(w, a, it, row0 + P::row(lane), lane);
+  P::keep(w.q);
   for (;;) {
     clear_row<P>(w);
     if (lo < hi) {
-      get(lo, w0);
+      if (careful) get(lo, w0);
       for (int t0 = lo; t0 < hi; t0 += 2 * NW * P::KT) {
         step(t0, w0, w1);
         if (t0 + NW * P::KT < hi) step(t0 + NW * P::KT, w1, w0);

@@ -50,6 +50,19 @@ FI uint32_t lds_addr(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
 
+// A buffer load of 16 bytes a lane from p + off to LDS (to + 16 lane), which the
+// compiler counts neither as a load nor as an LDS access: only explicit waits order it.
+FI void load_lds_unseen(const void* p, int off, void* to) {
+  const uint64_t v = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  const u32x4 rsrc = {lo, hi & 0xffffu, 0x7fffffffu, 0x00020000u};
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(lds_addr(to))), "v"(off), "s"(rsrc)
+               : "memory", "m0");
+}
+
 FI uint32_t pack_bf16(float a, float b) {
   bf16x2 v = {(__bf16)a, (__bf16)b};
   return __builtin_bit_cast(uint32_t, v);

@@ -563,12 +563,21 @@ def _raw_stream(dev) -> int:
     return _torch()._C._cuda_getCurrentRawStream(dev.index)
 
 
+_I32_ARRAYS = {}
+
+
 def _lens(a, name, B=None):
-    """Host int32 array and list of a batch's lengths."""
-    a = np.ascontiguousarray(a, dtype=np.int32)
-    if a.ndim != 1 or (B is not None and a.size != B):
+    """ctypes int32 array and list of a batch's lengths."""
+    v = a.tolist() if isinstance(a, np.ndarray) else [int(x) for x in a]
+    n = len(v)
+    if (B is not None and n != B) or (n and isinstance(v[0], list)):
         raise ValueError(f"{name} must be one length for each sequence")
-    return a, a.tolist()
+    if n and not -2**31 <= min(v) <= max(v) < 2**31:
+        raise ValueError(f"{name} does not fit 32 bits")
+    t = _I32_ARRAYS.get(n)
+    if t is None:
+        t = _I32_ARRAYS[n] = C.c_int32 * n
+    return t(*v), v
 
 
 def _head_rows(t, lens, name, dev, layers=None) -> hf_rows:
@@ -628,9 +637,9 @@ def hf_attention_workspace_bytes(q_len, kv_len, H_q: int, H: int, d_h: int, dtyp
                                  paged: bool = False) -> int:
     """dtype: HF_BF16 or HF_F32."""
     q_len, _ = _lens(q_len, "q_len")
-    kv_len, _ = _lens(kv_len, "kv_len", q_len.size)
-    return int(lib().hf_attention_workspace_bytes(q_len.size, _p32(q_len), _p32(kv_len), int(H_q),
-                                                  int(H), int(d_h), int(dtype), int(bool(paged))))
+    kv_len, _ = _lens(kv_len, "kv_len", len(q_len))
+    return int(lib().hf_attention_workspace_bytes(len(q_len), q_len, kv_len, int(H_q), int(H),
+                                                  int(d_h), int(dtype), int(bool(paged))))
 
 
 def _attention_outputs(q, rq, rows, q_len, kv_len, H, paged, scale, out, lse, return_lse,
@@ -648,8 +657,8 @@ def _attention_outputs(q, rq, rows, q_len, kv_len, H, paged, scale, out, lse, re
             or lse.numel() < rows * rq.H:
         raise TypeError("lse must be a contiguous fp32 CUDA tensor [rows, H_q]")
     if workspace is None:
-        nbytes = lib().hf_attention_workspace_bytes(q_len.size, _p32(q_len), _p32(kv_len), rq.H, H,
-                                                    rq.d_h, rq.dtype, paged)
+        nbytes = lib().hf_attention_workspace_bytes(len(q_len), q_len, kv_len, rq.H, H, rq.d_h,
+                                                    rq.dtype, paged)
         if nbytes:
             workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
     elif workspace.device != q.device or not workspace.is_contiguous():
@@ -668,7 +677,7 @@ def hf_prompt_attention(q, k, v, q_len, kv_len=None, causal=True, scale=None, ou
     q_len, kv_len: lengths [B] (kv_len None: q_len, whole prompts); scale None: 1/sqrt(d_h).
     Returns out [N, H_q, d_h], with ``return_lse`` (out, lse [N, H_q] fp32)."""
     nq, lq = _lens(q_len, "q_len")
-    nk, lk = (nq, lq) if kv_len is None else _lens(kv_len, "kv_len", nq.size)
+    nk, lk = (nq, lq) if kv_len is None else _lens(kv_len, "kv_len", len(lq))
     dev = q.device
     if not q.is_cuda:
         raise TypeError("q must be a CUDA tensor")
@@ -680,7 +689,7 @@ def hf_prompt_attention(q, k, v, q_len, kv_len=None, causal=True, scale=None, ou
                                                         lse, return_lse, workspace)
         ro = _head_rows(out, lq, "out", dev)
         st = lib().hf_prompt_attention(
-            nq.size, _p32(nq), _p32(nk), rq, rk, rv, ro, scale, 1 if causal else 0, _ptr(lse),
+            len(lq), nq, nk, rq, rk, rv, ro, scale, 1 if causal else 0, _ptr(lse),
             _ptr(workspace), 0 if workspace is None else _nbytes(workspace), _raw_stream(dev))
     _check(st, "hf_prompt_attention")
     return (out, lse) if return_lse else out
@@ -690,9 +699,9 @@ def hf_paged_attention(q, cache: PagedKV, q_len, kv_len, layer=0, causal=True, s
                        out=None, lse=None, return_lse=False, workspace=None, stream=None):
     """hf_prompt_attention over the first kv_len [B] tokens of one layer of a paged cache."""
     nq, lq = _lens(q_len, "q_len")
-    nk, lk = _lens(kv_len, "kv_len", nq.size)
-    if nq.size > cache.batch:
-        raise ValueError(f"{nq.size} sequences, the table has {cache.batch}")
+    nk, lk = _lens(kv_len, "kv_len", len(lq))
+    if len(lq) > cache.batch:
+        raise ValueError(f"{len(lq)} sequences, the table has {cache.batch}")
     dev = cache.pages.device
     with _call_on(dev, stream):
         rq = _head_rows(q, lq, "q", dev)
@@ -700,7 +709,7 @@ def hf_paged_attention(q, cache: PagedKV, q_len, kv_len, layer=0, causal=True, s
                                                         out, lse, return_lse, workspace)
         ro = _head_rows(out, lq, "out", dev)
         st = lib().hf_paged_attention(
-            nq.size, _p32(nq), _p32(nk), rq, cache.desc, int(layer), ro, scale,
+            len(lq), nq, nk, rq, cache.desc, int(layer), ro, scale,
             1 if causal else 0, _ptr(lse), _ptr(workspace),
             0 if workspace is None else _nbytes(workspace), _raw_stream(dev))
     _check(st, "hf_paged_attention")
@@ -709,9 +718,9 @@ def hf_paged_attention(q, cache: PagedKV, q_len, kv_len, layer=0, causal=True, s
 
 def _paged_rows(cache, start, n, k, v):
     start, _ = _lens(start, "start")
-    n, ln = _lens(n, "n", start.size)
-    if n.size > cache.batch:
-        raise ValueError(f"{n.size} sequences, the table has {cache.batch}")
+    n, ln = _lens(n, "n", len(start))
+    if len(ln) > cache.batch:
+        raise ValueError(f"{len(ln)} sequences, the table has {cache.batch}")
     layers = k.shape[1] if k.dim() == 5 else 1
     dev = cache.pages.device
     return start, n, _head_rows(k, ln, "k", dev, layers), _head_rows(v, ln, "v", dev, layers), layers
@@ -723,12 +732,11 @@ def hf_paged_append(cache: PagedKV, start, n, k, v, theta=0.0, pos0=None, layer=
     (``R[:, :, 0]``, ``R[:, :, 1]`` of a transferred cache).  theta > 0 rotates the keys at
     positions pos0[b] + start[b] + i; 0 stores them as given."""
     start, n, rk, rv, layers = _paged_rows(cache, start, n, k, v)
-    p0 = None if pos0 is None else _lens(pos0, "pos0", n.size)[0]
+    p0 = None if pos0 is None else _lens(pos0, "pos0", len(n))[0]
     dev = cache.pages.device
     with _call_on(dev, stream):
-        st = lib().hf_paged_append(n.size, _p32(start), _p32(n), cache.desc, int(layer), layers, rk,
-                                   rv, float(theta), None if p0 is None else _p32(p0),
-                                   _raw_stream(dev))
+        st = lib().hf_paged_append(len(n), start, n, cache.desc, int(layer), layers, rk, rv,
+                                   float(theta), p0, _raw_stream(dev))
     _check(st, "hf_paged_append")
     return cache
 
@@ -739,8 +747,8 @@ def hf_paged_read(cache: PagedKV, start, n, k, v, layer=0, stream=None):
     start, n, rk, rv, layers = _paged_rows(cache, start, n, k, v)
     dev = cache.pages.device
     with _call_on(dev, stream):
-        st = lib().hf_paged_read(n.size, _p32(start), _p32(n), cache.desc, int(layer), layers, rk,
-                                 rv, _raw_stream(dev))
+        st = lib().hf_paged_read(len(n), start, n, cache.desc, int(layer), layers, rk, rv,
+                                 _raw_stream(dev))
     _check(st, "hf_paged_read")
     return k, v
 
