@@ -434,7 +434,7 @@ size_t hf_attention_workspace_bytes(int32_t B, const int32_t* q_len, const int32
  * decoded token, has q_len < kv_len.  A row that sees no key (kv_len == 0, or
  * causal with q_len > kv_len) gets out = 0 and lse = -infinity.  What a row does
  * not see has no influence on it, whatever its bits are.
- *   q_len, kv_len  host int32 [B], >= 0.
+ *   q_len, kv_len  host int32 [B], >= 0; kv_len <= 2^30.
  *   q, out    hf_rows of H_q heads; out may be q itself, element for element.
  *   k, v      hf_rows of H heads, H_q % H == 0, stride_t <= 2^23; same dtype and
  *             d_h throughout.
@@ -445,7 +445,10 @@ size_t hf_attention_workspace_bytes(int32_t B, const int32_t* q_len, const int32
  * Numerics: HF_BF16 multiplies on the bf16 matrix cores with fp32 accumulation;
  * the softmax runs in fp32, its weights are rounded once to bf16 for the second
  * product (their sum is taken before that), and the result is rounded once.
- * HF_F32 computes in fp32 throughout.  Supported: d_h 64 and 128.
+ * HF_F32 computes in fp32 throughout.  Supported: d_h 64 and 128.  The result of a
+ * row does not depend on the other rows of the call, nor on where the call runs;
+ * how a key range is split (which follows from the lengths of the whole batch)
+ * changes it by rounding.  Forward only: both models are frozen.
  */
 int32_t hf_prompt_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len,
                             const hf_rows* q, const hf_rows* k, const hf_rows* v,

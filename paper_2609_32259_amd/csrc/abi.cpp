@@ -768,6 +768,9 @@ int32_t hf_transfer_kv_taps(int32_t B, const int32_t* s_len, const int32_t* r_le
 
 namespace {
 
+constexpr int32_t kMaxKeys = 1 << 30;     // of a sequence: key numbers plus a few tiles stay in int32
+constexpr int64_t kMaxGroups = 1 << 22;  // workgroups along a grid's x axis: 2^32 threads
+
 int32_t check_lens(int32_t B, const char* na, const int32_t* a, const char* nb, const int32_t* b) {
   if (B < 1 || B > HF_MAX_BATCH) return fail(HF_ERR_SHAPE, "B=%d outside [1, %d]", B, HF_MAX_BATCH);
   if (!a || !b) return fail(HF_ERR_NULL, "%s / %s is NULL", na, nb);
@@ -806,6 +809,8 @@ int32_t plan_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len, i
   for (int b = 0; b < B; ++b) {
     max_rows = std::max(max_rows, (int64_t)q_len[b] * G);
     total += q_len[b];
+    if (kv_len[b] > kMaxKeys)
+      return fail(HF_ERR_UNSUPPORTED, "sequence %d: %d keys, at most %d are served", b, kv_len[b], kMaxKeys);
   }
   if (total > INT32_MAX || max_rows > INT32_MAX - 1024 || total * H_q > ((int64_t)1 << 40))
     return fail(HF_ERR_SHAPE, "too many query rows");
@@ -871,7 +876,7 @@ int32_t plan_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len, i
       split += mine * H;
       slots += mine * H * parts;
     }
-    if (items * H > INT32_MAX || split > INT32_MAX || slots > INT32_MAX)
+    if (items * H > kMaxGroups || split > INT32_MAX || slots > INT32_MAX)
       return fail(HF_ERR_SHAPE, "too many work items");
     if (key > INT32_MAX) return fail(HF_ERR_SHAPE, "too many keys");
   }
@@ -908,7 +913,7 @@ int32_t attention_common(int32_t B, const int32_t* q_len, const int32_t* kv_len,
   if (q->H != out->H || q->d_h != out->d_h || q->d_h != d_h)
     return fail(HF_ERR_SHAPE, "q, out and the cache differ in heads or d_h");
   if ((st = check_heads(q->H, H, d_h))) return st;
-  if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(HF_ERR_SHAPE, "scale must be finite and > 0");
+  if (!(scale > 0.0f) || !std::isfinite(scale * 1.5f)) return fail(HF_ERR_SHAPE, "scale must be finite and > 0");
   if (reinterpret_cast<uintptr_t>(lse) & 3u) return fail(HF_ERR_SHAPE, "lse not 4-byte aligned");
   int64_t slots = 0;
   if ((st = plan_attention(B, q_len, kv_len, q->H, H, q->dtype, d_h, paged, causal, sh, s, slots)))
@@ -1007,7 +1012,7 @@ int32_t paged_rows(bool append, int32_t B, const int32_t* start, const int32_t* 
     a.q[b] = {(int32_t)blocks, start[b], n[b], (int32_t)p0, (int32_t)row, {}};
     row += n[b];
     if (n[b] > 0) blocks += (end - 1) / 32 - start[b] / 32 + 1;
-    if (blocks * cache->H > INT32_MAX || row > INT32_MAX) return fail(HF_ERR_SHAPE, "too many rows");
+    if (blocks * cache->H > kMaxGroups || row > INT32_MAX) return fail(HF_ERR_SHAPE, "too many rows");
   }
   a.n_blocks = (int32_t)blocks;
   if (blocks == 0) return ok();
