@@ -6,6 +6,12 @@ packed maps, the receiver cache and the workspaces -- and ``step()`` runs the
 path once: ``hf_build_alignment`` -> ``hf_build_layer_map`` ->
 ``hf_transfer_kv`` (with ``layer_map="neighbor3"``: ``hf_build_layer_taps`` ->
 ``hf_transfer_kv_taps``).  It does no arithmetic of the method itself.
+
+What the receiver does with the transferred cache goes through the same object:
+``attend()`` answers queries over it (``hf_prompt_attention``) and ``store()`` moves
+it into a paged cache held in 4 bits (``hf_paged_append``), from which
+``dense_cache()`` gives back the rows that the next hand-off takes as its sender
+cache (``hf_paged_read``).
 """
 
 from __future__ import annotations
@@ -109,3 +115,32 @@ class TransferPath:
         self.build_layer_map()
         self.transfer(stream)
         return self.R
+
+    def attend(self, layer: int, q, q_len, kv_len=None, **kw):
+        """Attention of packed queries [sum q_len, H_q, d_h] over one layer of the receiver
+        cache (arguments as ``hf_prompt_attention``).  kv_len None: the transferred rows;
+        a suffix whose rows lie behind them in ``R`` passes r_len + q_len."""
+        return hf.hf_prompt_attention(q, self.R[:, layer, 0], self.R[:, layer, 1], q_len,
+                                      self.r_len if kv_len is None else kv_len, **kw)
+
+    def store(self, cache: "hf.PagedKV", start=None, layer: int = 0, stream=None):
+        """Append the transferred rows of all receiver layers to a paged cache, as they are
+        (their keys are rotated already), behind the start [B] tokens it holds (None: 0)."""
+        if start is None:
+            start = np.zeros(len(self.r_len), np.int32)
+        return hf.hf_paged_append(cache, start, self.r_len, self.R[:, :, 0], self.R[:, :, 1],
+                                  layer=layer, stream=stream)
+
+
+def dense_cache(cache: "hf.PagedKV", lengths, dtype=None, T_cap: Optional[int] = None):
+    """The first lengths [B] tokens of all layers of a paged cache as a dense cache
+    [B, L, 2, H, T_cap, d_h] (dtype None: bf16; rows behind a length are 0): the sender
+    cache of the next hand-off.  Runs on the current stream of the cache's device."""
+    import torch
+
+    lengths = np.asarray(lengths, np.int32)
+    T_cap = max(1, int(lengths.max(initial=0))) if T_cap is None else int(T_cap)
+    S = torch.zeros((lengths.size, cache.L, 2, cache.H, T_cap, cache.d_h),
+                    dtype=dtype or torch.bfloat16, device=cache.pages.device)
+    hf.hf_paged_read(cache, np.zeros(lengths.size, np.int32), lengths, S[:, :, 0], S[:, :, 1])
+    return S
