@@ -445,10 +445,11 @@ size_t hf_attention_workspace_bytes(int32_t B, const int32_t* q_len, const int32
  * Numerics: HF_BF16 multiplies on the bf16 matrix cores with fp32 accumulation;
  * the softmax runs in fp32, its weights are rounded once to bf16 for the second
  * product (their sum is taken before that), and the result is rounded once.
- * HF_F32 computes in fp32 throughout.  Supported: d_h 64 and 128.  The result of a
- * row does not depend on the other rows of the call, nor on where the call runs;
- * how a key range is split (which follows from the lengths of the whole batch)
- * changes it by rounding.  Forward only: both models are frozen.
+ * HF_F32 computes in fp32 throughout.  Supported: d_h 64 and 128.  The bits of a
+ * result row depend on its own queries, keys and values and on the lengths, heads
+ * and types of the call (by which key ranges are split, in a fixed order), not on
+ * what the other rows hold, on timing or on the device.  No gradients are formed:
+ * both models are frozen.
  */
 int32_t hf_prompt_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len,
                             const hf_rows* q, const hf_rows* k, const hf_rows* v,
@@ -522,7 +523,7 @@ int32_t hf_paged_read(int32_t B, const int32_t* start, const int32_t* n, const h
 
 /*
  * hf_prompt_attention over the first kv_len[b] tokens of one layer of a paged
- * cache, for decoded tokens and short runs (any q_len is served; each 32 query
+ * cache, for decoded tokens and short runs (any q_len is served; each 16 query
  * rows of a group read the cache once more).  Arguments, masks, results and
  * errors as there; workspace >= hf_attention_workspace_bytes(..., paged = 1).
  * Numerics: the codes enter the matrix products as whole numbers, exactly, and

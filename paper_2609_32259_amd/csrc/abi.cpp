@@ -797,9 +797,48 @@ int32_t check_rows(const char* name, const hf_rows* r, bool used, bool written, 
   return HF_OK;
 }
 
-// Cuts the batch into work items and long key ranges into parts.  A part is as long
-// as the whole work over the workgroups that fill the chip, so that the parts of one
-// launch take about equally long; a range that needs no cutting has one part.
+// The length of the parts that long key ranges are cut into, and the estimated time of
+// that.  Where the items are many rounds of workgroups anyway nothing is cut.  Of the other
+// cuts the one with the least time is taken: the rounds times a part's time, or, where
+// the items differ in length as those of causal prompts do, the whole work over the
+// workgroups; then the join, which writes and reads every part.
+struct Cut {
+  int64_t chunk, ns;
+  bool triangular;
+};
+Cut cut_keys(const hf::AttnShape& sh, int32_t B, const int32_t* q_len, const int32_t* kv_len,
+             int32_t G, int32_t H, int32_t d_h, bool causal) {
+  constexpr int64_t kJoin = 5000;     // ns of a second launch
+  constexpr int64_t kBytesNs = 6000;  // that the join moves in a ns (parts lie in the L2s)
+  int64_t longest = 1, rows = 0, seen = 0;
+  int64_t of_seq[HF_MAX_BATCH];
+  bool triangular = causal;
+  for (int b = 0; b < B; ++b) {
+    of_seq[b] = ((int64_t)q_len[b] * G + sh.rows - 1) / sh.rows * H;
+    rows += (int64_t)q_len[b] * G * H;
+    if (q_len[b] > 0) longest = std::max(longest, (int64_t)kv_len[b]);
+    if (2 * (int64_t)q_len[b] < kv_len[b]) triangular = false;
+    seen += of_seq[b] * (kv_len[b] / 2);
+  }
+  Cut best = {longest, INT64_MAX, triangular};
+  const int64_t most = std::min<int64_t>((longest + sh.step - 1) / sh.step, sh.wg_target);
+  for (int64_t k = 1; k <= most; ++k) {  // (k B H <= 4 wg_target: at most some thousand divisions)
+    const int64_t c = (longest + k * sh.step - 1) / (k * sh.step) * sh.step;
+    int64_t n = 0;
+    for (int b = 0; b < B; ++b)
+      n += of_seq[b] * std::max<uint32_t>(((uint32_t)kv_len[b] + (uint32_t)c - 1) / (uint32_t)c, 1);
+    const int64_t part = sh.ns_start + std::min(c, longest) * sh.ns_key;
+    const int64_t work =
+        triangular ? std::max(part, (seen * sh.ns_key + n * sh.ns_start) / sh.wg_target)
+                   : (n + sh.wg_target - 1) / sh.wg_target * part;
+    const int64_t ns = work + (k > 1 ? kJoin + rows * k * d_h * 8 / kBytesNs : 0);
+    if (ns < best.ns) best = {c, ns, triangular};
+    if (n > 4 * (int64_t)sh.wg_target) break;
+  }
+  return best;
+}
+
+// The kernel's shape and the batch's work items.
 int32_t plan_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len, int32_t H_q,
                        int32_t H, int32_t dtype, int32_t d_h, bool paged, int32_t causal,
                        hf::AttnShape& sh, hf::AttnSeqs& s, int64_t& slots) {
@@ -814,45 +853,32 @@ int32_t plan_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len, i
   }
   if (total > INT32_MAX || max_rows > INT32_MAX - 1024 || total * H_q > ((int64_t)1 << 40))
     return fail(HF_ERR_SHAPE, "too many query rows");
-  sh = paged ? hf::paged_shape(dtype, d_h, max_rows) : hf::prompt_shape(dtype, d_h, max_rows);
-  // The cut with the least estimated time, where the uncut items are not many rounds of
-  // workgroups anyway: the rounds times a part's time, or, where the items differ in
-  // length as those of causal prompts do, the whole work over the workgroups; then the
-  // join, which writes and reads every part.
-  constexpr int64_t kStart = 192;   // a part's fixed cost, in keys
-  constexpr int64_t kJoin = 5000;   // ns of a second launch
-  constexpr int64_t kBytesNs = 3000;  // that the join moves in a ns
-  int64_t longest = 1, uncut = 0, rows = 0, seen = 0;
-  int64_t of_seq[HF_MAX_BATCH];
-  bool triangular = causal != 0;
-  for (int b = 0; b < B; ++b) {
-    of_seq[b] = ((int64_t)q_len[b] * G + sh.rows - 1) / sh.rows * H;
-    uncut += of_seq[b];
-    rows += (int64_t)q_len[b] * H_q;
-    if (q_len[b] > 0) longest = std::max(longest, (int64_t)kv_len[b]);
-    if (2 * (int64_t)q_len[b] < kv_len[b]) triangular = false;
-    seen += of_seq[b] * (kv_len[b] / 2);
-  }
-  int64_t chunk = longest;
-  if (uncut > 0 && uncut < 4 * (int64_t)sh.wg_target) {
-    int64_t best = INT64_MAX;
-    const int64_t most = std::min<int64_t>((longest + sh.step - 1) / sh.step, sh.wg_target);
-    for (int64_t k = 1; k <= most; ++k) {  // (k B H <= 4 wg_target: at most some thousand divisions)
-      const int64_t c = (longest + k * sh.step - 1) / (k * sh.step) * sh.step;
-      int64_t n = 0;
-      for (int b = 0; b < B; ++b)
-        n += of_seq[b] * std::max<uint32_t>(((uint32_t)kv_len[b] + (uint32_t)c - 1) / (uint32_t)c, 1);
-      const int64_t part = std::min(c, longest) + kStart;
-      const int64_t keys = triangular ? std::max(part, (seen + n * kStart) / sh.wg_target)
-                                      : (n + sh.wg_target - 1) / sh.wg_target * part;
-      const int64_t cost = keys * sh.ns_key + (k > 1 ? kJoin + rows * k * d_h * 8 / kBytesNs : 0);
-      if (cost < best) {
-        best = cost;
-        chunk = c;
+  // Dense keys: by keys where the rows are one wave's.  Otherwise the faster shape by the
+  // estimate, where tiles of rows do not fill the chip (if they do it is by rows).  Measured
+  // by keys and by rows, us with the join, 32 heads on 8 of 128: 32 rows of a head over
+  // 29,119 keys 28.9 and 40.5, 64 rows 36.0 and 41.7, 128 rows 56.7 and 45.8, 128 rows over
+  // 2,000 keys 15.9 and 20.8; eight sequences of 80 rows over 4,000 keys 55.0 and 46.2.
+  Cut cut = {0, INT64_MAX, false};
+  if (paged) {
+    sh = hf::paged_shape(dtype, d_h);
+    cut = cut_keys(sh, B, q_len, kv_len, G, H, d_h, causal != 0);
+  } else {
+    const hf::AttnShape keys = hf::prompt_shape(dtype, d_h, true), by_rows = hf::prompt_shape(dtype, d_h, false);
+    int64_t tiles = 0;
+    for (int b = 0; b < B; ++b) tiles += ((int64_t)q_len[b] * G + by_rows.rows - 1) / by_rows.rows * H;
+    if (max_rows > keys.rows) {
+      sh = by_rows;
+      cut = cut_keys(sh, B, q_len, kv_len, G, H, d_h, causal != 0);
+    }
+    if (max_rows <= keys.rows || tiles < by_rows.wg_target) {
+      const Cut other = cut_keys(keys, B, q_len, kv_len, G, H, d_h, causal != 0);
+      if (other.ns < cut.ns) {
+        sh = keys;
+        cut = other;
       }
-      if (n > 4 * (int64_t)sh.wg_target) break;
     }
   }
+  int64_t chunk = cut.chunk;
   chunk = (chunk + sh.step - 1) / sh.step * sh.step;
   s.chunk = (int32_t)std::min<int64_t>(chunk, INT32_MAX / 2 / sh.step * sh.step);
   s.B = B;
@@ -880,7 +906,7 @@ int32_t plan_attention(int32_t B, const int32_t* q_len, const int32_t* kv_len, i
       return fail(HF_ERR_SHAPE, "too many work items");
     if (key > INT32_MAX) return fail(HF_ERR_SHAPE, "too many keys");
   }
-  if (sh.resident > 1 && triangular && B == 1) s.snake = std::max(sh.wg_target / H, 1);
+  if (sh.resident > 1 && cut.triangular && B == 1) s.snake = std::max(sh.wg_target / H, 1);
   s.n_items = (int32_t)items;
   s.n_split = (int32_t)split;
   return HF_OK;
@@ -1123,7 +1149,7 @@ int32_t hf_paged_attention(int32_t B, const int32_t* q_len, const int32_t* kv_le
   hipError_t e;
   {
     TimedLaunch t(HF_KERNEL_PAGED_ATTENTION, s);
-    e = hf::launch_paged_attention(q->dtype, cache->d_h, sh, a, s);
+    e = hf::launch_paged_attention(q->dtype, cache->d_h, a, s);
   }
   if (e != hipSuccess) return hip_fail(e, "paged attention launch");
   return join_parts(q->dtype, cache->d_h, a.io, a.s, s);

@@ -537,6 +537,7 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
   };
   auto step = [&](int t0, unsigned char* st, unsigned char* nst) {
     const bool next = t0 + NW * P::KT < hi;
+    __builtin_amdgcn_s_waitcnt(kWaitLds);  // (what was read of nst is in registers)
     if (next) get(t0 + NW * P::KT, nst);
     ready(next, Flag<false>());
     float s[P::NS];
@@ -693,16 +694,25 @@ void join(const JoinArgs& a, int most_parts, hipStream_t st) {
 
 }  // namespace
 
-AttnShape prompt_shape(int dtype, int d_h, int64_t max_rows) {
+// Times as measured, d_h 128 and 64, with every workgroup on a CU of its own: parts of
+// 64 to 1,024 keys by rows, of 128 to 4,096 by keys (keys from L2; where HBM bounds it,
+// one tile of rows over 29K keys, 20 ns a key).
+AttnShape prompt_shape(int dtype, int d_h, bool by_keys) {
   AttnShape sh;
-  const int rw = dtype == HF_BF16 ? 32 : 16;
-  sh.by_keys = max_rows <= rw;
-  sh.rows = sh.by_keys ? rw : rw * (dtype == HF_BF16 ? kRowWaves : kRowWavesF32);
+  const bool f32 = dtype == HF_F32, wide = d_h == 128;
+  const int rw = f32 ? 16 : 32;
+  sh.by_keys = by_keys;
+  sh.rows = by_keys ? rw : rw * (f32 ? kRowWavesF32 : kRowWaves);
   sh.wg_target = 256;
-  sh.step = sh.by_keys ? 32 * kKeyWaves : 64;
-  sh.resident = sh.by_keys || dtype == HF_BF16 ? 1 : 3;
-  // (measured: 8192 keys of 8 -> 4 -> 1 heads, one workgroup a CU)
-  sh.ns_key = sh.by_keys ? (d_h == 128 ? 20 : 12) : dtype == HF_BF16 ? (d_h == 128 ? 33 : 24) : d_h == 128 ? 56 : 28;
+  sh.step = by_keys ? 32 * kKeyWaves : 64;
+  sh.resident = by_keys || !f32 ? 1 : 3;
+  if (by_keys) {
+    sh.ns_start = f32 || !wide ? 6000 : 9600;
+    sh.ns_key = f32 ? (wide ? 32 : 14) : wide ? 12 : 7;
+  } else {
+    sh.ns_start = f32 ? (wide ? 8000 : 6400) : wide ? 12000 : 10500;
+    sh.ns_key = f32 ? (wide ? 80 : 44) : wide ? 30 : 17;
+  }
   return sh;
 }
 

@@ -35,8 +35,9 @@ constexpr float kRaise = 8.0f;
 // s_waitcnt immediate that waits until at most n vector-memory operations are
 // outstanding and leaves the other counters alone (gfx9 encoding).
 constexpr int wait_vm_only(int n) { return (n & 0xF) | ((n >> 4) << 14) | (7 << 4) | (0xF << 8); }
-// All vector-memory and LDS operations.
+// All vector-memory and LDS operations; the LDS operations alone.
 constexpr int kWaitMemory = 7 << 4;
+constexpr int kWaitLds = 0xF | (3 << 14) | (7 << 4);
 
 // A buffer resource of 2 GiB from a pointer that every lane holds.
 FI __amdgpu_buffer_rsrc_t buffer_at(const void* p) {

@@ -236,14 +236,14 @@ struct AttnShape {
   int32_t wg_target;  // workgroups that fill the chip
   int32_t resident;   // workgroups of several tiles' lengths that a CU runs at once
   int32_t step;       // keys that parts are cut in multiples of
-  int32_t ns_key;     // time of a workgroup for each key of its part, when the chip is full
+  int32_t ns_start;   // time of a workgroup: fixed, and for each key of its part
+  int32_t ns_key;
 };
-AttnShape prompt_shape(int dtype, int d_h, int64_t max_rows);
-AttnShape paged_shape(int dtype, int d_h, int64_t max_rows);
+AttnShape prompt_shape(int dtype, int d_h, bool by_keys);
+AttnShape paged_shape(int dtype, int d_h);
 hipError_t launch_prompt_attention(int dtype, int d_h, const AttnShape& sh, const AttnArgs& a,
                                    hipStream_t s);
-hipError_t launch_paged_attention(int dtype, int d_h, const AttnShape& sh, const PagedAttnArgs& a,
-                                  hipStream_t s);
+hipError_t launch_paged_attention(int dtype, int d_h, const PagedAttnArgs& a, hipStream_t s);
 hipError_t launch_attention_join(int dtype, int d_h, const AttnIO& io, const AttnSeqs& s,
                                  hipStream_t st);
 

@@ -24,6 +24,8 @@ namespace {
 // codes' order) of one sequence, layer, role and head; 16 channels a thread.
 // ---------------------------------------------------------------------------
 
+constexpr int kHeads = 4;  // that a workgroup takes at most
+
 struct RowItem {
   int b, l, h, role;
   int start, pos0, src0;  // the sequence's first token, position offset, rows before it
@@ -226,7 +228,7 @@ __global__ __launch_bounds__(2 * D) void paged_append_kernel(const PagedRowsArgs
   constexpr int TPT = D / 16;  // threads a token
   constexpr int G = D / 32, O = D / 8;
   constexpr int LD = O + (D == 128 ? 4 : 2);  // dwords a token in LDS: tokens 4 apart on other banks
-  constexpr int NH = 4;
+  constexpr int NH = kHeads;
   __shared__ float2 cs[ROT ? 32 * D / 2 : 1];
   __shared__ uint32_t codes[NH][32 * LD];
   const RowItem it = row_item<D>(a, hpw);
@@ -238,82 +240,80 @@ __global__ __launch_bounds__(2 * D) void paged_append_kernel(const PagedRowsArgs
   const int row = it.row0 + tok;
   const T* src = static_cast<const T*>(it.role == 0 ? a.k : a.v) + rows_at(a, it, tok);
   const long long sh = it.role == 0 ? a.k_sh : a.v_sh;
-  const int h_end = min(it.h + hpw, a.H);
-  for (int h0 = it.h; h0 < h_end; h0 += NH) {
-    Raw8<T> r0[NH], r1[NH];  // channels 8 j .. and D/2 + 8 j ..: rotation pairs
-    if (on) {  // (a group's four lanes hold the same token)
+  const int heads = min(hpw, a.H - it.h);
+  Raw8<T> r0[NH], r1[NH];  // channels 8 j .. and D/2 + 8 j ..: rotation pairs
+  if (on) {  // (a group's four lanes hold the same token)
 #pragma unroll
-      for (int i = 0; i < NH; ++i)
-        if (h0 + i < h_end) {
-          r0[i].load(src + (h0 + i) * sh + 8 * j);
-          r1[i].load(src + (h0 + i) * sh + D / 2 + 8 * j);
-        }
-    }
-    if (ROT && rot && h0 == it.h) {  // (while the rows are on their way)
-      fill_angles<D>(a, it, cs);
-      __syncthreads();
-    }
-    if (on) {
+    for (int i = 0; i < NH; ++i)
+      if (i < heads) {
+        r0[i].load(src + (it.h + i) * sh + 8 * j);
+        r1[i].load(src + (it.h + i) * sh + D / 2 + 8 * j);
+      }
+  }
+  if (rot) {  // (while the rows are on their way)
+    fill_angles<D>(a, it, cs);
+    __syncthreads();
+  }
+  if (on) {
 #pragma unroll
-      for (int i = 0; i < NH; ++i) {
-        if (h0 + i >= h_end) break;
-        float x0[8], x1[8];
-        r0[i].values(x0);
-        r1[i].values(x1);
-        if (ROT && rot) {
+    for (int i = 0; i < NH; ++i) {
+      if (i >= heads) break;
+      float x0[8], x1[8];
+      r0[i].values(x0);
+      r1[i].values(x1);
+      if (ROT && rot) {
 #pragma clang fp contract(off)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float2 r = cs[tok * (D / 2) + 8 * j + e];
-            const float u = x0[e], v = x1[e];
-            x0[e] = u * r.x - v * r.y;
-            x1[e] = v * r.x + u * r.y;
-          }
+        for (int e = 0; e < 8; ++e) {
+          const float2 r = cs[tok * (D / 2) + 8 * j + e];
+          const float u = x0[e], v = x1[e];
+          x0[e] = u * r.x - v * r.y;
+          x1[e] = v * r.x + u * r.y;
         }
-        uint32_t w0, w1;
-        const uint32_t c0 = code_group(x0, w0), c1 = code_group(x1, w1);
-        uint8_t* head = it.head + (long long)(h0 + i) * ph.bytes();
-        uint32_t* words = reinterpret_cast<uint32_t*>(head + ph.word(it.role, row));
-        if ((j & 3) == 0) {
-          words[j >> 2] = w0;
-          words[G / 2 + (j >> 2)] = w1;
-        }
-        if (it.role == 0) {
-          uint32_t* kc = reinterpret_cast<uint32_t*>(head + ph.kcode(row));
-          kc[(j & 3) * G + (j >> 2)] = c0;
-          kc[(j & 3) * G + G / 2 + (j >> 2)] = c1;
-        } else {
-          codes[i][tok * LD + j] = c0;
-          codes[i][tok * LD + O / 2 + j] = c1;
-        }
+      }
+      uint32_t w0, w1;
+      const uint32_t c0 = code_group(x0, w0), c1 = code_group(x1, w1);
+      uint8_t* head = it.head + (long long)(it.h + i) * ph.bytes();
+      uint32_t* words = reinterpret_cast<uint32_t*>(head + ph.word(it.role, row));
+      if ((j & 3) == 0) {
+        words[j >> 2] = w0;
+        words[G / 2 + (j >> 2)] = w1;
+      }
+      if (it.role == 0) {
+        uint32_t* kc = reinterpret_cast<uint32_t*>(head + ph.kcode(row));
+        kc[(j & 3) * G + (j >> 2)] = c0;
+        kc[(j & 3) * G + G / 2 + (j >> 2)] = c1;
+      } else {
+        codes[i][tok * LD + j] = c0;
+        codes[i][tok * LD + O / 2 + j] = c1;
       }
     }
-    if (it.role == 0) continue;
-    // Value codes to the order of the block, eight tokens by eight channels a thread.
-    // Tokens that are not the call's keep what is there.
-    __syncthreads();
-    const int i = threadIdx.x / (D / 2), m = threadIdx.x / O % 4, oct = threadIdx.x % O;
-    if (h0 + i < h_end) {
-      uint32_t c[8], mask = 0;
+  }
+  if (it.role == 0) return;
+  // Value codes to the order of the block, eight tokens by eight channels a thread.
+  // Tokens that are not the call's keep what is there.
+  __syncthreads();
+  static_assert(NH == 2 * D / (D / 2), "a thread of each head, block quarter and octet");
+  const int i = threadIdx.x / (D / 2), m = threadIdx.x / O % 4, oct = threadIdx.x % O;
+  if (i < heads) {
+    uint32_t c[8], mask = 0;
 #pragma unroll
-      for (int y = 0; y < 8; ++y) {
-        const int t = 16 * (y >> 2) + 4 * m + (y & 3);
-        const bool in = t >= it.lo && t < it.hi;
-        c[y] = in ? codes[i][t * LD + oct] : 0u;
-        mask |= in ? 15u << (4 * y) : 0u;
-      }
-      transpose_nibbles(c);
-      uint32_t* vc = reinterpret_cast<uint32_t*>(it.head + (long long)(h0 + i) * ph.bytes() + ph.vcode(it.row0)) +
-                     (m * 16 + 8 * (oct & 1)) * (D / 16) + oct / 2;
-      if (mask == 0xffffffffu) {
-#pragma unroll
-        for (int y = 0; y < 8; ++y) vc[y * (D / 16)] = c[y];
-      } else if (mask) {
-#pragma unroll
-        for (int y = 0; y < 8; ++y) vc[y * (D / 16)] = (vc[y * (D / 16)] & ~mask) | c[y];
-      }
+    for (int y = 0; y < 8; ++y) {
+      const int t = 16 * (y >> 2) + 4 * m + (y & 3);
+      const bool in = t >= it.lo && t < it.hi;
+      c[y] = in ? codes[i][t * LD + oct] : 0u;
+      mask |= in ? 15u << (4 * y) : 0u;
     }
-    if (h0 + NH < h_end) __syncthreads();
+    transpose_nibbles(c);
+    uint32_t* vc = reinterpret_cast<uint32_t*>(it.head + (long long)(it.h + i) * ph.bytes() + ph.vcode(it.row0)) +
+                   (m * 16 + 8 * (oct & 1)) * (D / 16) + oct / 2;
+    if (mask == 0xffffffffu) {
+#pragma unroll
+      for (int y = 0; y < 8; ++y) vc[y * (D / 16)] = c[y];
+    } else if (mask) {
+#pragma unroll
+      for (int y = 0; y < 8; ++y) vc[y * (D / 16)] = (vc[y * (D / 16)] & ~mask) | c[y];
+    }
   }
 }
 
@@ -375,14 +375,14 @@ __global__ __launch_bounds__(2 * D) void paged_read_kernel(const PagedRowsArgs a
 }
 
 // ---------------------------------------------------------------------------
-// Attention.  A workgroup takes 16 NT query rows of a group and a part of the
+// Attention.  A workgroup takes 16 query rows of a group and a part of the
 // tokens; its four waves deal the blocks of 32 tokens among them.  On
 // v_mfma_f32_16x16x32_bf16, with m = lane / 16, S^T = K Q^T gives the lane its row
 // lane % 16 and tokens 4 m + i of each half of the block (i: the result register),
 // which is how the value codes lie: the lane's dword for channel block n holds
 // channel 16 n + lane % 16 of those eight tokens.
 // ---------------------------------------------------------------------------
-constexpr int kPagedWaves = 4;
+constexpr int kPagedWaves = 4, kPagedRows = 16;
 
 // Two codes of a dword, nibbles n and n + 4, as bf16 16 + code: moved to bits 3..6 of
 // each half, under the exponent of 16.  The two constants are kept in registers
@@ -532,10 +532,9 @@ struct Flag {
 // are stored, are eight bf16 numbers (o_g, s_g), and the other operand holds
 // sum(q_g) and what takes the operands' 16 out again, -16 sum(q_g), each split into
 // three bf16 terms (24 bits) over three of its four octets.
-template <int D, int NT, bool F32>
-__global__ __launch_bounds__(kPagedWaves * 64, NT == 1 || D == 64 ? 2 : 1) void paged_attention_kernel(
-    const PagedAttnArgs a) {
-  constexpr int G = D / 32, NC = D / 16, S = F32 ? 3 : 1, R = 16 * NT;
+template <int D, bool F32>
+__global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_attention_kernel(const PagedAttnArgs a) {
+  constexpr int G = D / 32, NC = D / 16, S = F32 ? 3 : 1, R = kPagedRows;
   constexpr int NW = kPagedWaves;
   typedef Stage<D> St;
   constexpr int WB = 64 * G * 2;  // floats a wave: scales and offsets [role][G][32]
@@ -590,59 +589,46 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 || D == 64 ? 2 : 1) void 
   };
   // the queries and the first block on their way before either is used
   typedef uint32_t QRaw[F32 ? 8 : 4];
-  QRaw raw_q[NT][G];
-  int last[NT];
-  const long long q0 = seq_at(it.b, it.row0, a.io.q_sb, a.io.q_st);
+  QRaw raw_q[G];
+  const int r = min(row0 + col, n_rows - 1);
+  const int token = divide(r, s.by_g), head = it.h * s.G + r - token * s.G;
+  const int last = last_key(s, it, token);
+  const uint8_t* row = static_cast<const uint8_t*>(a.io.q) +
+                       (seq_at(it.b, it.row0, a.io.q_sb, a.io.q_st) + token * a.io.q_st + head * a.io.q_sh) *
+                           (F32 ? 4 : 2);
 #pragma unroll
-  for (int x = 0; x < NT; ++x) {
-    const int r = min(row0 + 16 * x + col, n_rows - 1);
-    const int token = divide(r, s.by_g), head = it.h * s.G + r - token * s.G;
-    last[x] = last_key(s, it, token);
-    const long long at = q0 + token * a.io.q_st + head * a.io.q_sh;
-    const uint8_t* row = static_cast<const uint8_t*>(a.io.q) + at * (F32 ? 4 : 2);
-#pragma unroll
-    for (int y = 0; y < G; ++y) load_dwords<F32 ? 8 : 4>(row + (32 * y + 8 * m4) * (F32 ? 4 : 2), raw_q[x][y]);
-  }
+  for (int y = 0; y < G; ++y) load_dwords<F32 ? 8 : 4>(row + (32 * y + 8 * m4) * (F32 ? 4 : 2), raw_q[y]);
   fill(0, 0);
   fill(1, 1);
 
-  bf16x8 q[NT][S][G];
-  bf16x8 qo[NT];   // against the words
+  bf16x8 q[S][G];
+  bf16x8 qo = {};  // against the words
 #pragma unroll
-  for (int x = 0; x < NT; ++x) {
-    qo[x] = bf16x8{};
+  for (int y = 0; y < G; ++y) {
+    float sum = 0.0f;
 #pragma unroll
-    for (int y = 0; y < G; ++y) {
-      float sum = 0.0f;
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t w = raw_q[y][F32 ? e : e / 2];
+      const float f = __builtin_bit_cast(float, F32 ? w : e & 1 ? w & 0xffff0000u : w << 16);
+      sum += f;
+      float p[S];
+      split<S>(f, p);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t w = raw_q[x][y][F32 ? e : e / 2];
-        const float f = __builtin_bit_cast(float, F32 ? w : e & 1 ? w & 0xffff0000u : w << 16);
-        sum += f;
-        float p[S];
-        split<S>(f, p);
-#pragma unroll
-        for (int z = 0; z < S; ++z) q[x][z][y][e < 4 ? 2 * e : 2 * (e - 4) + 1] = (__bf16)p[z];
-      }
-      sum = add_xor32(add_xor16(sum));
-      float p[3];
-      split<3>(sum, p);
-      const float mine = m4 == 0 ? p[0] : m4 == 1 ? p[1] : m4 == 2 ? p[2] : 0.0f;
-      qo[x][2 * y] = (__bf16)mine;
-      qo[x][2 * y + 1] = (__bf16)(mine * (F32 ? 8.0f : -16.0f));
+      for (int z = 0; z < S; ++z) q[z][y][e < 4 ? 2 * e : 2 * (e - 4) + 1] = (__bf16)p[z];
     }
+    sum = add_xor32(add_xor16(sum));
+    float p[3];
+    split<3>(sum, p);
+    const float mine = m4 == 0 ? p[0] : m4 == 1 ? p[1] : m4 == 2 ? p[2] : 0.0f;
+    qo[2 * y] = (__bf16)mine;
+    qo[2 * y + 1] = (__bf16)(mine * (F32 ? 8.0f : -16.0f));
   }
 
   const Codes codes;
-  f32x4 o[NT][NC] = {};    // sum of (p s) times the operand: row col, channels 16 n + 4 m4 + i
-  f32x4 ps[NT][G] = {};    // sum of the rounded p s
-  float po[NT][G] = {};    // sum of p times the offset, over the lane's tokens
-  float m[NT], l[NT];
-#pragma unroll
-  for (int x = 0; x < NT; ++x) {
-    m[x] = kNoMax;
-    l[x] = 0.0f;
-  }
+  f32x4 o[NC] = {};    // sum of (p s) times the operand: row col, channels 16 n + 4 m4 + i
+  f32x4 ps[G] = {};    // sum of the rounded p s
+  float po[G] = {};    // sum of p times the offset, over the lane's tokens
+  float m = kNoMax, l = 0.0f;
 
   // masked: some row of the tile does not see all of the block's tokens, or it is a hole
   auto block = [&](auto masked, const Block<D>& x, int t0, bool in) {
@@ -660,7 +646,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 || D == 64 ? 2 : 1) void 
     }
     __builtin_amdgcn_wave_barrier();
 
-    float p[NT][8];
+    float p[8];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       union {
@@ -669,60 +655,49 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 || D == 64 ? 2 : 1) void 
       } wk = {{0, 0, 0, 0}};
 #pragma unroll
       for (int y = 0; y < G; ++y) wk.d[y] = x.wk[u][y];
-      f32x4 v[NT];
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-        v[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wk.v, qo[n], f32x4{}, 0, 0, 0);
+      f32x4 v = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wk.v, qo, f32x4{}, 0, 0, 0);
 #pragma unroll
       for (int y = 0; y < G; ++y) {
         const bf16x8 kc = codes.operand<F32>(x.key(u, y));
         const f32x4 ks = *reinterpret_cast<const f32x4*>(sc + 32 * y + 16 * u + 4 * m4);
+        f32x4 d = {};
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          f32x4 d = {};
+        for (int z = 0; z < S; ++z)
+          d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kc, q[z][y], d, 0, 0, 0);
 #pragma unroll
-          for (int z = 0; z < S; ++z)
-            d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kc, q[n][z][y], d, 0, 0, 0);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[n][i] = fmaf(ks[i], d[i], v[n][i]);
-        }
+        for (int i = 0; i < 4; ++i) v[i] = fmaf(ks[i], d[i], v[i]);
       }
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[n][4 * u + i] = v[n][i];
+      for (int i = 0; i < 4; ++i) p[4 * u + i] = v[i];
     }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      if (M) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int k = t0 + 16 * (i >> 2) + 4 * m4 + (i & 3);
-          if (!in || k > last[n] || k >= hi) p[n][i] = -INFINITY;
-        }
-      }
-      float mx = p[n][0];
-#pragma unroll
-      for (int i = 1; i < 8; ++i) mx = fmaxf(mx, p[n][i]);
-      mx = max_xor32(max_xor16(mx)) * c;
-      if (__any(mx > m[n] + kRaise)) {
-        const float nm = mx > m[n] + kRaise ? mx : m[n];  // (each row by its own scores alone)
-        const float f = __builtin_amdgcn_exp2f(m[n] - nm);
-        m[n] = nm;
-        l[n] *= f;
-#pragma unroll
-        for (int y = 0; y < NC; ++y) o[n][y] *= f;
-#pragma unroll
-        for (int y = 0; y < G; ++y) {
-          if (!F32) ps[n][y] *= f;
-          po[n][y] *= f;
-        }
-      }
+    if (M) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        p[n][i] = __builtin_amdgcn_exp2f(fmaf(p[n][i], c, -m[n]));
-        l[n] += p[n][i];
+        const int k = t0 + 16 * (i >> 2) + 4 * m4 + (i & 3);
+        if (!in || k > last || k >= hi) p[i] = -INFINITY;
       }
+    }
+    float mx = p[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) mx = fmaxf(mx, p[i]);
+    mx = max_xor32(max_xor16(mx)) * c;
+    if (__any(mx > m + kRaise)) {
+      const float nm = mx > m + kRaise ? mx : m;  // (each row by its own scores alone)
+      const float f = __builtin_amdgcn_exp2f(m - nm);
+      m = nm;
+      l *= f;
+#pragma unroll
+      for (int y = 0; y < NC; ++y) o[y] *= f;
+#pragma unroll
+      for (int y = 0; y < G; ++y) {
+        if (!F32) ps[y] *= f;
+        po[y] *= f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], c, -m));
+      l += p[i];
     }
 
     const bf16x8 one = {(__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f,
@@ -736,37 +711,34 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 || D == 64 ? 2 : 1) void 
         zs[u] = *reinterpret_cast<const f32x4*>(sc + 32 * G + 32 * y + 16 * u + 4 * m4);
         zo[u] = *reinterpret_cast<const f32x4*>(of + 32 * G + 32 * y + 16 * u + 4 * m4);
       }
+      float f[8], sum = po[y];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        float f[8], sum = po[n][y];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          f[i] = p[n][i] * zs[i >> 2][i & 3];
-          if (M) {
-            // what a row does not see has weight 0, and may be NaN
-            const bool seen = t0 + 16 * (i >> 2) + 4 * m4 + (i & 3) <= last[n];
-            f[i] = seen ? f[i] : 0.0f;
-            sum = seen ? fmaf(p[n][i], zo[i >> 2][i & 3], sum) : sum;
-          } else {
-            sum = fmaf(p[n][i], zo[i >> 2][i & 3], sum);
-          }
+      for (int i = 0; i < 8; ++i) {
+        f[i] = p[i] * zs[i >> 2][i & 3];
+        if (M) {
+          // what a row does not see has weight 0, and may be NaN
+          const bool seen = t0 + 16 * (i >> 2) + 4 * m4 + (i & 3) <= last;
+          f[i] = seen ? f[i] : 0.0f;
+          sum = seen ? fmaf(p[i], zo[i >> 2][i & 3], sum) : sum;
+        } else {
+          sum = fmaf(p[i], zo[i >> 2][i & 3], sum);
         }
-        po[n][y] = sum;
-        float w[8][S];
+      }
+      po[y] = sum;
+      float w[8][S];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) split<S>(f[i], w[i]);
+      for (int i = 0; i < 8; ++i) split<S>(f[i], w[i]);
 #pragma unroll
-        for (int z = 0; z < S; ++z) {
-          union {
-            uint32_t u[4];
-            bf16x8 v;
-          } pw;
+      for (int z = 0; z < S; ++z) {
+        union {
+          uint32_t u[4];
+          bf16x8 v;
+        } pw;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) pw.u[i] = pack_bf16(w[i][z], w[4 + i][z]);
-          if (!F32) ps[n][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, pw.v, ps[n][y], 0, 0, 0);
-          o[n][2 * y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pw.v, o[n][2 * y], 0, 0, 0);
-          o[n][2 * y + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pw.v, o[n][2 * y + 1], 0, 0, 0);
-        }
+        for (int i = 0; i < 4; ++i) pw.u[i] = pack_bf16(w[i][z], w[4 + i][z]);
+        if (!F32) ps[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, pw.v, ps[y], 0, 0, 0);
+        o[2 * y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pw.v, o[2 * y], 0, 0, 0);
+        o[2 * y + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pw.v, o[2 * y + 1], 0, 0, 0);
       }
     }
   };
@@ -799,56 +771,51 @@ __global__ __launch_bounds__(kPagedWaves * 64, NT == 1 || D == 64 ? 2 : 1) void 
 
   // the lane's rows: out of the codes' 16 (with the 8 of the moved offsets), the
   // offsets of all lanes' tokens
+  l = add_xor32(add_xor16(l));
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    l[n] = add_xor32(add_xor16(l[n]));
+  for (int y = 0; y < G; ++y) {
+    const float x = add_xor32(add_xor16(po[y]));
 #pragma unroll
-    for (int y = 0; y < G; ++y) {
-      const float x = add_xor32(add_xor16(po[n][y]));
+    for (int z = 0; z < 2; ++z)
 #pragma unroll
-      for (int z = 0; z < 2; ++z)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[n][2 * y + z][i] += F32 ? x : fmaf(-24.0f, ps[n][y][i], x);
-    }
-    if (m4 == 0) {
-      sm[wave][16 * n + col] = m[n];
-      sl[wave][16 * n + col] = l[n];
-    }
+      for (int i = 0; i < 4; ++i) o[2 * y + z][i] += F32 ? x : fmaf(-24.0f, ps[y][i], x);
+  }
+  if (m4 == 0) {
+    sm[wave][col] = m;
+    sl[wave][col] = l;
   }
   __syncthreads();
   f32x4* sums = reinterpret_cast<f32x4*>(stages);
+  float mm = sm[0][col];
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int r = 16 * n + col;
-    float mm = sm[0][r];
+  for (int x = 1; x < NW; ++x) mm = fmaxf(mm, sm[x][col]);
+  const float f = __builtin_amdgcn_exp2f(m - mm);
 #pragma unroll
-    for (int x = 1; x < NW; ++x) mm = fmaxf(mm, sm[x][r]);
-    const float f = __builtin_amdgcn_exp2f(m[n] - mm);
-#pragma unroll
-    for (int y = 0; y < NC; ++y) sums[sum_slot<R, D>(wave, r, 4 * y + m4)] = o[n][y] * f;
-  }
+  for (int y = 0; y < NC; ++y) sums[sum_slot<R, D>(wave, col, 4 * y + m4)] = o[y] * f;
   __syncthreads();
   write_joined<R, D, NW, F32>(a.io, s, it, row0, sums, sm, sl);
 }
 
 template <int D>
-hipError_t launch(int dtype, const AttnShape& sh, const PagedAttnArgs& a, hipStream_t st) {
+hipError_t launch(int dtype, const PagedAttnArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)(a.s.n_items * a.s.H));
   const int threads = kPagedWaves * 64;
-  if (dtype == HF_F32) {
-    if (sh.rows == 16) paged_attention_kernel<D, 1, true><<<grid, threads, 0, st>>>(a);
-    else paged_attention_kernel<D, 2, true><<<grid, threads, 0, st>>>(a);
-  } else {
-    if (sh.rows == 16) paged_attention_kernel<D, 1, false><<<grid, threads, 0, st>>>(a);
-    else paged_attention_kernel<D, 2, false><<<grid, threads, 0, st>>>(a);
-  }
+  if (dtype == HF_F32)
+    paged_attention_kernel<D, true><<<grid, threads, 0, st>>>(a);
+  else
+    paged_attention_kernel<D, false><<<grid, threads, 0, st>>>(a);
   return hipGetLastError();
 }
 
-// Heads a workgroup: with many blocks to do all of them, so that the angles of a
-// block are formed once.
+// Heads a workgroup, one or four: four where there are so many blocks that one launch's
+// workgroups come and go many times, and where a block's angles are worth sharing.
+// Measured with one and with four, us, rows of 8 heads of 128 in bf16, append and read:
+// 10 layers of 7,282 tokens 94 + 69 and 100 + 67, 20 layers 204 + 152 and 178 + 134,
+// 40 layers 408 + 308 and 363 + 283; rotated, one layer of 2,000 tokens 7.5 and 8.0, of
+// 8,000 18.9 and 16.4, of 30,000 64 and 46.
 int heads_per_workgroup(const PagedRowsArgs& a) {
-  return (int64_t)a.n_blocks * a.n_layers * a.H >= 4096 ? a.H : 1;
+  const int64_t heads = (int64_t)a.n_blocks * a.n_layers * a.H;
+  return heads >= (a.rotate ? 1024 : 32768) ? kHeads : 1;
 }
 
 template <class T, int D>
@@ -861,20 +828,22 @@ void append(dim3 grid, const PagedRowsArgs& a, int hpw, hipStream_t s) {
 
 }  // namespace
 
-AttnShape paged_shape(int dtype, int d_h, int64_t max_rows) {
+// Times as measured with two workgroups a CU, parts of 128 to 7,296 tokens.
+AttnShape paged_shape(int dtype, int d_h) {
   AttnShape sh;
-  sh.rows = max_rows <= 16 ? 16 : 32;
+  const bool f32 = dtype == HF_F32, wide = d_h == 128;
+  sh.rows = kPagedRows;
   sh.by_keys = 1;
   sh.resident = 1;
   sh.wg_target = 512;
   sh.step = 32 * kPagedWaves;
-  sh.ns_key = d_h == 128 ? 16 : 10;
+  sh.ns_start = f32 ? (wide ? 10000 : 3000) : wide ? 6000 : 4800;
+  sh.ns_key = f32 ? (wide ? 33 : 21) : wide ? 16 : 11;
   return sh;
 }
 
-hipError_t launch_paged_attention(int dtype, int d_h, const AttnShape& sh, const PagedAttnArgs& a,
-                                  hipStream_t s) {
-  return d_h == 128 ? launch<128>(dtype, sh, a, s) : launch<64>(dtype, sh, a, s);
+hipError_t launch_paged_attention(int dtype, int d_h, const PagedAttnArgs& a, hipStream_t s) {
+  return d_h == 128 ? launch<128>(dtype, a, s) : launch<64>(dtype, a, s);
 }
 
 hipError_t launch_paged_append(int dtype, int d_h, const PagedRowsArgs& a0, hipStream_t s) {

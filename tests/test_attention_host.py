@@ -144,17 +144,28 @@ def test_sizes(L):
         assert f(*bad) == 0
 
 
-def test_every_cut_covers_the_keys(L):
-    """The workspace a call asks for is that of its own plan: random lengths with less
-    memory than asked for are refused, with as much as asked for are not."""
+def test_workspaces_are_those_of_the_plan(L):
+    """Random lengths: with the bytes that a call asks for it passes the workspace check,
+    causal or not (and is refused for its row stride, which is looked at after that); with
+    less it does not, causal or not."""
     rng = np.random.default_rng(0)
+    far = _rows(st=(1 << 23) + 8)
+    cut = 0
     for _ in range(200):
         B = int(rng.integers(1, 9))
         q_len = [int(x) for x in rng.integers(1, [2, 40, 3000][int(rng.integers(3))], size=B)]
         kv = [int(x) for x in rng.integers(0, [50, 3000, 100000][int(rng.integers(3))], size=B)]
         need = hf.hf_attention_workspace_bytes(q_len, kv, 32, 8, 128, hf.HF_BF16)
-        if need:   # a workspace without its alignment comes back as such, past the size check
-            assert _prompt(L, B=B, q_len=q_len, kv_len=kv, ws=FAKE + 128, wsb=need) in (SHAPE,)
+        call = lambda ws, n, causal: L.hf_prompt_attention(  # noqa: E731
+            B, _i(*q_len), _i(*kv), _rows(32), far, far, _rows(32), 0.1, causal, None, ws, n, None)
+        for causal in (0, 1):
+            assert call(FAKE, need, causal) == UNSUPPORTED
+        if need:
+            cut += 1
+            assert CAPACITY in [call(FAKE, need - 256, causal) for causal in (0, 1)]
+            assert SHAPE in [call(FAKE + 128, need, causal) for causal in (0, 1)]
+            assert NULL in [call(None, 0, causal) for causal in (0, 1)]
+    assert 20 < cut < 180
 
 
 def test_binding_refuses(L):
