@@ -809,7 +809,7 @@ struct Cut {
 Cut cut_keys(const hf::AttnShape& sh, int32_t B, const int32_t* q_len, const int32_t* kv_len,
              int32_t G, int32_t H, int32_t d_h, bool causal) {
   constexpr int64_t kJoin = 5000;     // ns of a second launch
-  constexpr int64_t kBytesNs = 6000;  // that the join moves in a ns (parts lie in the L2s)
+  constexpr int64_t kBytesNs = 4000;  // that the join moves in a ns (parts lie in the L2s)
   int64_t longest = 1, rows = 0, seen = 0;
   int64_t of_seq[HF_MAX_BATCH];
   bool triangular = causal;

@@ -36,6 +36,22 @@ namespace {
 // Operand layouts of one wave's tile: RW query rows against KT keys.
 // ---------------------------------------------------------------------------
 
+// The order of a block's LDS reads and matrix instructions: AHEAD of N steps of R reads
+// each first, then one step's instruction and a later step's reads in turn.  Left to
+// itself the compiler waits for most reads right after it issues them: prompts of 8,192
+// tokens with heads of 128 519 us, with 4 steps ahead 505; of 5,000 with heads of 64 139,
+// with 2 ahead 134 (with 4 ahead 139.5, for want of reads).
+template <int AHEAD, int R, int N>
+FI void reads_ahead() {
+  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * R, 0);
+#pragma unroll
+  for (int i = 0; i < N - AHEAD; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+}
+
 // bf16 on v_mfma_f32_32x32x16_bf16: lane l is row l % 32; with h = l / 32, result
 // register i of a 32-key block is key 8 (i / 4) + 4 h + i % 4, and of a 32-channel
 // block the channel of that number.
@@ -45,6 +61,7 @@ struct Bf16Tile {
   static constexpr int RW = 32;
   static constexpr int NS = KT / 2, NO = D / 2;  // score and output registers
   static constexpr int ROWB = D * 2;             // bytes of a row
+  static constexpr int AHEAD = D == 128 ? 4 : 2;
   typedef uint16_t T;
   struct Q {
     bf16x8 f[D / 16];
@@ -87,6 +104,7 @@ struct Bf16Tile {
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[16 * kb + i] = acc[i];
     }
+    reads_ahead<AHEAD, 1, KT / 32 * D / 16>();
   }
 
   typedef f32x16 O[D / 32];
@@ -125,6 +143,7 @@ struct Bf16Tile {
         o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, o[n], 0, 0, 0);
       }
     }
+    if (!CLEAN) reads_ahead<AHEAD, 2, KT / 16 * D / 32>();
   }
 
   FI static float value_at(const unsigned char* sv, int r, int ch) {
@@ -336,25 +355,10 @@ struct Fetch {
   }
 };
 
-// The result of a finished row r, or its part.
+// The part of row r.
 template <class P>
-FI void write_row(const AttnIO& io, const AttnSeqs& s, const AttnItem& it, int r, float m, float l,
-                  const typename P::O& o, int lane) {
-  typedef typename P::T T;
-  if (it.parts == 1) {
-    const int token = divide(r, s.by_g), head = it.h * s.G + r - token * s.G;
-    const float inv = inverse_weight(l);
-    T* out = static_cast<T*>(io.out) + out_at(io, s, it, token, head);
-#pragma unroll
-    for (int i = 0; i < P::NO; i += 4) {
-      float x[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = P::get(o, i + j) * inv;
-      P::store4(out + P::channel(lane, i), x);
-    }
-    if (lane < P::RW) write_lse(io, s, it, token, head, m, l);
-    return;
-  }
+FI void write_part(const AttnIO& io, const AttnItem& it, int r, float m, float l, const typename P::O& o,
+                   int lane) {
   const long long slot = part_slot(it, r);
   float* po = io.part + slot * P::D;
 #pragma unroll
@@ -365,6 +369,52 @@ FI void write_row(const AttnIO& io, const AttnSeqs& s, const AttnItem& it, int r
   if (lane < P::RW) {
     io.ml[2 * slot] = m;
     io.ml[2 * slot + 1] = l;
+  }
+}
+
+// The results of a wave's finished rows.  In bf16 through RW rows of LDS of its own: a
+// lane holds four channels of its row, 8 bytes, and written from there an instruction
+// would touch 32 rows (a packed batch of six prompts 241 and like this 236 us; 256 queries
+// over 300 keys each 47.8 and 43.9).  In fp32 an instruction writes 64 bytes of a row
+// anyway, and the detour costs 2%.
+// 16-byte chunk c of row r lies at c ^ (r % 16) (r % 8 in rows of 8 chunks).
+template <class P>
+FI void write_rows(const AttnIO& io, const AttnSeqs& s, const AttnItem& it, int row0, float m, float l,
+                   const typename P::O& o, unsigned char* lds, int lane) {
+  typedef typename P::T T;
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int CPR = P::ROWB / 16, EPC = 16 / sizeof(T);
+  auto slot = [](int r, int c) { return r * P::ROWB + (c ^ (r & (CPR < 16 ? CPR - 1 : 15))) * 16; };
+  auto place = [&](int r) {
+    const int token = divide(r, s.by_g), head = it.h * s.G + r - token * s.G;
+    return static_cast<T*>(io.out) + out_at(io, s, it, token, head);
+  };
+  const int mine = P::row(lane);
+  const bool on = row0 + mine < it.rows;
+  const float inv = inverse_weight(l);
+  T* out = F32 && on ? place(row0 + mine) : nullptr;
+#pragma unroll
+  for (int i = 0; i < P::NO; i += 4) {
+    const int ch = P::channel(lane, i);
+    float x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = P::get(o, i + j) * inv;
+    if (!F32)
+      P::store4(reinterpret_cast<T*>(lds + slot(mine, ch / EPC)) + ch % EPC, x);
+    else if (on)
+      P::store4(out + ch, x);
+  }
+  if (lane < P::RW && on) {
+    const int token = divide(row0 + mine, s.by_g), head = it.h * s.G + row0 + mine - token * s.G;
+    write_lse(io, s, it, token, head, m, l);
+  }
+  if (F32) return;
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int i = 0; i < P::RW * CPR / 64; ++i) {
+    const int rl = i * (64 / CPR) + lane / CPR, c = lane % CPR;
+    const u32x4 v = *reinterpret_cast<const u32x4*>(lds + slot(rl, c));
+    if (row0 + rl < it.rows) *reinterpret_cast<u32x4*>(place(row0 + rl) + c * EPC) = v;
   }
 }
 
@@ -413,7 +463,6 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_rows_kernel(const AttnAr
   const int t = it.t, n_rows = it.rows;
   const int row0 = it.tile * NW * WR, my0 = row0 + wave * WR;
   Rows<P> w;
-  load_row<P>(w, a, it, my0 + P::row(lane), lane);
 
   // keys of this part that some row of the workgroup sees, and that all of them see
   const int wg_last = last_key(s, it, divide(min(row0 + NW * WR - 1, n_rows - 1), s.by_g));
@@ -462,14 +511,20 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_rows_kernel(const AttnAr
     if (t0 <= wave_last) finish<P, true>(w, s, sv, lane, c, t0, careful);
     if (t0 + KT <= wave_last && t0 + KT < hi) P::scores(w.q, nk, lane, s);
   };
+  // what the first two steps need is on its way at once
+  auto get_first = [&]() {
+    get_k(lo, k0);
+    get_v(lo, v0);
+    get_k(lo + KT, k1);
+  };
+  get_first();
+  load_row<P>(w, a, it, my0 + P::row(lane), lane);
   for (;;) {
     clear_row<P>(w);
     if (lo < hi) {
       Scores s0, s1;
-      get_k(lo, k0);
+      if (careful) get_first();
       ready();
-      get_k(lo + KT, k1);
-      get_v(lo, v0);
       P::scores(w.q, k0, lane, s0);
       // pairs of tiles that every row sees whole, with a tile after them
       int t0 = lo;
@@ -485,9 +540,16 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_rows_kernel(const AttnAr
     if (careful || !__syncthreads_or(not_finite(w))) break;
     careful = true;
   }
-  const int r = my0 + P::row(lane);
   const float l = P::row_sum(w.l);
-  if (r < n_rows) write_row<P>(a.io, s, it, r, w.m, l, w.o, lane);
+  if (it.parts > 1) {
+    const int r = my0 + P::row(lane);
+    if (r < n_rows) write_part<P>(a.io, it, r, w.m, l, w.o, lane);
+    return;
+  }
+  // (no wave reads keys or values any more: the loop ended with a barrier)
+  static_assert(NW % 4 == 0 && NW / 4 * WR * P::ROWB <= KT * P::ROWB, "rows in the stages");
+  unsigned char* mine = (wave & 3) == 0 ? k0 : (wave & 3) == 1 ? v0 : (wave & 3) == 2 ? k1 : v1;
+  write_rows<P>(a.io, s, it, my0, w.m, l, w.o, mine + wave / 4 * WR * P::ROWB, lane);
 }
 
 // By keys: one block of RW rows, the tiles of keys dealt to NW waves.
