@@ -14,18 +14,17 @@
 // Keys and values stream through two LDS stages filled by global-to-LDS loads, the
 // next tile's in flight while the current one is multiplied.
 //
-// Two kernel shapes, chosen by the number of query rows (prompt_shape):
+// Two kernel shapes; a call takes the faster one by their measured times (prompt_shape
+// holds them, the call's planning compares):
 //  - by rows: the waves of a workgroup share a tile of keys, each with query rows
 //    of its own;
 //  - by keys: the waves share the rows (one block) and deal the tiles of keys among
 //    them, each with LDS stages of its own and no barrier in the loop; their
-//    results are joined in LDS at the end.  For single tokens and short runs, which
-//    the reading of the keys bounds.
+//    results are joined in LDS at the end.  For single tokens and short runs and
+//    prompts, which the reading of the keys or the latency of a few tiles bounds.
 // Where the workgroups are too few to fill the chip the key range is cut into parts
 // as well, joined by attention_join_kernel.
 #include <hip/hip_runtime.h>
-
-#include <algorithm>
 
 #include "hf_attn.h"
 
@@ -445,6 +444,16 @@ struct Flag {
 // By rows: NW waves, each with RW rows of the tile, all against the same keys.  A wave
 // computes the scores of the next tile before it finishes this one's, so
 // that matrix instructions and the softmax's are there to be issued side by side.
+// Bound by the matrix cores and the softmax's instructions beside them: causal prompts of
+// 32 heads of 128 on 8, 8,192 tokens in 505 us (1.09 PFLOP/s; a library product of 8192^3
+// reaches 1.14 on the same card) and 16,000 in 1,861 (1.13); 14 fp32 heads of 64, 2,001
+// tokens, in 87 (83 TFLOP/s: its longest tile alone takes that; 3,001 tokens of 32 heads of
+// 128 reach 113 of the 153 that a library product does).
+// Eight waves and one workgroup a CU in bf16: with 64 rows a wave the registers spill (777
+// against 540 us for 8,192 tokens), with four waves and two workgroups a CU the tiles are
+// loaded twice (701 against 588), and waves started half a tile apart, given
+// priority in turn or held back between the products gained nothing (600, 568, 565 against
+// 540).  In fp32 four waves and up to four workgroups a CU.
 template <class P, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void attention_rows_kernel(const AttnArgs a) {
   typedef typename P::T T;
@@ -552,7 +561,12 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_rows_kernel(const AttnAr
   write_rows<P>(a.io, s, it, my0, w.m, l, w.o, mine + wave / 4 * WR * P::ROWB, lane);
 }
 
-// By keys: one block of RW rows, the tiles of keys dealt to NW waves.
+// By keys: one block of RW rows, the tiles of keys dealt to NW waves.  Bound by HBM for
+// one block of rows: a token of 32 heads on 8 of 128 over 29K keys 23 us (5.2 TB/s), four
+// over 12K keys together 14.9 and 3.9 us for the join; for few keys by the latency of the
+// loads that follow each other (8.6 us for a prompt of 100 tokens).  Tiles of 32 keys: two
+// stages of four waves fill 128 KB of LDS (fp32 rows of 128 channels are twice as long, and
+// take 16).
 template <class P, int NW>
 __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs a) {
   typedef typename P::T T;
@@ -654,7 +668,8 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
 // The parts of split rows: out = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p.
 // A row has D / 4 threads of four channels for every SL-th part, so that its parts are
 // loaded at the same time: one wave a row, part after part, took 19 us for 57 parts of
-// 40 rows, this takes 4.5.  With few parts a workgroup takes several rows.
+// 40 rows, this takes 4.9.  Bound by a launch's time with few rows, by the parts' bytes with
+// many (31 MB in 9.5 us).
 // ---------------------------------------------------------------------------
 struct JoinArgs {
   AttnIO io;
@@ -744,12 +759,14 @@ void join_by(const JoinArgs& a, hipStream_t st) {
   constexpr int NR = 256 / (D / 4 * SL);
   attention_join_kernel<F32, D, SL><<<(unsigned)((a.s.n_split + NR - 1) / NR), 256, 0, st>>>(a);
 }
+// With few rows eight threads of a channel share its parts, with many, which fill the chip
+// anyway, as few as make a wave a row's.  Measured with eight and with two, us, d_h 128: 40
+// rows of 57 parts 4.9 and 7.0, 448 rows of 17 parts 3.9 and 4.4; 5,120 rows of 4 parts 7.5
+// and 5.4, 10,240 of 6 parts 10.7 and 9.5.
 template <bool F32, int D>
-void join(const JoinArgs& a, int most_parts, hipStream_t st) {
-  if (most_parts > 4)
+void join(const JoinArgs& a, hipStream_t st) {
+  if (a.s.n_split < 1024)
     join_by<F32, D, 8>(a, st);
-  else if (D == 128 && most_parts > 2)
-    join_by<F32, D, 4>(a, st);
   else
     join_by<F32, D, 256 / D>(a, st);
 }
@@ -786,12 +803,10 @@ hipError_t launch_prompt_attention(int dtype, int d_h, const AttnShape& sh, cons
 hipError_t launch_attention_join(int dtype, int d_h, const AttnIO& io, const AttnSeqs& s,
                                  hipStream_t st) {
   JoinArgs a{io, s};
-  int most = 0;
-  for (int b = 0; b < s.B; ++b) most = std::max(most, s.q[b].parts);
   if (dtype == HF_F32)
-    d_h == 128 ? join<true, 128>(a, most, st) : join<true, 64>(a, most, st);
+    d_h == 128 ? join<true, 128>(a, st) : join<true, 64>(a, st);
   else
-    d_h == 128 ? join<false, 128>(a, most, st) : join<false, 64>(a, most, st);
+    d_h == 128 ? join<false, 128>(a, st) : join<false, 64>(a, st);
   return hipGetLastError();
 }
 

@@ -191,7 +191,8 @@ FI void transpose_nibbles(uint32_t (&a)[8]) {
 // cos and sin of pos * w_k for the block's 32 positions, to LDS [32][D/2], fp64
 // angles rounded once.  Four chains a channel pair, eight positions each: one sine
 // and cosine at the chain's first position, then a complex product with the step's
-// (error 8 * 2^-53).  A block with up to four tokens computes just theirs.
+// (error 8 * 2^-53).  A block with up to four tokens computes just theirs, one chain's
+// step a thread.
 template <int D>
 FI void fill_angles(const PagedRowsArgs& a, const RowItem& it, float2* cs) {
   constexpr int HD = D / 2;
@@ -219,10 +220,12 @@ FI void fill_angles(const PagedRowsArgs& a, const RowItem& it, float2* cs) {
   }
 }
 
-// A transfer's cache of 40 layers and 7.3K tokens (1.19 GB in, 0.37 GB out) takes
-// 365 us, 4.3 TB/s.  Four heads' rows are loaded at a time.
-// ROT: a call that rotates its keys.  (Their angles take registers that a call which
-// only moves rows would miss for loads in flight: 377 -> 365 us at that size.)
+// Bound by HBM: a transfer's cache of 40 layers and 7.3K tokens (1.19 GB in, 0.37 GB out)
+// takes 336 to 363 us, 4.3 to 4.6 TB/s (a device copy reaches 4.7); a token for each of
+// eight sequences 4.9 us, the latency of its loads one after another.
+// ROT: a call that rotates its keys.  (Their angles take registers and LDS that a call which
+// only moves rows would miss for loads in flight: 377 and 365 us at that size with and
+// without.)
 template <class T, int D, bool ROT>
 __global__ __launch_bounds__(2 * D) void paged_append_kernel(const PagedRowsArgs a, const int hpw) {
   constexpr int TPT = D / 16;  // threads a token
@@ -317,6 +320,8 @@ __global__ __launch_bounds__(2 * D) void paged_append_kernel(const PagedRowsArgs
   }
 }
 
+// The same blocks back; value codes through LDS, whose order is by channels.  Bound by HBM
+// (281 us, 5.5 TB/s, for the cache above).
 template <class T, int D>
 __global__ __launch_bounds__(2 * D) void paged_read_kernel(const PagedRowsArgs a, const int hpw) {
   constexpr int TPT = D / 16;
@@ -523,10 +528,18 @@ struct Flag {
   static constexpr bool value = M;
 };
 
-// Four waves a workgroup (two workgroups a CU with up to 16 rows), blocks of the part
-// dealt to them in turn, the next block's 5 KB in flight.  Per block a wave spends
-// about 130 instructions on taking codes out of dwords, 110 on scales and 60 on the
-// softmax, beside 22 matrix instructions.
+// Four waves a workgroup, two workgroups a CU, blocks of the part dealt to the waves in
+// turn, the next two blocks' 5 KB each in flight.  Per block a wave spends about 130
+// instructions on taking codes out of dwords, 110 on scales and 60 on the softmax, beside
+// 22 matrix instructions; that and HBM bound it together: 29K tokens of 40 heads on 8 of
+// 128 (37 MB) in 16.0 us and 4.9 for the join, 16 sequences of 4 to 8K tokens (64 MB) in
+// 22.2 and 4.0.  One query token over 200 takes 7.5 us, most of it a few loads that need
+// each other (arguments, page, block).
+// Measured and dropped: the next block in registers instead of LDS (17.0 us against 16.3,
+// 25.5 against 22.4 for the 16 sequences); two tiles of 16 rows a workgroup, which read the
+// codes once for both but leave one workgroup a CU (32 rows over 29K tokens 38.2 us against
+// 24.6, 256 rows 174 against 125; d_h 64 within 6% either way); parts for 256, 384 or 1,024
+// workgroups instead of 512 (18.4, 17.8 and 19.5 us against 16.7).
 //
 // The keys' offsets cost a matrix instruction a tile: the words of a token, as they
 // are stored, are eight bf16 numbers (o_g, s_g), and the other operand holds
