@@ -305,9 +305,10 @@ FI bool not_finite(const Rows<P>& w) {
 }
 
 // Loads of one tile (keys t0 .. t0 + KT) into a stage: NB of the tile's 1 KB blocks
-// from block b0 in steps of `bstep`.  Rows past the last key hold copies of it.  The
-// tile's address is in scalar registers, a lane's place in the tile a 32-bit offset
-// (rows lie at most 2^23 elements apart: host check).
+// from block b0 in steps of `bstep`.  The tile's address is in scalar registers, a lane's
+// place in the tile a 32-bit offset (rows lie at most 2^23 elements apart: host check).
+// The buffer ends with the last key: rows past it are not read (what their place in the
+// stage holds is masked), and no lane compares.
 // UNSEEN: as instructions that the compiler does not see as LDS accesses.  By keys it
 // would wait for all loads before it reads a stage, the next tile's in flight among
 // them; the kernel's own waits are what there has to be.
@@ -335,21 +336,16 @@ struct Fetch {
       off[i] = r * (int)st + chunk(r, lane);
     }
   }
-  FI void get(int t0, unsigned char* stage, int b0, int bstep, int lane) const {
+  FI void get(int t0, unsigned char* stage, int b0, int bstep) const {
     const char* tile = base + t0 * st;
-    const bool whole = t0 + P::KT <= t;
+    const int bytes = (int)min((t - 1 - t0) * st + P::ROWB, (long long)INT32_MAX);
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-      int at = off[i];
-      if (!whole) {
-        const int r = row(i, b0, bstep, lane);
-        at = min(r, t - 1 - t0) * (int)st + chunk(r, lane);
-      }
       unsigned char* to = stage + (b0 + i * bstep) * 1024;
       if (UNSEEN)
-        load_lds_unseen(tile, at, to);
+        load_lds_unseen(tile, bytes, off[i], to);
       else
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer_at(tile), (lds_void_t*)to, 16, at, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer_at(tile, bytes), (lds_void_t*)to, 16, off[i], 0, 0, 0);
     }
   }
 };
@@ -489,10 +485,10 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_rows_kernel(const AttnAr
   fv.init(vb, a.v_st, t, wave, NW, lane);
   // nothing past the range's last tile is loaded, or used
   auto get_k = [&](int t0, unsigned char* st) {
-    if (t0 < hi) fk.get(t0, st, wave, NW, lane);
+    if (t0 < hi) fk.get(t0, st, wave, NW);
   };
   auto get_v = [&](int t0, unsigned char* st) {
-    if (t0 < hi) fv.get(t0, st, wave, NW, lane);
+    if (t0 < hi) fv.get(t0, st, wave, NW);
   };
   auto ready = [&]() {  // every wave's loads are there, and no wave reads what is loaded next
     __builtin_amdgcn_s_waitcnt(kWaitMemory);
@@ -596,8 +592,8 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
   fk.init(kb, a.k_st, t, 0, 1, lane);
   fv.init(vb, a.v_st, t, 0, 1, lane);
   auto get = [&](int t0, unsigned char* st) {
-    fk.get(t0, st, 0, 1, lane);
-    fv.get(t0, st + TB, 0, 1, lane);
+    fk.get(t0, st, 0, 1);
+    fv.get(t0, st + TB, 0, 1);
   };
   Rows<P> w;
   bool careful = false;

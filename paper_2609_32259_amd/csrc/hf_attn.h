@@ -39,25 +39,26 @@ constexpr int wait_vm_only(int n) { return (n & 0xF) | ((n >> 4) << 14) | (7 << 
 constexpr int kWaitMemory = 7 << 4;
 constexpr int kWaitLds = 0xF | (3 << 14) | (7 << 4);
 
-// A buffer resource of 2 GiB from a pointer that every lane holds.
-FI __amdgpu_buffer_rsrc_t buffer_at(const void* p) {
+// A buffer resource of `bytes` from a pointer that every lane holds.
+FI __amdgpu_buffer_rsrc_t buffer_at(const void* p, int bytes) {
   const uint64_t v = (uint64_t)p;
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
   const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
-  return __builtin_amdgcn_make_buffer_rsrc((void*)(((uint64_t)hi << 32) | lo), 0, 0x7fffffff, 0x00020000);
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(((uint64_t)hi << 32) | lo), 0, __builtin_amdgcn_readfirstlane(bytes),
+                                           0x00020000);
 }
 
 FI uint32_t lds_addr(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
 
-// A buffer load of 16 bytes a lane from p + off to LDS (to + 16 lane), which the
+// A buffer load of 16 bytes a lane from p + off (within `bytes`) to LDS (to + 16 lane), which the
 // compiler counts neither as a load nor as an LDS access: only explicit waits order it.
-FI void load_lds_unseen(const void* p, int off, void* to) {
+FI void load_lds_unseen(const void* p, int bytes, int off, void* to) {
   const uint64_t v = (uint64_t)p;
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
   const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
-  const u32x4 rsrc = {lo, hi & 0xffffu, 0x7fffffffu, 0x00020000u};
+  const u32x4 rsrc = {lo, hi & 0xffffu, (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
                : "s"(__builtin_amdgcn_readfirstlane(lds_addr(to))), "v"(off), "s"(rsrc)
