@@ -39,7 +39,8 @@ namespace {
 // each first, then one step's instruction and a later step's reads in turn.  Left to
 // itself the compiler waits for most reads right after it issues them: prompts of 8,192
 // tokens with heads of 128 519 us, with 4 steps ahead 505; of 5,000 with heads of 64 139,
-// with 2 ahead 134 (with 4 ahead 139.5, for want of reads).
+// with 2 ahead 134 (with 4 139.5, for want of reads); fp32 prompts of 2,001 tokens with
+// heads of 64 84.0, with 8 reads of values ahead 81.6.
 template <int AHEAD, int R, int N>
 FI void reads_ahead() {
   __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * R, 0);
@@ -224,6 +225,7 @@ struct F32Tile {
         o[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, p[k], o[n], 0, 0, 0);
       }
     }
+    if (!CLEAN) reads_ahead<8, 1, NS * D / 16>();
   }
 
   FI static float value_at(const unsigned char* sv, int r, int ch) {
@@ -441,10 +443,10 @@ struct Flag {
 // computes the scores of the next tile before it finishes this one's, so
 // that matrix instructions and the softmax's are there to be issued side by side.
 // Bound by the matrix cores and the softmax's instructions beside them: causal prompts of
-// 32 heads of 128 on 8, 8,192 tokens in 505 us (1.09 PFLOP/s; a library product of 8192^3
-// reaches 1.14 on the same card) and 16,000 in 1,861 (1.13); 14 fp32 heads of 64, 2,001
-// tokens, in 87 (83 TFLOP/s: its longest tile alone takes that; 3,001 tokens of 32 heads of
-// 128 reach 113 of the 153 that a library product does).
+// 32 heads of 128 on 8, 8,192 tokens in 481 to 516 us, by card (1.07 to 1.14 PFLOP/s; a
+// library product of 8192^3 reaches 1.14); 14 fp32 heads of 64, 2,001 tokens, in 82 (88
+// TFLOP/s: its longest tile alone takes that; 3,001 tokens of 32 heads of 128 reach 127 of
+// the 153 that a library product does).
 // Eight waves and one workgroup a CU in bf16: with 64 rows a wave the registers spill (777
 // against 540 us for 8,192 tokens), with four waves and two workgroups a CU the tiles are
 // loaded twice (701 against 588), and waves started half a tile apart, given
