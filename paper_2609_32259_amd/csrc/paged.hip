@@ -538,7 +538,9 @@ struct Flag {
 // Measured and dropped: the next block in registers instead of LDS (17.0 us against 16.3,
 // 25.5 against 22.4 for the 16 sequences); two tiles of 16 rows a workgroup, which read the
 // codes once for both but leave one workgroup a CU (32 rows over 29K tokens 38.2 us against
-// 24.6, 256 rows 174 against 125; d_h 64 within 6% either way); parts for 256, 384 or 1,024
+// 24.6, 256 rows 174 against 125; d_h 64 within 6% either way); eight waves and one workgroup
+// a CU (29K tokens 17.1 against 16.8 us, 64 sequences of 1,000 29.8 against 24.2, though 32 of
+// 1.5 to 3K 30.5 against 33.8); parts for 256, 384 or 1,024
 // workgroups instead of 512 (18.4, 17.8 and 19.5 us against 16.7).
 //
 // The keys' offsets cost a matrix instruction a tile: the words of a token, as they

@@ -642,14 +642,20 @@ def hf_attention_workspace_bytes(q_len, kv_len, H_q: int, H: int, d_h: int, dtyp
                                                   int(d_h), int(dtype), int(bool(paged))))
 
 
-def _attention_outputs(q, rq, rows, q_len, kv_len, H, paged, scale, out, lse, return_lse,
+def _attention_outputs(q, rq, lq, q_len, kv_len, H, paged, scale, out, lse, return_lse,
                        workspace):
-    """What both attention calls allocate where the caller passes nothing."""
+    """What both attention calls allocate where the caller passes nothing; out's descriptor."""
     torch = _torch()
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        d, st = rq.d_h, out.stride()
+        ro = hf_rows(out.data_ptr(), rq.dtype, rq.H, d, *((-1, 0, d, st[0]) if len(st) == 3 else
+                                                          (st[0], 0, st[1], d)))
     elif out.shape != q.shape:
         raise ValueError("out must have q's shape")
+    else:
+        ro = _head_rows(out, lq, "out", q.device)
+    rows = sum(lq)
     if lse is None:
         if return_lse:
             lse = torch.empty((rows, rq.H), dtype=torch.float32, device=q.device)
@@ -663,7 +669,7 @@ def _attention_outputs(q, rq, rows, q_len, kv_len, H, paged, scale, out, lse, re
             workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
     elif workspace.device != q.device or not workspace.is_contiguous():
         raise TypeError("workspace must be a contiguous CUDA tensor on q's device")
-    return out, lse, workspace, 1.0 / math.sqrt(rq.d_h) if scale is None else float(scale)
+    return out, ro, lse, workspace, 1.0 / math.sqrt(rq.d_h) if scale is None else float(scale)
 
 
 def _ptr(t):
@@ -675,7 +681,8 @@ def hf_prompt_attention(q, k, v, q_len, kv_len=None, causal=True, scale=None, ou
     """Attention of packed query runs q [N, H_q, d_h] over keys and values k, v: packed
     [N_k, H, d_h], or views [B, H, T, d_h] of a cache (``R[:, l, 0]``, ``R[:, l, 1]``).
     q_len, kv_len: lengths [B] (kv_len None: q_len, whole prompts); scale None: 1/sqrt(d_h).
-    Returns out [N, H_q, d_h], with ``return_lse`` (out, lse [N, H_q] fp32)."""
+    Returns out [N, H_q, d_h], with ``return_lse`` (out, lse [sum q_len, H_q] fp32); rows that no
+    length names are not written.  No gradients."""
     nq, lq = _lens(q_len, "q_len")
     nk, lk = (nq, lq) if kv_len is None else _lens(kv_len, "kv_len", len(lq))
     dev = q.device
@@ -685,9 +692,8 @@ def hf_prompt_attention(q, k, v, q_len, kv_len=None, causal=True, scale=None, ou
         rq = _head_rows(q, lq, "q", dev)
         rk = _head_rows(k, lk, "k", dev)
         rv = _head_rows(v, lk, "v", dev)
-        out, lse, workspace, scale = _attention_outputs(q, rq, sum(lq), nq, nk, rk.H, 0, scale, out,
-                                                        lse, return_lse, workspace)
-        ro = _head_rows(out, lq, "out", dev)
+        out, ro, lse, workspace, scale = _attention_outputs(q, rq, lq, nq, nk, rk.H, 0, scale, out,
+                                                            lse, return_lse, workspace)
         st = lib().hf_prompt_attention(
             len(lq), nq, nk, rq, rk, rv, ro, scale, 1 if causal else 0, _ptr(lse),
             _ptr(workspace), 0 if workspace is None else _nbytes(workspace), _raw_stream(dev))
@@ -705,9 +711,8 @@ def hf_paged_attention(q, cache: PagedKV, q_len, kv_len, layer=0, causal=True, s
     dev = cache.pages.device
     with _call_on(dev, stream):
         rq = _head_rows(q, lq, "q", dev)
-        out, lse, workspace, scale = _attention_outputs(q, rq, sum(lq), nq, nk, cache.H, 1, scale,
-                                                        out, lse, return_lse, workspace)
-        ro = _head_rows(out, lq, "out", dev)
+        out, ro, lse, workspace, scale = _attention_outputs(q, rq, lq, nq, nk, cache.H, 1, scale,
+                                                            out, lse, return_lse, workspace)
         st = lib().hf_paged_attention(
             len(lq), nq, nk, rq, cache.desc, int(layer), ro, scale,
             1 if causal else 0, _ptr(lse), _ptr(workspace),
