@@ -647,7 +647,9 @@ def _attention_outputs(q, rq, lq, q_len, kv_len, H, paged, scale, out, lse, retu
     """What both attention calls allocate where the caller passes nothing; out's descriptor."""
     torch = _torch()
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        # (empty_like is the quicker, and keeps the strides of what is contiguous)
+        out = torch.empty_like(q) if q.is_contiguous() else \
+            torch.empty(q.shape, dtype=q.dtype, device=q.device)
         d, st = rq.d_h, out.stride()
         ro = hf_rows(out.data_ptr(), rq.dtype, rq.H, d, *((-1, 0, d, st[0]) if len(st) == 3 else
                                                           (st[0], 0, st[1], d)))
