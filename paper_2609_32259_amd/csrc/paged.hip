@@ -191,26 +191,16 @@ FI void transpose_nibbles(uint32_t (&a)[8]) {
 // cos and sin of pos * w_k for the block's 32 positions, to LDS [32][D/2], fp64
 // angles rounded once.  Four chains a channel pair, eight positions each: one sine
 // and cosine at the chain's first position, then a complex product with the step's
-// (error 8 * 2^-53).  A block with up to four tokens computes just theirs, one chain's
-// step a thread.
+// (error 8 * 2^-53).  (For blocks of one token, forming its angle alone gains nothing: 4.7 us a
+// call either way.)
 template <int D>
 FI void fill_angles(const PagedRowsArgs& a, const RowItem& it, float2* cs) {
   constexpr int HD = D / 2;
   const int k = threadIdx.x % HD, m = threadIdx.x / HD;  // m < 4
   const double w = a.w[k];
-  const double base = (double)it.pos0 + it.tok0;
-  double c, s;
-  if (it.hi - it.lo <= 4) {
-    const int j = it.lo + m;
-    if (j < it.hi) {
-      sincos((base + j) * w, &s, &c);
-      cs[j * HD + k] = make_float2((float)c, (float)s);
-    }
-    return;
-  }
-  double dc, ds;
+  double c, s, dc, ds;
   sincos(w, &ds, &dc);
-  sincos((base + 8 * m) * w, &s, &c);
+  sincos(((double)it.pos0 + it.tok0 + 8 * m) * w, &s, &c);
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     cs[(8 * m + j) * HD + k] = make_float2((float)c, (float)s);
