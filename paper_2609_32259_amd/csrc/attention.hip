@@ -544,7 +544,9 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_rows_kernel(const AttnAr
         if (t0 + KT < hi) masked_step(t0 + KT, s0, k1, v1, k0, v0);
       }
     }
-    if (careful || !__syncthreads_or(not_finite(w))) break;
+    // a barrier in both passes: after it no wave reads keys or values of this pass
+    const bool again = __syncthreads_or(not_finite(w));
+    if (careful || !again) break;
     careful = true;
   }
   const float l = P::row_sum(w.l);
@@ -553,7 +555,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_rows_kernel(const AttnAr
     if (r < n_rows) write_part<P>(a.io, it, r, w.m, l, w.o, lane);
     return;
   }
-  // (no wave reads keys or values any more: the loop ended with a barrier)
+  // (no wave reads keys or values any more: both passes end with a barrier)
   static_assert(NW % 4 == 0 && NW / 4 * WR * P::ROWB <= KT * P::ROWB, "rows in the stages");
   unsigned char* mine = (wave & 3) == 0 ? k0 : (wave & 3) == 1 ? v0 : (wave & 3) == 2 ? k1 : v1;
   write_rows<P>(a.io, s, it, my0, w.m, l, w.o, mine + wave / 4 * WR * P::ROWB, lane);
