@@ -433,7 +433,9 @@ size_t hf_attention_workspace_bytes(int32_t B, const int32_t* q_len, const int32
  * A whole prompt has kv_len == q_len; a suffix over a transferred cache, or one
  * decoded token, has q_len < kv_len.  A row that sees no key (kv_len == 0, or
  * causal with q_len > kv_len) gets out = 0 and lse = -infinity.  What a row does
- * not see has no influence on it, whatever its bits are.
+ * not see has no influence on it, whatever its bits are.  A score of -infinity has
+ * weight 0; a row all of whose scores are that has weights 0/0: out is NaN and lse
+ * -infinity.
  *   q_len, kv_len  host int32 [B], >= 0; kv_len <= 2^30.
  *   q, out    hf_rows of H_q heads; out may be q itself, element for element.
  *   k, v      hf_rows of H heads, H_q % H == 0, stride_t <= 2^23; same dtype and

@@ -298,9 +298,10 @@ FI void finish(Rows<P>& w, float (&s)[P::NS], const unsigned char* sv, int lane,
   }
 }
 
+// Whether a row is to be computed a second time.  saw: it saw a key.
 template <class P>
-FI bool not_finite(const Rows<P>& w) {
-  bool bad = false;
+FI bool second_pass(const Rows<P>& w, bool saw) {
+  bool bad = saw && w.m == kNoMax;
 #pragma unroll
   for (int i = 0; i < P::NO; ++i) bad |= !finite_bits(P::get(w.o, i));
   return bad;
@@ -388,7 +389,7 @@ FI void write_rows(const AttnIO& io, const AttnSeqs& s, const AttnItem& it, int 
   };
   const int mine = P::row(lane);
   const bool on = row0 + mine < it.rows;
-  const float inv = inverse_weight(l);
+  const float inv = inverse_weight(m, l);
   T* out = F32 && on ? place(row0 + mine) : nullptr;
 #pragma unroll
   for (int i = 0; i < P::NO; i += 4) {
@@ -545,11 +546,12 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_rows_kernel(const AttnAr
       }
     }
     // a barrier in both passes: after it no wave reads keys or values of this pass
-    const bool again = __syncthreads_or(not_finite(w));
+    const bool again = __syncthreads_or(second_pass(w, lo < hi && lo <= w.last));
     if (careful || !again) break;
     careful = true;
   }
   const float l = P::row_sum(w.l);
+  if (careful) w.m = end_max(w.m, l, lo < hi && lo <= w.last);
   if (it.parts > 1) {
     const int r = my0 + P::row(lane);
     if (r < n_rows) write_part<P>(a.io, it, r, w.m, l, w.o, lane);
@@ -638,20 +640,21 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
         if (t0 + NW * P::KT < hi) step(t0 + NW * P::KT, w1, w0);
       }
     }
-    if (careful || !__any(not_finite(w))) break;
+    if (careful || !__any(second_pass(w, lo < hi && lo <= w.last))) break;
     careful = true;
   }
 
   const int rl = P::row(lane);
   const float l = P::row_sum(w.l);
+  if (careful) w.m = end_max(w.m, l, lo < hi && lo <= w.last);
   if (lane < P::RW) {
     sm[wave][rl] = w.m;
     sl[wave][rl] = l;
   }
   __syncthreads();
-  float m = sm[0][rl];
+  float m = kNoMax;
 #pragma unroll
-  for (int x = 1; x < NW; ++x) m = fmaxf(m, sm[x][rl]);
+  for (int x = 0; x < NW; ++x) m = fmaxf(m, sm[x][rl]);
   const float f = __builtin_amdgcn_exp2f(w.m - m);
   f32x4* sums = reinterpret_cast<f32x4*>(s0);
   static_assert(NW * P::RW * P::D * 4 <= NW * 2 * TB, "joining buffer");
@@ -695,10 +698,13 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const JoinArgs a) {
   const long long slot = sq.part0 + (long long)i * parts;
   const float* ml = a.io.ml + 2 * slot;
   const float* po = a.io.part + slot * D + 4 * c;
-  float m = kNoMax, l = 0.0f;
+  float m = kNoMax, least = kNoMax, l = 0.0f;
   f32x4 o = {};
 #pragma unroll 4
-  for (int p = q; p < parts; p += SL) m = fmaxf(m, ml[2 * p]);
+  for (int p = q; p < parts; p += SL) {
+    m = fmaxf(m, ml[2 * p]);
+    least = fminf(least, ml[2 * p]);
+  }
 #pragma unroll 4
   for (int p = q; p < parts; p += SL) {
     const float f = __builtin_amdgcn_exp2f(ml[2 * p] - m);
@@ -708,12 +714,15 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const JoinArgs a) {
   }
   so[rr][q][c] = o;
   if (c == 0) {
-    sm[rr][q] = m;
+    sm[rr][q] = l == 0.0f ? least : m;
     sl[rr][q] = l;
   }
   __syncthreads();
   if (q != 0 || !on) return;
-  for (int x = 1; x < SL; ++x) m = fmaxf(m, sm[rr][x]);
+  for (int x = 0; x < SL; ++x) {
+    m = fmaxf(m, sm[rr][x]);
+    least = fminf(least, sm[rr][x]);
+  }
   o = f32x4{};
   l = 0.0f;
   for (int x = 0; x < SL; ++x) {
@@ -721,10 +730,11 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const JoinArgs a) {
     o += so[rr][x][c] * f;
     l = fmaf(sl[rr][x], f, l);
   }
+  if (l == 0.0f) m = least;
   const int n_rows = sq.n * s.G, h = i / n_rows, r = i - h * n_rows;
   const int token = divide(r, s.by_g), head = h * s.G + r - token * s.G;
   const long long at = out_at(a.io, s, it, token, head) + 4 * c;
-  o *= inverse_weight(l);
+  o *= inverse_weight(m, l);
   if (F32) {
     *reinterpret_cast<f32x4*>(static_cast<float*>(a.io.out) + at) = o;
   } else {

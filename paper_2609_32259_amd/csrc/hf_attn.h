@@ -32,6 +32,11 @@ constexpr float kNoMax = -FLT_MAX;
 // alike, and the sums need no rescaling.  Most steps skip it.
 constexpr float kRaise = 8.0f;
 
+// The maximum that a row of weight l ends with.  Where it saw keys and all their scores were
+// -infinity it is that (weights 0/0, whose result is NaN); kNoMax stays for a row that saw
+// none (result 0).  l is 0 for these two alone.
+FI float end_max(float m, float l, bool saw) { return l == 0.0f && saw ? -INFINITY : m; }
+
 // s_waitcnt immediate that waits until at most n vector-memory operations are
 // outstanding and leaves the other counters alone (gfx9 encoding).
 constexpr int wait_vm_only(int n) { return (n & 0xF) | ((n >> 4) << 14) | (7 << 4) | (0xF << 8); }
@@ -178,7 +183,7 @@ FI void write_lse(const AttnIO& io, const AttnSeqs& s, const AttnItem& it, int t
     io.lse[(long long)(it.row0 + token) * (s.H * s.G) + head] =
         l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
-FI float inverse_weight(float l) { return l > 0.0f || l != l ? 1.0f / l : 0.0f; }
+FI float inverse_weight(float m, float l) { return l == 0.0f && m == kNoMax ? 0.0f : 1.0f / l; }
 FI long long part_slot(const AttnItem& it, int r) {
   return it.part0 + ((long long)it.h * it.rows + r) * it.parts + it.part;
 }
@@ -198,19 +203,23 @@ FI void write_joined(const AttnIO& io, const AttnSeqs& s, const AttnItem& it, in
   const int rows = min(R, it.rows - row0);
   for (int at = threadIdx.x; at < rows * (D / 4); at += 64 * NW) {
     const int rl = at / (D / 4), ch = at % (D / 4), r = row0 + rl;
-    float m = sm[0][rl], l = 0.0f;
+    float m = kNoMax, least = kNoMax, l = 0.0f;
     f32x4 v = {};
 #pragma unroll
-    for (int y = 1; y < NW; ++y) m = fmaxf(m, sm[y][rl]);
+    for (int y = 0; y < NW; ++y) {
+      m = fmaxf(m, sm[y][rl]);
+      least = fminf(least, sm[y][rl]);
+    }
 #pragma unroll
     for (int y = 0; y < NW; ++y) {
       v += sums[sum_slot<R, D>(y, rl, ch)];
       l = fmaf(sl[y][rl], __builtin_amdgcn_exp2f(sm[y][rl] - m), l);
     }
+    if (l == 0.0f) m = least;  // (-infinity if some wave saw keys)
     if (it.parts == 1) {
       const int token = divide(r, s.by_g), head = it.h * s.G + r - token * s.G;
       const long long to = out_at(io, s, it, token, head) + 4 * ch;
-      v *= inverse_weight(l);
+      v *= inverse_weight(m, l);
       if (F32) {
         *reinterpret_cast<f32x4*>(static_cast<float*>(io.out) + to) = v;
       } else {

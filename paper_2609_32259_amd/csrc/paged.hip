@@ -777,6 +777,12 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_attention_kernel(co
   // the lane's rows: out of the codes' 16 (with the 8 of the moved offsets), the
   // offsets of all lanes' tokens
   l = add_xor32(add_xor16(l));
+  if (__any(m == kNoMax)) {  // (rare: whether the row saw a key, by the wave's first token in a page)
+    unsigned long long in = 0;
+    int i = 0;
+    for (; i < n_blocks && !in; i += 64) in = __ballot((unsigned)pages_from(i) < (unsigned)a.n_pages);
+    m = end_max(m, l, in && first + (i - 64 + __builtin_ctzll(in)) * 32 * NW <= last);
+  }
 #pragma unroll
   for (int y = 0; y < G; ++y) {
     const float x = add_xor32(add_xor16(po[y]));
@@ -791,9 +797,9 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_attention_kernel(co
   }
   __syncthreads();
   f32x4* sums = reinterpret_cast<f32x4*>(stages);
-  float mm = sm[0][col];
+  float mm = kNoMax;
 #pragma unroll
-  for (int x = 1; x < NW; ++x) mm = fmaxf(mm, sm[x][col]);
+  for (int x = 0; x < NW; ++x) mm = fmaxf(mm, sm[x][col]);
   const float f = __builtin_amdgcn_exp2f(m - mm);
 #pragma unroll
   for (int y = 0; y < NC; ++y) sums[sum_slot<R, D>(wave, col, 4 * y + m4)] = o[y] * f;

@@ -103,3 +103,28 @@ def test_bad_values_and_keys_in_every_tile(torch, G, H, d, B, span, cache):
             if what == "k":
                 keep[q0 + row:q0 + n, G:2 * G] = False
             assert torch.equal(l2[keep], lse[keep]), (what, bad, key)
+
+
+@pytest.mark.parametrize("G,H,d,B,span,cache", BATCHES, ids=["G1-128", "G1-64", "G4-128", "G4-64"])
+def test_bad_queries_in_every_wave(torch, G, H, d, B, span, cache):
+    """A query that is not finite makes its workgroup compute a second time: every other row keeps
+    its bits."""
+    from paper_2609_32259_amd import heterofold as hf
+    q_len, kv_len = _lengths(3, B, *span, cache=cache)
+    _by_rows("bf16", q_len, kv_len, G * H, H, d)
+    q, k, v = _draw(torch, "bf16", q_len, kv_len, G * H, H, d, 4)
+    ref = hf.hf_prompt_attention(q, k, v, q_len, kv_len)
+    torch.cuda.synchronize()
+    b = B // 3
+    n, q0 = q_len[b], sum(q_len[:b])
+    for token in range(0, n, 29):
+        head = token % (G * H)
+        was = q[q0 + token, head, 5].clone()
+        q[q0 + token, head, 5] = math.nan if token % 2 else math.inf
+        out = hf.hf_prompt_attention(q, k, v, q_len, kv_len)
+        q[q0 + token, head, 5] = was
+        torch.cuda.synchronize()
+        hit = torch.zeros(out.shape[:2], dtype=torch.bool, device="cuda")
+        hit[q0 + token, head] = True
+        assert bool(torch.isnan(out[hit].float()).all()), token
+        assert torch.equal(_bits(torch, out)[~hit], _bits(torch, ref)[~hit]), token
