@@ -435,7 +435,7 @@ size_t hf_attention_workspace_bytes(int32_t B, const int32_t* q_len, const int32
  * causal with q_len > kv_len) gets out = 0 and lse = -infinity.  What a row does
  * not see has no influence on it, whatever its bits are.  A score of -infinity has
  * weight 0; a row all of whose scores are that has weights 0/0: out is NaN and lse
- * -infinity.
+ * -infinity.  Scores of any size up to 2^127 are served.
  *   q_len, kv_len  host int32 [B], >= 0; kv_len <= 2^30.
  *   q, out    hf_rows of H_q heads; out may be q itself, element for element.
  *   k, v      hf_rows of H heads, H_q % H == 0, stride_t <= 2^23; same dtype and

@@ -247,19 +247,22 @@ struct Rows {
   typename P::Q q;
   typename P::O o;
   float m, l;  // the row's maximum; this lane's share of its weight
+  bool far;    // m is in units of far_unit(c), not of c (second pass)
   int last;    // the last key it sees
 };
 
 // The weights of a tile's scores and their product with its values.  MASK: some row
-// of the wave does not see every key of the tile (t0 is its first).
+// of the wave may not see every key of the tile (t0 is its first); edge: there is one.
 // In such a tile a value that is not finite would reach rows that do not see it, as
 // 0 * NaN.  That shows in their results: the kernels look at them at the end and in
 // that case compute once more with `careful`, where such a value enters the product
 // as 0 and is added to the rows that see its key.  (In other tiles all rows see all
-// keys, and the product does what it should.)
+// keys, and the product does what it should.)  The second pass, whose tiles are all taken
+// with MASK, also gives each row the unit that its scores need.
 template <class P, bool MASK>
 FI void finish(Rows<P>& w, float (&s)[P::NS], const unsigned char* sv, int lane, float c, int t0,
-               bool careful) {
+               bool careful, bool edge) {
+  float cr = MASK && w.far ? far_unit(c) : c;
   if (MASK) {
 #pragma unroll
     for (int i = 0; i < P::NS; ++i)
@@ -268,21 +271,20 @@ FI void finish(Rows<P>& w, float (&s)[P::NS], const unsigned char* sv, int lane,
   float mx = s[0];
 #pragma unroll
   for (int i = 1; i < P::NS; ++i) mx = fmaxf(mx, s[i]);
-  mx = P::row_max(mx) * c;
-  if (__any(mx > w.m + kRaise)) {
-    const float m = mx > w.m + kRaise ? mx : w.m;  // (each row by its own scores alone)
-    const float f = __builtin_amdgcn_exp2f(w.m - m);
-    w.m = m;
+  mx = P::row_max(mx);
+  if (__any(mx * cr > w.m + kRaise)) {
+    const float f = raise(mx, c, MASK && careful, cr, w.m);  // (each row by its own scores alone)
+    if (MASK) w.far = cr != c;
     w.l *= f;
 #pragma unroll
     for (int i = 0; i < P::NO; ++i) P::set(w.o, i, P::get(w.o, i) * f);
   }
 #pragma unroll
   for (int i = 0; i < P::NS; ++i) {
-    s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -w.m));
+    s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], cr, -w.m));
     w.l += s[i];
   }
-  if (!MASK || !careful) {
+  if (!MASK || !careful || !edge) {
     P::template values<false>(w.o, sv, lane, s);
     return;
   }
@@ -301,7 +303,7 @@ FI void finish(Rows<P>& w, float (&s)[P::NS], const unsigned char* sv, int lane,
 // Whether a row is to be computed a second time.  saw: it saw a key.
 template <class P>
 FI bool second_pass(const Rows<P>& w, bool saw) {
-  bool bad = saw && w.m == kNoMax;
+  bool bad = saw && far_max(w.m);
 #pragma unroll
   for (int i = 0; i < P::NO; ++i) bad |= !finite_bits(P::get(w.o, i));
   return bad;
@@ -428,11 +430,12 @@ FI void load_row(Rows<P>& w, const AttnArgs& a, const AttnItem& it, int r, int l
   w.last = last_key(s, it, token);
 }
 template <class P>
-FI void clear_row(Rows<P>& w) {
+FI void clear_row(Rows<P>& w, bool careful) {
 #pragma unroll
   for (int i = 0; i < P::NO; ++i) P::set(w.o, i, 0.0f);
   w.m = kNoMax;
   w.l = 0.0f;
+  w.far = careful;
 }
 
 template <bool M>
@@ -452,7 +455,7 @@ struct Flag {
 // against 540 us for 8,192 tokens), with four waves and two workgroups a CU the tiles are
 // loaded twice (701 against 588), and waves started half a tile apart, given
 // priority in turn or held back between the products gained nothing (600, 568, 565 against
-// 540).  In fp32 four waves and up to four workgroups a CU.
+// 540).  In fp32 four waves and up to four workgroups a CU (with heads of 64; two with 128).
 template <class P, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void attention_rows_kernel(const AttnArgs a) {
   typedef typename P::T T;
@@ -507,7 +510,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_rows_kernel(const AttnAr
     get_k(t0 + 2 * KT, sk);
     get_v(t0 + KT, nv);
     P::scores(w.q, nk, lane, s1);
-    finish<P, false>(w, s0, sv, lane, c, t0, false);
+    finish<P, false>(w, s0, sv, lane, c, t0, false, false);
   };
   bool careful = false;
   // Near a causal edge or the last key, one tile's scores at a time.
@@ -516,7 +519,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_rows_kernel(const AttnAr
     ready();
     get_k(t0 + 2 * KT, sk);
     get_v(t0 + KT, nv);
-    if (t0 <= wave_last) finish<P, true>(w, s, sv, lane, c, t0, careful);
+    if (t0 <= wave_last) finish<P, true>(w, s, sv, lane, c, t0, careful, t0 + KT - 1 > wg_first);
     if (t0 + KT <= wave_last && t0 + KT < hi) P::scores(w.q, nk, lane, s);
   };
   // what the first two steps need is on its way at once
@@ -528,7 +531,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_rows_kernel(const AttnAr
   get_first();
   load_row<P>(w, a, it, my0 + P::row(lane), lane);
   for (;;) {
-    clear_row<P>(w);
+    clear_row<P>(w, careful);
     if (lo < hi) {
       Scores s0, s1;
       if (careful) get_first();
@@ -536,7 +539,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_rows_kernel(const AttnAr
       P::scores(w.q, k0, lane, s0);
       // pairs of tiles that every row sees whole, with a tile after them
       int t0 = lo;
-      for (; t0 + 2 * KT - 1 <= wg_first && t0 + 2 * KT < hi; t0 += 2 * KT) {
+      for (; !careful && t0 + 2 * KT - 1 <= wg_first && t0 + 2 * KT < hi; t0 += 2 * KT) {
         step(t0, s0, s1, k0, v0, k1, v1);
         step(t0 + KT, s1, s0, k1, v1, k0, v0);
       }
@@ -551,7 +554,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_rows_kernel(const AttnAr
     careful = true;
   }
   const float l = P::row_sum(w.l);
-  if (careful) w.m = end_max(w.m, l, lo < hi && lo <= w.last);
+  if (careful) w.m = end_max(w.m, w.far ? far_unit(c) : c, c, l, lo < hi && lo <= w.last);
   if (it.parts > 1) {
     const int r = my0 + P::row(lane);
     if (r < n_rows) write_part<P>(a.io, it, r, w.m, l, w.o, lane);
@@ -621,10 +624,11 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
     float s[P::NS];
     P::scores(w.q, st, lane, s);
     ready(next, Flag<true>());
-    if (t0 + P::KT - 1 > first)
-      finish<P, true>(w, s, st + TB, lane, c, t0, careful);
+    const bool edge = t0 + P::KT - 1 > first;
+    if (careful || edge)
+      finish<P, true>(w, s, st + TB, lane, c, t0, careful, edge);
     else
-      finish<P, false>(w, s, st + TB, lane, c, t0, false);
+      finish<P, false>(w, s, st + TB, lane, c, t0, false, false);
   };
   // The first tile on its way, then the queries; both are waited for here, for a wait for
   // the queries inside the loop would wait for the tiles in flight as well.
@@ -632,7 +636,7 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
   load_row<P>(w, a, it, row0 + P::row(lane), lane);
   P::keep(w.q);
   for (;;) {
-    clear_row<P>(w);
+    clear_row<P>(w, careful);
     if (lo < hi) {
       if (careful) get(lo, w0);
       for (int t0 = lo; t0 < hi; t0 += 2 * NW * P::KT) {
@@ -646,7 +650,7 @@ __global__ __launch_bounds__(NW * 64) void attention_keys_kernel(const AttnArgs 
 
   const int rl = P::row(lane);
   const float l = P::row_sum(w.l);
-  if (careful) w.m = end_max(w.m, l, lo < hi && lo <= w.last);
+  if (careful) w.m = end_max(w.m, w.far ? far_unit(c) : c, c, l, lo < hi && lo <= w.last);
   if (lane < P::RW) {
     sm[wave][rl] = w.m;
     sl[wave][rl] = l;

@@ -32,10 +32,44 @@ constexpr float kNoMax = -FLT_MAX;
 // alike, and the sums need no rescaling.  Most steps skip it.
 constexpr float kRaise = 8.0f;
 
-// The maximum that a row of weight l ends with.  Where it saw keys and all their scores were
-// -infinity it is that (weights 0/0, whose result is NaN); kNoMax stays for a row that saw
-// none (result 0).  l is 0 for these two alone.
-FI float end_max(float m, float l, bool saw) { return l == 0.0f && saw ? -INFINITY : m; }
+// Scores far from 0.  A weight is 2^(s c - m), formed by one fused multiply-add, and m the
+// rounded product top * c of the row's largest score.  From 2^31 on its rounding alone is up
+// to 2^7 and more, and every weight of the row may overflow or vanish.  From 2^30 on a row
+// therefore multiplies by the power of two below c, which makes m exact.  Its softmax stays the
+// same: there two scores differ by 2^6 at least in units of c, by 2^5 in the other's, and all
+// weights but the largest scores' are below the rounding of their sum in either.
+// A unit for each row, in a vector register, costs the dense loops 1% (8,192 tokens 487 -> 491
+// us), so they have c, and a row that ends far away is computed in the second pass.  The paged
+// kernel, which has none, keeps a unit for each row (16 sequences of 4 to 8K tokens 25.4 -> 25.7
+// us; a second pass there measured the same).
+constexpr float kFar = 0x1p30f;
+FI bool far_max(float m) { return !(fabsf(m) < kFar); }  // (kNoMax is: c times a score may lie below it)
+FI float far_unit(float c) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, c) & 0x7f800000u); }
+
+// Raises a row's maximum m, in units of cr, to that of its largest score `top` where that
+// passes it, and returns the factor for what was summed (0 where the unit changes: then all of
+// it is as far away).  units: cr may become far_unit(c).
+FI float raise(float top, float c, bool units, float& cr, float& m) {
+  if (!(top * cr > m + kRaise)) return 1.0f;
+  float now = c, to = top * c;
+  if (units && far_max(to)) {
+    now = far_unit(c);
+    to = top * now;
+  }
+  const float f = now == cr ? __builtin_amdgcn_exp2f(m - to) : 0.0f;
+  cr = now;
+  m = to;
+  return f;
+}
+
+// The maximum that a row of weight l ends with, in units of c, which is what it is joined to
+// others by.  Where it saw keys and all their scores were -infinity it is that (weights 0/0,
+// whose result is NaN); kNoMax stays for a row that saw none (result 0).  l is 0 for these
+// two alone.
+FI float end_max(float m, float cr, float c, float l, bool saw) {
+  if (l == 0.0f) return saw ? -INFINITY : kNoMax;
+  return cr == c ? m : fminf(fmaxf(m / cr * c, -FLT_MAX), FLT_MAX);
+}
 
 // s_waitcnt immediate that waits until at most n vector-memory operations are
 // outstanding and leaves the other counters alone (gfx9 encoding).

@@ -634,6 +634,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_attention_kernel(co
   f32x4 ps[G] = {};    // sum of the rounded p s
   float po[G] = {};    // sum of p times the offset, over the lane's tokens
   float m = kNoMax, l = 0.0f;
+  float cr = c;        // the unit of m
 
   // masked: some row of the tile does not see all of the block's tokens, or it is a hole
   auto block = [&](auto masked, const Block<D>& x, int t0, bool in) {
@@ -685,11 +686,15 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_attention_kernel(co
     float mx = p[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) mx = fmaxf(mx, p[i]);
-    mx = max_xor32(max_xor16(mx)) * c;
+    const float top = max_xor32(max_xor16(mx));
+    mx = top * cr;
     if (__any(mx > m + kRaise)) {
       const float nm = mx > m + kRaise ? mx : m;  // (each row by its own scores alone)
-      const float f = __builtin_amdgcn_exp2f(m - nm);
-      m = nm;
+      float f = __builtin_amdgcn_exp2f(m - nm);
+      if (__any(far_max(nm) || cr != c))
+        f = raise(top, c, true, cr, m);
+      else
+        m = nm;
       l *= f;
 #pragma unroll
       for (int y = 0; y < NC; ++y) o[y] *= f;
@@ -701,7 +706,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_attention_kernel(co
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], c, -m));
+      p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], cr, -m));
       l += p[i];
     }
 
@@ -777,11 +782,11 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_attention_kernel(co
   // the lane's rows: out of the codes' 16 (with the 8 of the moved offsets), the
   // offsets of all lanes' tokens
   l = add_xor32(add_xor16(l));
-  if (__any(m == kNoMax)) {  // (rare: whether the row saw a key, by the wave's first token in a page)
+  if (__any(far_max(m))) {  // (rare: whether the row saw a key, by the wave's first token in a page)
     unsigned long long in = 0;
     int i = 0;
     for (; i < n_blocks && !in; i += 64) in = __ballot((unsigned)pages_from(i) < (unsigned)a.n_pages);
-    m = end_max(m, l, in && first + (i - 64 + __builtin_ctzll(in)) * 32 * NW <= last);
+    m = end_max(m, cr, c, l, in && first + (i - 64 + __builtin_ctzll(in)) * 32 * NW <= last);
   }
 #pragma unroll
   for (int y = 0; y < G; ++y) {
