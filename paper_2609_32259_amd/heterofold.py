@@ -542,6 +542,8 @@ def _other_stream(dev, stream):
     else:
         if isinstance(stream, int):
             stream = torch.cuda.ExternalStream(stream, device=dev)
+        elif stream.device != dev:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on {dev}")
         with torch.cuda.stream(stream):
             yield
 
