@@ -570,7 +570,13 @@ _I32_ARRAYS = {}
 
 def _lens(a, name, B=None):
     """ctypes int32 array and list of a batch's lengths."""
-    v = a.tolist() if isinstance(a, np.ndarray) else [int(x) for x in a]
+    if isinstance(a, np.ndarray):
+        v = a.tolist()
+    else:
+        a = list(a)
+        v = [int(x) for x in a]
+        if v != a:
+            raise ValueError(f"{name} must be whole numbers")
     n = len(v)
     if (B is not None and n != B) or (n and isinstance(v[0], list)):
         raise ValueError(f"{name} must be one length for each sequence")

@@ -139,7 +139,7 @@ def dense_cache(cache: "hf.PagedKV", lengths, dtype=None, T_cap: Optional[int] =
     cache of the next hand-off.  Runs on the current stream of the cache's device."""
     import torch
 
-    lengths = np.asarray(lengths, np.int32)
+    lengths = np.asarray(hf._lens(lengths, "lengths")[1], np.int32)
     T_cap = max(1, int(lengths.max(initial=0))) if T_cap is None else int(T_cap)
     S = torch.zeros((lengths.size, cache.L, 2, cache.H, T_cap, cache.d_h),
                     dtype=dtype or torch.bfloat16, device=cache.pages.device)
