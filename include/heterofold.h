@@ -416,7 +416,8 @@ typedef struct hf_rows {
  * (paged = 1) needs for these lengths, heads, d_h and dtype: the unnormalized
  * sums, maxima and weights of the parts that a long key range is split into when
  * there are few query rows (each 4 (d_h + 2) bytes a query row, head and part),
- * 0 when nothing is split.  Calls that share a workspace must not overlap.
+ * 0 when nothing is split and on bad arguments (hf_last_error() then says why).
+ * Calls that share a workspace must not overlap.
  */
 size_t hf_attention_workspace_bytes(int32_t B, const int32_t* q_len, const int32_t* kv_len,
                                     int32_t H_q, int32_t H, int32_t d_h, int32_t dtype,
@@ -435,8 +436,12 @@ size_t hf_attention_workspace_bytes(int32_t B, const int32_t* q_len, const int32
  * causal with q_len > kv_len) gets out = 0 and lse = -infinity.  What a row does
  * not see has no influence on it, whatever its bits are.  A score of -infinity has
  * weight 0; a row all of whose scores are that has weights 0/0: out is NaN and lse
- * -infinity.  Scores of any size up to 2^127 are served.
- *   q_len, kv_len  host int32 [B], >= 0; kv_len <= 2^30.
+ * -infinity.  Scores may have any size up to 2^120.  Sums are formed with weights of
+ * up to 2^9 (2^72 in rows whose scores pass 2^24) and divided by the weights' own at
+ * the end: they overflow where such a weight times a value does.
+ *   q_len, kv_len  host int32 [B], >= 0; kv_len <= 2^30.  They go into the launch
+ *             (a captured call replays with those it was captured with), as do the
+ *             lengths and positions of the paged calls.
  *   q, out    hf_rows of H_q heads; out may be q itself, element for element.
  *   k, v      hf_rows of H heads, H_q % H == 0, stride_t <= 2^23; same dtype and
  *             d_h throughout.

@@ -822,7 +822,7 @@ Cut cut_keys(const hf::AttnShape& sh, int32_t B, const int32_t* q_len, const int
   }
   Cut best = {longest, INT64_MAX, triangular};
   const int64_t most = std::min<int64_t>((longest + sh.step - 1) / sh.step, sh.wg_target);
-  for (int64_t k = 1; k <= most; ++k) {  // (k B H <= 4 wg_target: at most some thousand divisions)
+  for (int64_t k = 1; k <= most; ++k) {  // (up to wg_target cuts, of B divisions each)
     const int64_t c = (longest + k * sh.step - 1) / (k * sh.step) * sh.step;
     int64_t n = 0;
     for (int b = 0; b < B; ++b)

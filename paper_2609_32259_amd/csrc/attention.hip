@@ -111,7 +111,11 @@ struct Bf16Tile {
   // O += V^T P^T.  CLEAN: values that are not finite enter as 0.
   template <bool CLEAN>
   FI static void values(O& o, const unsigned char* sv, int lane, const float (&p)[NS]) {
-    // the transposing read gives lane i of 16 the values of 4 rows at channel i; its
+    // Weights of one bf16 rounding: in two terms, which would hold 16 bits, the product would
+    // take twice its instructions, for an error that is the result's own rounding once more
+    // (over prompts 2.1e-3 of the result's size in all against 1.7e-3 of the rounding alone).
+    // The sum of the weights is of those before it.
+    // The transposing read gives lane i of 16 the values of 4 rows at channel i; its
     // lane i names row i / 4 of them and 8 bytes there
     const int h = lane >> 5, gb = (lane >> 4) & 1, i = lane & 15;
     const int r = 4 * h + (i >> 2);
@@ -447,10 +451,11 @@ struct Flag {
 // computes the scores of the next tile before it finishes this one's, so
 // that matrix instructions and the softmax's are there to be issued side by side.
 // Bound by the matrix cores and the softmax's instructions beside them: causal prompts of
-// 32 heads of 128 on 8, 8,192 tokens in 481 to 516 us, by card (1.07 to 1.14 PFLOP/s; a
-// library product of 8192^3 reaches 1.14); 14 fp32 heads of 64, 2,001 tokens, in 82 (88
-// TFLOP/s: its longest tile alone takes that; 3,001 tokens of 32 heads of 128 reach 127 of
-// the 153 that a library product does).
+// 32 heads of 128 on 8, 8,192 tokens in 475 to 515 us, by card (1.07 to 1.16 PFLOP/s; a large
+// library product, 16384^3, reaches 1.37); 14 fp32 heads of 64, 2,001 tokens, in 81 (88
+// TFLOP/s: the longest tile has a CU almost to itself and takes all of it, 2,001 keys at 37 ns
+// and 5.8 us of start; 3,000 tokens of 32 heads of 128 reach 127 of the 153 that a library
+// product does).
 // Eight waves and one workgroup a CU in bf16: with 64 rows a wave the registers spill (777
 // against 540 us for 8,192 tokens), with four waves and two workgroups a CU the tiles are
 // loaded twice (701 against 588), and waves started half a tile apart, given
@@ -568,7 +573,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_rows_kernel(const AttnAr
 
 // By keys: one block of RW rows, the tiles of keys dealt to NW waves.  Bound by HBM for
 // one block of rows: a token of 32 heads on 8 of 128 over 29K keys 23 us (5.2 TB/s), four
-// over 12K keys together 14.9 and 3.9 us for the join; for few keys by the latency of the
+// over 12K keys together 14.7 and 4.0 us for the join; for few keys by the latency of the
 // loads that follow each other (8.6 us for a prompt of 100 tokens).  Tiles of 32 keys: two
 // stages of four waves fill 128 KB of LDS (fp32 rows of 128 channels are twice as long, and
 // take 16).
@@ -787,12 +792,17 @@ void join(const JoinArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// Times as measured, d_h 128 and 64, with every workgroup on a CU of its own: parts of
-// 64 to 1,024 keys by rows, of 128 to 4,096 by keys (keys from L2; where HBM bounds it,
-// one tile of rows over 29K keys, 20 ns a key).  Parts for one workgroup a CU: for two, by
+// Times as the rule weighs them, d_h 128 and 64, with every workgroup on a CU of its own:
+// parts of 64 to 1,024 keys by rows, of 128 to 4,096 by keys (keys from L2; where HBM bounds
+// it, one tile of rows over 29K keys, 20 ns a key).  They were measured when the kernels took 5
+// to 30% longer; now, us of start and ns a key by rows and by keys: bf16 of 128 11.2 + 26.6
+// and 7.3 + 9.4, of 64 8.7 + 15.9 and 5.0 + 5.5; fp32 of 128 7.2 + 68.5 and 5.8 + 30.7, of 64
+// 5.8 + 37.3 and 4.9 + 12.7.  What decides is how the two stand to each other, which has stayed
+// the same within a fifth.  Parts for one workgroup a CU: for two, by
 // keys with heads of 64, which LDS has room for, 18.9 us against 15.7 for a token over 29K.
-// fp32 tiles by rows have up to three workgroups a CU: a causal prompt's deal turns
-// every other round (2,001 tokens with heads of 64: 113 us without, 95 with).
+// fp32 tiles by rows share a CU, up to four with heads of 64 and two with 128 (three is what
+// the rule counts): a causal prompt's deal turns every other round (2,001 tokens with heads
+// of 64: 113 us without, 95 with).
 AttnShape prompt_shape(int dtype, int d_h, bool by_keys) {
   AttnShape sh;
   const bool f32 = dtype == HF_F32, wide = d_h == 128;

@@ -211,8 +211,9 @@ FI void fill_angles(const PagedRowsArgs& a, const RowItem& it, float2* cs) {
 }
 
 // Bound by HBM: a transfer's cache of 40 layers and 7.3K tokens (1.19 GB in, 0.37 GB out)
-// takes 336 to 363 us, 4.3 to 4.6 TB/s (a device copy reaches 4.7); a token for each of
-// eight sequences 4.9 us, the latency of its loads one after another.
+// takes 305 to 323 us, 4.8 to 5.1 TB/s (a device copy, which writes as much as it reads,
+// reaches 4.7); a token for each of eight sequences 4.8 us, the latency of its loads one after
+// another.
 // ROT: a call that rotates its keys.  (Their angles take registers and LDS that a call which
 // only moves rows would miss for loads in flight: 377 and 365 us at that size with and
 // without.)
@@ -311,7 +312,7 @@ __global__ __launch_bounds__(2 * D) void paged_append_kernel(const PagedRowsArgs
 }
 
 // The same blocks back; value codes through LDS, whose order is by channels.  Bound by HBM
-// (281 us, 5.5 TB/s, for the cache above).
+// (272 to 278 us, 5.6 TB/s, for the cache above).
 template <class T, int D>
 __global__ __launch_bounds__(2 * D) void paged_read_kernel(const PagedRowsArgs a, const int hpw) {
   constexpr int TPT = D / 16;
@@ -413,7 +414,9 @@ struct Codes {
 };
 
 // x as S bf16 terms whose sum holds 8 S bits of it.
-// (S = 1: x itself, which the conversion after it rounds)
+// (S = 1: x itself, which the conversion after it rounds.  So bf16 calls take a weight times
+// its value's scale: three terms would take three times the second product's instructions, for
+// an error the size of the result's own rounding, 2.3e-3 in all against 1.7e-3.)
 template <int S>
 FI void split(float x, float (&t)[S]) {
 #pragma unroll
@@ -522,8 +525,8 @@ struct Flag {
 // turn, the next two blocks' 5 KB each in flight.  Per block a wave spends about 130
 // instructions on taking codes out of dwords, 110 on scales and 60 on the softmax, beside
 // 22 matrix instructions; that and HBM bound it together: 29K tokens of 40 heads on 8 of
-// 128 (37 MB) in 16.0 us and 4.9 for the join, 16 sequences of 4 to 8K tokens (64 MB) in
-// 22.2 and 4.0.  One query token over 200 takes 7.5 us, most of it a few loads that need
+// 128 (37 MB) in 16.6 us and 4.8 for the join, 16 sequences of 4 to 8K tokens (64 MB) in
+// 23.0 and 4.0.  One query token over 200 takes 7.6 us, most of it a few loads that need
 // each other (arguments, page, block).
 // Measured and dropped: the next block in registers instead of LDS (17.0 us against 16.3,
 // 25.5 against 22.4 for the 16 sequences); two tiles of 16 rows a workgroup, which read the
@@ -844,7 +847,9 @@ void append(dim3 grid, const PagedRowsArgs& a, int hpw, hipStream_t s) {
 
 }  // namespace
 
-// Times as measured with two workgroups a CU, parts of 128 to 7,296 tokens.
+// Times as the rule weighs them, with two workgroups a CU, parts of 128 to 7,296 tokens; now,
+// from L2, us of start and ns a key: bf16 of 128 6.4 + 14.1, of 64 4.7 + 8.6; fp32 8.4 + 29.1
+// and 5.6 + 16.3.
 AttnShape paged_shape(int dtype, int d_h) {
   AttnShape sh;
   const bool f32 = dtype == HF_F32, wide = d_h == 128;

@@ -119,8 +119,9 @@ class TransferPath:
     def attend(self, layer: int, q, q_len, kv_len=None, **kw):
         """Attention of packed queries [sum q_len, H_q, d_h] over one layer of the receiver
         cache (arguments as ``hf_prompt_attention``).  kv_len None: the transferred rows,
-        with causal=False for queries that are not the last of them; a suffix whose rows lie
-        behind them in ``R`` passes r_len + q_len."""
+        with causal=False for queries that are not the last of them; a suffix whose keys
+        (rotated) and values the caller has written behind them in ``R`` passes r_len +
+        q_len."""
         return hf.hf_prompt_attention(q, self.R[:, layer, 0], self.R[:, layer, 1], q_len,
                                       self.r_len if kv_len is None else kv_len, **kw)
 
