@@ -544,6 +544,151 @@ int32_t hf_paged_attention(int32_t B, const int32_t* q_len, const int32_t* kv_le
                            void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* Answering from a cache: which of its tokens matter, and the next token.   */
+/* ------------------------------------------------------------------------ */
+/*
+ * A cache that goes from hand-off to hand-off, or that a receiver keeps answering
+ * from, grows with every token.  The calls below shorten it: the attention weight
+ * that each key gets is added up beside the attention, the tokens of the greatest
+ * weight are chosen for each layer and head, and their rows are moved together.
+ * Keys are held rotated, so that a row means the same wherever it lies, and
+ * attention without a causal mask, or of queries behind the cache, does not ask
+ * for the rows' order.  hf_sample_tokens ends a step with the token that the
+ * receiver answers.
+ */
+
+/*
+ * fp32 numbers for the keys of a cache in device memory: that of token t, layer l
+ * (where a call has layers) and head h of sequence b lies at
+ * ptr + b*stride_b + l*stride_l + h*stride_h + t (in elements).  Strides are >= 0;
+ * rows that a call writes must not overlap.
+ */
+typedef struct hf_key_weights {
+  float* ptr;
+  int64_t stride_b, stride_l, stride_h;
+} hf_key_weights;
+
+/*
+ * The attention weight that each key gets from a batch of query runs, over dense
+ * keys (hf_attention_weights) and over the first kv_len[b] tokens of one layer of a
+ * paged cache (hf_paged_attention_weights).  Queries, keys, grouping and masks as
+ * in hf_prompt_attention; lse is what the attention of the same queries over the
+ * same keys returned (or of a longer run of keys: then these are the weights in it):
+ *   w_j = decay * prior_j + sum over the H_q / H heads g of the group and the rows i
+ *         that see key j of exp(scale * <q_ig, k_j> - lse_ig).
+ * Every key below kv_len[b] is written, with a sum of 0 where no row sees it (and in
+ * a hole of the pages); what lies behind keeps its bits.  A row all of whose scores
+ * are -infinity has weights 0/0, which make the keys it sees NaN, as they make its
+ * result.  What a row does not see has no influence, whatever its bits are.
+ *   q         hf_rows of H_q heads; k hf_rows of H heads; same dtype and d_h.
+ *   lse       device fp32 [sum q_len][H_q] (rows packed).
+ *   scale     as in the attention that made lse.
+ *   prior     weights so far, or NULL for none (decay is not used then).  May be w
+ *             itself, element for element.
+ *   decay     finite: 1 adds up, less lets older weights fade.
+ *   w         the result (stride_l is not used).
+ * Numerics: scores as the attention forms them; exponentials and sums in fp32, the
+ * sums by halves within 16 (paged: 4) rows, in an order that depends on the lengths,
+ * heads and types alone.  A weight carries the rounding of lse, about |lse| 2^-22 of
+ * itself; in rows with |lse| > 2800 one that this would lift above 1 counts as 1.
+ */
+int32_t hf_attention_weights(int32_t B, const int32_t* q_len, const int32_t* kv_len,
+                             const hf_rows* q, const hf_rows* k, const float* lse, float scale,
+                             int32_t causal, const hf_key_weights* prior, float decay,
+                             const hf_key_weights* w, void* stream);
+int32_t hf_paged_attention_weights(int32_t B, const int32_t* q_len, const int32_t* kv_len,
+                                   const hf_rows* q, const hf_paged_kv* cache, int32_t layer,
+                                   const float* lse, float scale, int32_t causal,
+                                   const hf_key_weights* prior, float decay,
+                                   const hf_key_weights* w, void* stream);
+
+/*
+ * Which tokens of each layer and head stay: of the kv_len[b] tokens of a sequence
+ * keep[b] (all, where keep[b] >= kv_len[b]).  The first n_first and the last n_last
+ * of them stay anyway; of the others those of the greatest weight, of equal ones
+ * those of the lowest number (0 and -0 are equal; a NaN lies below every number).
+ *   w      the weights (L layers, H heads).
+ *   index  device int32 [B][L][H][index_stride]: the min(keep[b], kv_len[b]) tokens
+ *          that stay, rising; entries behind them keep their bits.
+ * n_first + n_last <= keep[b] wherever keep[b] < kv_len[b].
+ */
+int32_t hf_evict_select(int32_t B, int32_t L, int32_t H, const int32_t* kv_len,
+                        const int32_t* keep, int32_t n_first, int32_t n_last,
+                        const hf_key_weights* w, int32_t* index, int64_t index_stride,
+                        void* stream);
+
+/*
+ * Moves rows of a dense cache together: row i < n[b] of the result is row
+ * index[b][l][h][i] of the keys and of the values.
+ *   n         host int32 [B], n[b] <= kv_len[b], the rows there are.
+ *   index     device int32 [B][n_layers][H][index_stride], index_stride >= every n[b];
+ *             entries are clamped to [0, kv_len[b]).
+ *   k, v      hf_rows, same dtype, heads and d_h; rows of at most 16,384 bytes, a
+ *             multiple of 16.
+ *   k_to, v_to  where the rows go (not overlapping k and v), or NULL both: in place.
+ *             Then index must rise, as hf_evict_select writes it: entry i is at least
+ *             i.  (Anything else gives unspecified rows.)  Packed sequences
+ *             (stride_b == -1) stay where they begin in place; elsewhere they lie back
+ *             to back by n.
+ *   w, w_to   the tokens' weights moved with them, or NULL; in place w_to is NULL.
+ * Rows from n[b] on keep their bits.
+ */
+int32_t hf_evict_rows(int32_t B, const int32_t* n, const int32_t* kv_len, int32_t n_layers,
+                      const int32_t* index, int64_t index_stride, const hf_rows* k,
+                      const hf_rows* v, const hf_rows* k_to, const hf_rows* v_to,
+                      const hf_key_weights* w, const hf_key_weights* w_to, void* stream);
+
+/*
+ * hf_evict_rows for layers layer .. layer + n_layers - 1 of a paged cache.  The codes
+ * and words move as they are: a row stands for the same values after it.
+ *   to      the cache that the rows go to, in the same layers of it: same H, d_h and
+ *           page_tokens, pages that `cache` does not name; or NULL: in place.  Pages
+ *           that hold no token below n[b] any more are the caller's again.
+ * A token from a hole becomes codes and words of 0 (values of 0); one that would go to
+ * a hole is dropped.  Pages that one call writes must be named once.
+ */
+int32_t hf_paged_evict(int32_t B, const int32_t* n, const int32_t* kv_len,
+                       const hf_paged_kv* cache, const hf_paged_kv* to, int32_t layer,
+                       int32_t n_layers, const int32_t* index, int64_t index_stride,
+                       const hf_key_weights* w, const hf_key_weights* w_to, void* stream);
+
+/*
+ * The next token of each row of logits x [n][vocab], from a given random number.
+ * With w_j = exp((x_j - max x) / temperature), and the tokens in falling order of w,
+ * equal ones by rising number:
+ *   - the first top_k stay (top_k <= 0 or >= vocab: all);
+ *   - of these the shortest prefix whose w sum to at least top_p times theirs
+ *     (top_p >= 1: all; the first always stays);
+ *   - of these those with w_j >= min_p (min_p <= 0: all; the first always stays);
+ *   - the token is the first in that order at which the running sum of w passes
+ *     u times the sum of all that stay.
+ * temperature <= 0: the first token of the largest logit.  A logit of -infinity has
+ * weight 0 and is not drawn; of several of +infinity each has weight 1 and all others 0.
+ * A row that holds a NaN or nothing but -infinity, or whose temperature is +infinity or
+ * NaN, gives token -1 and a log-probability of NaN.  A NaN in top_p or min_p counts as
+ * no limit, in u as 0; u is taken into [0, 1 - 2^-24].
+ *   n            >= 0 rows;  vocab in [1, 2^20].
+ *   dtype        HF_F32 or HF_BF16; x device, row i at x + i * stride (elements),
+ *                stride >= vocab; rows may begin at any element.
+ *   temperature, top_p, min_p  device fp32 [n], top_k device int32 [n]; each NULL for 1,
+ *                1, 0 and 0.
+ *   u            device fp32 [n].
+ *   token        device int32 [n].
+ *   logprob      device fp32 [n] or NULL: log of the token's w over the sum of those that
+ *                stay (0 for temperature <= 0).
+ *   workspace    device, >= hf_sample_workspace_bytes(n, vocab, dtype), 256-B aligned; may be
+ *                NULL where that is 0.  Calls that share one must not overlap.
+ * Numerics: sums are held to 2^-29 of themselves or better, so that a token differs from
+ * the definition's only where u times the sum, or top_p's border, is that close to a
+ * running sum.  The result of a row depends on that row alone.
+ */
+size_t hf_sample_workspace_bytes(int32_t n, int32_t vocab, int32_t dtype);
+int32_t hf_sample_tokens(int32_t n, int32_t vocab, int32_t dtype, const void* x, int64_t stride,
+                         const float* temperature, const int32_t* top_k, const float* top_p,
+                         const float* min_p, const float* u, int32_t* token, float* logprob,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Offline construction of the maps (fp64, off the transfer path).           */
 /* ------------------------------------------------------------------------ */
 /*
@@ -684,7 +829,11 @@ typedef enum {
   HF_KERNEL_ATTENTION_JOIN = 13,   /* both: joining the parts of split key ranges */
   HF_KERNEL_PAGED_APPEND = 14,     /* hf_paged_append */
   HF_KERNEL_PAGED_READ = 15,       /* hf_paged_read */
-  HF_KERNEL_COUNT = 16
+  HF_KERNEL_ATTENTION_WEIGHTS = 16, /* hf_attention_weights, hf_paged_attention_weights */
+  HF_KERNEL_EVICT_SELECT = 17,     /* hf_evict_select */
+  HF_KERNEL_EVICT_MOVE = 18,       /* hf_evict_rows, hf_paged_evict */
+  HF_KERNEL_SAMPLE = 19,           /* all launches of hf_sample_tokens */
+  HF_KERNEL_COUNT = 20
 } hf_kernel_id;
 
 /*

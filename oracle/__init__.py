@@ -21,9 +21,11 @@ Everything here is written to be checked against the paper by eye:
   low-rank correction folded into the map (Eq. 9).
 * ``attention``  -- attention with a causal mask and grouped heads, and the 4-bit
   rows of the paged cache.
+* ``answer``     -- the attention weight of each key, the tokens that stay in a shortened
+  cache, and the next token from a row of logits.
 
 Integer results are exact.  Floating-point results are fp64 computed from the
 exact stored input values (bf16 or fp32 widened to fp64).
 """
 
-from . import alignment, attention, layer_map, recolor, rope, transfer  # noqa: F401
+from . import alignment, answer, attention, layer_map, recolor, rope, transfer  # noqa: F401

@@ -1,0 +1,82 @@
+"""What a receiver does beside its attention, in fp64 from the definitions: the attention
+weight that each key gets, the tokens that stay in a shortened cache, the next token."""
+
+from __future__ import annotations
+
+import numpy as np
+
+
+def key_weights(q, k, lse, scale, causal=True, seen=None, prior=None, decay=1.0):
+    """q [n, H_q, d], k [t, H, d], lse [n, H_q] -> dict of w [H, t] and err [H, t], the sum of
+    w_ij (scale * sum |q_e k_e| + 3 |lse_i| / d) that error bounds are made of.  Row i sees key
+    j <= i + t - n (causal), of those the ones that `seen` [t] names."""
+    q, k, lse = (np.asarray(x, np.float64) for x in (q, k, lse))
+    n, Hq, d = q.shape
+    t, H = k.shape[0], k.shape[1]
+    w, err = np.zeros((H, t)), np.zeros((H, t))
+    for i in range(n):
+        ok = np.ones(t, bool) if seen is None else np.array(seen, bool)
+        if causal:
+            ok = ok & (np.arange(t) <= i + t - n)
+        js = np.nonzero(ok)[0]
+        for h in range(Hq if js.size else 0):
+            kk = k[js, h // (Hq // H)]
+            with np.errstate(invalid="ignore", over="ignore"):
+                x = np.exp(scale * (kk @ q[i, h]) - lse[i, h])
+                w[h // (Hq // H), js] += x
+                err[h // (Hq // H), js] += x * (scale * (np.abs(kk) @ np.abs(q[i, h])) + 3 * abs(lse[i, h]) / d)
+    if prior is not None:
+        w = w + decay * np.asarray(prior, np.float64)
+    return dict(w=w, err=err)
+
+
+def evict_select(w, keep, first=0, last=0):
+    """Numbers of the tokens of one row of weights [t] that stay, rising."""
+    t = len(w)
+    if keep >= t:
+        return np.arange(t)
+    x = np.asarray(w, np.float64)
+    ends = set(range(first)) | set(range(t - last, t))
+    # (greater before less, a NaN after everything, then by number)
+    mid = sorted((i for i in range(t) if i not in ends),
+                 key=lambda i: (np.isnan(x[i]), 0.0 if np.isnan(x[i]) else -x[i], i))
+    return np.array(sorted(ends | set(mid[:keep - first - last])), np.int64)
+
+
+def sample(x, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """One row of logits -> dict of token, logprob, kept (the tokens that stay, in falling
+    order) and margin: how near, relative to the sums compared, the draw or the nucleus came
+    to a running sum (inf where nothing was compared)."""
+    x = np.asarray(x, np.float64)
+    bad = dict(token=-1, logprob=np.nan, kept=np.zeros(0, np.int64), margin=np.inf)
+    if np.isnan(x).any() or x.max() == -np.inf or not temperature < np.inf:
+        return bad
+    top = x.max()
+    if temperature <= 0:
+        i = int(np.argmax(x))
+        return dict(token=i, logprob=0.0, kept=np.array([i]), margin=np.inf)
+    with np.errstate(invalid="ignore"):
+        w = np.where(x == top, 1.0, np.exp((x - top) / temperature))
+    order = np.argsort(-x, kind="stable")
+    if 0 < top_k < len(order):
+        order = order[:top_k]
+    margin = np.inf
+    v = w[order]
+    c = np.cumsum(v)
+    n = len(order)
+    if top_p < 1:
+        target = max(float(top_p), 0.0) * c[-1]
+        n = max(1, int((c < target).sum()) + 1)
+        if target > 0:
+            margin = float(np.abs(c - target).min() / c[-1])
+    if min_p > 0:
+        n = min(n, max(1, int((v >= min(float(min_p), 1.0)).sum())))
+    kept, v = order[:n], v[:n]
+    c = np.cumsum(v)
+    u = min(max(0.0 if np.isnan(u) else float(u), 0.0), 1.0 - 2.0 ** -24)
+    target = u * c[-1]
+    i = min(int((c <= target).sum()), n - 1)
+    if target > 0:
+        margin = min(margin, float(np.abs(c[:-1] - target).min() / c[-1]) if n > 1 else np.inf)
+    with np.errstate(divide="ignore"):
+        return dict(token=int(kept[i]), logprob=float(np.log(v[i] / c[-1])), kept=kept, margin=margin)

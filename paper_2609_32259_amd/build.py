@@ -26,7 +26,7 @@ HIPCC = os.path.join(ROCM, "bin", "hipcc")
 ARCH = "gfx950"
 
 HIP_SOURCES = ["align.hip", "transfer.hip", "transfer_f32.hip", "staged.hip", "recolor.hip",
-               "attention.hip", "paged.hip"]
+               "attention.hip", "paged.hip", "weights.hip", "evict.hip", "sample.hip"]
 HOST_SOURCES = ["abi.cpp"]
 
 # Packed fp32 VALU instructions are disabled for all device code.

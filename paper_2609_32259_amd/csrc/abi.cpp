@@ -1002,6 +1002,15 @@ int32_t check_paged(const hf_paged_kv* c, int32_t layer, int32_t n_layers) {
   return HF_OK;
 }
 
+// Whether a cache's table has the pages for a batch's tokens.
+int32_t check_pages(const char* what, int32_t B, const int32_t* tokens, const hf_paged_kv* c) {
+  for (int b = 0; b < B; ++b)
+    if (((int64_t)tokens[b] + c->page_tokens - 1) / c->page_tokens > c->table_stride)
+      return fail(HF_ERR_CAPACITY, "%ssequence %d: %d tokens, the table has %lld pages of %d", what, b, tokens[b],
+                  (long long)c->table_stride, c->page_tokens);
+  return HF_OK;
+}
+
 int log2_of(int32_t p) {
   int k = 0;
   while ((1 << k) < p) ++k;
@@ -1170,6 +1179,375 @@ int32_t hf_paged_read(int32_t B, const int32_t* start, const int32_t* n, const h
                       int32_t layer, int32_t n_layers, const hf_rows* k, const hf_rows* v,
                       void* stream) {
   return paged_rows(false, B, start, n, cache, layer, n_layers, k, v, 0.0, nullptr, stream);
+}
+
+// ---------------------------------------------------------------------------
+// Weights of keys, eviction by them, sampling.
+// ---------------------------------------------------------------------------
+
+namespace {
+
+// layers: stride_l is used.
+int32_t check_weights(const char* name, const hf_key_weights* w, bool used, bool layers) {
+  if (!w) return fail(HF_ERR_NULL, "%s is NULL", name);
+  if (used && !w->ptr) return fail(HF_ERR_NULL, "%s->ptr is NULL", name);
+  if (reinterpret_cast<uintptr_t>(w->ptr) & 3u) return fail(HF_ERR_SHAPE, "%s->ptr not 4-byte aligned", name);
+  if (w->stride_b < 0 || w->stride_h < 0 || (layers && w->stride_l < 0))
+    return fail(HF_ERR_SHAPE, "%s: strides must be >= 0", name);
+  return HF_OK;
+}
+
+// What both weight calls check, and the batch's work items.
+int32_t weights_common(int32_t B, const int32_t* q_len, const int32_t* kv_len, const hf_rows* q, int32_t H,
+                       int32_t d_h, const float* lse, float scale, int32_t causal,
+                       const hf_key_weights* prior, float decay, const hf_key_weights* w, bool paged,
+                       hf::WeighShape& sh, hf::WeighArgs& a) {
+  int64_t pairs = 0, rows = 0, keys = 0, longest = 0;
+  for (int b = 0; b < B; ++b) {
+    pairs += std::min(q_len[b], kv_len[b]);
+    rows += q_len[b];
+    keys += kv_len[b];
+    longest = std::max(longest, (int64_t)q_len[b]);
+    if (kv_len[b] > kMaxKeys)
+      return fail(HF_ERR_UNSUPPORTED, "sequence %d: %d keys, at most %d are served", b, kv_len[b], kMaxKeys);
+  }
+  int32_t st;
+  if ((st = check_rows("q", q, pairs > 0, false, false))) return st;
+  if (q->d_h != d_h) return fail(HF_ERR_SHAPE, "q and the keys differ in d_h");
+  if ((st = check_heads(q->H, H, d_h))) return st;
+  if (!(scale > 0.0f) || !std::isfinite(scale * 1.5f)) return fail(HF_ERR_SHAPE, "scale must be finite and > 0");
+  if (pairs > 0 && !lse) return fail(HF_ERR_NULL, "lse is NULL");
+  if (reinterpret_cast<uintptr_t>(lse) & 3u) return fail(HF_ERR_SHAPE, "lse not 4-byte aligned");
+  if ((st = check_weights("w", w, keys > 0, false))) return st;
+  if (prior && (st = check_weights("prior", prior, keys > 0, false))) return st;
+  if (prior && !std::isfinite(decay)) return fail(HF_ERR_SHAPE, "decay must be finite");
+  const int64_t G = q->H / H;
+  if (rows > INT32_MAX || longest * G > INT32_MAX - 1024 || rows * q->H > ((int64_t)1 << 40))
+    return fail(HF_ERR_SHAPE, "too many query rows");
+  std::memset(&a, 0, sizeof a);
+  sh = hf::weigh_shape(q->dtype, paged, H, keys, longest * G);
+  int64_t items = 0, row = 0, key = 0;
+  for (int b = 0; b < B; ++b) {
+    a.s[b] = {(int32_t)items, q_len[b], kv_len[b], (int32_t)row, (int32_t)key, {}};
+    items += ((int64_t)kv_len[b] + sh.keys - 1) / sh.keys;
+    row += q_len[b];
+    key += kv_len[b];
+    if (items * H > kMaxGroups) return fail(HF_ERR_SHAPE, "too many work items");
+    if (key > INT32_MAX) return fail(HF_ERR_SHAPE, "too many keys");
+  }
+  a.q = q->ptr;
+  a.lse = lse;
+  a.out = w->ptr;
+  a.q_sb = q->stride_b; a.q_st = q->stride_t; a.q_sh = q->stride_h;
+  a.o_sb = w->stride_b; a.o_sh = w->stride_h;
+  if (prior) {
+    a.prior = prior->ptr;
+    a.p_sb = prior->stride_b;
+    a.p_sh = prior->stride_h;
+    a.decay = decay;
+  }
+  a.c = scale * 1.44269504088896340736f;
+  a.B = B;
+  a.H = H;
+  a.G = (int32_t)G;
+  a.causal = causal ? 1 : 0;
+  a.n_items = (int32_t)items;
+  a.by_g = hf::make_divide((uint32_t)G);
+  a.by_h = hf::make_divide(H);
+  return HF_OK;
+}
+
+// The lists of rows that stay, and the weights that move with them.
+int32_t evict_common(int32_t B, const int32_t* n, const int32_t* kv_len, int32_t n_layers, int32_t H,
+                     const int32_t* index, int64_t index_stride, const hf_key_weights* w,
+                     const hf_key_weights* w_to, bool in_place, int32_t block, hf::EvictArgs& a) {
+  int64_t total = 0, blocks = 0, from = 0, to = 0;
+  int32_t most = 0;
+  std::memset(&a, 0, sizeof a);
+  for (int b = 0; b < B; ++b) {
+    if (n[b] > kv_len[b]) return fail(HF_ERR_SHAPE, "sequence %d: %d rows stay of %d", b, n[b], kv_len[b]);
+    if (kv_len[b] > kMaxKeys)
+      return fail(HF_ERR_UNSUPPORTED, "sequence %d: %d rows, at most %d are served", b, kv_len[b], kMaxKeys);
+    a.s[b] = {(int32_t)blocks, n[b], kv_len[b], (int32_t)from, (int32_t)(in_place ? from : to), {}};
+    total += n[b];
+    blocks += ((int64_t)n[b] + block - 1) / block;
+    from += kv_len[b];
+    to += n[b];
+    most = std::max(most, n[b]);
+    if (blocks > kMaxGroups || from > INT32_MAX) return fail(HF_ERR_SHAPE, "too many rows");
+  }
+  if (n_layers < 1 || n_layers > 65535) return fail(HF_ERR_SHAPE, "n_layers %d outside [1, 65535]", n_layers);
+  if (H > 65535 / 3) return fail(HF_ERR_UNSUPPORTED, "at most %d heads are served", 65535 / 3);
+  if (total > 0 && !index) return fail(HF_ERR_NULL, "index is NULL");
+  if (reinterpret_cast<uintptr_t>(index) & 3u) return fail(HF_ERR_SHAPE, "index not 4-byte aligned");
+  if (index_stride < most) return fail(HF_ERR_CAPACITY, "index_stride %lld < %d", (long long)index_stride, most);
+  int32_t st;
+  if (!w && w_to) return fail(HF_ERR_NULL, "w is NULL");
+  if (w && in_place && w_to) return fail(HF_ERR_SHAPE, "in place w_to must be NULL");
+  if (w) {
+    if ((st = check_weights("w", w, total > 0, true))) return st;
+    if (!in_place && (st = check_weights("w_to", w_to, total > 0, true))) return st;
+    if (!in_place && total > 0 && w_to->ptr == w->ptr) return fail(HF_ERR_SHAPE, "w_to is w");
+    const hf_key_weights* d = in_place ? w : w_to;
+    a.w = w->ptr;
+    a.w_to = d->ptr;
+    a.w_sb = w->stride_b; a.w_sl = w->stride_l; a.w_sh = w->stride_h;
+    a.wt_sb = d->stride_b; a.wt_sl = d->stride_l; a.wt_sh = d->stride_h;
+  }
+  a.index = index;
+  a.i_stride = index_stride;
+  a.B = B;
+  a.H = H;
+  a.n_layers = n_layers;
+  a.n_blocks = (int32_t)blocks;
+  a.in_place = in_place;
+  return HF_OK;
+}
+
+}  // namespace
+
+int32_t hf_attention_weights(int32_t B, const int32_t* q_len, const int32_t* kv_len, const hf_rows* q,
+                             const hf_rows* k, const float* lse, float scale, int32_t causal,
+                             const hf_key_weights* prior, float decay, const hf_key_weights* w,
+                             void* stream) {
+  int32_t st;
+  if ((st = check_lens(B, "q_len", q_len, "kv_len", kv_len))) return st;
+  int64_t keys = 0;  // (all: a sequence without queries is written as well, and its keys are loaded)
+  for (int b = 0; b < B; ++b) keys += kv_len[b];
+  if ((st = check_rows("k", k, keys > 0, false, false))) return st;
+  hf::WeighShape sh;
+  hf::WeighArgs a;
+  if ((st = weights_common(B, q_len, kv_len, q, k->H, k->d_h, lse, scale, causal, prior, decay, w, false, sh, a)))
+    return st;
+  if (k->dtype != q->dtype) return fail(HF_ERR_DTYPE, "q and k dtypes differ");
+  a.k = k->ptr;
+  a.k_sb = k->stride_b; a.k_st = k->stride_t; a.k_sh = k->stride_h;
+  if (a.n_items == 0) return ok();
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  {
+    TimedLaunch t(HF_KERNEL_ATTENTION_WEIGHTS, s);
+    e = hf::launch_attention_weights(q->dtype, k->d_h, sh, a, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "attention weights launch");
+  return ok();
+}
+
+int32_t hf_paged_attention_weights(int32_t B, const int32_t* q_len, const int32_t* kv_len, const hf_rows* q,
+                                   const hf_paged_kv* cache, int32_t layer, const float* lse, float scale,
+                                   int32_t causal, const hf_key_weights* prior, float decay,
+                                   const hf_key_weights* w, void* stream) {
+  int32_t st;
+  if ((st = check_lens(B, "q_len", q_len, "kv_len", kv_len)) || (st = check_paged(cache, layer, 1)) ||
+      (st = check_pages("", B, kv_len, cache)))
+    return st;
+  hf::WeighShape sh;
+  hf::WeighArgs a;
+  if ((st = weights_common(B, q_len, kv_len, q, cache->H, cache->d_h, lse, scale, causal, prior, decay, w, true,
+                           sh, a)))
+    return st;
+  a.page_bytes = (long long)page_bytes(cache->H, cache->d_h, cache->page_tokens);
+  a.pages = static_cast<const uint8_t*>(cache->pages) + (int64_t)layer * cache->n_pages * a.page_bytes;
+  a.table = cache->table;
+  a.table_stride = cache->table_stride;
+  a.n_pages = cache->n_pages;
+  a.log2_page = log2_of(cache->page_tokens);
+  if (a.n_items == 0) return ok();
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  {
+    TimedLaunch t(HF_KERNEL_ATTENTION_WEIGHTS, s);
+    e = hf::launch_paged_weights(q->dtype, cache->d_h, a, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "paged attention weights launch");
+  return ok();
+}
+
+int32_t hf_evict_select(int32_t B, int32_t L, int32_t H, const int32_t* kv_len, const int32_t* keep,
+                        int32_t n_first, int32_t n_last, const hf_key_weights* w, int32_t* index,
+                        int64_t index_stride, void* stream) {
+  int32_t st;
+  if ((st = check_lens(B, "kv_len", kv_len, "keep", keep))) return st;
+  if (L < 1 || H < 1 || (int64_t)B * L > (kMaxGroups - 1) / H)
+    return fail(HF_ERR_SHAPE, "need L, H >= 1 and less than 2^22 rows");
+  if (n_first < 0 || n_last < 0) return fail(HF_ERR_SHAPE, "n_first and n_last must be >= 0");
+  hf::SelectArgs a;
+  std::memset(&a, 0, sizeof a);
+  int32_t most = 0;
+  for (int b = 0; b < B; ++b) {
+    if (kv_len[b] > kMaxKeys)
+      return fail(HF_ERR_UNSUPPORTED, "sequence %d: %d tokens, at most %d are served", b, kv_len[b], kMaxKeys);
+    if (keep[b] < kv_len[b] && (int64_t)n_first + n_last > keep[b])
+      return fail(HF_ERR_SHAPE, "sequence %d: n_first + n_last > keep = %d", b, keep[b]);
+    a.s[b] = {kv_len[b], std::min(keep[b], kv_len[b])};
+    most = std::max(most, a.s[b].keep);
+  }
+  if ((st = check_weights("w", w, most > 0, true))) return st;
+  if (most > 0 && !index) return fail(HF_ERR_NULL, "index is NULL");
+  if (reinterpret_cast<uintptr_t>(index) & 3u) return fail(HF_ERR_SHAPE, "index not 4-byte aligned");
+  if (index_stride < most) return fail(HF_ERR_CAPACITY, "index_stride %lld < %d", (long long)index_stride, most);
+  if (most == 0) return ok();
+  a.w = w->ptr;
+  a.w_sb = w->stride_b; a.w_sl = w->stride_l; a.w_sh = w->stride_h;
+  a.index = index;
+  a.i_stride = index_stride;
+  a.B = B;
+  a.L = L;
+  a.H = H;
+  a.first = n_first;
+  a.last = n_last;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  {
+    TimedLaunch t(HF_KERNEL_EVICT_SELECT, s);
+    e = hf::launch_evict_select(a, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "eviction choice launch");
+  return ok();
+}
+
+int32_t hf_evict_rows(int32_t B, const int32_t* n, const int32_t* kv_len, int32_t n_layers,
+                      const int32_t* index, int64_t index_stride, const hf_rows* k, const hf_rows* v,
+                      const hf_rows* k_to, const hf_rows* v_to, const hf_key_weights* w,
+                      const hf_key_weights* w_to, void* stream) {
+  int32_t st;
+  if ((st = check_lens(B, "n", n, "kv_len", kv_len))) return st;
+  const bool in_place = !k_to && !v_to;
+  int64_t total = 0;
+  for (int b = 0; b < B; ++b) total += n[b];
+  if ((st = check_rows("k", k, total > 0, in_place, true)) || (st = check_rows("v", v, total > 0, in_place, true)))
+    return st;
+  if (k->dtype != v->dtype) return fail(HF_ERR_DTYPE, "k and v dtypes differ");
+  if (k->H != v->H || k->d_h != v->d_h) return fail(HF_ERR_SHAPE, "k and v differ in heads or d_h");
+  if (!in_place) {
+    if ((st = check_rows("k_to", k_to, total > 0, true, true)) ||
+        (st = check_rows("v_to", v_to, total > 0, true, true)))
+      return st;
+    if (k_to->dtype != k->dtype || v_to->dtype != v->dtype) return fail(HF_ERR_DTYPE, "k_to, v_to and k dtypes differ");
+    if (k_to->H != k->H || v_to->H != k->H || k_to->d_h != k->d_h || v_to->d_h != k->d_h)
+      return fail(HF_ERR_SHAPE, "k_to, v_to and k differ in heads or d_h");
+    if (total > 0 && (k_to->ptr == k->ptr || v_to->ptr == v->ptr || k_to->ptr == v_to->ptr))
+      return fail(HF_ERR_SHAPE, "k_to and v_to must be other memory (NULL both: in place)");
+  }
+  const int64_t el = k->dtype == HF_BF16 ? 2 : 4, bytes = k->d_h * el;
+  if (bytes % 16) return fail(HF_ERR_SHAPE, "rows must be a multiple of 16 bytes (d_h %d)", k->d_h);
+  if (bytes > 16384) return fail(HF_ERR_UNSUPPORTED, "rows of at most 16,384 bytes are served (d_h %d)", k->d_h);
+  hf::EvictArgs a;
+  if ((st = evict_common(B, n, kv_len, n_layers, k->H, index, index_stride, w, w_to, in_place,
+                         hf::evict_block((int)bytes), a)))
+    return st;
+  if (a.n_blocks == 0) return ok();
+  const hf_rows* from[2] = {k, v};
+  const hf_rows* to[2] = {in_place ? k : k_to, in_place ? v : v_to};
+  for (int i = 0; i < 2; ++i) {  // strides in bytes
+    a.from[i] = from[i]->ptr;
+    a.to[i] = to[i]->ptr;
+    a.f_sb[i] = from[i]->stride_b == -1 ? -1 : from[i]->stride_b * el;
+    a.f_sl[i] = from[i]->stride_l * el; a.f_st[i] = from[i]->stride_t * el; a.f_sh[i] = from[i]->stride_h * el;
+    a.t_sb[i] = to[i]->stride_b == -1 ? -1 : to[i]->stride_b * el;
+    a.t_sl[i] = to[i]->stride_l * el; a.t_st[i] = to[i]->stride_t * el; a.t_sh[i] = to[i]->stride_h * el;
+  }
+  a.row_bytes = (int32_t)bytes;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  {
+    TimedLaunch t(HF_KERNEL_EVICT_MOVE, s);
+    e = hf::launch_evict_rows(a, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "eviction launch");
+  return ok();
+}
+
+int32_t hf_paged_evict(int32_t B, const int32_t* n, const int32_t* kv_len, const hf_paged_kv* cache,
+                       const hf_paged_kv* to, int32_t layer, int32_t n_layers, const int32_t* index,
+                       int64_t index_stride, const hf_key_weights* w, const hf_key_weights* w_to,
+                       void* stream) {
+  int32_t st;
+  if ((st = check_lens(B, "n", n, "kv_len", kv_len)) || (st = check_paged(cache, layer, n_layers)) ||
+      (st = check_pages("", B, kv_len, cache)))
+    return st;
+  if (to) {
+    if ((st = check_paged(to, layer, n_layers)) || (st = check_pages("to: ", B, n, to))) return st;
+    if (to->H != cache->H || to->d_h != cache->d_h || to->page_tokens != cache->page_tokens)
+      return fail(HF_ERR_SHAPE, "to and the cache differ in heads, d_h or page_tokens");
+    if (to->table == cache->table) return fail(HF_ERR_SHAPE, "to must name other pages (NULL: in place)");
+    if (to->pages == cache->pages && to->n_pages != cache->n_pages)
+      return fail(HF_ERR_SHAPE, "to and the cache share their pages but differ in n_pages");
+  }
+  hf::EvictArgs a;
+  if ((st = evict_common(B, n, kv_len, n_layers, cache->H, index, index_stride, w, w_to, !to, 32, a))) return st;
+  if (a.n_blocks == 0) return ok();
+  const hf_paged_kv* d = to ? to : cache;
+  a.page_bytes = (long long)page_bytes(cache->H, cache->d_h, cache->page_tokens);
+  a.pages = static_cast<const uint8_t*>(cache->pages) + (int64_t)layer * cache->n_pages * a.page_bytes;
+  a.pages_to = static_cast<uint8_t*>(d->pages) + (int64_t)layer * d->n_pages * a.page_bytes;
+  a.table = cache->table;
+  a.table_to = d->table;
+  a.table_stride = cache->table_stride;
+  a.table_to_stride = d->table_stride;
+  a.n_pages = cache->n_pages;
+  a.n_pages_to = d->n_pages;
+  a.log2_page = log2_of(cache->page_tokens);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  {
+    TimedLaunch t(HF_KERNEL_EVICT_MOVE, s);
+    e = hf::launch_paged_evict(cache->d_h, a, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "paged eviction launch");
+  return ok();
+}
+
+namespace {
+
+constexpr int32_t kMaxVocab = 1 << 20;
+
+int32_t check_sample(int32_t n, int32_t vocab, int32_t dtype) {
+  if (n < 0) return fail(HF_ERR_SHAPE, "n must be >= 0");
+  if (dtype != HF_F32 && dtype != HF_BF16) return fail(HF_ERR_DTYPE, "dtype %d unknown", dtype);
+  if (vocab < 1) return fail(HF_ERR_SHAPE, "vocab must be >= 1");
+  if (vocab > kMaxVocab) return fail(HF_ERR_UNSUPPORTED, "vocab %d, at most %d is served", vocab, kMaxVocab);
+  if (n >= kMaxGroups) return fail(HF_ERR_SHAPE, "too many rows");
+  return HF_OK;
+}
+
+}  // namespace
+
+size_t hf_sample_workspace_bytes(int32_t n, int32_t vocab, int32_t dtype) {
+  if (check_sample(n, vocab, dtype)) return 0;
+  ok();
+  return hf::sample_workspace_bytes(dtype, n, vocab);
+}
+
+int32_t hf_sample_tokens(int32_t n, int32_t vocab, int32_t dtype, const void* x, int64_t stride,
+                         const float* temperature, const int32_t* top_k, const float* top_p,
+                         const float* min_p, const float* u, int32_t* token, float* logprob,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+  int32_t st;
+  if ((st = check_sample(n, vocab, dtype))) return st;
+  if (n > 0 && (!x || !u || !token)) return fail(HF_ERR_NULL, "x, u or token is NULL");
+  if (stride < vocab) return fail(HF_ERR_SHAPE, "stride %lld < vocab %d", (long long)stride, vocab);
+  if (reinterpret_cast<uintptr_t>(x) & (dtype == HF_BF16 ? 1u : 3u)) return fail(HF_ERR_SHAPE, "x not aligned");
+  for (const void* p : {(const void*)temperature, (const void*)top_k, (const void*)top_p, (const void*)min_p,
+                        (const void*)u, (const void*)token, (const void*)logprob})
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return fail(HF_ERR_SHAPE, "settings and results must be 4-byte aligned");
+  const size_t need = hf::sample_workspace_bytes(dtype, n, vocab);
+  if (need) {
+    if (!workspace) return fail(HF_ERR_NULL, "workspace is NULL");
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(HF_ERR_SHAPE, "workspace is not 256-byte aligned");
+    if (workspace_bytes < need)
+      return fail(HF_ERR_CAPACITY, "workspace %zu bytes < required %zu", workspace_bytes, need);
+  }
+  if (n == 0) return ok();
+  hf::SampleArgs a = {x, stride, temperature, top_k, top_p, min_p, u, token, logprob, workspace, n, vocab};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  {
+    TimedLaunch t(HF_KERNEL_SAMPLE, s);
+    e = hf::launch_sample(dtype, a, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "sampling launch");
+  return ok();
 }
 
 // ---------------------------------------------------------------------------

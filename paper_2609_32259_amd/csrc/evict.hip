@@ -1,0 +1,354 @@
+// Eviction from a cache by the weight of its keys: which tokens of each layer and head stay
+// (hf_evict_select), and their rows moved together, in place or into another cache, dense
+// (hf_evict_rows) or held in 4 bits (hf_paged_evict).
+#include <hip/hip_runtime.h>
+
+#include "hf_paged.h"
+
+namespace hf {
+namespace {
+
+// ---------------------------------------------------------------------------
+// Choice.  Of the tokens between the first and the last ones that stay anyway, the `need` of
+// the greatest weight, equal ones by number.  Weights are mapped to whole numbers of the same
+// order, the need-th greatest of them is found 11, 11 and 10 bits at a time by counting
+// (a histogram of those that agree in the bits found so far), and a last walk in the order
+// of the tokens writes those above it, and as many equal to it as there is room for.  A
+// workgroup has a row; its waves have runs of consecutive tokens, kept in registers where
+// the row is short enough.
+// ---------------------------------------------------------------------------
+constexpr int kBins = 2048;
+constexpr int kKept = 32;  // weights that a lane keeps in registers
+
+// NaN below everything, the two zeros equal.
+FI uint32_t ordered(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.0f);
+  const uint32_t k = u & 0x80000000u ? ~u : u | 0x80000000u;
+  return x != x ? 0u : k;
+}
+
+FI int scan_add(int x, int lane) {  // inclusive, over the wave
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+
+template <int NW, bool REG>
+__global__ __launch_bounds__(64 * NW) void evict_select_kernel(const SelectArgs a) {
+  constexpr int NT = 64 * NW, BPT = kBins / NT;
+  __shared__ int hist[kBins];
+  __shared__ int part[NW], part2[NW];
+  __shared__ int found[3];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = blockIdx.x, bl = row / a.H, h = row - bl * a.H, b = bl / a.L, l = bl - b * a.L;
+  const int t = a.s[b].t, keep = a.s[b].keep;
+  int32_t* index = a.index + row * a.i_stride;
+  if (keep >= t) {
+    for (int i = threadIdx.x; i < t; i += NT) index[i] = i;
+    return;
+  }
+  const float* w = a.w + b * a.w_sb + l * a.w_sl + h * a.w_sh;
+  const int lo = a.first, hi = t - a.last;
+  int need = keep - a.first - a.last;
+  const int seg = (t + NT - 1) / NT * 64, base = wave * seg;
+  uint32_t kept[REG ? kKept : 1];
+  if (REG) {
+#pragma unroll
+    for (int e = 0; e < kKept; ++e) {
+      const int i = base + 64 * e + lane;
+      kept[e] = 64 * e < seg && i < t ? ordered(w[i]) : 0u;
+    }
+  }
+  // f(key, token) for the wave's tokens in order, 64 at a time (all lanes together)
+  auto each = [&](auto f) {
+    if (REG) {
+#pragma unroll
+      for (int e = 0; e < kKept; ++e) {
+        if (64 * e >= seg) break;
+        f(kept[e], base + 64 * e + lane);
+      }
+    } else {
+      for (int e = 0; e < seg && base + e < t; e += 64) {
+        const int i = base + e + lane;
+        f(i < t ? ordered(w[i]) : 0u, i);
+      }
+    }
+  };
+
+  uint32_t prefix = 0, same = 0;  // the bits found, and which they are
+  bool whole = need == 0;         // all that agree with the prefix stay (or none is wanted)
+  for (int shift = 21; !whole && shift >= 0; shift = shift == 21 ? 10 : shift == 10 ? 0 : -1) {
+    const uint32_t bins = shift == 0 ? 1023u : 2047u;
+    for (int i = threadIdx.x; i < kBins; i += NT) hist[i] = 0;
+    __syncthreads();
+    each([&](uint32_t k, int i) {
+      if (i >= lo && i < hi && (k & same) == prefix) atomicAdd(&hist[(k >> shift) & bins], 1);
+    });
+    __syncthreads();
+    // thread x has bins from the top: kBins - 1 - x BPT, ..
+    int n[BPT], sum = 0;
+#pragma unroll
+    for (int i = 0; i < BPT; ++i) sum += n[i] = hist[kBins - 1 - threadIdx.x * BPT - i];
+    const int upto = scan_add(sum, lane);
+    if (lane == 63) part[wave] = upto;
+    __syncthreads();
+    int above = upto - sum;
+    for (int y = 0; y < wave; ++y) above += part[y];
+    if (above < need && need <= above + sum) {
+#pragma unroll
+      for (int i = 0; i < BPT; ++i) {
+        if (above < need && need <= above + n[i]) {
+          found[0] = kBins - 1 - threadIdx.x * BPT - i;
+          found[1] = need - above;
+          found[2] = n[i];
+        }
+        above += n[i];
+      }
+    }
+    __syncthreads();
+    prefix |= (uint32_t)found[0] << shift;
+    same |= bins << shift;
+    need = found[1];
+    whole = need == found[2];
+  }
+  // Tokens that stay: those above `over`, and the first `ties` of those equal to it.
+  const int ties = whole ? 0 : need;
+  const bool none = need == 0;
+  auto stays = [&](uint32_t k, int i, bool& equal) {
+    const bool mid = i >= lo && i < hi;
+    equal = mid && !whole && k == prefix;
+    return i < t && (!mid || (!none && (whole ? k >= prefix : k > prefix)));
+  };
+  int over = 0, level = 0;
+  each([&](uint32_t k, int i) {
+    bool equal;
+    const bool s = stays(k, i, equal);
+    over += __popcll(__ballot(s));
+    level += __popcll(__ballot(equal));
+  });
+  if (lane == 0) {
+    part[wave] = over;
+    part2[wave] = level;
+  }
+  __syncthreads();
+  over = level = 0;
+  for (int y = 0; y < wave; ++y) {
+    over += part[y];
+    level += part2[y];
+  }
+  const unsigned long long below = (1ull << lane) - 1;
+  each([&](uint32_t k, int i) {
+    bool equal;
+    const bool s = stays(k, i, equal);
+    const unsigned long long ms = __ballot(s), me = __ballot(equal);
+    const int rank = level + __popcll(me & below);  // among the equal ones
+    if (s || (equal && rank < ties)) index[over + __popcll(ms & below) + min(rank, ties)] = i;
+    over += __popcll(ms);
+    level += __popcll(me);
+  });
+}
+
+// ---------------------------------------------------------------------------
+// Moving.  In place a workgroup takes all rows of a layer, head and role, block after block:
+// an index never lies below its place in the list, so what a block writes was needed by it
+// or by the blocks before it, and a barrier between a block's reads and its writes is enough.
+// Into other memory every block is a workgroup of its own.
+// ---------------------------------------------------------------------------
+
+// Before a block's rows are written: every wave's loads are there.
+FI void all_read() {
+  __builtin_amdgcn_s_waitcnt(kWaitMemory);
+  __syncthreads();
+}
+
+// Rows at the front that stay where they are (at least; whole 256ths of n).
+FI int unmoved(const int32_t* index, int n) {
+  const int step = (n + blockDim.x - 1) / blockDim.x, i = threadIdx.x * step;
+  const int same = __syncthreads_count(i < n && index[i] == i);
+  return same > 0 ? (same - 1) * step : 0;
+}
+
+FI void evict_weights(const EvictArgs& a, const EvictSeq& q, const int32_t* index, int b, int l, int h, int r0,
+                      int rows) {
+  const float* w = a.w + b * a.w_sb + l * a.w_sl + h * a.w_sh;
+  float* to = a.w_to + b * a.wt_sb + l * a.wt_sl + h * a.wt_sh;
+  for (int r = threadIdx.x; r - (int)threadIdx.x < rows; r += blockDim.x) {  // (all threads meet at the barrier)
+    const bool on = r < rows && r0 + r < q.n;
+    const float x = on ? w[min(max(index[r0 + r], 0), q.t - 1)] : 0.0f;
+    if (a.in_place) all_read();
+    if (on) to[r0 + r] = x;
+  }
+}
+
+constexpr int kChunks = 4;  // of 16 bytes a thread and block
+
+__global__ __launch_bounds__(256) void evict_rows_kernel(const EvictArgs a) {
+  const int cpr = a.row_bytes / 16, block = kChunks * 256 / cpr;
+  const int role = blockIdx.y / a.H, h = blockIdx.y - role * a.H, l = blockIdx.z;
+  const int b = a.in_place ? blockIdx.x : find_seq(a.s, &EvictSeq::blk0, a.B, blockIdx.x);
+  const EvictSeq q = a.s[b];
+  const int32_t* index = a.index + (((long long)b * a.n_layers + l) * a.H + h) * a.i_stride;
+  int r0 = a.in_place ? unmoved(index, q.n) : (blockIdx.x - q.blk0) * block;
+  const int end = a.in_place ? q.n : min(q.n, r0 + block);
+  const bool keys = role == 0;
+  const char* from = static_cast<const char*>(keys ? a.from[0] : a.from[1]) +
+                     seq_at(b, q.from0, keys ? a.f_sb[0] : a.f_sb[1], keys ? a.f_st[0] : a.f_st[1]) +
+                     l * (keys ? a.f_sl[0] : a.f_sl[1]) + h * (keys ? a.f_sh[0] : a.f_sh[1]);
+  char* to = static_cast<char*>(keys ? a.to[0] : a.to[1]) +
+             seq_at(b, q.to0, keys ? a.t_sb[0] : a.t_sb[1], keys ? a.t_st[0] : a.t_st[1]) +
+             l * (keys ? a.t_sl[0] : a.t_sl[1]) + h * (keys ? a.t_sh[0] : a.t_sh[1]);
+  const long long f_st = keys ? a.f_st[0] : a.f_st[1], t_st = keys ? a.t_st[0] : a.t_st[1];
+  for (; r0 < end; r0 += block) {
+    if (role == 2) {
+      evict_weights(a, q, index, b, l, h, r0, block);
+      continue;
+    }
+    u32x4 v[kChunks];
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+      const int c = i * 256 + threadIdx.x, r = c / cpr, x = c - r * cpr;
+      if (r < block && r0 + r < end) {
+        const int src = min(max(index[r0 + r], 0), q.t - 1);
+        v[i] = *reinterpret_cast<const u32x4*>(from + src * f_st + x * 16);
+      }
+    }
+    if (a.in_place) all_read();
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+      const int c = i * 256 + threadIdx.x, r = c / cpr, x = c - r * cpr;
+      if (r < block && r0 + r < end) *reinterpret_cast<u32x4*>(to + (r0 + r) * t_st + x * 16) = v[i];
+    }
+  }
+}
+
+// Pages: a block is 32 tokens, the unit of the value codes' order, with both roles of a
+// head.  Key codes and words move as they are, 16 and 4 bytes a thread.  A thread of the
+// value codes has 16 bytes of the block, a nibble of eight tokens in each; it loads the
+// same 16 bytes of each of those tokens' old blocks and takes a nibble out of each.
+template <int D>
+__global__ __launch_bounds__(2 * D) void paged_evict_kernel(const EvictArgs a) {
+  constexpr int G = D / 32;
+  __shared__ const uint8_t* src_head[32];
+  __shared__ int src_row[32];
+  const int h = blockIdx.y, l = blockIdx.z;
+  const int b = a.in_place ? blockIdx.x : find_seq(a.s, &EvictSeq::blk0, a.B, blockIdx.x);
+  const EvictSeq q = a.s[b];
+  const int32_t* index = a.index + (((long long)b * a.n_layers + l) * a.H + h) * a.i_stride;
+  const PageHead<D> ph(a.log2_page);
+  const int P = 1 << a.log2_page;
+  const long long head_at = (long long)h * ph.bytes();
+  int r0 = a.in_place ? unmoved(index, q.n) & ~31 : (blockIdx.x - q.blk0) * 32;
+  const int end = a.in_place ? q.n : min(q.n, r0 + 32);
+  const int tid = threadIdx.x;
+  for (; r0 < end; r0 += 32) {
+    const int page_to = a.table_to[b * a.table_to_stride + (r0 >> a.log2_page)];
+    const bool drop = (unsigned)page_to >= (unsigned)a.n_pages_to;
+    uint8_t* to = a.pages_to + ((long long)l * a.n_pages_to + (drop ? 0 : page_to)) * a.page_bytes + head_at;
+    const int row_to = r0 & (P - 1);
+    if (a.in_place) __syncthreads();  // (nobody reads the last block's list any more)
+    float weight = 0.0f;
+    if (tid < 32) {
+      const uint8_t* head = nullptr;
+      int row = 0;
+      if (r0 + tid < q.n) {
+        const int tok = min(max(index[r0 + tid], 0), q.t - 1);
+        const int page = a.table[b * a.table_stride + (tok >> a.log2_page)];
+        if ((unsigned)page < (unsigned)a.n_pages)
+          head = a.pages + ((long long)l * a.n_pages + page) * a.page_bytes + head_at;
+        row = tok & (P - 1);
+        if (a.w) weight = a.w[b * a.w_sb + l * a.w_sl + h * a.w_sh + tok];
+      }
+      src_head[tid] = head;
+      src_row[tid] = row;
+    }
+    __syncthreads();
+    // the words
+    const int wt = (tid & (D - 1)) / G, wg = tid % G, wr = tid / D;
+    uint32_t word = 0;
+    const bool word_on = !drop && r0 + wt < q.n;
+    if (word_on && src_head[wt])
+      word = reinterpret_cast<const uint32_t*>(src_head[wt] + ph.word(wr, src_row[wt]))[wg];
+    // the codes
+    u32x4 code = {};
+    uint32_t mask = 0;  // nibbles of tokens that are the call's
+    const int piece = tid & (D - 1), kt = piece / G, m = piece / (D / 4), x = piece % (D / 4);
+    uint32_t* code_to;
+    if (tid < D) {
+      code_to = reinterpret_cast<uint32_t*>(to + ph.kcode(row_to + kt)) + 4 * (piece % G);
+      if (r0 + kt < q.n) {
+        mask = 0xffffffffu;
+        if (src_head[kt])
+          code = *reinterpret_cast<const u32x4*>(src_head[kt] + ph.kcode(src_row[kt]) + (piece % G) * 16);
+      }
+    } else {
+      code_to = reinterpret_cast<uint32_t*>(to + ph.vcode(row_to)) + 4 * piece;
+      u32x4 v[8];
+#pragma unroll
+      for (int y = 0; y < 8; ++y) {
+        const int tok = 16 * (y >> 2) + 4 * m + (y & 3);
+        v[y] = u32x4{};
+        if (r0 + tok < q.n) mask |= 15u << (4 * y);
+        if (src_head[tok]) {
+          const int s = src_row[tok];
+          v[y] = *reinterpret_cast<const u32x4*>(src_head[tok] + ph.vcode(s & ~31) +
+                                                 (((s >> 2) & 3) * (D / 4) + x) * 16);
+        }
+      }
+#pragma unroll
+      for (int y = 0; y < 8; ++y) {
+        const int s = src_row[16 * (y >> 2) + 4 * m + (y & 3)];
+        const int shift = 4 * (4 * ((s >> 4) & 1) + (s & 3));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) code[e] |= ((v[y][e] >> shift) & 15u) << (4 * y);
+      }
+    }
+    if (a.in_place) all_read();
+    if (tid < 32 && a.w && r0 + tid < q.n) a.w_to[b * a.wt_sb + l * a.wt_sl + h * a.wt_sh + r0 + tid] = weight;
+    if (drop) continue;
+    if (word_on) reinterpret_cast<uint32_t*>(to + ph.word(wr, row_to + wt))[wg] = word;
+    if (mask == 0xffffffffu) {
+      *reinterpret_cast<u32x4*>(code_to) = code;
+    } else if (mask) {  // (tokens behind the last that stays keep their nibbles)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) code_to[e] = (code_to[e] & ~mask) | code[e];
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_evict_select(const SelectArgs& a, hipStream_t s) {
+  const unsigned rows = (unsigned)(a.B * a.L * a.H);
+  int longest = 0;
+  for (int b = 0; b < a.B; ++b) longest = a.s[b].t > longest ? a.s[b].t : longest;
+  if (longest <= 4 * 64 * kKept)
+    evict_select_kernel<4, true><<<rows, 256, 0, s>>>(a);
+  else if (longest <= 16 * 64 * kKept)
+    evict_select_kernel<16, true><<<rows, 1024, 0, s>>>(a);
+  else
+    evict_select_kernel<16, false><<<rows, 1024, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+int evict_block(int row_bytes) { return kChunks * 256 / (row_bytes / 16); }
+
+hipError_t launch_evict_rows(const EvictArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)(a.in_place ? a.B : a.n_blocks), (unsigned)(a.H * (a.w ? 3 : 2)), (unsigned)a.n_layers);
+  evict_rows_kernel<<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_evict(int d_h, const EvictArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)(a.in_place ? a.B : a.n_blocks), (unsigned)a.H, (unsigned)a.n_layers);
+  if (d_h == 128)
+    paged_evict_kernel<128><<<grid, 256, 0, s>>>(a);
+  else
+    paged_evict_kernel<64><<<grid, 128, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace hf

@@ -272,4 +272,99 @@ static_assert(sizeof(PagedRowsArgs) <= 4096, "kernel argument size");
 hipError_t launch_paged_append(int dtype, int d_h, const PagedRowsArgs& a, hipStream_t s);
 hipError_t launch_paged_read(int dtype, int d_h, const PagedRowsArgs& a, hipStream_t s);
 
+// Key weights (weights.hip): work items are tiles of keys of a sequence and head.
+struct WeighSeq {
+  int32_t item0;       // first tile of the sequence among those of a head
+  int32_t n, t;        // query tokens, keys
+  int32_t row0, key0;  // rows and keys of the sequences before it
+  int32_t pad[3];
+};
+struct WeighArgs {
+  const void* q;
+  const float* lse;
+  const float* prior;  // or nullptr
+  float* out;
+  long long q_sb, q_st, q_sh, p_sb, p_sh, o_sb, o_sh;
+  const void* k;       // dense
+  long long k_sb, k_st, k_sh;
+  const uint8_t* pages;  // paged: the layer's first page
+  const int32_t* table;
+  long long table_stride, page_bytes;
+  int32_t n_pages, log2_page;
+  float c, decay;      // c: scale * log2(e)
+  int32_t B, H, G, causal, n_items;
+  Divide by_g, by_h;
+  alignas(32) WeighSeq s[HF_MAX_BATCH];
+};
+static_assert(sizeof(WeighArgs) <= 4096, "kernel argument size");
+struct WeighShape {
+  int32_t keys;       // of a work item
+  int32_t row_waves;  // waves that share an item's rows
+};
+WeighShape weigh_shape(int dtype, bool paged, int64_t heads, int64_t keys, int64_t rows);
+hipError_t launch_attention_weights(int dtype, int d_h, const WeighShape& sh, const WeighArgs& a,
+                                    hipStream_t s);
+hipError_t launch_paged_weights(int dtype, int d_h, const WeighArgs& a, hipStream_t s);
+
+// Eviction (evict.hip): which tokens stay, and their rows moved together.
+struct SelectSeq {
+  int32_t t, keep;   // keys, and how many stay (<= t)
+};
+struct SelectArgs {
+  const float* w;
+  int32_t* index;
+  long long w_sb, w_sl, w_sh, i_stride;  // i_stride: entries of a layer and head
+  int32_t B, L, H, first, last;
+  SelectSeq s[HF_MAX_BATCH];
+};
+hipError_t launch_evict_select(const SelectArgs& a, hipStream_t s);
+
+struct EvictSeq {
+  int32_t blk0;      // first block of rows of the sequence
+  int32_t n, t;      // rows that stay, rows there are
+  int32_t from0, to0;  // rows of the sequences before it, where rows lie packed
+  int32_t pad[3];
+};
+struct EvictArgs {
+  const void* from[2];       // dense: keys, values
+  void* to[2];
+  long long f_sb[2], f_sl[2], f_st[2], f_sh[2];
+  long long t_sb[2], t_sl[2], t_st[2], t_sh[2];
+  const uint8_t* pages;      // paged: of the call's first layer
+  uint8_t* pages_to;
+  const int32_t* table;
+  const int32_t* table_to;
+  long long table_stride, table_to_stride, page_bytes;
+  int32_t n_pages, n_pages_to, log2_page;
+  const int32_t* index;
+  long long i_stride;
+  const float* w;            // or nullptr
+  float* w_to;
+  long long w_sb, w_sl, w_sh, wt_sb, wt_sl, wt_sh;
+  int32_t B, H, n_layers, n_blocks, row_bytes;
+  int32_t in_place;
+  alignas(32) EvictSeq s[HF_MAX_BATCH];
+};
+static_assert(sizeof(EvictArgs) <= 4096, "kernel argument size");
+int evict_block(int row_bytes);  // rows of a block of dense rows
+hipError_t launch_evict_rows(const EvictArgs& a, hipStream_t s);
+hipError_t launch_paged_evict(int d_h, const EvictArgs& a, hipStream_t s);
+
+// Sampling (sample.hip).
+struct SampleArgs {
+  const void* x;
+  long long stride;
+  const float* temperature;  // [n] each, or nullptr
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  const float* u;
+  int32_t* token;
+  float* logprob;            // or nullptr
+  void* ws;
+  int32_t n, vocab;
+};
+size_t sample_workspace_bytes(int dtype, int n, int vocab);
+hipError_t launch_sample(int dtype, const SampleArgs& a, hipStream_t s);
+
 }  // namespace hf

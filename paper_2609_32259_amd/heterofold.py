@@ -38,6 +38,7 @@ HF_KERNEL_TRANSFER_STAGE = 8
 HF_KERNEL_STAGED_BUILD, HF_KERNEL_STAGED_GEMM = 9, 10
 HF_KERNEL_PROMPT_ATTENTION, HF_KERNEL_PAGED_ATTENTION, HF_KERNEL_ATTENTION_JOIN = 11, 12, 13
 HF_KERNEL_PAGED_APPEND, HF_KERNEL_PAGED_READ = 14, 15
+HF_KERNEL_ATTENTION_WEIGHTS, HF_KERNEL_EVICT_SELECT, HF_KERNEL_EVICT_MOVE, HF_KERNEL_SAMPLE = 16, 17, 18, 19
 HF_MAX_BATCH = 64
 ALIGN_MODES = {"overlap": HF_ALIGN_OVERLAP, "ta": HF_ALIGN_TA}
 
@@ -75,6 +76,11 @@ class hf_paged_kv(C.Structure):
     _fields_ = [("pages", C.c_void_p), ("table", C.c_void_p), ("table_stride", C.c_int64),
                 ("n_pages", C.c_int32), ("L", C.c_int32), ("H", C.c_int32), ("d_h", C.c_int32),
                 ("page_tokens", C.c_int32)]
+
+
+class hf_key_weights(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("stride_b", C.c_int64), ("stride_l", C.c_int64),
+                ("stride_h", C.c_int64)]
 
 
 class hf_recolor_info(C.Structure):
@@ -139,6 +145,31 @@ _SIGNATURES = {
                                        C.POINTER(hf_paged_kv), C.c_int32, C.POINTER(hf_rows),
                                        C.c_float, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t,
                                        C.c_void_p]),
+    "hf_attention_weights": (C.c_int32, [C.c_int32, _I32P, _I32P, C.POINTER(hf_rows),
+                                         C.POINTER(hf_rows), C.c_void_p, C.c_float, C.c_int32,
+                                         C.POINTER(hf_key_weights), C.c_float,
+                                         C.POINTER(hf_key_weights), C.c_void_p]),
+    "hf_paged_attention_weights": (C.c_int32, [C.c_int32, _I32P, _I32P, C.POINTER(hf_rows),
+                                               C.POINTER(hf_paged_kv), C.c_int32, C.c_void_p,
+                                               C.c_float, C.c_int32, C.POINTER(hf_key_weights),
+                                               C.c_float, C.POINTER(hf_key_weights),
+                                               C.c_void_p]),
+    "hf_evict_select": (C.c_int32, [C.c_int32, C.c_int32, C.c_int32, _I32P, _I32P, C.c_int32,
+                                    C.c_int32, C.POINTER(hf_key_weights), C.c_void_p, C.c_int64,
+                                    C.c_void_p]),
+    "hf_evict_rows": (C.c_int32, [C.c_int32, _I32P, _I32P, C.c_int32, C.c_void_p, C.c_int64,
+                                  C.POINTER(hf_rows), C.POINTER(hf_rows), C.POINTER(hf_rows),
+                                  C.POINTER(hf_rows), C.POINTER(hf_key_weights),
+                                  C.POINTER(hf_key_weights), C.c_void_p]),
+    "hf_paged_evict": (C.c_int32, [C.c_int32, _I32P, _I32P, C.POINTER(hf_paged_kv),
+                                   C.POINTER(hf_paged_kv), C.c_int32, C.c_int32, C.c_void_p,
+                                   C.c_int64, C.POINTER(hf_key_weights),
+                                   C.POINTER(hf_key_weights), C.c_void_p]),
+    "hf_sample_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
+    "hf_sample_tokens": (C.c_int32, [C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int64,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                     C.c_void_p]),
     "hf_recolor_moments_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int32, C.c_int32]),
     "hf_recolor_moments": (C.c_int32, [C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
                                        C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
@@ -766,6 +797,240 @@ def hf_paged_read(cache: PagedKV, start, n, k, v, layer=0, stream=None):
                                  _raw_stream(dev))
     _check(st, "hf_paged_read")
     return k, v
+
+
+# ---------------------------------------------------------------------------
+# Weights of keys, eviction by them, sampling
+# ---------------------------------------------------------------------------
+
+def _weights(t, shape, name, dev) -> hf_key_weights:
+    """Descriptor of fp32 numbers of keys [B, H, T] or [B, L, H, T], of which the first
+    shape[-1] of each row are meant."""
+    torch = _torch()
+    if t.dtype is not torch.float32 or t.device != dev:
+        raise TypeError(f"{name} must be a float32 tensor on {dev}")
+    s, st = t.shape, t.stride()
+    if len(s) != len(shape) or tuple(s[:-1]) != tuple(shape[:-1]) or s[-1] < shape[-1]:
+        raise ValueError(f"{name}: shape {tuple(s)} does not hold {tuple(shape)}")
+    if st[-1] != 1 and s[-1] > 1:
+        raise TypeError(f"{name} must have contiguous tokens")
+    return hf_key_weights(t.data_ptr(), st[0], st[1] if len(s) == 4 else 0, st[-2])
+
+
+def _own_rows(t, name):
+    """Refuses results whose rows lie in one another (expanded tensors)."""
+    if any(st == 0 and n > 1 for n, st in zip(t.shape, t.stride())):
+        raise TypeError(f"{name} is written: its rows must not overlap")
+
+
+def _weigh(call, q, lse, lq, lk, H, scale, prior, decay, out, dev, launch):
+    torch = _torch()
+    rq = _head_rows(q, lq, "q", dev)
+    if lse.dtype is not torch.float32 or lse.device != dev or not lse.is_contiguous() \
+            or lse.numel() < sum(lq) * rq.H:
+        raise TypeError("lse must be a contiguous fp32 CUDA tensor [rows, H_q]")
+    shape = (len(lq), H, max(lk, default=0))
+    if out is None:
+        out = torch.zeros(shape, dtype=torch.float32, device=dev)
+    _own_rows(out, "out")
+    w = _weights(out, shape, "out", dev)
+    p = None if prior is None else _weights(prior, shape, "prior", dev)
+    scale = 1.0 / math.sqrt(rq.d_h) if scale is None else float(scale)
+    _check(launch(rq, scale, p, float(decay), w), call)
+    return out
+
+
+def hf_attention_weights(q, k, lse, q_len, kv_len=None, causal=True, scale=None, prior=None,
+                         decay=1.0, out=None, stream=None):
+    """The attention weight that each key gets from packed query runs, as fp32 [B, H, T]:
+    decay * prior plus the sum over heads and rows of exp(score - lse).  q, k, lengths, causal
+    and scale as in the ``hf_prompt_attention`` that returned lse.  out None: a new tensor (0
+    behind a sequence's keys); it may be prior itself."""
+    nq, lq = _lens(q_len, "q_len")
+    nk, lk = (nq, lq) if kv_len is None else _lens(kv_len, "kv_len", len(lq))
+    dev = q.device
+    if not q.is_cuda:
+        raise TypeError("q must be a CUDA tensor")
+    with _call_on(dev, stream):
+        rk = _head_rows(k, lk, "k", dev)
+        return _weigh("hf_attention_weights", q, lse, lq, lk, rk.H, scale, prior, decay, out, dev,
+                      lambda rq, scale, p, decay, w: lib().hf_attention_weights(
+                          len(lq), nq, nk, rq, rk, lse.data_ptr(), scale, 1 if causal else 0, p,
+                          decay, w, _raw_stream(dev)))
+
+
+def hf_paged_attention_weights(q, cache: PagedKV, lse, q_len, kv_len, layer=0, causal=True,
+                               scale=None, prior=None, decay=1.0, out=None, stream=None):
+    """hf_attention_weights over the first kv_len [B] tokens of one layer of a paged cache."""
+    nq, lq = _lens(q_len, "q_len")
+    nk, lk = _lens(kv_len, "kv_len", len(lq))
+    if len(lq) > cache.batch:
+        raise ValueError(f"{len(lq)} sequences, the table has {cache.batch}")
+    dev = cache.pages.device
+    with _call_on(dev, stream):
+        return _weigh("hf_paged_attention_weights", q, lse, lq, lk, cache.H, scale, prior, decay,
+                      out, dev,
+                      lambda rq, scale, p, decay, w: lib().hf_paged_attention_weights(
+                          len(lq), nq, nk, rq, cache.desc, int(layer), lse.data_ptr(), scale,
+                          1 if causal else 0, p, decay, w, _raw_stream(dev)))
+
+
+def hf_evict_select(weights, kv_len, keep, n_first=0, n_last=0, out=None, stream=None):
+    """Which of its first kv_len [B] tokens each head keeps, of the weights [B, H, T] or
+    [B, L, H, T]: keep [B] of them, the first n_first and the last n_last among them, the
+    others by weight.  Returns their numbers, rising, as int32 [B, H, N] or [B, L, H, N] with
+    N the most that stay (entries behind a sequence's are not written)."""
+    torch = _torch()
+    nk, lk = _lens(kv_len, "kv_len")
+    nn, ln = _lens(keep, "keep", len(lk))
+    if weights.dim() not in (3, 4):
+        raise TypeError("weights must be [B, H, T] or [B, L, H, T]")
+    if not weights.is_cuda:
+        raise TypeError("weights must be a CUDA tensor")
+    dev = weights.device
+    lead = tuple(weights.shape[1:-1])
+    most = max((min(a, b) for a, b in zip(lk, ln)), default=0)
+    with _call_on(dev, stream):
+        w = _weights(weights, (len(lk),) + lead + (max(lk, default=0),), "weights", dev)
+        if out is None:
+            out = torch.empty((len(lk),) + lead + (most,), dtype=torch.int32, device=dev)
+        else:
+            _index(out, (len(lk),) + lead, dev)
+        st = lib().hf_evict_select(len(lk), lead[0] if len(lead) == 2 else 1, lead[-1], nk, nn,
+                                   int(n_first), int(n_last), w, out.data_ptr(), out.shape[-1],
+                                   _raw_stream(dev))
+    _check(st, "hf_evict_select")
+    return out
+
+
+def _index(t, lead, dev):
+    torch = _torch()
+    if t.dtype is not torch.int32 or t.device != dev or not t.is_contiguous():
+        raise TypeError(f"index must be a contiguous int32 tensor on {dev}")
+    if t.dim() != len(lead) + 1 or tuple(t.shape[:-1]) != lead:
+        raise ValueError(f"index: shape {tuple(t.shape)} is not {lead} and the tokens that stay")
+
+
+def _evicted_weights(weights, weights_out, lead, lk, ln, dev, in_place):
+    """Descriptors of the weights that move with the rows."""
+    if weights is None:
+        if weights_out is not None:
+            raise ValueError("weights_out without weights")
+        return None, None
+    w = _weights(weights, lead + (max(lk, default=0),), "weights", dev)
+    if in_place:
+        if weights_out is not None:
+            raise ValueError("in place the weights move in place")
+        _own_rows(weights, "weights")
+        return w, None
+    if weights_out is None:
+        raise ValueError("weights need weights_out")
+    _own_rows(weights_out, "weights_out")
+    return w, _weights(weights_out, lead + (max(ln, default=0),), "weights_out", dev)
+
+
+def hf_evict_rows(k, v, index, n, kv_len, out=None, weights=None, weights_out=None, stream=None):
+    """Moves the rows index[b, .., h, :n[b]] of the keys and values k, v (packed [N, H, d_h],
+    [B, H, T, d_h], or [B, L, H, T, d_h]) to the front: in place (out None; index rising, as
+    hf_evict_select gives it), or into out = (k_to, v_to).  index: int32 [B, H, N], with layers
+    [B, L, H, N].  The tokens' weights move with them, in place or into weights_out.  Returns
+    (k, v) that hold the rows."""
+    nn, ln = _lens(n, "n")
+    nk, lk = _lens(kv_len, "kv_len", len(ln))
+    if not k.is_cuda:
+        raise TypeError("k must be a CUDA tensor")
+    dev = k.device
+    layers = k.shape[1] if k.dim() == 5 else 1
+    with _call_on(dev, stream):
+        rk, rv = _head_rows(k, lk, "k", dev, layers), _head_rows(v, lk, "v", dev, layers)
+        lead = (len(ln), layers, rk.H) if k.dim() == 5 else (len(ln), rk.H)
+        _index(index, lead, dev)
+        to = (None, None)
+        if out is None:
+            _own_rows(k, "k")
+            _own_rows(v, "v")
+        else:
+            for t, name in zip(out, ("k_to", "v_to")):
+                _own_rows(t, name)
+            to = tuple(_head_rows(t, ln, name, dev, layers) for t, name in zip(out, ("k_to", "v_to")))
+        w, w_to = _evicted_weights(weights, weights_out, lead, lk, ln, dev, out is None)
+        st = lib().hf_evict_rows(len(ln), nn, nk, layers, index.data_ptr(), index.shape[-1], rk,
+                                 rv, to[0], to[1], w, w_to, _raw_stream(dev))
+    _check(st, "hf_evict_rows")
+    return (k, v) if out is None else out
+
+
+def hf_paged_evict(cache: PagedKV, index, n, kv_len, out: Optional[PagedKV] = None, layer=0,
+                   weights=None, weights_out=None, stream=None):
+    """hf_evict_rows for layers layer .. layer + L of a paged cache, L that of index
+    [B, L, H, N] (1 where it is [B, H, N]): in place, or into the same layers of another
+    cache.  Returns the cache that holds the rows."""
+    nn, ln = _lens(n, "n")
+    nk, lk = _lens(kv_len, "kv_len", len(ln))
+    if len(ln) > cache.batch or (out is not None and len(ln) > out.batch):
+        raise ValueError(f"{len(ln)} sequences, the tables have fewer")
+    dev = cache.pages.device
+    layers = index.shape[1] if index.dim() == 4 else 1
+    lead = (len(ln), layers, cache.H) if index.dim() == 4 else (len(ln), cache.H)
+    if out is not None and out.pages.device != dev:
+        raise TypeError(f"out must be on {dev}")
+    with _call_on(dev, stream):
+        _index(index, lead, dev)
+        w, w_to = _evicted_weights(weights, weights_out, lead, lk, ln, dev, out is None)
+        st = lib().hf_paged_evict(len(ln), nn, nk, cache.desc, None if out is None else out.desc,
+                                  int(layer), layers, index.data_ptr(), index.shape[-1], w, w_to,
+                                  _raw_stream(dev))
+    _check(st, "hf_paged_evict")
+    return cache if out is None else out
+
+
+def hf_sample_workspace_bytes(n: int, vocab: int, dtype: int) -> int:
+    """dtype: HF_BF16 or HF_F32."""
+    return int(lib().hf_sample_workspace_bytes(int(n), int(vocab), int(dtype)))
+
+
+def _setting(t, n, dtype, name, dev):
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.device != dev or not t.is_contiguous() or t.numel() != n:
+        raise TypeError(f"{name} must be a contiguous {dtype} tensor [{n}] on {dev}")
+    return t.data_ptr()
+
+
+def hf_sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, out=None,
+                     return_logprob=False, logprob=None, workspace=None, stream=None):
+    """The next token of each row of logits [n, vocab] (bf16 or fp32, contiguous rows) from the
+    given random numbers u [n] in [0, 1).  Settings are tensors [n]: temperature, top_p, min_p
+    fp32, top_k int32; None: 1, all, 1, 0.  Returns int32 [n], with ``return_logprob`` (tokens,
+    fp32 [n] log-probabilities among the tokens that stay)."""
+    torch = _torch()
+    if logits.dim() != 2 or not logits.is_cuda:
+        raise TypeError("logits must be a CUDA tensor [n, vocab]")
+    n, vocab = logits.shape
+    code, dev = _dtype_code(logits), logits.device
+    if logits.stride(1) != 1 and vocab > 1:
+        raise TypeError("logits must have contiguous rows")
+    stride = logits.stride(0) if n > 1 else max(vocab, 1)
+    f32 = torch.float32
+    with _call_on(dev, stream):
+        args = [_setting(t, n, d, name, dev) for t, d, name in (
+            (temperature, f32, "temperature"), (top_k, torch.int32, "top_k"), (top_p, f32, "top_p"),
+            (min_p, f32, "min_p"), (u, f32, "u"))]
+        if out is None:
+            out = torch.empty(n, dtype=torch.int32, device=dev)
+        if logprob is None and return_logprob:
+            logprob = torch.empty(n, dtype=f32, device=dev)
+        args += [_setting(out, n, torch.int32, "out", dev), _setting(logprob, n, f32, "logprob", dev)]
+        if workspace is None:
+            nbytes = lib().hf_sample_workspace_bytes(n, vocab, code)
+            if nbytes:
+                workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        elif workspace.device != dev or not workspace.is_contiguous():
+            raise TypeError("workspace must be a contiguous CUDA tensor on logits' device")
+        st = lib().hf_sample_tokens(n, vocab, code, logits.data_ptr(), stride, *args, _ptr(workspace),
+                                    0 if workspace is None else _nbytes(workspace), _raw_stream(dev))
+    _check(st, "hf_sample_tokens")
+    return (out, logprob) if return_logprob else out
 
 
 # ---------------------------------------------------------------------------
