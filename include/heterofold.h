@@ -587,15 +587,21 @@ typedef struct hf_key_weights {
  *             itself, element for element.
  *   decay     finite: 1 adds up, less lets older weights fade.
  *   w         the result (stride_l is not used).
+ *   workspace device, >= hf_attention_weights_workspace_bytes(..), 256-B aligned: sums of
+ *             parts of the rows, where there are few keys and many rows; may be NULL where
+ *             that is 0.  Calls that share one must not overlap.  (Pages need none.)
  * Numerics: scores as the attention forms them; exponentials and sums in fp32, the
  * sums by halves within 16 (paged: 4) rows, in an order that depends on the lengths,
  * heads and types alone.  A weight carries the rounding of lse, about |lse| 2^-22 of
  * itself; in rows with |lse| > 2800 one that this would lift above 1 counts as 1.
  */
+size_t hf_attention_weights_workspace_bytes(int32_t B, const int32_t* q_len, const int32_t* kv_len,
+                                            int32_t H_q, int32_t H, int32_t d_h, int32_t dtype);
 int32_t hf_attention_weights(int32_t B, const int32_t* q_len, const int32_t* kv_len,
                              const hf_rows* q, const hf_rows* k, const float* lse, float scale,
                              int32_t causal, const hf_key_weights* prior, float decay,
-                             const hf_key_weights* w, void* stream);
+                             const hf_key_weights* w, void* workspace, size_t workspace_bytes,
+                             void* stream);
 int32_t hf_paged_attention_weights(int32_t B, const int32_t* q_len, const int32_t* kv_len,
                                    const hf_rows* q, const hf_paged_kv* cache, int32_t layer,
                                    const float* lse, float scale, int32_t causal,

@@ -1197,11 +1197,16 @@ int32_t check_weights(const char* name, const hf_key_weights* w, bool used, bool
   return HF_OK;
 }
 
+// The sums of parts of the rows.
+size_t weigh_part_bytes(const hf::WeighShape& sh, int64_t rows, int64_t keys, int32_t H) {
+  return sh.chunk ? align_up((size_t)hf::weigh_parts(sh, rows) * H * keys * 4, 256) : 0;
+}
+
 // What both weight calls check, and the batch's work items.
 int32_t weights_common(int32_t B, const int32_t* q_len, const int32_t* kv_len, const hf_rows* q, int32_t H,
                        int32_t d_h, const float* lse, float scale, int32_t causal,
                        const hf_key_weights* prior, float decay, const hf_key_weights* w, bool paged,
-                       hf::WeighShape& sh, hf::WeighArgs& a) {
+                       void* workspace, size_t workspace_bytes, hf::WeighShape& sh, hf::WeighArgs& a) {
   int64_t pairs = 0, rows = 0, keys = 0, longest = 0;
   for (int b = 0; b < B; ++b) {
     pairs += std::min(q_len[b], kv_len[b]);
@@ -1225,16 +1230,32 @@ int32_t weights_common(int32_t B, const int32_t* q_len, const int32_t* kv_len, c
   if (rows > INT32_MAX || longest * G > INT32_MAX - 1024 || rows * q->H > ((int64_t)1 << 40))
     return fail(HF_ERR_SHAPE, "too many query rows");
   std::memset(&a, 0, sizeof a);
-  sh = hf::weigh_shape(q->dtype, paged, H, keys, longest * G);
-  int64_t items = 0, row = 0, key = 0;
+  sh = hf::weigh_shape(q->dtype, paged, B, q_len, kv_len, (int32_t)G, H, d_h, causal);
+  int64_t items = 0, all_tiles = 0, row = 0, key = 0;
   for (int b = 0; b < B; ++b) {
-    a.s[b] = {(int32_t)items, q_len[b], kv_len[b], (int32_t)row, (int32_t)key, {}};
-    items += ((int64_t)kv_len[b] + sh.keys - 1) / sh.keys;
+    const int64_t tiles = ((int64_t)kv_len[b] + sh.keys - 1) / sh.keys;
+    const int32_t parts = hf::weigh_parts(sh, q_len[b] * G);
+    a.s[b] = {(int32_t)items, q_len[b], kv_len[b], (int32_t)row, (int32_t)key, (int32_t)tiles, parts, (int32_t)all_tiles};
+    for (int32_t p = 0; p < parts && tiles > 0; ++p) {
+      items += hf::weigh_tiles(a.s[b], (int32_t)G, sh.chunk, sh.keys, causal, p);
+      if (items * H > kMaxGroups) break;
+    }
+    all_tiles += tiles;
     row += q_len[b];
     key += kv_len[b];
     if (items * H > kMaxGroups) return fail(HF_ERR_SHAPE, "too many work items");
     if (key > INT32_MAX) return fail(HF_ERR_SHAPE, "too many keys");
   }
+  if (const size_t need = weigh_part_bytes(sh, longest * G, keys, H)) {
+    if (!workspace) return fail(HF_ERR_NULL, "workspace is NULL");
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(HF_ERR_SHAPE, "workspace is not 256-byte aligned");
+    if (workspace_bytes < need)
+      return fail(HF_ERR_CAPACITY, "workspace %zu bytes < required %zu", workspace_bytes, need);
+    a.part = static_cast<float*>(workspace);
+  }
+  a.keys = keys;
+  a.chunk = sh.chunk ? sh.chunk : INT32_MAX;
+  a.tile = sh.keys;
   a.q = q->ptr;
   a.lse = lse;
   a.out = w->ptr;
@@ -1252,6 +1273,7 @@ int32_t weights_common(int32_t B, const int32_t* q_len, const int32_t* kv_len, c
   a.G = (int32_t)G;
   a.causal = causal ? 1 : 0;
   a.n_items = (int32_t)items;
+  a.n_tiles = (int32_t)all_tiles;
   a.by_g = hf::make_divide((uint32_t)G);
   a.by_h = hf::make_divide(H);
   return HF_OK;
@@ -1306,10 +1328,31 @@ int32_t evict_common(int32_t B, const int32_t* n, const int32_t* kv_len, int32_t
 
 }  // namespace
 
+size_t hf_attention_weights_workspace_bytes(int32_t B, const int32_t* q_len, const int32_t* kv_len,
+                                            int32_t H_q, int32_t H, int32_t d_h, int32_t dtype) {
+  if (check_lens(B, "q_len", q_len, "kv_len", kv_len) || check_heads(H_q, H, d_h)) return 0;
+  if (dtype != HF_F32 && dtype != HF_BF16) {
+    fail(HF_ERR_DTYPE, "dtype %d unknown", dtype);
+    return 0;
+  }
+  int64_t keys = 0, longest = 0;
+  for (int b = 0; b < B; ++b) {
+    keys += kv_len[b];
+    longest = std::max(longest, (int64_t)q_len[b]);
+  }
+  ok();
+  const int32_t G = H_q / H;
+  size_t most = 0;
+  for (int causal = 0; causal < 2; ++causal)  // (the cut depends on it)
+    most = std::max(most, weigh_part_bytes(hf::weigh_shape(dtype, false, B, q_len, kv_len, G, H, d_h, causal),
+                                           longest * G, keys, H));
+  return most;
+}
+
 int32_t hf_attention_weights(int32_t B, const int32_t* q_len, const int32_t* kv_len, const hf_rows* q,
                              const hf_rows* k, const float* lse, float scale, int32_t causal,
                              const hf_key_weights* prior, float decay, const hf_key_weights* w,
-                             void* stream) {
+                             void* workspace, size_t workspace_bytes, void* stream) {
   int32_t st;
   if ((st = check_lens(B, "q_len", q_len, "kv_len", kv_len))) return st;
   int64_t keys = 0;  // (all: a sequence without queries is written as well, and its keys are loaded)
@@ -1317,7 +1360,8 @@ int32_t hf_attention_weights(int32_t B, const int32_t* q_len, const int32_t* kv_
   if ((st = check_rows("k", k, keys > 0, false, false))) return st;
   hf::WeighShape sh;
   hf::WeighArgs a;
-  if ((st = weights_common(B, q_len, kv_len, q, k->H, k->d_h, lse, scale, causal, prior, decay, w, false, sh, a)))
+  if ((st = weights_common(B, q_len, kv_len, q, k->H, k->d_h, lse, scale, causal, prior, decay, w, false,
+                           workspace, workspace_bytes, sh, a)))
     return st;
   if (k->dtype != q->dtype) return fail(HF_ERR_DTYPE, "q and k dtypes differ");
   a.k = k->ptr;
@@ -1344,7 +1388,7 @@ int32_t hf_paged_attention_weights(int32_t B, const int32_t* q_len, const int32_
   hf::WeighShape sh;
   hf::WeighArgs a;
   if ((st = weights_common(B, q_len, kv_len, q, cache->H, cache->d_h, lse, scale, causal, prior, decay, w, true,
-                           sh, a)))
+                           nullptr, 0, sh, a)))
     return st;
   a.page_bytes = (long long)page_bytes(cache->H, cache->d_h, cache->page_tokens);
   a.pages = static_cast<const uint8_t*>(cache->pages) + (int64_t)layer * cache->n_pages * a.page_bytes;

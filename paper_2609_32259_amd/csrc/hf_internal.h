@@ -274,11 +274,25 @@ hipError_t launch_paged_read(int dtype, int d_h, const PagedRowsArgs& a, hipStre
 
 // Key weights (weights.hip): work items are tiles of keys of a sequence and head.
 struct WeighSeq {
-  int32_t item0;       // first tile of the sequence among those of a head
+  int32_t item0;       // first work item of the sequence among those of a head
   int32_t n, t;        // query tokens, keys
   int32_t row0, key0;  // rows and keys of the sequences before it
-  int32_t pad[3];
+  int32_t tiles;       // of its keys
+  int32_t parts;       // that its rows are cut into
+  int32_t tile0;       // tiles of the sequences before it
 };
+// Tiles of keys that some row of part p sees, the first ones of the sequence (all of them for
+// the last part: every key gets a number).
+#ifdef __HIPCC__
+__host__ __device__
+#endif
+inline int32_t weigh_tiles(const WeighSeq& s, int32_t G, int32_t chunk, int32_t tile, int32_t causal, int32_t p) {
+  if (!causal || p == s.parts - 1) return s.tiles;
+  const int64_t tokens = (((int64_t)p + 1) * chunk + G - 1) / G;  // that begin before the part's end
+  const int64_t last = (int64_t)s.t - s.n + tokens - 1;           // the last key they see
+  const int64_t n = last < 0 ? 0 : last / tile + 1;
+  return n < s.tiles ? (int32_t)n : s.tiles;
+}
 struct WeighArgs {
   const void* q;
   const float* lse;
@@ -291,17 +305,23 @@ struct WeighArgs {
   const int32_t* table;
   long long table_stride, page_bytes;
   int32_t n_pages, log2_page;
+  float* part;         // [parts][H][keys] sums of the rows' parts, or nullptr
+  long long keys;      // of all sequences
   float c, decay;      // c: scale * log2(e)
-  int32_t B, H, G, causal, n_items;
+  int32_t B, H, G, causal, n_items, n_tiles;
+  int32_t chunk, tile;  // rows of a part (of a head's query rows); keys of a tile
   Divide by_g, by_h;
   alignas(32) WeighSeq s[HF_MAX_BATCH];
 };
 static_assert(sizeof(WeighArgs) <= 4096, "kernel argument size");
 struct WeighShape {
-  int32_t keys;       // of a work item
-  int32_t row_waves;  // waves that share an item's rows
+  int32_t keys;   // of a work item
+  int32_t chunk;  // rows of a part, where the rows are cut into parts, or 0
+  int32_t few;    // few rows: a wave takes them all
 };
-WeighShape weigh_shape(int dtype, bool paged, int64_t heads, int64_t keys, int64_t rows);
+WeighShape weigh_shape(int dtype, bool paged, int32_t B, const int32_t* q_len, const int32_t* kv_len,
+                       int32_t G, int32_t H, int32_t d_h, int32_t causal);
+int32_t weigh_parts(const WeighShape& sh, int64_t rows);  // of a sequence with so many rows a head
 hipError_t launch_attention_weights(int dtype, int d_h, const WeighShape& sh, const WeighArgs& a,
                                     hipStream_t s);
 hipError_t launch_paged_weights(int dtype, int d_h, const WeighArgs& a, hipStream_t s);

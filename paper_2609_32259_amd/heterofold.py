@@ -145,10 +145,13 @@ _SIGNATURES = {
                                        C.POINTER(hf_paged_kv), C.c_int32, C.POINTER(hf_rows),
                                        C.c_float, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t,
                                        C.c_void_p]),
+    "hf_attention_weights_workspace_bytes": (C.c_size_t, [C.c_int32, _I32P, _I32P, C.c_int32,
+                                                          C.c_int32, C.c_int32, C.c_int32]),
     "hf_attention_weights": (C.c_int32, [C.c_int32, _I32P, _I32P, C.POINTER(hf_rows),
                                          C.POINTER(hf_rows), C.c_void_p, C.c_float, C.c_int32,
                                          C.POINTER(hf_key_weights), C.c_float,
-                                         C.POINTER(hf_key_weights), C.c_void_p]),
+                                         C.POINTER(hf_key_weights), C.c_void_p, C.c_size_t,
+                                         C.c_void_p]),
     "hf_paged_attention_weights": (C.c_int32, [C.c_int32, _I32P, _I32P, C.POINTER(hf_rows),
                                                C.POINTER(hf_paged_kv), C.c_int32, C.c_void_p,
                                                C.c_float, C.c_int32, C.POINTER(hf_key_weights),
@@ -840,8 +843,17 @@ def _weigh(call, q, lse, lq, lk, H, scale, prior, decay, out, dev, launch):
     return out
 
 
+def hf_attention_weights_workspace_bytes(q_len, kv_len, H_q: int, H: int, d_h: int,
+                                         dtype: int) -> int:
+    """dtype: HF_BF16 or HF_F32."""
+    q_len, _ = _lens(q_len, "q_len")
+    kv_len, _ = _lens(kv_len, "kv_len", len(q_len))
+    return int(lib().hf_attention_weights_workspace_bytes(len(q_len), q_len, kv_len, int(H_q),
+                                                          int(H), int(d_h), int(dtype)))
+
+
 def hf_attention_weights(q, k, lse, q_len, kv_len=None, causal=True, scale=None, prior=None,
-                         decay=1.0, out=None, stream=None):
+                         decay=1.0, out=None, workspace=None, stream=None):
     """The attention weight that each key gets from packed query runs, as fp32 [B, H, T]:
     decay * prior plus the sum over heads and rows of exp(score - lse).  q, k, lengths, causal
     and scale as in the ``hf_prompt_attention`` that returned lse.  out None: a new tensor (0
@@ -853,10 +865,18 @@ def hf_attention_weights(q, k, lse, q_len, kv_len=None, causal=True, scale=None,
         raise TypeError("q must be a CUDA tensor")
     with _call_on(dev, stream):
         rk = _head_rows(k, lk, "k", dev)
+        if workspace is None:
+            nbytes = lib().hf_attention_weights_workspace_bytes(len(lq), nq, nk, q.shape[-2] if q.dim() == 3
+                                                                else q.shape[1], rk.H, rk.d_h, rk.dtype)
+            if nbytes:
+                workspace = _torch().empty(nbytes, dtype=_torch().uint8, device=dev)
+        elif workspace.device != dev or not workspace.is_contiguous():
+            raise TypeError("workspace must be a contiguous CUDA tensor on q's device")
         return _weigh("hf_attention_weights", q, lse, lq, lk, rk.H, scale, prior, decay, out, dev,
                       lambda rq, scale, p, decay, w: lib().hf_attention_weights(
                           len(lq), nq, nk, rq, rk, lse.data_ptr(), scale, 1 if causal else 0, p,
-                          decay, w, _raw_stream(dev)))
+                          decay, w, _ptr(workspace), 0 if workspace is None else _nbytes(workspace),
+                          _raw_stream(dev)))
 
 
 def hf_paged_attention_weights(q, cache: PagedKV, lse, q_len, kv_len, layer=0, causal=True,
