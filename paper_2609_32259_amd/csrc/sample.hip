@@ -3,13 +3,13 @@
 // With w_j = exp((x_j - max x) / T), and the tokens in falling order of w (equal ones by
 // number), what stays under top-k, top-p and min-p is a prefix of that order, and the token
 // is where the running sum of w passes u times the prefix's.  No sort is needed for that: the
-// row is counted into bins of 1/32 in log w, which gives counts and sums up to every bin
+// row is counted into bins of 1/128 in log w, which gives counts and sums up to every bin
 // border, and only the bins in which one of the borders or the draw falls are looked at
 // token by token.
 //
 // Sums.  A border decides a token, so that sums hold more than 32 bits.  A bin adds up the
-// tokens' shortfalls 1 - exp(-f / 32) below the bin's upper edge (f: the place in the bin)
-// as whole numbers of 2^-28, which fp32 forms to 2^-29: with the count that is the bin's sum
+// tokens' shortfalls 1 - exp(-f / 128) below the bin's upper edge (f: the place in the bin)
+// as whole numbers of 2^-30, which fp32 forms to 2^-30: with the count that is the bin's sum
 // of w to 2^-29 of itself, in whatever order the tokens come.  The bins reach down to
 // exp(-32); what lies below has in all less than 2^20 exp(-32) = 2^-26 of the largest w and
 // cannot be drawn (u < 1 - 2^-25).  Everything after the bins is in 64 bits.
@@ -20,9 +20,11 @@
 namespace hf {
 namespace {
 
-constexpr int kBins = 1024;  // of 1/32 each
-constexpr int kNT = 1024;    // threads of a row: one a bin
-constexpr int kList = 4096;  // tokens that are put in order at a time
+constexpr int kBins = 4096;  // of 1/128 each
+constexpr int kNT = 1024;    // threads of a row
+constexpr int kBPT = kBins / kNT;
+constexpr int kList = 2048;  // tokens that are put in order at a time
+constexpr int kFew = 512;    // of top-k: half the threads, whose maxima bound it
 constexpr int kFracBits = 43;  // shortfalls below, the count above
 
 FI uint32_t ordered(float x) {  // whole numbers of the same order
@@ -39,17 +41,29 @@ FI float place_logit(uint64_t p) { return unordered((uint32_t)(p >> 20)); }
 FI int place_token(uint64_t p) { return 0xfffff - (int)(p & 0xfffff); }
 
 struct Row {
-  float top;     // the largest logit
-  double by_bin, by_t;  // 32 / T, 1 / T
-  FI double below(float x) const { return x == top ? 0.0 : (double)top - (double)x; }
-  FI double weight(float x) const { return exp(-(below(x) * by_t)); }
-  // The bin, or kBins; frac: the place in it.
-  FI int bin(float x, float& frac) const {
-    const double a = below(x) * by_bin;
-    if (!(a < kBins)) return kBins;
-    const double f = floor(a);
-    frac = (float)(a - f);
-    return (int)f;
+  float top;             // the largest logit
+  float by_bin, by_bin_low;  // 128 / T as the sum of two
+  double by_t;           // 1 / T
+  FI void set(float top_, float t) {
+    top = top_;
+    by_t = 1.0 / (double)t;
+    // (under T = 2^-90, where anything below the top lies below the bins, as for that)
+    const double f = fmin(128.0 * by_t, 0x1p97);
+    by_bin = (float)f;
+    by_bin_low = (float)(f - (double)by_bin);
+  }
+  FI double weight(float x) const { return x == top ? 1.0 : exp(-(((double)top - (double)x) * by_t)); }
+  // The place among the bins, rounded: its whole part is the bin, kBins and more lie below them.
+  // (It falls with x whatever is rounded.)
+  FI float bin(float x) const { return x == top ? 0.0f : (top - x) * by_bin; }
+  // What is missing from 1 of exp(-f / 128), f the place in the bin, to 2^-30: a's own rounding
+  // and that of the difference are taken in.
+  FI float shortfall(float x, float a) const {
+    const float d = x == top ? 0.0f : top - x, y = d - top;
+    float low = fmaf(d, by_bin, -a) + d * by_bin_low;
+    if (x != top) low = fmaf((top - (d - y)) + (-x - y), by_bin, low);
+    const float f = ((a - floorf(a)) + low) * 0.0078125f;
+    return f * (1.0f - f * (0.5f - f * 0.16666667f));
   }
 };
 
@@ -92,6 +106,29 @@ FI void each(const T* x, int n, F f) {
   if (tail < n) f(logit(x, tail), tail);
 }
 
+// f(logit, token) for the tokens of those threads of `each` whose numbers stand in a list.
+template <class T, class F>
+FI void again(const T* x, int n, const int* group, int groups, F f) {
+  constexpr int E = 16 / sizeof(T);
+  const int tid = threadIdx.x;
+  const int head = min(n, (int)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T));
+  if (tid < head) f(logit(x, tid), tid);
+  const u32x4* v = reinterpret_cast<const u32x4*>(x + head);
+  const int nv = (n - head) / E, per = (nv + kNT - 1) / kNT;
+  for (int item = tid; item < groups * per; item += kNT) {
+    const int g = item / per, c = group[g] + (item - g * per) * kNT;
+    if (c >= nv) continue;
+    const u32x4 r = v[c];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const uint32_t w = sizeof(T) == 4 ? r[e & 3] : r[e / 2];
+      f(__builtin_bit_cast(float, sizeof(T) == 4 ? w : e & 1 ? w & 0xffff0000u : w << 16), head + c * E + e);
+    }
+  }
+  const int tail = head + nv * E + tid;
+  if (tail < n) f(logit(x, tail), tail);
+}
+
 // Sums over the workgroup in a fixed order; every thread gets the result.
 FI double wave_scan(double x, int lane) {  // inclusive
 #pragma unroll
@@ -113,17 +150,22 @@ FI int wave_scan(int x, int lane) {
 struct Shared {
   union {
     unsigned long long hist[kBins];
-    int cursor[kBins];
+    struct {
+      unsigned long long list[kList];
+      double upto[kList];  // sums of w up to and with the list's token
+    };
   };
   double mass[kBins];      // sums of w up to and with the bin
   int count[kBins];        // tokens up to and with the bin
   int offset[kBins];       // of the bin's tokens in the list, or -1
-  unsigned long long list[kList];
-  double upto[kList];      // sums of w up to and with the list's token, from its bin's start
+  union {
+    int cursor[kBins];
+    int group[kNT];        // threads whose tokens are looked at again
+  };
   double part[kNT / 64];
   int ipart[kNT / 64];
-  double at_mass;
-  int at;
+  float fpart[kNT / 64];
+  int at, groups;
 };
 
 // A whole workgroup's scan; the total in `total`.
@@ -170,8 +212,7 @@ FI uint64_t search(Shared& s, const T* x, int n, const Row& row, int bin, int co
     int c = 0;
     double m = 0.0;
     each(x, n, [&](float v, int i) {
-      float frac;
-      if (row.bin(v, frac) == bin && place(v, i) >= cand) {
+      if ((int)fminf(row.bin(v), kBins) == bin && place(v, i) >= cand) {
         ++c;
         m += row.weight(v);
       }
@@ -188,8 +229,7 @@ FI uint64_t search(Shared& s, const T* x, int n, const Row& row, int bin, int co
   if (to == 0) {  // (sums from the bins may lie above those of the tokens by 2^-29: the last one)
     uint64_t last = ~0ull;
     each(x, n, [&](float v, int i) {
-      float frac;
-      if (row.bin(v, frac) == bin) last = min(last, place(v, i));
+      if ((int)fminf(row.bin(v), kBins) == bin) last = min(last, place(v, i));
     });
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) last = min(last, (uint64_t)__shfl_xor((unsigned long long)last, d));
@@ -218,22 +258,32 @@ __global__ __launch_bounds__(kNT) void sample_kernel(const SampleArgs a) {
     if (a.logprob) a.logprob[r] = logprob;
   };
 
-  // the largest logit (NaN if there is one)
-  float top = -INFINITY;
-  each(x, n, [&](float v, int) { top = __builtin_elementwise_maximum(top, v); });
+  // the largest logit (NaN if there is one), and of each thread's
+  float mine_top = -INFINITY;
+  each(x, n, [&](float v, int) { mine_top = __builtin_elementwise_maximum(mine_top, v); });
+  float top = mine_top;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) top = __builtin_elementwise_maximum(top, __shfl_xor(top, d));
-  if (lane == 0) s.part[wave] = top;
+  if (lane == 0) s.fpart[wave] = top;
   __syncthreads();
 #pragma unroll
-  for (int y = 0; y < kNT / 64; ++y) top = __builtin_elementwise_maximum(top, (float)s.part[y]);
+  for (int y = 0; y < kNT / 64; ++y) top = __builtin_elementwise_maximum(top, s.fpart[y]);
   if (!(top > -INFINITY) || !(temperature < INFINITY)) {
     if (tid == 0) answer(-1, NAN);
     return;
   }
+  // The threads with a logit of at least a bound, whose tokens are all that has to be looked
+  // at for those of at least that.
+  auto list_groups = [&](float least) {
+    if (tid == 0) s.groups = 0;
+    __syncthreads();
+    if (mine_top >= least) s.group[atomicAdd(&s.groups, 1)] = tid;
+    __syncthreads();
+  };
   if (temperature <= 0.0f) {  // the first of the largest
+    list_groups(top);
     int first = n;
-    each(x, n, [&](float v, int i) {
+    again(x, n, s.group, s.groups, [&](float v, int i) {
       if (v == top) first = min(first, i);
     });
 #pragma unroll
@@ -246,76 +296,20 @@ __global__ __launch_bounds__(kNT) void sample_kernel(const SampleArgs a) {
     return;
   }
   Row row;
-  row.top = top;
-  row.by_t = 1.0 / (double)temperature;
-  row.by_bin = 32.0 / (double)temperature;
-
-  // counts and shortfalls of the bins
-  s.hist[tid] = 0;
-  __syncthreads();
-  each(x, n, [&](float v, int) {
-    float frac;
-    const int b = row.bin(v, frac);
-    if (b < kBins) {
-      const float d = frac * 0.03125f;
-      const float e = d * (1.0f - d * (0.5f - d * (0.16666667f - d * 0.041666668f)));
-      atomicAdd(&s.hist[b], (1ull << kFracBits) + (unsigned long long)rintf(e * 0x1p28f));
-    }
-  });
-  __syncthreads();
-  const unsigned long long raw = s.hist[tid];
-  const int mine = (int)(raw >> kFracBits);
-  const double short_of = (double)(raw & ((1ull << kFracBits) - 1)) * 0x1p-28;
-  double sum;
-  int in_bins;
-  s.mass[tid] = scan(s, ((double)mine - short_of) * exp(-0.03125 * tid), sum);
-  s.count[tid] = scan(s, mine, in_bins);
-  __syncthreads();
-  auto mass_before = [&](int b) { return b > 0 ? s.mass[b - 1] : 0.0; };
-  auto count_before = [&](int b) { return b > 0 ? s.count[b - 1] : 0; };
-  // bins whose sum up to them is below (not above) a target: the number of the one in which it lies
-  auto bin_of = [&](double target, bool strict) {
-    return min(__syncthreads_count(strict ? s.mass[tid] <= target : s.mass[tid] < target), kBins - 1);
-  };
-
-  // The bins in which the borders can lie.
+  row.set(top, temperature);
   const int k = k_in <= 0 || k_in > n ? n : k_in;
-  const int bk = __syncthreads_count(s.count[tid] < k);  // kBins: below them
-  const double sk_lo = bk < kBins ? mass_before(bk) : sum, sk_hi = bk < kBins ? s.mass[bk] : sum;
   const bool by_p = p_in < 1.0f, by_m = m_in > 0.0f;
   const double p = by_p ? fmax((double)p_in, 0.0) : 1.0;
-  const int bp_lo = by_p ? bin_of(p * sk_lo, false) : kBins, bp_hi = by_p ? bin_of(p * sk_hi, false) : kBins;
   const double m = by_m ? fmin((double)m_in, 1.0) : 0.0;
-  const double am = by_m ? -32.0 * log(m) : kBins;
-  const int bm = am < kBins ? (int)am : kBins;
-  const int be_lo = min(min(bk, bm), bp_lo), be_hi = min(min(bk, bm), bp_hi);
   const double u = fmin(fmax(u_in == u_in ? (double)u_in : 0.0, 0.0), 1.0 - 0x1p-24);
-  const double total_lo = be_lo < kBins ? fmax(mass_before(be_lo), 1.0) : sum;
-  const double total_hi = be_hi < kBins ? s.mass[be_hi] : sum;
-  const int bd_lo = bin_of(u * total_lo, true), bd_hi = min(bin_of(u * total_hi, true), be_hi);
-  const bool wanted = tid == bk || (by_p && tid >= bp_lo && tid <= bp_hi) || tid == bm || (tid >= bd_lo && tid <= bd_hi);
-  int in_list;
-  const int here = wanted ? mine : 0;
-  const int off = scan(s, here, in_list) - here;
 
-  int best = n;          // tokens that stay, and their sum
-  double total = sum;
-  uint64_t drawn;
-  if (in_list <= kList) {
-    s.offset[tid] = wanted ? off : -1;
-    s.cursor[tid] = 0;
+  // The list in falling order, and the sums of w up to each of its tokens.
+  auto sort_list = [&](int count) {
     int padded = 64;
-    while (padded < in_list) padded *= 2;
-    for (int i = tid; i < padded; i += kNT) s.list[i] = 0;
+    while (padded < count) padded *= 2;
+    for (int i = count + tid; i < padded; i += kNT) s.list[i] = 0;  // (below every token)
     __syncthreads();
-    each(x, n, [&](float v, int i) {
-      float frac;
-      const int b = row.bin(v, frac);
-      if (b < kBins && s.offset[b] >= 0) s.list[s.offset[b] + atomicAdd(&s.cursor[b], 1)] = place(v, i);
-    });
-    __syncthreads();
-    // bitonic, falling (what pads the list is 0, below every token)
-    for (int size = 2; size <= padded; size *= 2)
+    for (int size = 2; size <= padded; size *= 2)  // bitonic
       for (int step = size / 2; step > 0; step /= 2) {
         for (int i = tid; i < padded / 2; i += kNT) {
           const int lo = 2 * i - (i & (step - 1)), hi = lo + step;
@@ -325,43 +319,183 @@ __global__ __launch_bounds__(kNT) void sample_kernel(const SampleArgs a) {
             s.list[hi] = p0;
           }
         }
-        __syncthreads();
+        // (up to 128 numbers are one wave's)
+        if (padded > 128) __syncthreads();
+        else __builtin_amdgcn_wave_barrier();
       }
-    // sums up to each token of the list; a thread has consecutive ones
-    constexpr int PT = kList / kNT;
+    if (padded <= 128) __syncthreads();
+    constexpr int PT = kList / kNT;  // a thread has consecutive ones
+    const int per = count <= kNT ? 1 : PT;
     double w[PT], run = 0.0, all;
 #pragma unroll
     for (int y = 0; y < PT; ++y) {
-      const int i = PT * tid + y;
-      w[y] = i < in_list ? row.weight(place_logit(s.list[i])) : 0.0;
+      const int i = per * tid + y;
+      w[y] = y < per && i < count ? row.weight(place_logit(s.list[i])) : 0.0;
       run += w[y];
     }
     run = scan(s, run, all) - run;
 #pragma unroll
     for (int y = 0; y < PT; ++y) {
       run += w[y];
-      s.upto[PT * tid + y] = run;
+      if (y < per) s.upto[per * tid + y] = run;
     }
     __syncthreads();
+  };
+  // Items 0 .. c - 1 for which f holds, those a prefix of them.
+  auto prefix = [&](int c, auto f) {
+    if (c <= kNT) return __syncthreads_count(tid < c && f(tid));
+    int got = 0;
+    for (int i = tid; i < c; i += kNT) got += f(i);
+    int all;
+    scan(s, got, all);
+    return all;
+  };
+
+  // Where the tokens that stay are few and a bound tells which can be among them, those are
+  // listed and the rest is not looked at again: of k tokens none lies below the k-th largest of
+  // the threads' maxima; min_p alone bounds the logit itself.
+  const bool by_k = k <= kFew;
+  if (by_k || (by_m && !by_p && k == n)) {
+    float least;
+    if (by_k) {
+      const uint32_t key = ordered(mine_top);  // (the upper 16 bits are bound enough)
+      uint32_t to = 0;
+      for (int bit = 31; bit >= 16; --bit)
+        if (__syncthreads_count(key >= (to | 1u << bit)) >= k) to |= 1u << bit;
+      least = unordered(to);
+      if (!(least >= -FLT_MAX)) least = -FLT_MAX;  // (also the words of a NaN; -infinity never stays)
+    } else {
+      least = (float)((double)top + log(m) * temperature * (1.0 + 1e-6) - fabs((double)top) * 0x1p-22);
+      if (!(least <= top)) least = top;  // (+infinity)
+    }
+    if (tid == 0) s.at = 0;
+    list_groups(least);
+    again(x, n, s.group, s.groups, [&](float v, int i) {
+      if (v >= least) {
+        const int at = atomicAdd(&s.at, 1);
+        if (at < kList) s.list[at] = place(v, i);
+      }
+    });
+    __syncthreads();
+    const int count = s.at;
+    __syncthreads();
+    if (count <= kList) {
+      sort_list(count);
+      int best = min(k, count);
+      if (by_p) {
+        const double target = p * s.upto[best - 1];
+        best = min(best, prefix(best, [&](int i) { return s.upto[i] < target; }) + 1);
+      }
+      if (by_m) best = max(prefix(best, [&](int i) { return row.weight(place_logit(s.list[i])) >= m; }), 1);
+      const double total = s.upto[best - 1], target = u * total;
+      const int at = min(prefix(best, [&](int i) { return s.upto[i] <= target; }), best - 1);
+      if (tid == 0) {
+        const uint64_t drawn = s.list[at];
+        answer(place_token(drawn), (float)log(row.weight(place_logit(drawn)) / total));
+      }
+      return;
+    }
+  }
+
+  // counts and shortfalls of the bins; a thread has kBPT bins after each other
+#pragma unroll
+  for (int y = 0; y < kBPT; ++y) s.hist[tid + y * kNT] = 0;
+  __syncthreads();
+  each(x, n, [&](float v, int) {
+    const float place = row.bin(v);
+    if (place < kBins)
+      atomicAdd(&s.hist[(int)place], (1ull << kFracBits) +
+                                         (unsigned long long)(uint32_t)rintf(row.shortfall(v, place) * 0x1p30f));
+  });
+  __syncthreads();
+  int mine[kBPT], in_bins = 0;
+  double sum = 0.0;
+  {
+    double m_mine[kBPT], edge = exp(-0x1p-7 * (kBPT * tid));
+    int c_all = 0;
+    double m_all = 0.0;
+#pragma unroll
+    for (int y = 0; y < kBPT; ++y) {
+      const unsigned long long raw = s.hist[kBPT * tid + y];
+      mine[y] = (int)(raw >> kFracBits);
+      m_mine[y] = ((double)mine[y] - (double)(raw & ((1ull << kFracBits) - 1)) * 0x1p-30) * edge;
+      edge *= 0.992217938260243;  // exp(-1/128)
+      c_all += mine[y];
+      m_all += m_mine[y];
+    }
+    double m_up = scan(s, m_all, sum) - m_all;
+    int c_up = scan(s, c_all, in_bins) - c_all;
+#pragma unroll
+    for (int y = 0; y < kBPT; ++y) {
+      s.mass[kBPT * tid + y] = m_up += m_mine[y];
+      s.count[kBPT * tid + y] = c_up += mine[y];
+    }
+  }
+  __syncthreads();
+  sum = s.mass[kBins - 1];  // (as the bins have it)
+  auto mass_before = [&](int b) { return b > 0 ? s.mass[b - 1] : 0.0; };
+  auto count_before = [&](int b) { return b > 0 ? s.count[b - 1] : 0; };
+  // The number of bins for which f holds, those a prefix of them.
+  auto bins_with = [&](auto f) {
+    const int t = __syncthreads_count(f(kBPT * tid + kBPT - 1));
+    int b = kBPT * t;
+    if (t < kNT)
+#pragma unroll
+      for (int y = 0; y < kBPT - 1; ++y) b += f(kBPT * t + y);
+    return b;
+  };
+  // the bin in which the sum reaches (strict: passes) a target
+  auto bin_of = [&](double target, bool strict) {
+    return min(bins_with([&](int b) { return strict ? s.mass[b] <= target : s.mass[b] < target; }), kBins - 1);
+  };
+
+  // The bins in which the borders can lie.
+  const int bk = bins_with([&](int b) { return s.count[b] < k; });  // kBins: below them
+  const double sk_lo = bk < kBins ? mass_before(bk) : sum, sk_hi = bk < kBins ? s.mass[bk] : sum;
+  const int bp_lo = by_p ? bin_of(p * sk_lo, false) : kBins, bp_hi = by_p ? bin_of(p * sk_hi, false) : kBins;
+  const double am = by_m ? -128.0 * log(m) : kBins;
+  const int bm = am < kBins ? (int)am : kBins;
+  const int be_lo = min(min(bk, bm), bp_lo), be_hi = min(min(bk, bm), bp_hi);
+  const double total_lo = be_lo < kBins ? fmax(mass_before(be_lo), 1.0) : sum;
+  const double total_hi = be_hi < kBins ? s.mass[be_hi] : sum;
+  const int bd_lo = bin_of(u * total_lo, true), bd_hi = min(bin_of(u * total_hi, true), be_hi);
+  int in_list, here = 0;
+  bool wanted[kBPT];
+#pragma unroll
+  for (int y = 0; y < kBPT; ++y) {
+    const int b = kBPT * tid + y;
+    wanted[y] = b == bk || (by_p && b >= bp_lo && b <= bp_hi) || b == bm || (b >= bd_lo && b <= bd_hi);
+    here += wanted[y] ? mine[y] : 0;
+  }
+  int off = scan(s, here, in_list) - here;
+
+  int best = n;          // tokens that stay, and their sum
+  double total = sum;
+  uint64_t drawn;
+  if (in_list <= kList) {
+#pragma unroll
+    for (int y = 0; y < kBPT; ++y) {
+      s.offset[kBPT * tid + y] = wanted[y] ? off : -1;
+      s.cursor[kBPT * tid + y] = 0;
+      off += wanted[y] ? mine[y] : 0;
+    }
+    const float past = min(max(max(bk < kBins ? bk : 0, bm < kBins ? bm : 0), max(by_p ? bp_hi : 0, bd_hi)), kBins - 1) + 1;
+    __syncthreads();
+    each(x, n, [&](float v, int i) {
+      const float at = row.bin(v);
+      if (at < past) {
+        const int b = (int)at;
+        if (s.offset[b] >= 0) s.list[s.offset[b] + atomicAdd(&s.cursor[b], 1)] = place(v, i);
+      }
+    });
+    __syncthreads();
+    sort_list(in_list);
     // sum up to and with the c-th token of a bin (c = 0: before it)
     auto sum_at = [&](int b, int c) {
       const int o = s.offset[b];
       return mass_before(b) + (c > 0 ? s.upto[o + c - 1] - (o > 0 ? s.upto[o - 1] : 0.0) : 0.0);
     };
     auto tokens_of = [&](int b) { return s.count[b] - count_before(b); };
-    // tokens of a bin for which f holds, those a prefix of it
-    auto prefix = [&](int b, auto f) {
-      if (tid == 0) s.at = 0;
-      __syncthreads();
-      const int o = s.offset[b], c = tokens_of(b);
-      int got = 0;
-      for (int i = tid; i < c; i += kNT) got += f(o + i, i);
-      if (got) atomicAdd(&s.at, got);
-      __syncthreads();
-      const int res = s.at;
-      __syncthreads();
-      return res;
-    };
     if (bk < kBins) {
       best = k;
       total = sum_at(bk, k - count_before(bk));
@@ -369,7 +503,7 @@ __global__ __launch_bounds__(kNT) void sample_kernel(const SampleArgs a) {
     if (by_p) {
       const double target = p * total;
       const int b = min(max(bin_of(target, false), bp_lo), bp_hi);
-      const int c = min(prefix(b, [&](int, int i) { return sum_at(b, i + 1) < target; }) + 1, tokens_of(b));
+      const int c = min(prefix(tokens_of(b), [&](int i) { return sum_at(b, i + 1) < target; }) + 1, tokens_of(b));
       const int stay = max(count_before(b) + c, 1);
       if (stay < best) {
         best = stay;
@@ -377,7 +511,7 @@ __global__ __launch_bounds__(kNT) void sample_kernel(const SampleArgs a) {
       }
     }
     if (bm < kBins) {
-      const int c = prefix(bm, [&](int at, int) { return row.weight(place_logit(s.list[at])) >= m; });
+      const int c = prefix(tokens_of(bm), [&](int i) { return row.weight(place_logit(s.list[s.offset[bm] + i])) >= m; });
       const int stay = max(count_before(bm) + c, 1);
       if (stay < best) {
         best = stay;
@@ -387,7 +521,7 @@ __global__ __launch_bounds__(kNT) void sample_kernel(const SampleArgs a) {
     total = fmax(total, 1.0);
     const double target = u * total;
     const int b = min(max(bin_of(target, true), bd_lo), bd_hi);
-    const int c = min(prefix(b, [&](int, int i) { return sum_at(b, i + 1) <= target; }), tokens_of(b) - 1);
+    const int c = min(prefix(tokens_of(b), [&](int i) { return sum_at(b, i + 1) <= target; }), tokens_of(b) - 1);
     // (a sum that rounds past the last one that stays: that one, in the same bin)
     drawn = s.list[s.offset[b] + min(c, max(best - count_before(b), 1) - 1)];
   } else {
@@ -412,8 +546,7 @@ __global__ __launch_bounds__(kNT) void sample_kernel(const SampleArgs a) {
       int c = 0;
       double w = 0.0;
       each(x, n, [&](float v, int) {
-        float frac;
-        if (row.bin(v, frac) == bm && row.weight(v) >= m) {
+        if ((int)fminf(row.bin(v), kBins) == bm && row.weight(v) >= m) {
           ++c;
           w += row.weight(v);
         }
