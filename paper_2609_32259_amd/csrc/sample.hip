@@ -24,6 +24,7 @@ constexpr int kBins = 4096;  // of 1/128 each
 constexpr int kNT = 1024;    // threads of a row
 constexpr int kBPT = kBins / kNT;
 constexpr int kList = 2048;  // tokens that are put in order at a time
+constexpr int kRank = 128;   // that are put in order by counting for each those before it
 constexpr int kFew = 512;    // of top-k: half the threads, whose maxima bound it
 constexpr int kFracBits = 43;  // shortfalls below, the count above
 
@@ -55,13 +56,14 @@ struct Row {
   FI double weight(float x) const { return x == top ? 1.0 : exp(-(((double)top - (double)x) * by_t)); }
   // The place among the bins, rounded: its whole part is the bin, kBins and more lie below them.
   // (It falls with x whatever is rounded.)
-  FI float bin(float x) const { return x == top ? 0.0f : (top - x) * by_bin; }
+  FI float below(float x) const { return fmaxf(top - x, 0.0f); }  // (0 too between infinities)
+  FI float bin(float x) const { return below(x) * by_bin; }
   // What is missing from 1 of exp(-f / 128), f the place in the bin, to 2^-30: a's own rounding
   // and that of the difference are taken in.
   FI float shortfall(float x, float a) const {
-    const float d = x == top ? 0.0f : top - x, y = d - top;
-    float low = fmaf(d, by_bin, -a) + d * by_bin_low;
-    if (x != top) low = fmaf((top - (d - y)) + (-x - y), by_bin, low);
+    const float d = below(x), y = d - top;
+    float low = fmaf(d, by_bin_low, fmaf(d, by_bin, -a));
+    low = fmaf((top - (d - y)) + (-x - y), by_bin, low);  // (NaN at a top of infinity: becomes 0)
     const float f = ((a - floorf(a)) + low) * 0.0078125f;
     return f * (1.0f - f * (0.5f - f * 0.16666667f));
   }
@@ -79,54 +81,82 @@ FI float logit<float>(const float* p, int i) {
   return p[i];
 }
 template <class T, class F>
-FI void each(const T* x, int n, F f) {
-  constexpr int E = 16 / sizeof(T), U = 4;
-  const int tid = threadIdx.x;
-  const int head = min(n, (int)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T));
-  if (tid < head) f(logit(x, tid), tid);
-  const u32x4* v = reinterpret_cast<const u32x4*>(x + head);
-  const int nv = (n - head) / E;
-  for (int c = tid; c < nv; c += U * kNT) {
-    u32x4 r[U];
+FI void of_vector(u32x4 r, int i, F f) {
 #pragma unroll
-    for (int y = 0; y < U; ++y)
-      if (c + y * kNT < nv) r[y] = v[c + y * kNT];
-#pragma unroll
-    for (int y = 0; y < U; ++y) {
-      if (c + y * kNT >= nv) break;
-      const int i = head + (c + y * kNT) * E;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const uint32_t w = sizeof(T) == 4 ? r[y][e & 3] : r[y][e / 2];
-        f(__builtin_bit_cast(float, sizeof(T) == 4 ? w : e & 1 ? w & 0xffff0000u : w << 16), i + e);
-      }
-    }
+  for (int e = 0; e < 16 / (int)sizeof(T); ++e) {
+    const uint32_t w = sizeof(T) == 4 ? r[e & 3] : r[e / 2];
+    f(__builtin_bit_cast(float, sizeof(T) == 4 ? w : e & 1 ? w & 0xffff0000u : w << 16), i + e);
   }
-  const int tail = head + nv * E + tid;
-  if (tail < n) f(logit(x, tail), tail);
 }
-
-// f(logit, token) for the tokens of those threads of `each` whose numbers stand in a list.
-template <class T, class F>
-FI void again(const T* x, int n, const int* group, int groups, F f) {
+// Whole 16-byte vectors, U a thread at a time with the next U on their way (without them a walk
+// waits for memory once a round: 8 us instead of 4 for a row of 50,000 numbers), and what lies
+// before and behind them, fewer than two vectors.
+template <int U, class T, class F>
+FI void each(const T* x, int n, F f) {
   constexpr int E = 16 / sizeof(T);
   const int tid = threadIdx.x;
   const int head = min(n, (int)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T));
-  if (tid < head) f(logit(x, tid), tid);
   const u32x4* v = reinterpret_cast<const u32x4*>(x + head);
-  const int nv = (n - head) / E, per = (nv + kNT - 1) / kNT;
-  for (int item = tid; item < groups * per; item += kNT) {
-    const int g = item / per, c = group[g] + (item - g * per) * kNT;
-    if (c >= nv) continue;
-    const u32x4 r = v[c];
+  const int nv = (n - head) / E, rest = n - nv * E;
+  u32x4 r[U], next[U] = {};
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const uint32_t w = sizeof(T) == 4 ? r[e & 3] : r[e / 2];
-      f(__builtin_bit_cast(float, sizeof(T) == 4 ? w : e & 1 ? w & 0xffff0000u : w << 16), head + c * E + e);
-    }
+  for (int y = 0; y < U; ++y)
+    if (tid + y * kNT < nv) next[y] = v[tid + y * kNT];
+  if (tid < rest) {
+    const int i = tid < head ? tid : tid + nv * E;
+    f(logit(x, i), i);
   }
-  const int tail = head + nv * E + tid;
-  if (tail < n) f(logit(x, tail), tail);
+#pragma unroll 1
+  for (int c = tid; c < nv; c += U * kNT) {
+#pragma unroll
+    for (int y = 0; y < U; ++y) {
+      r[y] = next[y];
+      if (c + (U + y) * kNT < nv) next[y] = v[c + (U + y) * kNT];
+    }
+#pragma unroll
+    for (int y = 0; y < U; ++y)
+      if (c + y * kNT < nv) of_vector<T>(r[y], head + (c + y * kNT) * E, f);
+  }
+}
+
+// g(logit, token) for the tokens of a vector for which f(logit) holds.  f is asked without
+// branches, of all of a lane's numbers, and the lanes then take their hits in turn: a branch
+// that a wave takes costs some 30 cycles, more than most of what is asked.
+template <class T, class F, class G>
+FI void hits(u32x4 r, int i, F f, G g) {
+  constexpr int E = 16 / sizeof(T);
+  uint32_t hit = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const uint32_t w = sizeof(T) == 4 ? r[e & 3] : r[e / 2];
+    hit |= (uint32_t)f(__builtin_bit_cast(float, sizeof(T) == 4 ? w : e & 1 ? w & 0xffff0000u : w << 16)) << e;
+  }
+#pragma unroll 1
+  while (hit) {
+    const int e = __builtin_ctz(hit), d = sizeof(T) == 4 ? e : e / 2;
+    hit &= hit - 1;
+    const uint32_t lo = d & 1 ? r[1] : r[0], hi = d & 1 ? r[3] : r[2], w = d & 2 ? hi : lo;
+    g(__builtin_bit_cast(float, sizeof(T) == 4 ? w : e & 1 ? w & 0xffff0000u : w << 16), i + e);
+  }
+}
+// g(logit, token) for the tokens for which f(logit) holds, of those threads of `each` whose
+// numbers stand in a list.
+template <class T, class F, class G>
+FI void again(const T* x, int n, const int* group, int groups, F f, G g) {
+  constexpr int E = 16 / sizeof(T);
+  const int tid = threadIdx.x;
+  const int head = min(n, (int)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T));
+  const u32x4* v = reinterpret_cast<const u32x4*>(x + head);
+  const int nv = (n - head) / E, rest = n - nv * E, per = (nv + kNT - 1) / kNT;
+  if (tid < rest) {
+    const int i = tid < head ? tid : tid + nv * E;
+    if (f(logit(x, i))) g(logit(x, i), i);
+  }
+#pragma unroll 1
+  for (int item = tid; item < groups * per; item += kNT) {
+    const int at = item / per, c = group[at] + (item - at * per) * kNT;
+    if (c < nv) hits<T>(v[c], head + c * E, f, g);
+  }
 }
 
 // Sums over the workgroup in a fixed order; every thread gets the result.
@@ -163,7 +193,7 @@ struct Shared {
     int group[kNT];        // threads whose tokens are looked at again
   };
   double part[kNT / 64];
-  int ipart[kNT / 64];
+  int ipart[kNT / 64], ipart2[kNT / 64];
   float fpart[kNT / 64];
   int at, groups;
 };
@@ -199,47 +229,58 @@ FI int scan(Shared& s, int x, int& total) {
 }
 
 // Where the list is too short for the tokens of the bins that matter (many equal or nearly
-// equal logits): the last place `to` in a bin for which the tokens of the bin up to it are at
-// most / sum to what is asked for, found bit by bit with a walk over the row for each.
-// count > 0: the count-th token of the bin.  Otherwise the first token at which `base` and the
-// sum of w reach `target` (strict: pass it); the last of the bin where none does.
+// equal logits): the last place `to` in a bin for which the tokens of the bin up to it number
+// or sum to what is asked for, found bit by bit with a walk over the row for each.
+struct Search {
+  int bin;
+  int count;        // > 0: the count-th token of the bin
+  double least;     // > 0: the tokens of the bin of at least that weight
+  double target;    // else the first at which the sum of w reaches (strict: passes) this
+  bool strict;
+  uint64_t to;      // results: the place, tokens of the bin up to it, sum of w up to it
+  int tokens;
+  double mass;
+};
 template <class T>
-FI uint64_t search(Shared& s, const T* x, int n, const Row& row, int bin, int count, double base, double target,
-                   bool strict, int& tokens, double& mass) {
-  uint64_t to = 0;
-  for (int bit = 51; bit >= -1; --bit) {  // (the last walk is for the result)
-    const uint64_t cand = bit < 0 ? to : to | 1ull << bit;
+FI void search(Shared& s, const T* x, int n, const Row& row, Search& q) {
+  const double base = q.bin > 0 ? s.mass[q.bin - 1] : 0.0;
+  q.to = 0;
+#pragma unroll 1
+  for (int bit = q.least > 0.0 ? -1 : 51; bit >= -1; --bit) {  // (the last walk is for the result)
+    const uint64_t cand = bit < 0 ? q.to : q.to | 1ull << bit;
     int c = 0;
     double m = 0.0;
-    each(x, n, [&](float v, int i) {
-      if ((int)fminf(row.bin(v), kBins) == bin && place(v, i) >= cand) {
-        ++c;
-        m += row.weight(v);
-      }
-    });
+    unsigned long long last = ~0ull;
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n; i += kNT) {
+      const float v = logit(x, i);
+      if ((int)fminf(row.bin(v), kBins) != q.bin) continue;
+      last = min(last, (unsigned long long)place(v, i));
+      if (place(v, i) < cand) continue;
+      const double w = row.weight(v);
+      if (w < q.least) continue;
+      ++c;
+      m += w;
+    }
     double m_all;
     int c_all;
     scan(s, m, m_all);
     scan(s, c, c_all);
     const double sum = base + m_all;
-    if (bit >= 0 && (count > 0 ? c_all >= count : c_all > 0 && (strict ? sum > target : sum >= target))) to = cand;
-    tokens = c_all;
-    mass = sum;
-  }
-  if (to == 0) {  // (sums from the bins may lie above those of the tokens by 2^-29: the last one)
-    uint64_t last = ~0ull;
-    each(x, n, [&](float v, int i) {
-      if ((int)fminf(row.bin(v), kBins) == bin) last = min(last, place(v, i));
-    });
+    if (bit >= 0 && (q.count > 0 ? c_all >= q.count : c_all > 0 && (q.strict ? sum > q.target : sum >= q.target)))
+      q.to = cand;
+    q.tokens = c_all;
+    q.mass = sum;
+    if (bit < 0 && q.to == 0) {  // (sums from the bins may lie above those of the tokens by 2^-29: the last one)
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) last = min(last, (uint64_t)__shfl_xor((unsigned long long)last, d));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) s.list[threadIdx.x >> 6] = last;
-    __syncthreads();
-    for (int y = 0; y < kNT / 64; ++y) last = min(last, (uint64_t)s.list[y]);
-    to = last;
+      for (int d = 1; d < 64; d *= 2) last = min(last, (unsigned long long)__shfl_xor(last, d));
+      __syncthreads();
+      if ((threadIdx.x & 63) == 0) s.list[threadIdx.x >> 6] = last;
+      __syncthreads();
+      for (int y = 0; y < kNT / 64; ++y) last = min(last, s.list[y]);
+      q.to = last;
+    }
   }
-  return to;
 }
 
 template <class T>
@@ -260,7 +301,7 @@ __global__ __launch_bounds__(kNT) void sample_kernel(const SampleArgs a) {
 
   // the largest logit (NaN if there is one), and of each thread's
   float mine_top = -INFINITY;
-  each(x, n, [&](float v, int) { mine_top = __builtin_elementwise_maximum(mine_top, v); });
+  each<4>(x, n, [&](float v, int) { mine_top = __builtin_elementwise_maximum(mine_top, v); });
   float top = mine_top;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) top = __builtin_elementwise_maximum(top, __shfl_xor(top, d));
@@ -283,9 +324,7 @@ __global__ __launch_bounds__(kNT) void sample_kernel(const SampleArgs a) {
   if (temperature <= 0.0f) {  // the first of the largest
     list_groups(top);
     int first = n;
-    again(x, n, s.group, s.groups, [&](float v, int i) {
-      if (v == top) first = min(first, i);
-    });
+    again(x, n, s.group, s.groups, [&](float v) { return v == top; }, [&](float, int i) { first = min(first, i); });
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) first = min(first, __shfl_xor(first, d));
     if (lane == 0) s.ipart[wave] = first;
@@ -303,42 +342,53 @@ __global__ __launch_bounds__(kNT) void sample_kernel(const SampleArgs a) {
   const double m = by_m ? fmin((double)m_in, 1.0) : 0.0;
   const double u = fmin(fmax(u_in == u_in ? (double)u_in : 0.0, 0.0), 1.0 - 0x1p-24);
 
-  // The list in falling order, and the sums of w up to each of its tokens.
-  auto sort_list = [&](int count) {
-    int padded = 64;
-    while (padded < count) padded *= 2;
-    for (int i = count + tid; i < padded; i += kNT) s.list[i] = 0;  // (below every token)
-    __syncthreads();
-    for (int size = 2; size <= padded; size *= 2)  // bitonic
-      for (int step = size / 2; step > 0; step /= 2) {
-        for (int i = tid; i < padded / 2; i += kNT) {
-          const int lo = 2 * i - (i & (step - 1)), hi = lo + step;
-          const unsigned long long p0 = s.list[lo], p1 = s.list[hi];
-          if ((p0 < p1) == ((lo & size) == 0)) {
-            s.list[lo] = p1;
-            s.list[hi] = p0;
+  // The list in falling order, and the sums of w up to each of its tokens.  span(i): where the
+  // tokens lie that token i has to be put in order with; `longest` of these spans.
+  auto sort_list = [&](int count, int longest, auto span) {
+    if (longest <= kRank && count <= kNT) {  // by counting what comes before each
+      unsigned long long mine = 0;
+      int at = 0;
+      if (tid < count) {
+        mine = s.list[tid];
+        const int2 r = span(tid);
+        at = r.x;
+        for (int i = r.x; i < r.y; i += 8)  // (eight reads on their way at once)
+#pragma unroll
+          for (int y = 0; y < 8; ++y) {
+            const unsigned long long other = s.list[min(i + y, r.y - 1)];
+            at += (int)(i + y < r.y) & (int)(other > mine);
+          }
+      }
+      __syncthreads();
+      if (tid < count) s.list[at] = mine;
+    } else {  // bitonic
+      int padded = 64;
+      while (padded < count) padded *= 2;
+      for (int i = count + tid; i < padded; i += kNT) s.list[i] = 0;  // (below every token)
+      for (int size = 2; size <= padded; size *= 2)
+        for (int step = size / 2; step > 0; step /= 2) {
+          __syncthreads();
+          for (int i = tid; i < padded / 2; i += kNT) {
+            const int lo = 2 * i - (i & (step - 1)), hi = lo + step;
+            const unsigned long long p0 = s.list[lo], p1 = s.list[hi];
+            if ((p0 < p1) == ((lo & size) == 0)) {
+              s.list[lo] = p1;
+              s.list[hi] = p0;
+            }
           }
         }
-        // (up to 128 numbers are one wave's)
-        if (padded > 128) __syncthreads();
-        else __builtin_amdgcn_wave_barrier();
-      }
-    if (padded <= 128) __syncthreads();
-    constexpr int PT = kList / kNT;  // a thread has consecutive ones
-    const int per = count <= kNT ? 1 : PT;
-    double w[PT], run = 0.0, all;
-#pragma unroll
-    for (int y = 0; y < PT; ++y) {
-      const int i = per * tid + y;
-      w[y] = y < per && i < count ? row.weight(place_logit(s.list[i])) : 0.0;
-      run += w[y];
     }
-    run = scan(s, run, all) - run;
-#pragma unroll
-    for (int y = 0; y < PT; ++y) {
-      run += w[y];
-      if (y < per) s.upto[per * tid + y] = run;
+    __syncthreads();
+    const int per = count <= kNT ? 1 : kList / kNT;  // a thread has consecutive ones
+    double run = 0.0, all;
+#pragma unroll 1
+    for (int i = per * tid; i < per * tid + per; ++i) {
+      run += i < count ? row.weight(place_logit(s.list[i])) : 0.0;
+      s.upto[i] = run;
     }
+    const double before = scan(s, run, all) - run;
+#pragma unroll 1
+    for (int i = per * tid; i < per * tid + per; ++i) s.upto[i] += before;
     __syncthreads();
   };
   // Items 0 .. c - 1 for which f holds, those a prefix of them.
@@ -355,13 +405,31 @@ __global__ __launch_bounds__(kNT) void sample_kernel(const SampleArgs a) {
   // listed and the rest is not looked at again: of k tokens none lies below the k-th largest of
   // the threads' maxima; min_p alone bounds the logit itself.
   const bool by_k = k <= kFew;
+  int listed = 0;  // tokens of the list, where it holds all that can stay
   if (by_k || (by_m && !by_p && k == n)) {
     float least;
     if (by_k) {
-      const uint32_t key = ordered(mine_top);  // (the upper 16 bits are bound enough)
+      // (the upper 16 bits are bound enough; two at a time, three counts a round)
+      const uint32_t key = ordered(mine_top);
       uint32_t to = 0;
-      for (int bit = 31; bit >= 16; --bit)
-        if (__syncthreads_count(key >= (to | 1u << bit)) >= k) to |= 1u << bit;
+#pragma unroll 1
+      for (int bit = 30; bit >= 16; bit -= 2) {
+        const uint32_t one = 1u << bit;
+        const int c1 = __popcll(__ballot(key >= to + one)), c2 = __popcll(__ballot(key >= to + 2 * one)),
+                  c3 = __popcll(__ballot(key >= to + 3 * one));
+        int* part = bit & 2 ? s.ipart : s.ipart2;  // (in turn: a barrier a round)
+        if (lane == 0) part[wave] = c1 | c2 << 10 | c3 << 20;
+        __syncthreads();
+        int n1 = 0, n2 = 0, n3 = 0;
+#pragma unroll
+        for (int y = 0; y < kNT / 64; ++y) {
+          const int c = part[y];
+          n1 += c & 1023;
+          n2 += c >> 10 & 1023;
+          n3 += c >> 20;
+        }
+        to += n3 >= k ? 3 * one : n2 >= k ? 2 * one : n1 >= k ? one : 0u;
+      }
       least = unordered(to);
       if (!(least >= -FLT_MAX)) least = -FLT_MAX;  // (also the words of a NaN; -infinity never stays)
     } else {
@@ -370,203 +438,251 @@ __global__ __launch_bounds__(kNT) void sample_kernel(const SampleArgs a) {
     }
     if (tid == 0) s.at = 0;
     list_groups(least);
-    again(x, n, s.group, s.groups, [&](float v, int i) {
-      if (v >= least) {
-        const int at = atomicAdd(&s.at, 1);
-        if (at < kList) s.list[at] = place(v, i);
+    again(x, n, s.group, s.groups, [&](float v) { return v >= least; }, [&](float v, int i) {
+      const int at = atomicAdd(&s.at, 1);
+      if (at < kList) s.list[at] = place(v, i);
+    });
+    __syncthreads();
+    listed = s.at <= kList ? s.at : 0;
+    __syncthreads();
+  }
+
+  // Otherwise the bins: of those in which a border or the draw can lie the tokens are listed.
+  int bk = kBins, bm = kBins, in_list = listed, widest = listed;
+  int2 bp = make_int2(kBins, kBins), bd = make_int2(0, 0);
+  double sum = 0.0;
+  auto mass_before = [&](int b) { return b > 0 && !listed ? s.mass[b - 1] : 0.0; };
+  auto count_before = [&](int b) { return b > 0 && !listed ? s.count[b - 1] : 0; };
+  // The numbers of bins for which f and g hold, those a prefix of them: of threads first, whose
+  // last bins are looked at, then in the thread after them.
+  auto bins_with = [&](auto f, auto g) {
+    const unsigned long long mf = __ballot(f(kBPT * tid + kBPT - 1)), mg = __ballot(g(kBPT * tid + kBPT - 1));
+    __syncthreads();
+    if (lane == 0) s.ipart[wave] = __popcll(mf) << 16 | __popcll(mg);
+    __syncthreads();
+    int both = 0;
+#pragma unroll
+    for (int y = 0; y < kNT / 64; ++y) both += s.ipart[y];
+    int2 n = make_int2(kBPT * (both >> 16), kBPT * (both & 0xffff));
+    const int2 t = n;
+    if (t.x < kBins)
+#pragma unroll
+      for (int y = 0; y < kBPT - 1; ++y) n.x += f(t.x + y);
+    if (t.y < kBins)
+#pragma unroll
+      for (int y = 0; y < kBPT - 1; ++y) n.y += g(t.y + y);
+    return n;
+  };
+  // the bins in which the sum reaches (strict: passes) two targets
+  auto bins_of = [&](double t0, double t1, bool strict) {
+    auto short_of = [&](int b, double t) { return strict ? s.mass[b] <= t : s.mass[b] < t; };
+    const int2 n = bins_with([&](int b) { return short_of(b, t0); }, [&](int b) { return short_of(b, t1); });
+    return make_int2(min(n.x, kBins - 1), min(n.y, kBins - 1));
+  };
+  auto bin_of = [&](double target, bool strict) { return bins_of(target, target, strict).x; };
+
+  if (!listed) {
+    // counts and shortfalls of the bins; a thread has kBPT bins after each other
+    int mine[kBPT];
+#pragma unroll
+    for (int y = 0; y < kBPT; ++y) s.hist[tid + y * kNT] = 0;
+    __syncthreads();
+    each<2>(x, n, [&](float v, int) {
+      const float place = row.bin(v);
+      if (place < kBins) {
+        const uint32_t missing = (uint32_t)rintf(row.shortfall(v, place) * 0x1p30f);
+        atomicAdd(&s.hist[(int)place], (1ull << kFracBits) + missing);
       }
     });
     __syncthreads();
-    const int count = s.at;
+    {
+      double m_mine[kBPT], edge = exp(-0x1p-7 * (kBPT * tid));
+      int c_all = 0;
+      double m_all = 0.0;
+#pragma unroll
+      for (int y = 0; y < kBPT; ++y) {
+        const unsigned long long raw = s.hist[kBPT * tid + y];
+        mine[y] = (int)(raw >> kFracBits);
+        m_mine[y] = ((double)mine[y] - (double)(raw & ((1ull << kFracBits) - 1)) * 0x1p-30) * edge;
+        edge *= 0.992217938260243;  // exp(-1/128)
+        c_all += mine[y];
+        m_all += m_mine[y];
+      }
+      double m_up;
+      int c_up;
+      {
+        const double m_in = wave_scan(m_all, lane);
+        const int c_in = wave_scan(c_all, lane);
+        if (lane == 63) {
+          s.part[wave] = m_in;
+          s.ipart[wave] = c_in;
+        }
+        __syncthreads();
+        double m_before = 0.0;
+        int c_before = 0;
+        for (int y = 0; y < wave; ++y) {
+          m_before += s.part[y];
+          c_before += s.ipart[y];
+        }
+        m_up = m_before + m_in - m_all;
+        c_up = c_before + c_in - c_all;
+      }
+#pragma unroll
+      for (int y = 0; y < kBPT; ++y) {
+        s.mass[kBPT * tid + y] = m_up += m_mine[y];
+        s.count[kBPT * tid + y] = c_up += mine[y];
+      }
+    }
     __syncthreads();
-    if (count <= kList) {
-      sort_list(count);
-      int best = min(k, count);
-      if (by_p) {
-        const double target = p * s.upto[best - 1];
-        best = min(best, prefix(best, [&](int i) { return s.upto[i] < target; }) + 1);
-      }
-      if (by_m) best = max(prefix(best, [&](int i) { return row.weight(place_logit(s.list[i])) >= m; }), 1);
-      const double total = s.upto[best - 1], target = u * total;
-      const int at = min(prefix(best, [&](int i) { return s.upto[i] <= target; }), best - 1);
-      if (tid == 0) {
-        const uint64_t drawn = s.list[at];
-        answer(place_token(drawn), (float)log(row.weight(place_logit(drawn)) / total));
-      }
-      return;
-    }
-  }
-
-  // counts and shortfalls of the bins; a thread has kBPT bins after each other
-#pragma unroll
-  for (int y = 0; y < kBPT; ++y) s.hist[tid + y * kNT] = 0;
-  __syncthreads();
-  each(x, n, [&](float v, int) {
-    const float place = row.bin(v);
-    if (place < kBins)
-      atomicAdd(&s.hist[(int)place], (1ull << kFracBits) +
-                                         (unsigned long long)(uint32_t)rintf(row.shortfall(v, place) * 0x1p30f));
-  });
-  __syncthreads();
-  int mine[kBPT], in_bins = 0;
-  double sum = 0.0;
-  {
-    double m_mine[kBPT], edge = exp(-0x1p-7 * (kBPT * tid));
-    int c_all = 0;
-    double m_all = 0.0;
+    sum = s.mass[kBins - 1];
+    // The bins in which the borders can lie.
+    bk = bins_with([&](int b) { return s.count[b] < k; }, [](int) { return false; }).x;  // kBins: below them
+    const double sk_lo = bk < kBins ? mass_before(bk) : sum, sk_hi = bk < kBins ? s.mass[bk] : sum;
+    bp = by_p ? bins_of(p * sk_lo, p * sk_hi, false) : make_int2(kBins, kBins);
+    const double am = by_m ? -128.0 * log(m) : kBins;
+    bm = am < kBins ? (int)am : kBins;
+    const int be_lo = min(min(bk, bm), bp.x), be_hi = min(min(bk, bm), bp.y);
+    const double total_lo = be_lo < kBins ? fmax(mass_before(be_lo), 1.0) : sum;
+    const double total_hi = be_hi < kBins ? s.mass[be_hi] : sum;
+    bd = bins_of(u * total_lo, u * total_hi, true);
+    bd.y = min(bd.y, be_hi);
+    int here = 0;
+    bool wanted[kBPT];
 #pragma unroll
     for (int y = 0; y < kBPT; ++y) {
-      const unsigned long long raw = s.hist[kBPT * tid + y];
-      mine[y] = (int)(raw >> kFracBits);
-      m_mine[y] = ((double)mine[y] - (double)(raw & ((1ull << kFracBits) - 1)) * 0x1p-30) * edge;
-      edge *= 0.992217938260243;  // exp(-1/128)
-      c_all += mine[y];
-      m_all += m_mine[y];
+      const int b = kBPT * tid + y;
+      wanted[y] = b == bk || (by_p && b >= bp.x && b <= bp.y) || b == bm || (b >= bd.x && b <= bd.y);
+      here += wanted[y] ? mine[y] : 0;
     }
-    double m_up = scan(s, m_all, sum) - m_all;
-    int c_up = scan(s, c_all, in_bins) - c_all;
+    int off = scan(s, here, in_list) - here;
+    // (the largest wanted bin)
+    int most = 0;
 #pragma unroll
-    for (int y = 0; y < kBPT; ++y) {
-      s.mass[kBPT * tid + y] = m_up += m_mine[y];
-      s.count[kBPT * tid + y] = c_up += mine[y];
+    for (int y = 0; y < kBPT; ++y) most = max(most, wanted[y] ? mine[y] : 0);
+    widest = __syncthreads_or(most > kRank) ? kList : kRank;
+    if (in_list <= kList) {
+#pragma unroll
+      for (int y = 0; y < kBPT; ++y) {
+        s.offset[kBPT * tid + y] = off;
+        s.cursor[kBPT * tid + y] = 0;
+        off += wanted[y] ? mine[y] : 0;
+      }
+      const unsigned p_more = by_p ? bp.y - bp.x : 0u;  // (without top-p bp.x is kBins)
+      const float past = min(max(max(bk < kBins ? bk : 0, bm < kBins ? bm : 0), max(by_p ? bp.y : 0, bd.y)), kBins - 1) + 1;
+      __syncthreads();
+      // Most tokens lie outside of what is wanted by far, which intervals of logits around the
+      // bins show: the draw's, top-p's, and those of top-k and min_p.
+      float mid[3], half[3];
+      auto around = [&](int which, int first, int last) {
+        const float lo = fmaxf(row.top - (last + 1) / row.by_bin, -FLT_MAX), hi = row.top - first / row.by_bin;
+        const float edge = 4e-7f * (fabsf(row.top) + fabsf(lo)) + 1e-30f;
+        mid[which] = 0.5f * lo + 0.5f * hi;
+        half[which] = 0.5f * hi - 0.5f * lo + edge;
+        if (!(half[which] < FLT_MAX)) {  // (infinities)
+          mid[which] = 0.0f;
+          half[which] = INFINITY;
+        }
+      };
+      const int other = min(bk, bm), others = max(bk < kBins ? bk : 0, bm < kBins ? bm : 0);
+      around(0, bd.x, bd.y);
+      around(1, by_p ? bp.x : bd.x, by_p ? bp.y : bd.y);
+      around(2, other < kBins ? other : bd.x, other < kBins ? others : bd.y);
+      each<2>(x, n, [&](float v, int i) {
+        const int wanted = (int)(fabsf(v - mid[0]) <= half[0]) | (int)(fabsf(v - mid[1]) <= half[1]) |
+                           (int)(fabsf(v - mid[2]) <= half[2]);
+        if (!wanted) return;
+        const float at = row.bin(v);
+        if (at < past) {
+          const int b = (int)at;
+          if (b == bk || b == bm || (unsigned)(b - bd.x) <= (unsigned)(bd.y - bd.x) || (unsigned)(b - bp.x) <= p_more)
+            s.list[s.offset[b] + atomicAdd(&s.cursor[b], 1)] = place(v, i);
+        }
+      });
+      __syncthreads();
     }
   }
-  __syncthreads();
-  sum = s.mass[kBins - 1];  // (as the bins have it)
-  auto mass_before = [&](int b) { return b > 0 ? s.mass[b - 1] : 0.0; };
-  auto count_before = [&](int b) { return b > 0 ? s.count[b - 1] : 0; };
-  // The number of bins for which f holds, those a prefix of them.
-  auto bins_with = [&](auto f) {
-    const int t = __syncthreads_count(f(kBPT * tid + kBPT - 1));
-    int b = kBPT * t;
-    if (t < kNT)
-#pragma unroll
-      for (int y = 0; y < kBPT - 1; ++y) b += f(kBPT * t + y);
-    return b;
-  };
-  // the bin in which the sum reaches (strict: passes) a target
-  auto bin_of = [&](double target, bool strict) {
-    return min(bins_with([&](int b) { return strict ? s.mass[b] <= target : s.mass[b] < target; }), kBins - 1);
-  };
-
-  // The bins in which the borders can lie.
-  const int bk = bins_with([&](int b) { return s.count[b] < k; });  // kBins: below them
-  const double sk_lo = bk < kBins ? mass_before(bk) : sum, sk_hi = bk < kBins ? s.mass[bk] : sum;
-  const int bp_lo = by_p ? bin_of(p * sk_lo, false) : kBins, bp_hi = by_p ? bin_of(p * sk_hi, false) : kBins;
-  const double am = by_m ? -128.0 * log(m) : kBins;
-  const int bm = am < kBins ? (int)am : kBins;
-  const int be_lo = min(min(bk, bm), bp_lo), be_hi = min(min(bk, bm), bp_hi);
-  const double total_lo = be_lo < kBins ? fmax(mass_before(be_lo), 1.0) : sum;
-  const double total_hi = be_hi < kBins ? s.mass[be_hi] : sum;
-  const int bd_lo = bin_of(u * total_lo, true), bd_hi = min(bin_of(u * total_hi, true), be_hi);
-  int in_list, here = 0;
-  bool wanted[kBPT];
-#pragma unroll
-  for (int y = 0; y < kBPT; ++y) {
-    const int b = kBPT * tid + y;
-    wanted[y] = b == bk || (by_p && b >= bp_lo && b <= bp_hi) || b == bm || (b >= bd_lo && b <= bd_hi);
-    here += wanted[y] ? mine[y] : 0;
-  }
-  int off = scan(s, here, in_list) - here;
 
   int best = n;          // tokens that stay, and their sum
   double total = sum;
   uint64_t drawn;
   if (in_list <= kList) {
-#pragma unroll
-    for (int y = 0; y < kBPT; ++y) {
-      s.offset[kBPT * tid + y] = wanted[y] ? off : -1;
-      s.cursor[kBPT * tid + y] = 0;
-      off += wanted[y] ? mine[y] : 0;
-    }
-    const float past = min(max(max(bk < kBins ? bk : 0, bm < kBins ? bm : 0), max(by_p ? bp_hi : 0, bd_hi)), kBins - 1) + 1;
-    __syncthreads();
-    each(x, n, [&](float v, int i) {
-      const float at = row.bin(v);
-      if (at < past) {
-        const int b = (int)at;
-        if (s.offset[b] >= 0) s.list[s.offset[b] + atomicAdd(&s.cursor[b], 1)] = place(v, i);
-      }
-    });
-    __syncthreads();
-    sort_list(in_list);
+    // where a token's bin (or the one list) lies in the list
+    auto span = [&](int b) {
+      const int o = listed ? 0 : s.offset[b];
+      return make_int2(o, listed ? listed : o + s.count[b] - count_before(b));
+    };
+    sort_list(in_list, widest, [&](int i) { return span(listed ? 0 : (int)row.bin(place_logit(s.list[i]))); });
     // sum up to and with the c-th token of a bin (c = 0: before it)
     auto sum_at = [&](int b, int c) {
-      const int o = s.offset[b];
+      const int o = span(b).x;
       return mass_before(b) + (c > 0 ? s.upto[o + c - 1] - (o > 0 ? s.upto[o - 1] : 0.0) : 0.0);
     };
-    auto tokens_of = [&](int b) { return s.count[b] - count_before(b); };
-    if (bk < kBins) {
-      best = k;
-      total = sum_at(bk, k - count_before(bk));
-    }
-    if (by_p) {
-      const double target = p * total;
-      const int b = min(max(bin_of(target, false), bp_lo), bp_hi);
-      const int c = min(prefix(tokens_of(b), [&](int i) { return sum_at(b, i + 1) < target; }) + 1, tokens_of(b));
-      const int stay = max(count_before(b) + c, 1);
-      if (stay < best) {
-        best = stay;
-        total = sum_at(b, c);
-      }
-    }
-    if (bm < kBins) {
-      const int c = prefix(tokens_of(bm), [&](int i) { return row.weight(place_logit(s.list[s.offset[bm] + i])) >= m; });
-      const int stay = max(count_before(bm) + c, 1);
-      if (stay < best) {
-        best = stay;
-        total = sum_at(bm, c);
-      }
-    }
-    total = fmax(total, 1.0);
-    const double target = u * total;
-    const int b = min(max(bin_of(target, true), bd_lo), bd_hi);
-    const int c = min(prefix(tokens_of(b), [&](int i) { return sum_at(b, i + 1) <= target; }), tokens_of(b) - 1);
-    // (a sum that rounds past the last one that stays: that one, in the same bin)
-    drawn = s.list[s.offset[b] + min(c, max(best - count_before(b), 1) - 1)];
-  } else {
-    int tokens;
-    double mass;
-    if (bk < kBins) {
-      best = k;
-      search(s, x, n, row, bk, k - count_before(bk), mass_before(bk), 0.0, false, tokens, mass);
-      total = mass;
-    }
-    if (by_p) {
-      const double target = p * total;
-      const int b = bin_of(target, false);
-      search(s, x, n, row, b, 0, mass_before(b), target, false, tokens, mass);
-      const int stay = max(count_before(b) + tokens, 1);
-      if (stay < best) {
-        best = stay;
-        total = mass;
-      }
-    }
-    if (bm < kBins) {
-      int c = 0;
-      double w = 0.0;
-      each(x, n, [&](float v, int) {
-        if ((int)fminf(row.bin(v), kBins) == bm && row.weight(v) >= m) {
-          ++c;
-          w += row.weight(v);
-        }
+    // The tokens of a bin whose sums are below a target (strict: not above it).
+    auto short_of = [&](int b, double target, bool strict) {
+      const int2 r = span(b);
+      return prefix(r.y - r.x, [&](int i) {
+        const double t = sum_at(b, i + 1);
+        return strict ? t <= target : t < target;
       });
-      double w_all;
-      int c_all;
-      scan(s, w, w_all);
-      scan(s, c, c_all);
-      const int stay = max(count_before(bm) + c_all, 1);
-      if (stay < best) {
-        best = stay;
-        total = mass_before(bm) + w_all;
+    };
+    auto find_bin = [&](double target, bool strict, int2 within) {
+      return listed ? 0 : min(max(bin_of(target, strict), within.x), within.y);
+    };
+    if (listed) best = min(k, listed);
+    else if (bk < kBins) best = k;
+    if (listed || bk < kBins) total = sum_at(listed ? 0 : bk, best - count_before(bk));
+#pragma unroll 1
+    for (int draw = by_p ? 0 : 1; draw < 2; ++draw) {  // the nucleus, then (with min_p taken in) the draw
+      if (draw && by_m && (listed || bm < kBins)) {
+        const int2 r = span(bm);
+        const int c = prefix(r.y - r.x, [&](int i) { return row.weight(place_logit(s.list[r.x + i])) >= m; });
+        const int stay = max(count_before(bm) + c, 1);
+        if (stay < best) {
+          best = stay;
+          total = sum_at(bm, stay - count_before(bm));
+        }
+      }
+      if (draw) total = fmax(total, 1.0);
+      const double target = (draw ? u : p) * total;
+      const int b = find_bin(target, draw, draw ? bd : bp), before = count_before(b);
+      const int2 r = span(b);
+      const int c = min(short_of(b, target, draw), r.y - r.x - 1);
+      if (!draw) {
+        const int stay = before + c + 1;
+        if (stay < best) {
+          best = stay;
+          total = sum_at(b, c + 1);
+        }
+      } else {  // (a sum that rounds past the last one that stays: that one, in the same bin)
+        drawn = s.list[r.x + min(c, max(best - before, 1) - 1)];
       }
     }
-    total = fmax(total, 1.0);
-    const double target = u * total;
-    const int b = min(bin_of(target, true), be_hi);
-    drawn = search(s, x, n, row, b, 0, mass_before(b), target, true, tokens, mass);
-    if (count_before(b) + tokens > best)
-      drawn = search(s, x, n, row, b, max(best - count_before(b), 1), mass_before(b), 0.0, false, tokens, mass);
+  } else {
+    Search q;
+#pragma unroll 1
+    for (int stage = 0; stage < 5; ++stage) {  // top-k, top-p, min_p, the draw, the last that stays
+      if ((stage == 0 && bk == kBins) || (stage == 1 && !by_p) || (stage == 2 && bm == kBins)) continue;
+      q.count = 0;
+      q.least = 0.0;
+      q.strict = stage == 3;
+      if (stage == 3) total = fmax(total, 1.0);
+      q.target = (stage == 3 ? u : p) * total;
+      if (stage == 4) {
+        if (count_before(q.bin) + q.tokens <= best) break;
+        q.count = max(best - count_before(q.bin), 1);
+      } else {
+        q.bin = stage == 0 ? bk : stage == 2 ? bm : min(bin_of(q.target, q.strict), stage == 3 ? bd.y : kBins - 1);
+        if (stage == 0) q.count = k - count_before(bk);
+        if (stage == 2) q.least = m;
+      }
+      search(s, x, n, row, q);
+      const int stay = max(count_before(q.bin) + q.tokens, 1);
+      if (stage < 3 && (stay < best || stage == 0)) {
+        best = stay;
+        total = q.mass;
+      }
+    }
+    drawn = q.to;
   }
   if (tid == 0) answer(place_token(drawn), (float)log(row.weight(place_logit(drawn)) / total));
 }

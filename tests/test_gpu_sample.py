@@ -47,7 +47,7 @@ def _check(torch, x, u, T=None, k=None, p=None, m=None, what=""):
         if np.isnan(r["logprob"]):
             assert np.isnan(lp[i])
         else:  # (a sum to 2^-29, the logarithm and its rounding)
-            assert abs(lp[i] - r["logprob"]) <= 2.0 ** -28 + 1.5 * 2.0 ** -24 * abs(r["logprob"]), (i, lp[i], r["logprob"])
+            assert abs(float(lp[i]) - r["logprob"]) <= 2.0 ** -28 + 1.5 * 2.0 ** -24 * abs(r["logprob"]), (i, lp[i], r["logprob"])
     assert near <= n // 20 + 1
 
 
