@@ -11,14 +11,16 @@ namespace {
 // ---------------------------------------------------------------------------
 // Choice.  Of the tokens between the first and the last ones that stay anyway, the `need` of
 // the greatest weight, equal ones by number.  Weights are mapped to whole numbers of the same
-// order, the need-th greatest of them is found 11, 11 and 10 bits at a time by counting
+// order, the need-th greatest of them is found 12, 10 and 10 bits at a time by counting
 // (a histogram of those that agree in the bits found so far), and a last walk in the order
 // of the tokens writes those above it, and as many equal to it as there is room for.  A
-// workgroup has a row; its waves have runs of consecutive tokens, kept in registers where
-// the row is short enough.
+// workgroup has a row, its waves have runs of consecutive tokens, which each walk loads again:
+// 320 rows of 7,282 tokens take 26 us, 256 of up to 4,099 15 us and 24 of up to 2,001 9.5 us.  Kept in
+// registers, with every walk unrolled over them (25 KB of code), they took 37, 19 and 12 us;
+// bins that spread weights of one binade (by the distance to the greatest) took as long, with
+// a walk more.
 // ---------------------------------------------------------------------------
-constexpr int kBins = 2048;
-constexpr int kKept = 32;  // weights that a lane keeps in registers
+constexpr int kBins = 4096;
 
 // NaN below everything, the two zeros equal.
 FI uint32_t ordered(float x) {
@@ -36,7 +38,7 @@ FI int scan_add(int x, int lane) {  // inclusive, over the wave
   return x;
 }
 
-template <int NW, bool REG>
+template <int NW>
 __global__ __launch_bounds__(64 * NW) void evict_select_kernel(const SelectArgs a) {
   constexpr int NT = 64 * NW, BPT = kBins / NT;
   __shared__ int hist[kBins];
@@ -55,34 +57,32 @@ __global__ __launch_bounds__(64 * NW) void evict_select_kernel(const SelectArgs 
   const int lo = a.first, hi = t - a.last;
   int need = keep - a.first - a.last;
   const int seg = (t + NT - 1) / NT * 64, base = wave * seg;
-  uint32_t kept[REG ? kKept : 1];
-  if (REG) {
-#pragma unroll
-    for (int e = 0; e < kKept; ++e) {
-      const int i = base + 64 * e + lane;
-      kept[e] = 64 * e < seg && i < t ? ordered(w[i]) : 0u;
-    }
-  }
   // f(key, token) for the wave's tokens in order, 64 at a time (all lanes together)
   auto each = [&](auto f) {
-    if (REG) {
+    constexpr int U = 4;
+    const int end = min(base + seg, t);
+    float next[U];
 #pragma unroll
-      for (int e = 0; e < kKept; ++e) {
-        if (64 * e >= seg) break;
-        f(kept[e], base + 64 * e + lane);
+    for (int y = 0; y < U; ++y) next[y] = base + 64 * y + lane < end ? w[base + 64 * y + lane] : 0.0f;
+#pragma unroll 1
+    for (int i = base; i < end; i += 64 * U) {
+      float now[U];
+#pragma unroll
+      for (int y = 0; y < U; ++y) {
+        now[y] = next[y];
+        const int j = i + 64 * (U + y) + lane;
+        next[y] = j < end ? w[j] : 0.0f;
       }
-    } else {
-      for (int e = 0; e < seg && base + e < t; e += 64) {
-        const int i = base + e + lane;
-        f(i < t ? ordered(w[i]) : 0u, i);
-      }
+#pragma unroll
+      for (int y = 0; y < U; ++y) f(ordered(now[y]), i + 64 * y + lane < end ? i + 64 * y + lane : t);
     }
   };
 
   uint32_t prefix = 0, same = 0;  // the bits found, and which they are
   bool whole = need == 0;         // all that agree with the prefix stay (or none is wanted)
-  for (int shift = 21; !whole && shift >= 0; shift = shift == 21 ? 10 : shift == 10 ? 0 : -1) {
-    const uint32_t bins = shift == 0 ? 1023u : 2047u;
+#pragma unroll 1
+  for (int shift = 20; !whole && shift >= 0; shift -= 10) {
+    const uint32_t bins = shift == 20 ? 4095u : 1023u;
     for (int i = threadIdx.x; i < kBins; i += NT) hist[i] = 0;
     __syncthreads();
     each([&](uint32_t k, int i) {
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(64 * NW) void evict_select_kernel(const SelectArgs 
     need = found[1];
     whole = need == found[2];
   }
-  // Tokens that stay: those above `over`, and the first `ties` of those equal to it.
+  // Tokens that stay: those above `prefix`, and the first `ties` of those equal to it.
   const int ties = whole ? 0 : need;
   const bool none = need == 0;
   auto stays = [&](uint32_t k, int i, bool& equal) {
@@ -325,12 +325,10 @@ hipError_t launch_evict_select(const SelectArgs& a, hipStream_t s) {
   const unsigned rows = (unsigned)(a.B * a.L * a.H);
   int longest = 0;
   for (int b = 0; b < a.B; ++b) longest = a.s[b].t > longest ? a.s[b].t : longest;
-  if (longest <= 4 * 64 * kKept)
-    evict_select_kernel<4, true><<<rows, 256, 0, s>>>(a);
-  else if (longest <= 16 * 64 * kKept)
-    evict_select_kernel<16, true><<<rows, 1024, 0, s>>>(a);
+  if (longest <= 1024)
+    evict_select_kernel<4><<<rows, 256, 0, s>>>(a);
   else
-    evict_select_kernel<16, false><<<rows, 1024, 0, s>>>(a);
+    evict_select_kernel<16><<<rows, 1024, 0, s>>>(a);
   return hipGetLastError();
 }
 
