@@ -682,17 +682,14 @@ int32_t hf_paged_evict(int32_t B, const int32_t* n, const int32_t* kv_len,
  *   token        device int32 [n].
  *   logprob      device fp32 [n] or NULL: log of the token's w over the sum of those that
  *                stay (0 for temperature <= 0).
- *   workspace    device, >= hf_sample_workspace_bytes(n, vocab, dtype), 256-B aligned; may be
- *                NULL where that is 0.  Calls that share one must not overlap.
  * Numerics: sums are held to 2^-29 of themselves or better, so that a token differs from
  * the definition's only where u times the sum, or top_p's border, is that close to a
  * running sum.  The result of a row depends on that row alone.
  */
-size_t hf_sample_workspace_bytes(int32_t n, int32_t vocab, int32_t dtype);
 int32_t hf_sample_tokens(int32_t n, int32_t vocab, int32_t dtype, const void* x, int64_t stride,
                          const float* temperature, const int32_t* top_k, const float* top_p,
                          const float* min_p, const float* u, int32_t* token, float* logprob,
-                         void* workspace, size_t workspace_bytes, void* stream);
+                         void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Offline construction of the maps (fp64, off the transfer path).           */
@@ -838,7 +835,7 @@ typedef enum {
   HF_KERNEL_ATTENTION_WEIGHTS = 16, /* hf_attention_weights, hf_paged_attention_weights */
   HF_KERNEL_EVICT_SELECT = 17,     /* hf_evict_select */
   HF_KERNEL_EVICT_MOVE = 18,       /* hf_evict_rows, hf_paged_evict */
-  HF_KERNEL_SAMPLE = 19,           /* all launches of hf_sample_tokens */
+  HF_KERNEL_SAMPLE = 19,           /* hf_sample_tokens */
   HF_KERNEL_COUNT = 20
 } hf_kernel_id;
 

@@ -2,7 +2,8 @@
 
 * ``heterofold`` -- Python binding of the C ABI in ``include/heterofold.h``
   (``hf_build_alignment``, ``hf_build_layer_map``, ``hf_pack_maps``,
-  ``hf_transfer_kv``, ``hf_prompt_attention``, ``hf_paged_attention`` and helpers),
+  ``hf_transfer_kv``, ``hf_prompt_attention``, ``hf_paged_attention``,
+  ``hf_evict_select``, ``hf_sample_tokens`` and helpers),
   backed by ``libheterofold.so``.
 * ``synth``      -- seeded synthetic workloads.
 * ``build``      -- builds ``libheterofold.so`` in-tree.

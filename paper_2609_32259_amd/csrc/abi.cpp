@@ -1463,6 +1463,7 @@ int32_t hf_evict_rows(int32_t B, const int32_t* n, const int32_t* kv_len, int32_
     return st;
   if (k->dtype != v->dtype) return fail(HF_ERR_DTYPE, "k and v dtypes differ");
   if (k->H != v->H || k->d_h != v->d_h) return fail(HF_ERR_SHAPE, "k and v differ in heads or d_h");
+  if (in_place && total > 0 && k->ptr == v->ptr) return fail(HF_ERR_SHAPE, "in place k and v must be different rows");
   if (!in_place) {
     if ((st = check_rows("k_to", k_to, total > 0, true, true)) ||
         (st = check_rows("v_to", v_to, total > 0, true, true)))
@@ -1470,7 +1471,8 @@ int32_t hf_evict_rows(int32_t B, const int32_t* n, const int32_t* kv_len, int32_
     if (k_to->dtype != k->dtype || v_to->dtype != v->dtype) return fail(HF_ERR_DTYPE, "k_to, v_to and k dtypes differ");
     if (k_to->H != k->H || v_to->H != k->H || k_to->d_h != k->d_h || v_to->d_h != k->d_h)
       return fail(HF_ERR_SHAPE, "k_to, v_to and k differ in heads or d_h");
-    if (total > 0 && (k_to->ptr == k->ptr || v_to->ptr == v->ptr || k_to->ptr == v_to->ptr))
+    if (total > 0 && (k_to->ptr == k->ptr || v_to->ptr == v->ptr || k_to->ptr == v_to->ptr ||
+                      k_to->ptr == v->ptr || v_to->ptr == k->ptr))
       return fail(HF_ERR_SHAPE, "k_to and v_to must be other memory (NULL both: in place)");
   }
   const int64_t el = k->dtype == HF_BF16 ? 2 : 4, bytes = k->d_h * el;
@@ -1557,16 +1559,10 @@ int32_t check_sample(int32_t n, int32_t vocab, int32_t dtype) {
 
 }  // namespace
 
-size_t hf_sample_workspace_bytes(int32_t n, int32_t vocab, int32_t dtype) {
-  if (check_sample(n, vocab, dtype)) return 0;
-  ok();
-  return hf::sample_workspace_bytes(dtype, n, vocab);
-}
-
 int32_t hf_sample_tokens(int32_t n, int32_t vocab, int32_t dtype, const void* x, int64_t stride,
                          const float* temperature, const int32_t* top_k, const float* top_p,
                          const float* min_p, const float* u, int32_t* token, float* logprob,
-                         void* workspace, size_t workspace_bytes, void* stream) {
+                         void* stream) {
   int32_t st;
   if ((st = check_sample(n, vocab, dtype))) return st;
   if (n > 0 && (!x || !u || !token)) return fail(HF_ERR_NULL, "x, u or token is NULL");
@@ -1575,15 +1571,8 @@ int32_t hf_sample_tokens(int32_t n, int32_t vocab, int32_t dtype, const void* x,
   for (const void* p : {(const void*)temperature, (const void*)top_k, (const void*)top_p, (const void*)min_p,
                         (const void*)u, (const void*)token, (const void*)logprob})
     if (reinterpret_cast<uintptr_t>(p) & 3u) return fail(HF_ERR_SHAPE, "settings and results must be 4-byte aligned");
-  const size_t need = hf::sample_workspace_bytes(dtype, n, vocab);
-  if (need) {
-    if (!workspace) return fail(HF_ERR_NULL, "workspace is NULL");
-    if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(HF_ERR_SHAPE, "workspace is not 256-byte aligned");
-    if (workspace_bytes < need)
-      return fail(HF_ERR_CAPACITY, "workspace %zu bytes < required %zu", workspace_bytes, need);
-  }
   if (n == 0) return ok();
-  hf::SampleArgs a = {x, stride, temperature, top_k, top_p, min_p, u, token, logprob, workspace, n, vocab};
+  hf::SampleArgs a = {x, stride, temperature, top_k, top_p, min_p, u, token, logprob, n, vocab};
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e;
   {

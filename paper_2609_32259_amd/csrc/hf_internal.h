@@ -381,10 +381,8 @@ struct SampleArgs {
   const float* u;
   int32_t* token;
   float* logprob;            // or nullptr
-  void* ws;
   int32_t n, vocab;
 };
-size_t sample_workspace_bytes(int dtype, int n, int vocab);
 hipError_t launch_sample(int dtype, const SampleArgs& a, hipStream_t s);
 
 }  // namespace hf

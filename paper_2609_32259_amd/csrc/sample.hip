@@ -689,8 +689,6 @@ __global__ __launch_bounds__(kNT) void sample_kernel(const SampleArgs a) {
 
 }  // namespace
 
-size_t sample_workspace_bytes(int dtype, int n, int vocab) { return 0; }
-
 hipError_t launch_sample(int dtype, const SampleArgs& a, hipStream_t s) {
   if (dtype == HF_BF16)
     sample_kernel<uint16_t><<<(unsigned)a.n, kNT, 0, s>>>(a);

@@ -168,11 +168,9 @@ _SIGNATURES = {
                                    C.POINTER(hf_paged_kv), C.c_int32, C.c_int32, C.c_void_p,
                                    C.c_int64, C.POINTER(hf_key_weights),
                                    C.POINTER(hf_key_weights), C.c_void_p]),
-    "hf_sample_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
     "hf_sample_tokens": (C.c_int32, [C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int64,
                                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
-                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
-                                     C.c_void_p]),
+                                     C.c_void_p, C.c_void_p, C.c_void_p]),
     "hf_recolor_moments_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int32, C.c_int32]),
     "hf_recolor_moments": (C.c_int32, [C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
                                        C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
@@ -826,9 +824,8 @@ def _own_rows(t, name):
         raise TypeError(f"{name} is written: its rows must not overlap")
 
 
-def _weigh(call, q, lse, lq, lk, H, scale, prior, decay, out, dev, launch):
+def _weigh(call, rq, lse, lq, lk, H, scale, prior, decay, out, dev, launch):
     torch = _torch()
-    rq = _head_rows(q, lq, "q", dev)
     if lse.dtype is not torch.float32 or lse.device != dev or not lse.is_contiguous() \
             or lse.numel() < sum(lq) * rq.H:
         raise TypeError("lse must be a contiguous fp32 CUDA tensor [rows, H_q]")
@@ -839,7 +836,7 @@ def _weigh(call, q, lse, lq, lk, H, scale, prior, decay, out, dev, launch):
     w = _weights(out, shape, "out", dev)
     p = None if prior is None else _weights(prior, shape, "prior", dev)
     scale = 1.0 / math.sqrt(rq.d_h) if scale is None else float(scale)
-    _check(launch(rq, scale, p, float(decay), w), call)
+    _check(launch(scale, p, float(decay), w), call)
     return out
 
 
@@ -864,16 +861,16 @@ def hf_attention_weights(q, k, lse, q_len, kv_len=None, causal=True, scale=None,
     if not q.is_cuda:
         raise TypeError("q must be a CUDA tensor")
     with _call_on(dev, stream):
-        rk = _head_rows(k, lk, "k", dev)
+        rq, rk = _head_rows(q, lq, "q", dev), _head_rows(k, lk, "k", dev)
         if workspace is None:
-            nbytes = lib().hf_attention_weights_workspace_bytes(len(lq), nq, nk, q.shape[-2] if q.dim() == 3
-                                                                else q.shape[1], rk.H, rk.d_h, rk.dtype)
+            nbytes = lib().hf_attention_weights_workspace_bytes(len(lq), nq, nk, rq.H, rk.H, rk.d_h,
+                                                                rk.dtype)
             if nbytes:
                 workspace = _torch().empty(nbytes, dtype=_torch().uint8, device=dev)
         elif workspace.device != dev or not workspace.is_contiguous():
             raise TypeError("workspace must be a contiguous CUDA tensor on q's device")
-        return _weigh("hf_attention_weights", q, lse, lq, lk, rk.H, scale, prior, decay, out, dev,
-                      lambda rq, scale, p, decay, w: lib().hf_attention_weights(
+        return _weigh("hf_attention_weights", rq, lse, lq, lk, rk.H, scale, prior, decay, out, dev,
+                      lambda scale, p, decay, w: lib().hf_attention_weights(
                           len(lq), nq, nk, rq, rk, lse.data_ptr(), scale, 1 if causal else 0, p,
                           decay, w, _ptr(workspace), 0 if workspace is None else _nbytes(workspace),
                           _raw_stream(dev)))
@@ -888,9 +885,9 @@ def hf_paged_attention_weights(q, cache: PagedKV, lse, q_len, kv_len, layer=0, c
         raise ValueError(f"{len(lq)} sequences, the table has {cache.batch}")
     dev = cache.pages.device
     with _call_on(dev, stream):
-        return _weigh("hf_paged_attention_weights", q, lse, lq, lk, cache.H, scale, prior, decay,
-                      out, dev,
-                      lambda rq, scale, p, decay, w: lib().hf_paged_attention_weights(
+        rq = _head_rows(q, lq, "q", dev)
+        return _weigh("hf_paged_attention_weights", rq, lse, lq, lk, cache.H, scale, prior, decay,
+                      out, dev, lambda scale, p, decay, w: lib().hf_paged_attention_weights(
                           len(lq), nq, nk, rq, cache.desc, int(layer), lse.data_ptr(), scale,
                           1 if causal else 0, p, decay, w, _raw_stream(dev)))
 
@@ -1004,11 +1001,6 @@ def hf_paged_evict(cache: PagedKV, index, n, kv_len, out: Optional[PagedKV] = No
     return cache if out is None else out
 
 
-def hf_sample_workspace_bytes(n: int, vocab: int, dtype: int) -> int:
-    """dtype: HF_BF16 or HF_F32."""
-    return int(lib().hf_sample_workspace_bytes(int(n), int(vocab), int(dtype)))
-
-
 def _setting(t, n, dtype, name, dev):
     if t is None:
         return None
@@ -1018,7 +1010,7 @@ def _setting(t, n, dtype, name, dev):
 
 
 def hf_sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, out=None,
-                     return_logprob=False, logprob=None, workspace=None, stream=None):
+                     return_logprob=False, logprob=None, stream=None):
     """The next token of each row of logits [n, vocab] (bf16 or fp32, contiguous rows) from the
     given random numbers u [n] in [0, 1).  Settings are tensors [n]: temperature, top_p, min_p
     fp32, top_k int32; None: 1, all, 1, 0.  Returns int32 [n], with ``return_logprob`` (tokens,
@@ -1041,14 +1033,8 @@ def hf_sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=
         if logprob is None and return_logprob:
             logprob = torch.empty(n, dtype=f32, device=dev)
         args += [_setting(out, n, torch.int32, "out", dev), _setting(logprob, n, f32, "logprob", dev)]
-        if workspace is None:
-            nbytes = lib().hf_sample_workspace_bytes(n, vocab, code)
-            if nbytes:
-                workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-        elif workspace.device != dev or not workspace.is_contiguous():
-            raise TypeError("workspace must be a contiguous CUDA tensor on logits' device")
-        st = lib().hf_sample_tokens(n, vocab, code, logits.data_ptr(), stride, *args, _ptr(workspace),
-                                    0 if workspace is None else _nbytes(workspace), _raw_stream(dev))
+        st = lib().hf_sample_tokens(n, vocab, code, logits.data_ptr(), stride, *args,
+                                    _raw_stream(dev))
     _check(st, "hf_sample_tokens")
     return (out, logprob) if return_logprob else out
 

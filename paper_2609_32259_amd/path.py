@@ -125,6 +125,23 @@ class TransferPath:
         return hf.hf_prompt_attention(q, self.R[:, layer, 0], self.R[:, layer, 1], q_len,
                                       self.r_len if kv_len is None else kv_len, **kw)
 
+    def weigh(self, layer: int, q, lse, q_len, kv_len=None, **kw):
+        """The attention weight that each key of one layer of the receiver cache got from the
+        queries of an ``attend`` that returned lse (arguments as there and as
+        ``hf_attention_weights``), fp32 [B, H, T]."""
+        return hf.hf_attention_weights(q, self.R[:, layer, 0], lse, q_len,
+                                       self.r_len if kv_len is None else kv_len, **kw)
+
+    def evict(self, weights, keep, kv_len=None, n_first=0, n_last=0, stream=None):
+        """Shortens the receiver cache in place: each layer and head keeps keep [B] of its
+        first kv_len [B] tokens (None: the transferred ones), by weights [B, L, H, T], which
+        move with the rows.  Returns the lengths and the tokens that stay [B, L, H, N]."""
+        kv_len = self.r_len if kv_len is None else kv_len
+        index, n = _choice(weights, kv_len, keep, n_first, n_last, stream)
+        hf.hf_evict_rows(self.R[:, :, 0], self.R[:, :, 1], index, n, kv_len, weights=weights,
+                         stream=stream)
+        return n, index
+
     def store(self, cache: "hf.PagedKV", start=None, layer: int = 0, stream=None):
         """Append the transferred rows of all receiver layers to a paged cache, as they are
         (their keys are rotated already), behind the start [B] tokens it holds (None: 0)."""
@@ -132,6 +149,19 @@ class TransferPath:
             start = np.zeros(len(self.r_len), np.int32)
         return hf.hf_paged_append(cache, start, self.r_len, self.R[:, :, 0], self.R[:, :, 1],
                                   layer=layer, stream=stream)
+
+
+def _choice(weights, kv_len, keep, n_first, n_last, stream):
+    kv_len, keep = hf._lens(kv_len, "kv_len")[1], hf._lens(keep, "keep")[1]
+    index = hf.hf_evict_select(weights, kv_len, keep, n_first, n_last, stream=stream)
+    return index, np.minimum(kv_len, keep).astype(np.int32)
+
+
+def evict(cache: "hf.PagedKV", weights, keep, kv_len, n_first=0, n_last=0, stream=None):
+    """``TransferPath.evict`` for all layers of a paged cache that holds kv_len [B] tokens."""
+    index, n = _choice(weights, kv_len, keep, n_first, n_last, stream)
+    hf.hf_paged_evict(cache, index, n, kv_len, weights=weights, stream=stream)
+    return n, index
 
 
 def dense_cache(cache: "hf.PagedKV", lengths, dtype=None, T_cap: Optional[int] = None):
