@@ -435,77 +435,71 @@ __global__ __launch_bounds__(256, 2) void weights_few_kernel(const WeighArgs a) 
   }
 }
 
-// Over the pages: 16 NU tokens a wave, on v_mfma_f32_16x16x32_bf16 with the codes as they are
-// stored (the arithmetic of scales and offsets is that of the attention over the pages), 16
-// query rows at a time.  The lane has tokens lane % 16 of each 16 and, with m = lane / 16,
-// rows 4 m + i.
+// Over the pages: four waves of 16 NU tokens each, tile after tile, on v_mfma_f32_16x16x32_bf16
+// with the codes as they are stored (the arithmetic of scales and offsets is that of the
+// attention over the pages).  The lane has tokens lane % 16 of each 16 and, with m = lane / 16,
+// rows 4 m + i of 16 query rows.  The query rows, 64 at a time, are brought into the form that
+// the products take once for all tiles (each wave 16 of them) and lie in LDS; the codes of the
+// next tile are on their way while one is worked on.  Four bits a value are little to read: what
+// bounds long runs of queries are the products and exponentials (2,048 over 8,192 keys of 32 / 8
+// heads 399 us; with the rows prepared by each wave for itself 582), what bounds single tokens
+// is the way to the first codes (B = 16, up to 8,192 keys, 36 MB: 19.7 us; the loads alone 15).
+// With 64 tokens a wave there are registers for half as many waves: 25.3 us.
 template <int D, bool F32, int NU>
-__global__ __launch_bounds__(256, 2) void paged_weights_kernel(const WeighArgs a) {
-  constexpr int G = D / 32, S = F32 ? 3 : 1, KT = 16 * NU;
+__global__ __launch_bounds__(256, F32 ? 2 : 4) void paged_weights_kernel(const WeighArgs a) {
+  constexpr int G = D / 32, S = F32 ? 3 : 1, KT = 16 * NU, NQ = S * G + 2;
+  __shared__ u32x4 rows[4][NQ][64];  // a block's operands, those of the words, minus lse
+  __shared__ int far[4];
   const int lane = threadIdx.x & 63, col = lane & 15, m4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const WeighItem it = weigh_item(a, true);
-  const int t0 = (it.i * 4 + wave) * KT;
-  if (t0 >= it.t) return;
+  const int begin = it.i * a.tile, end = min(it.t, begin + a.tile);
   const PageHead<D> ph(a.log2_page);
   const int32_t* table = a.table + it.b * a.table_stride;
-  // the codes and words of all tokens on their way at once
+
   uint32_t code[NU][G], word[NU][G];
   bool in[NU];
+  auto load = [&](int t0) INLINE {
 #pragma unroll
-  for (int u = 0; u < NU; ++u) {
-    const int tok = t0 + 16 * u;
-    const int page = tok < it.t ? table[tok >> a.log2_page] : -1;
-    in[u] = (unsigned)page < (unsigned)a.n_pages;  // (a hole loads from page 0 and counts as 0)
-    const uint8_t* head = a.pages + (long long)(in[u] ? page : 0) * a.page_bytes + (long long)it.h * ph.bytes();
-    const int row = (in[u] ? tok & (ph.P - 1) : 0) + col;
-    const uint8_t* c = head + ph.kcode(row) + m4 * (4 * G);
-    const uint8_t* w = head + ph.word(0, row);
-    if (D == 128) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(c), y = *reinterpret_cast<const u32x4*>(w);
+    for (int u = 0; u < NU; ++u) {
+      const int tok = t0 + 16 * u;
+      const int page = tok < end ? table[tok >> a.log2_page] : -1;
+      in[u] = (unsigned)page < (unsigned)a.n_pages;  // (a hole loads from page 0 and counts as 0)
+      const uint8_t* head = a.pages + (long long)(in[u] ? page : 0) * a.page_bytes + (long long)it.h * ph.bytes();
+      const int row = (in[u] ? tok & (ph.P - 1) : 0) + col;
+      const uint8_t* c = head + ph.kcode(row) + m4 * (4 * G);
+      const uint8_t* w = head + ph.word(0, row);
+      if (D == 128) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(c), y = *reinterpret_cast<const u32x4*>(w);
 #pragma unroll
-      for (int g = 0; g < G; ++g) {
-        code[u][g] = x[g & 3];
-        word[u][g] = y[g & 3];
-      }
-    } else {
-      const u32x2 x = *reinterpret_cast<const u32x2*>(c), y = *reinterpret_cast<const u32x2*>(w);
+        for (int g = 0; g < G; ++g) {
+          code[u][g] = x[g & 3];
+          word[u][g] = y[g & 3];
+        }
+      } else {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(c), y = *reinterpret_cast<const u32x2*>(w);
 #pragma unroll
-      for (int g = 0; g < G; ++g) {
-        code[u][g] = x[g & 1];
-        word[u][g] = y[g & 1];
+        for (int g = 0; g < G; ++g) {
+          code[u][g] = x[g & 1];
+          word[u][g] = y[g & 1];
+        }
       }
     }
-  }
-  int see[NU];
-#pragma unroll
-  for (int u = 0; u < NU; ++u) see[u] = first_row(a, it, min(t0 + 16 * u + col, it.t - 1));
-  const int all = first_row(a, it, min(t0 + KT, it.t) - 1);
-  const int first = first_row(a, it, t0) / 16 * 16;
-
-  typedef uint32_t QRaw[F32 ? 8 : 4];
-  QRaw raw[G];
-  float lse = 0.0f;
-  auto fetch = [&](int r0) {
+  };
+  // rows r0 .. r0 + 15 into the wave's block
+  auto prepare = [&](int r0) INLINE {
     if (r0 >= it.rows) return;
+    typedef uint32_t QRaw[F32 ? 8 : 4];
+    QRaw raw[G];
+    float lse;
     const long long at = query_at(a, it, min(r0 + col, it.rows - 1), lse);
     const uint8_t* row = static_cast<const uint8_t*>(a.q) + at * (F32 ? 4 : 2);
 #pragma unroll
     for (int y = 0; y < G; ++y) load_dwords<F32 ? 8 : 4>(row + (32 * y + 8 * m4) * (F32 ? 4 : 2), raw[y]);
-  };
-  fetch(first);
-  const Codes codes;
-  bf16x8 kc[NU][G];
-  float acc[NU] = {};
-#pragma unroll
-  for (int u = 0; u < NU; ++u)
-#pragma unroll
-    for (int g = 0; g < G; ++g) kc[u][g] = codes.operand<F32>(code[u][g]);
-  for (int r0 = first; r0 < it.rows; r0 += 16) {
-    bf16x8 q[S][G];
     bf16x8 qo = {};  // against the words: the sums of the groups, in three terms
 #pragma unroll
     for (int y = 0; y < G; ++y) {
+      bf16x8 q[S];
       float sum = 0.0f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -515,8 +509,10 @@ __global__ __launch_bounds__(256, 2) void paged_weights_kernel(const WeighArgs a
         float p[S];
         split<S>(f, p);
 #pragma unroll
-        for (int z = 0; z < S; ++z) q[z][y][e < 4 ? 2 * e : 2 * (e - 4) + 1] = (__bf16)p[z];
+        for (int z = 0; z < S; ++z) q[z][e < 4 ? 2 * e : 2 * (e - 4) + 1] = (__bf16)p[z];
       }
+#pragma unroll
+      for (int z = 0; z < S; ++z) rows[wave][z * G + y][lane] = __builtin_bit_cast(u32x4, q[z]);
       sum = add_xor32(add_xor16(sum));
       float p[3];
       split<3>(sum, p);
@@ -524,53 +520,101 @@ __global__ __launch_bounds__(256, 2) void paged_weights_kernel(const WeighArgs a
       qo[2 * y] = (__bf16)mine;
       qo[2 * y + 1] = (__bf16)(mine * (F32 ? 8.0f : -16.0f));
     }
+    rows[wave][S * G][lane] = __builtin_bit_cast(u32x4, qo);
     const float x = -lse * kLog2e;
-    const f32x4 nl =
-        __builtin_amdgcn_mfma_f32_16x16x32_bf16(spread(terms(x), lane < 16), ones(lane < 16), f32x4{}, 0, 0, 0);
-    const bool plain = !__any(!(fabsf(x) <= kFarLse)) && r0 >= all && r0 + 16 <= it.rows;
-    fetch(r0 + 16);
+    rows[wave][S * G + 1][lane] = __builtin_bit_cast(
+        u32x4, __builtin_amdgcn_mfma_f32_16x16x32_bf16(spread(terms(x), lane < 16), ones(lane < 16), f32x4{}, 0, 0, 0));
+    const bool f = __any(!(fabsf(x) <= kFarLse));
+    if (lane == 0) far[wave] = f;
+  };
+
+  load(begin + wave * KT);
+  const Codes codes;
+  const int first = first_row(a, it, begin) / 16 * 16;
+  const bool once = it.rows - first <= 64;
+#pragma unroll 1
+  for (int base = begin; base < end; base += 4 * KT) {
+    const int t0 = base + wave * KT;
+    bf16x8 kc[NU][G];
+    uint32_t kw[NU][G];
+    bool here[NU];
+    int see[NU];
+    float acc[NU] = {};
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
-      union {
-        uint32_t d[4];
-        bf16x8 v;
-      } wk = {{0, 0, 0, 0}};
+      here[u] = in[u];
+      see[u] = first_row(a, it, min(t0 + 16 * u + col, it.t - 1));
 #pragma unroll
-      for (int y = 0; y < G; ++y) wk.d[y] = word[u][y];
-      f32x4 v = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qo, wk.v, f32x4{}, 0, 0, 0);
-#pragma unroll
-      for (int y = 0; y < G; ++y) {
-        f32x4 d = {};
-#pragma unroll
-        for (int z = 0; z < S; ++z) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[z][y], kc[u][y], d, 0, 0, 0);
-        const float ks = __builtin_bit_cast(float, word[u][y] & 0xffff0000u);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = fmaf(ks, d[i], v[i]);
+      for (int g = 0; g < G; ++g) {
+        kc[u][g] = codes.operand<F32>(code[u][g]);
+        kw[u][g] = word[u][g];
       }
-      float w[4];
-      if (plain) {
+    }
+    load(t0 + 4 * KT);
+    const int all = first_row(a, it, min(t0 + KT, it.t) - 1), from = first_row(a, it, min(t0, it.t - 1));
+#pragma unroll 1
+    for (int c0 = first; c0 < it.rows; c0 += 64) {
+      if (base == begin || !once) {
+        if (c0 != first || base != begin) __syncthreads();
+        prepare(c0 + 16 * wave);
+        __syncthreads();
+      }
+#pragma unroll 1
+      for (int x = 0; x < 4; ++x) {
+        const int r0 = c0 + 16 * x;
+        if (t0 >= end || r0 >= it.rows || r0 + 16 <= from) continue;
+        bf16x8 q[S][G];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_exp2f(fmaf(v[i], a.c, nl[i]));
-      } else {
+        for (int z = 0; z < S; ++z)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = r0 + 4 * m4 + i;
-          const float e = fmaf(v[i], a.c, nl[i]);
-          w[i] = r >= see[u] && r < it.rows ? __builtin_amdgcn_exp2f(e > 0.0f ? 0.0f : e) : 0.0f;
+          for (int y = 0; y < G; ++y) q[z][y] = __builtin_bit_cast(bf16x8, rows[x][z * G + y][lane]);
+        const bf16x8 qo = __builtin_bit_cast(bf16x8, rows[x][S * G][lane]);
+        const f32x4 nl = __builtin_bit_cast(f32x4, rows[x][S * G + 1][lane]);
+        const bool plain = !__builtin_amdgcn_readfirstlane(far[x]) && r0 >= all && r0 + 16 <= it.rows;
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+          union {
+            uint32_t d[4];
+            bf16x8 v;
+          } wk = {{0, 0, 0, 0}};
+#pragma unroll
+          for (int y = 0; y < G; ++y) wk.d[y] = kw[u][y];
+          f32x4 v = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qo, wk.v, f32x4{}, 0, 0, 0);
+#pragma unroll
+          for (int y = 0; y < G; ++y) {
+            f32x4 d = {};
+#pragma unroll
+            for (int z = 0; z < S; ++z) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[z][y], kc[u][y], d, 0, 0, 0);
+            const float ks = __builtin_bit_cast(float, kw[u][y] & 0xffff0000u);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = fmaf(ks, d[i], v[i]);
+          }
+          float w[4];
+          if (plain) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_exp2f(fmaf(v[i], a.c, nl[i]));
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int r = r0 + 4 * m4 + i;
+              const float e = fmaf(v[i], a.c, nl[i]);
+              w[i] = r >= see[u] && r < it.rows ? __builtin_amdgcn_exp2f(e > 0.0f ? 0.0f : e) : 0.0f;
+            }
+          }
+          acc[u] += sum_of(w);
         }
       }
-      acc[u] += sum_of(w);
     }
-  }
 #pragma unroll
-  for (int u = 0; u < NU; ++u) {
-    const float w = add_xor32(add_xor16(acc[u]));
-    const int key = t0 + 16 * u + col;
-    if (m4 == 0 && key < it.t) write_weight(a, it, key, in[u] ? w : 0.0f);
+    for (int u = 0; u < NU; ++u) {
+      const float w = add_xor32(add_xor16(acc[u]));
+      const int key = t0 + 16 * u + col;
+      if (m4 == 0 && key < end) write_weight(a, it, key, here[u] ? w : 0.0f);
+    }
   }
 }
 
-constexpr int kPagedTokens = 64;  // a wave
+constexpr int kPagedTokens = 32;  // a wave
 
 template <int D>
 void launch(int dtype, const WeighShape& sh, const WeighArgs& a, hipStream_t s) {
@@ -593,7 +637,12 @@ WeighShape weigh_shape(int dtype, bool paged, int32_t B, const int32_t* q_len, c
   sh.chunk = 0;
   sh.few = 1;
   if (paged) {
-    sh.keys = 4 * kPagedTokens;
+    // As many tiles a workgroup as leave four workgroups (what the registers admit) for each CU:
+    // 64 decoded tokens over 4,096 keys each, of 32 / 8 heads, 47 us, with two 69, with one tile
+    // each 61; one over 29,119 9.4 us, with two 11.2.
+    int64_t tiles = 0;
+    for (int b = 0; b < B; ++b) tiles += (kv_len[b] + 4 * kPagedTokens - 1) / (4 * kPagedTokens);
+    sh.keys = (int32_t)(4 * kPagedTokens * std::clamp<int64_t>((tiles * H + 1023) / 1024, 1, 64));
     return sh;
   }
   int64_t longest = 0, keys = 0;

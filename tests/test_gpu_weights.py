@@ -312,3 +312,35 @@ def test_streams_and_graphs(torch):
         total = hf.hf_attention_weights(q, k, lse, [1, 1], [200, 300], prior=total)
         torch.cuda.synchronize()
         assert torch.equal(out, total), f"replay {i}"
+
+
+@pytest.mark.parametrize("dtype,d,q", [("bf16", 128, 1), ("bf16", 64, 37), ("f32", 64, 3), ("f32", 128, 36)])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "all"])
+def test_a_large_paged_batch_is_its_sequences(torch, dtype, d, q, causal):
+    """Enough tokens that a workgroup has several tiles, of fewer than 65 query rows a head and of
+    more: the same bits as each sequence in a call of its own (one tile a workgroup), which the
+    definition is held against above.  (A key's sum goes by its rows, in the same order.)"""
+    from paper_2609_32259_amd import heterofold as hf
+    B, H, Hq, P, T = 48, 8, 16, 32, 700
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    print(f"[gpu-weights] large paged batch {dtype} d={d} q={q} causal={causal}", flush=True)
+    g = torch.Generator().manual_seed(d + q)
+    kv_len = [(T - 13 * b if b % 5 else b) for b in range(B)]
+    pages = -(-T // P)
+    order = torch.randperm(B * pages, generator=g).int().view(B, pages)
+    order[3, 2] = -1
+    cache = hf.PagedKV(torch.zeros(1, B * pages, hf.hf_paged_page_bytes(H, d, P), dtype=torch.uint8, device="cuda"),
+                       order.cuda(), H, d, P)
+    x = torch.randn(B, H, T, d, generator=g).to(t).cuda()
+    hf.hf_paged_append(cache, [0] * B, kv_len, x, x)
+    qs = torch.randn(B * q, Hq, d, generator=g).to(t).cuda()
+    _, lse = hf.hf_paged_attention(qs, cache, [q] * B, kv_len, causal=causal, return_lse=True)
+    out = torch.full((B, H, T), 7.0, device="cuda")
+    hf.hf_paged_attention_weights(qs, cache, lse, [q] * B, kv_len, causal=causal, out=out)
+    for b in range(B):
+        one = hf.PagedKV(cache.pages, cache.table[b:b + 1], H, d, P)
+        w = torch.full((1, H, T), 7.0, device="cuda")
+        hf.hf_paged_attention_weights(qs[b * q:(b + 1) * q], one, lse[b * q:(b + 1) * q], [q], kv_len[b:b + 1],
+                                      causal=causal, out=w)
+        assert torch.equal(out[b], w[0]), b
+        assert bool((w[0, :, kv_len[b]:] == 7.0).all())
