@@ -13,6 +13,11 @@
 // of w to 2^-29 of itself, in whatever order the tokens come.  The bins reach down to
 // exp(-32); what lies below has in all less than 2^20 exp(-32) = 2^-26 of the largest w and
 // cannot be drawn (u < 1 - 2^-25).  Everything after the bins is in 64 bits.
+//
+// A row is a workgroup's, of 1,024 threads.  What bounds it is latency, of memory once a walk, of
+// barriers and of code that is run for the first time: a row of 131,072 logits under top-k and
+// top-p 19.6 us (walks of the bins for every row took 59), 256 such rows of all settings, 67 MB,
+// 72 us; of these greedy ones alone take 14.6, top-k 27, top-p 55 to 75.
 #include <hip/hip_runtime.h>
 
 #include "hf_attn.h"

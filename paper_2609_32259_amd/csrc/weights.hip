@@ -185,8 +185,19 @@ struct Flag {
 };
 
 // Many rows: NW waves with KB blocks of 32 keys each, all against the same rows, which come
-// through two LDS stages of 64 rows.  Where there are too few tiles of keys to fill the chip the rows of each are cut into parts as
-// well, whose sums weights_join_kernel adds.
+// through two LDS stages of 64 rows, on their way in registers two stages ahead.  Where there are
+// too few tiles of keys to fill the chip the rows of each are cut into parts as well, whose sums
+// weights_join_kernel adds; of a causal mask only the pairs of a part and a tile are workgroups
+// in which some row sees some key (one that ends at once still keeps its CU for a while).
+// The products and the exponentials, 16 cycles a wave each, bound it: a prompt of 8,192 tokens,
+// 16 / 2 heads of 128, takes 327 to 383 us by card, 0.73 to 0.85 PFLOP/s, where the products alone
+// would take some 200.
+// Two waves a SIMD fill part of each other's phases.  Taking both in turn within a wave would
+// do better (in a loop of nothing else 1,450 cycles for what takes 2,205 in two waves), but with
+// a second block's scores and operands the keys no longer fit in registers: 450 us and more.
+// Each wave with rows of its own loads (no LDS) 450 us; keys of half the tile 420.
+// fp32: 2,001 tokens, 14 / 2 heads of 64, 56 us, at half the rate of the fp32 products; 161 before
+// the rows were cut into parts.
 template <class R, int KB, int NW>
 __global__ __launch_bounds__(64 * NW, R::WAVES) void weights_rows_kernel(const WeighArgs a) {
   typedef typename R::T T;
@@ -378,7 +389,9 @@ __global__ __launch_bounds__(256) void weights_join_kernel(const WeighArgs a) {
   }
 }
 
-// Few rows: four waves, each with KB blocks of 32 keys and all rows.
+// Few rows: four waves, each with KB blocks of 32 keys and all rows, which it loads for itself, the
+// next 32 on their way.  Reading the keys bounds it: four runs of 32 queries over up to 4,097 keys
+// of 32 / 8 heads, 29 MB, 14.7 us, of which some 6 are the way to the first keys and the end.
 template <class R, int KB>
 __global__ __launch_bounds__(256, 2) void weights_few_kernel(const WeighArgs a) {
   typedef typename R::T T;

@@ -12,7 +12,7 @@ from test_kernel_resources import _resources
     ("weights.hip", "weights_rows_kernelINS0_8RowsBf16ILi64EEELi2E", 0, 2, 80),
     ("weights.hip", "weights_rows_kernelINS0_8RowsBf16ILi64EEELi1E", 0, 2, 80),
     ("weights.hip", "weights_rows_kernelINS0_7RowsF32ILi64E", 0, 2, 80),
-    # (three terms of 128 channels need more registers than there are)
+    # (fp32 keys and rows of 128 channels need more registers than there are)
     ("weights.hip", "weights_rows_kernelINS0_7RowsF32ILi128E", 128, 2, 80),
     ("weights.hip", "weights_few_kernelINS0_8RowsBf16ILi128E", 0, 2, 0),
     ("weights.hip", "weights_few_kernelINS0_8RowsBf16ILi64E", 0, 2, 0),

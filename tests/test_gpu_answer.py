@@ -175,3 +175,40 @@ def test_a_captured_step_of_answering(torch, paged):
         for x, y in zip(results(), eager):
             assert torch.equal(x, y), i
         assert token.min() >= 0 and bool((index[:, :, 1:] > index[:, :, :-1]).all())
+
+
+def test_offsets_past_32_bits(torch):
+    """Rows 2 GiB apart, for every call that takes strides, against the same rows side by side."""
+    from paper_2609_32259_amd import heterofold as hf
+    print("[gpu-answer] far rows", flush=True)
+    g = torch.Generator().manual_seed(2)
+    far = torch.empty(9 << 30, dtype=torch.uint8, device="cuda").view(torch.bfloat16)
+    T, H, d, step = 4, 2, 64, 1 << 30
+
+    def spread(x, at):  # [1, H, T, d] with tokens `step` elements apart
+        y = far.as_strided((1, H, T, d), (0, d, step, 1), at)
+        y.copy_(x)
+        return y
+    x = torch.randn(2, 1, H, T, d, generator=g).bfloat16().cuda()
+    k, v = spread(x[0], 0), spread(x[1], 4096)
+    for n in (1, 40):  # few and many rows
+        q = torch.randn(n, 8, d, generator=g).bfloat16().cuda()
+        _, lse = hf.hf_prompt_attention(q, x[0], x[1], [n], [T], causal=False, return_lse=True)
+        w = [hf.hf_attention_weights(q, y, lse, [n], [T], causal=False) for y in (k, x[0].contiguous())]
+        assert torch.equal(*w)
+    index = torch.tensor([[[0, 3], [1, 2]]], dtype=torch.int32, device="cuda")
+    hf.hf_evict_rows(k, v, index, [2], [T])
+    hf.hf_evict_rows(x[0], x[1], index, [2], [T])
+    for y, z in ((k, x[0]), (v, x[1])):
+        assert torch.equal(y, z)
+
+    w = far.view(torch.float32).as_strided((2, 1, 50), (step, 50, 1), 8192)
+    w.copy_(torch.rand(2, 1, 50, generator=g))
+    ids = hf.hf_evict_select(w, [50, 50], [20, 20])
+    for b in range(2):
+        assert ids[b, 0].tolist() == answer.evict_select(w[b, 0].cpu().numpy(), 20).tolist()
+
+    logits = far.as_strided((4, 1000), (step, 1), 65536)
+    logits.copy_(torch.randn(4, 1000, generator=g).bfloat16())
+    u = torch.rand(4, generator=g).cuda()
+    assert torch.equal(hf.hf_sample_tokens(logits, u), hf.hf_sample_tokens(logits.contiguous(), u))
