@@ -159,6 +159,8 @@ def _choice(weights, kv_len, keep, n_first, n_last, stream):
 
 def evict(cache: "hf.PagedKV", weights, keep, kv_len, n_first=0, n_last=0, stream=None):
     """``TransferPath.evict`` for all layers of a paged cache that holds kv_len [B] tokens."""
+    if weights.dim() != 4 or weights.shape[1:3] != (cache.L, cache.H):
+        raise ValueError(f"weights must be [B, {cache.L}, {cache.H}, T]")
     index, n = _choice(weights, kv_len, keep, n_first, n_last, stream)
     hf.hf_paged_evict(cache, index, n, kv_len, weights=weights, stream=stream)
     return n, index

@@ -242,5 +242,14 @@ def test_host_tensors_are_refused():
         hf.hf_evict_select(torch.zeros(1, 2, 8), np.array([8, 8]), [4])
 
 
+def test_weights_of_some_layers_only_do_not_shorten_a_paged_cache():
+    """(The other layers would have kept their rows, and with them their length.)"""
+    from paper_2609_32259_amd.path import evict
+    cache = SimpleNamespace(batch=1, pages=torch.zeros(1), L=2, H=2)
+    for w in (torch.zeros(1, 2, 8), torch.zeros(1, 1, 2, 8), torch.zeros(1, 2, 3, 8)):
+        with pytest.raises(ValueError, match="weights"):
+            evict(cache, w, [4], [8])
+
+
 def test_the_structure_is_the_header_s():
     assert C.sizeof(hf.hf_key_weights) == 32
