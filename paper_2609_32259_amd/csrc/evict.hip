@@ -329,7 +329,10 @@ hipError_t launch_evict_select(const SelectArgs& a, hipStream_t s) {
   const unsigned rows = (unsigned)(a.B * a.L * a.H);
   int longest = 0;
   for (int b = 0; b < a.B; ++b) longest = a.s[b].t > longest ? a.s[b].t : longest;
-  if (longest <= 1024)
+  // us with 4 / 16 waves a row: 8 rows of 200 tokens 8.3 / 8.2, 320 of 1,024 11 / 15, of 2,048 15 /
+  // 16, of 4,096 22 / 17, 64 of 30,000 102 / 43.  More rows than fit at once (two workgroups of 16
+  // waves a CU): 640 of 2,048 16 / 23, 1,280 of 4,096 30 / 36, of 8,192 53 / 54, 2,048 of 8,192 84 / 80.
+  if (longest <= 1024 || (rows > 512 && longest <= 4096))
     evict_select_kernel<4><<<rows, 256, 0, s>>>(a);
   else
     evict_select_kernel<16><<<rows, 1024, 0, s>>>(a);

@@ -190,14 +190,14 @@ struct Flag {
 // weights_join_kernel adds; of a causal mask only the pairs of a part and a tile are workgroups
 // in which some row sees some key (one that ends at once still keeps its CU for a while).
 // The products and the exponentials, 16 cycles a wave each, bound it: a prompt of 8,192 tokens,
-// 16 / 2 heads of 128, takes 327 to 383 us by card, 0.73 to 0.85 PFLOP/s, where the products alone
-// would take some 200.
+// 32 / 8 heads of 128, takes 327 to 383 us by card, 0.73 to 0.85 PFLOP/s, where the products alone
+// would take some 200, and one of 2,048 42 us (with the rows in one piece 155).
 // Two waves a SIMD fill part of each other's phases.  Taking both in turn within a wave would
 // do better (in a loop of nothing else 1,450 cycles for what takes 2,205 in two waves), but with
 // a second block's scores and operands the keys no longer fit in registers: 450 us and more.
-// Each wave with rows of its own loads (no LDS) 450 us; keys of half the tile 420.
-// fp32: 2,001 tokens, 14 / 2 heads of 64, 56 us, at half the rate of the fp32 products; 161 before
-// the rows were cut into parts.
+// Each wave with rows of its own loads (no LDS) took 450 us.
+// fp32: 2,001 tokens, 14 / 2 heads of 64, 53 us, at half the rate of the fp32 products; 161 before
+// the rows went through LDS in parts.
 template <class R, int KB, int NW>
 __global__ __launch_bounds__(64 * NW, R::WAVES) void weights_rows_kernel(const WeighArgs a) {
   typedef typename R::T T;
@@ -390,8 +390,8 @@ __global__ __launch_bounds__(256) void weights_join_kernel(const WeighArgs a) {
 }
 
 // Few rows: four waves, each with KB blocks of 32 keys and all rows, which it loads for itself, the
-// next 32 on their way.  Reading the keys bounds it: four runs of 32 queries over up to 4,097 keys
-// of 32 / 8 heads, 29 MB, 14.7 us, of which some 6 are the way to the first keys and the end.
+// next 32 on their way.  Reading the keys bounds it: 16 single queries over 4,096 keys of 32 / 8
+// heads of 128 each, 134 MB, 28 us, 4.8 TB/s.
 template <class R, int KB>
 __global__ __launch_bounds__(256, 2) void weights_few_kernel(const WeighArgs a) {
   typedef typename R::T T;
@@ -663,13 +663,19 @@ WeighShape weigh_shape(int dtype, bool paged, int32_t B, const int32_t* q_len, c
     longest = std::max(longest, (int64_t)q_len[b] * G);
     keys += kv_len[b];
   }
-  if (longest <= 128) {
+  // Up to 32 query rows a head (fp32: 64) waves load them for themselves, more go through LDS.  us,
+  // for itself / through LDS, bf16 heads of 128, 32 / 8 of them: 16 x 1 token over 4,096 keys 28 /
+  // 35, 4 x 8 tokens 9.8 / 10.9, 4 x 16 12.5 / 10.3, 4 x 32 16.7 / 14.0; fp32, 16 / 4 heads of 128:
+  // 4 x 8 15.7 / 20.9, 4 x 32 37 / 30; 14 / 2 heads of 64: 8 over 2,001 keys 7.0 / 7.2, 32 15.5 / 13.9.
+  if (longest <= (dtype == HF_F32 ? 64 : 32)) {
     sh.keys = dtype == HF_F32 ? 128 : 256;
     return sh;
   }
   // Tiles of 256 keys (bf16) or 128, and the parts of the rows: the cut with the least time by
   // rounds of two workgroups a CU, of `start` and so much a stage (measured, us: one round of 8
-  // stages of bf16 heads of 128 22, of fp32 heads of 64 34), and the join of the parts.
+  // stages of bf16 heads of 128 22, of fp32 heads of 64 34), and the join of the parts.  Tiles of
+  // 128 keys alone: prompt of 8,192, 16 / 2 heads of 128, 234 us for 194; tiles of 256 alone: 1,024,
+  // 32 / 8 heads of 64, 16.7 for 13.3.
   sh.few = 0;
   const bool f32 = dtype == HF_F32, wide = d_h == 128;
   double best = 1e30;

@@ -282,3 +282,26 @@ def test_graph_of_choice_and_move(torch):
         assert torch.equal(got, to)
         at = index[1, 1, 1, :90].long()
         assert torch.equal(to[0, 1, 1, 1, :90], R[1, 1, 0, 1][at])
+
+
+def test_choice_of_many_rows_is_that_of_few(torch):
+    """(More rows than are worked on at once take fewer waves each.)"""
+    from paper_2609_32259_amd import heterofold as hf
+    print("[gpu-evict] many rows", flush=True)
+    rng = np.random.default_rng(9)
+    w = rng.standard_normal((2, 300, 1500)).astype(np.float32)
+    w[:, ::3] = np.round(w[:, ::3], 1)   # ties
+    w[:, ::7, ::5] = np.nan
+    t = torch.from_numpy(w).cuda()
+    kv, keep = [1500, 1111], [700, 300]
+    many = torch.full((2, 300, 700), -5, dtype=torch.int32, device="cuda")
+    few = many.clone()
+    hf.hf_evict_select(t, kv, keep, 3, 4, out=many)
+    for b in range(2):
+        part = few[b:b + 1]
+        hf.hf_evict_select(t[b:b + 1], kv[b:b + 1], keep[b:b + 1], 3, 4, out=part)
+    assert torch.equal(many, few)
+    for b, h in ((0, 0), (0, 7), (1, 21), (1, 299)):
+        want = ans.evict_select(w[b, h, :kv[b]], keep[b], 3, 4)
+        assert many[b, h, :keep[b]].tolist() == want.tolist()
+    assert bool((many[1, :, 300:] == -5).all())
