@@ -230,9 +230,9 @@ __global__ __launch_bounds__(256) void evict_rows_kernel(const EvictArgs a) {
 // head.  Key codes and words move as they are, 16 and 4 bytes a thread.  A thread of the
 // value codes has 16 bytes of the block, a nibble of eight tokens in each; it loads the
 // same 16 bytes of each of those tokens' old blocks and takes a nibble out of each.
-// Reading bounds it: of a token that stays its value block's other tokens come as well, so that
-// 40 layers of 7,282 tokens, of which 4,096 stay, read 275 MB for the 210 that they write: 151 us,
-// 3.2 TB/s.
+// Reading bounds it: with a token that stays come the other tokens of its value block and of its
+// lines of 128 bytes (two rows of key codes, eight of words), so that 40 layers of 7,282 tokens, of
+// which 4,096 stay, read 409 MB (by the counters) for the 210 that they write: 151 us, 4.1 TB/s.
 template <int D>
 __global__ __launch_bounds__(2 * D) void paged_evict_kernel(const EvictArgs a) {
   constexpr int G = D / 32;
