@@ -807,12 +807,11 @@ def hf_paged_read(cache: PagedKV, start, n, k, v, layer=0, stream=None):
 def _weights(t, shape, name, dev) -> hf_key_weights:
     """Descriptor of fp32 numbers of keys [B, H, T] or [B, L, H, T], of which the first
     shape[-1] of each row are meant."""
-    torch = _torch()
-    if t.dtype is not torch.float32 or t.device != dev:
+    if t.dtype is not _torch().float32 or t.device != dev:
         raise TypeError(f"{name} must be a float32 tensor on {dev}")
     s, st = t.shape, t.stride()
-    if len(s) != len(shape) or tuple(s[:-1]) != tuple(shape[:-1]) or s[-1] < shape[-1]:
-        raise ValueError(f"{name}: shape {tuple(s)} does not hold {tuple(shape)}")
+    if len(s) != len(shape) or s[:-1] != shape[:-1] or s[-1] < shape[-1]:
+        raise ValueError(f"{name}: shape {tuple(s)} does not hold {shape}")
     if st[-1] != 1 and s[-1] > 1:
         raise TypeError(f"{name} must have contiguous tokens")
     return hf_key_weights(t.data_ptr(), st[0], st[1] if len(s) == 4 else 0, st[-2])
@@ -820,7 +819,8 @@ def _weights(t, shape, name, dev) -> hf_key_weights:
 
 def _own_rows(t, name):
     """Refuses results whose rows lie in one another (expanded tensors)."""
-    if any(st == 0 and n > 1 for n, st in zip(t.shape, t.stride())):
+    st = t.stride()
+    if 0 in st and any(x == 0 and n > 1 for n, x in zip(t.shape, st)):
         raise TypeError(f"{name} is written: its rows must not overlap")
 
 
@@ -924,7 +924,7 @@ def _index(t, lead, dev):
     torch = _torch()
     if t.dtype is not torch.int32 or t.device != dev or not t.is_contiguous():
         raise TypeError(f"index must be a contiguous int32 tensor on {dev}")
-    if t.dim() != len(lead) + 1 or tuple(t.shape[:-1]) != lead:
+    if t.dim() != len(lead) + 1 or t.shape[:-1] != lead:
         raise ValueError(f"index: shape {tuple(t.shape)} is not {lead} and the tokens that stay")
 
 
